@@ -325,6 +325,75 @@ int zc_decode_attention_static(const zc_tensor4* q, const zc_packed* Kp, const z
                                const zc_tensor4* tail_k, const zc_tensor4* tail_v, int64_t tail_len,
                                float sm_scale, void* out, float* lse_out, void* stream);
 
+/* ---- a paged full-precision cache: requests before (or without) their compression -----------
+ * Keys and values of many requests lie in pages of two pools (one for keys, one for values):
+ * k_pages, v_pages [N, Hkv, page, D], `page` token rows to a page, a power of two from
+ * ZC_PAGE_MIN to ZC_PAGE_MAX, any strides (a page may hold its heads one after the other or its
+ * tokens).  N * page must stay below 2^31, the heads below 65536.  Request r's block table is row r
+ * of block_table (device int32 [R, max_blocks], rows row_stride elements apart): entry c is the page
+ * of its tokens c * page .. c * page + page - 1.  A step's new tokens lie request after request in
+ * tensors of T rows, q_start[r] .. q_start[r + 1] - 1 (device int32 [R + 1]) those of request r;
+ * kv_len[r] (device int32 [R]) counts all its tokens, the new ones, its last, included.  T may be
+ * larger than q_start[R] (calls captured for the largest step): rows behind the last request are
+ * neither read nor written.  R and T may be 0.  Unlike elsewhere, memory that no token of a call
+ * lies in or sees - slots past kv_len, pages behind every window, rows behind the last request -
+ * may hold anything, NaN included; the values of a request's tokens must be finite.
+ *
+ * zc_paged_tables: one step's bookkeeping from the requests' lengths.  Request r has kv_len[r] tokens
+ * of which q_len[r] are new (0 <= q_len <= kv_len; values outside are taken for the nearest inside), so
+ * it holds ceil((kv_len - q_len) / page) pages, whose entries are read, and needs ceil(kv_len / page):
+ * the missing ones are taken from the end of free_pages (device int32 [n_list], of which the first
+ * *n_free are free; n_free is device memory, NULL for all) - in the order of the requests, a request's in
+ * the order of its blocks, the first is free_pages[*n_free - 1] - and written to block_table.
+ * Outputs: q_start; slot_map (device int32 [T]), page * page_rows + row of every new token, -1 for rows
+ * behind the last request; *n_taken, the number of pages the requests needed: where it is more than
+ * *n_free, the entries without a page are -1 and so are their tokens' slots, and the caller has to find pages
+ * and repeat the step.  Entries a request does not need are left as they are.  Tokens past T, and
+ * blocks past max_blocks, get no slot and no entry.  free_pages and n_free are not changed: subtract
+ * *n_taken from *n_free before the next step, on the device if need be.  The new tokens of all
+ * requests and the pages they need must number less than 2^31 each.
+ *
+ * zc_paged_store: k, v [1, Hkv, T, D] (any strides) to the slots of their tokens; a token whose slot is
+ * outside [0, N * page) is left out.  Of two tokens with one slot either may stay.
+ *
+ * zc_paged_load: k[r, h, i, :] and v[r, h, i, :] = token i of request r, for i < min(kv_len[r], k->L,
+ * max_blocks * page); other rows are left as they are.  k, v [R, Hkv, L, D]: what zc_probe_saliency and
+ * zc_quantize_pack_kv take.  R <= 32767, L <= 2^28.
+ *
+ * A block-table entry that is no page (negative, N or more) reads as rows of zeros.  Nothing here needs a workspace.  Errors as elsewhere; a page size that is not
+ * supported is ZC_ERR_UNSUPPORTED. */
+#define ZC_PAGE_MIN 16
+#define ZC_PAGE_MAX 65536
+int zc_paged_tables(const int32_t* q_len, const int32_t* kv_len, int64_t R, int32_t* block_table, int64_t row_stride,
+                    int64_t max_blocks, const int32_t* free_pages, int64_t n_list, const int32_t* n_free, int64_t page,
+                    int32_t* q_start, int32_t* slot_map, int64_t T, int32_t* n_taken, void* stream);
+int zc_paged_store(const zc_tensor4* k, const zc_tensor4* v, const int32_t* slot_map, const zc_tensor4* k_pages,
+                   const zc_tensor4* v_pages, void* stream);
+int zc_paged_load(const zc_tensor4* k_pages, const zc_tensor4* v_pages, const int32_t* block_table, int64_t row_stride,
+                  int64_t max_blocks, const int32_t* kv_len, const zc_tensor4* k, const zc_tensor4* v, void* stream);
+
+/* ---- Eq. 2 / Eq. 4 over the pages: a step's new tokens, one a request or many ------------------
+ * Row j of request r's nq = q_start[r + 1] - q_start[r] new tokens stands at position
+ * pos = kv_len[r] - nq + j (its keys and values are in the pages already) and sees the tokens i <= pos,
+ * with window > 0 only those with i > pos - window or i < sinks:
+ *   out[h, t, :] = sum_i softmax_i(q[h, t] . k[h/G, i] * sm_scale) v[h/G, i, :]
+ * q, out [1, Hq, T, D] of the pools' type, Hq a multiple of Hkv (any group); sm_scale == 0 means
+ * 1/sqrt(D), a negative one is refused.  lse (device float [Hq, T], optional) receives the natural-log
+ * normalisers (for zc_probe_saliency's lse_ext).  A row that sees no token (kv_len < nq), or only logits of
+ * -inf, has zeros for its output and -inf for its normaliser.  A request may have no new tokens.
+ * fp32 tensors are multiplied on the fp32 matrix pipes; the probabilities of 16-bit tensors enter the
+ * second product rounded to the tensors' type.  Deterministic for equal lengths and shapes; a row's last bits may
+ * depend on the other requests (long rows are split by what the whole call has to do, and joined in fp32).
+ * Workspace: zc_paged_attention_workspace() bytes, 16-byte aligned, with any contents; calls that share one
+ * must not run concurrently.  q_start must ascend within [0, T], kv_len be 0 to max_blocks * page (values outside are
+ * taken for the nearest).
+ * Limits: R < 2^24, T * Hq < 2^31. */
+size_t zc_paged_attention_workspace(int64_t R, int64_t T, int64_t Hq, int64_t Hkv, int64_t D);
+int zc_paged_attention(const zc_tensor4* q, const zc_tensor4* k_pages, const zc_tensor4* v_pages, const int32_t* block_table,
+                       int64_t row_stride, int64_t max_blocks, const int32_t* q_start, const int32_t* kv_len, int64_t R,
+                       int32_t window, int32_t sinks, float sm_scale, const zc_tensor4* out, float* lse,
+                       void* ws, size_t ws_bytes, void* stream);
+
 /* ---- helpers ------------------------------------------------------------------ */
 /* Bytes of one code arena of `cap` slots. */
 size_t zc_arena_bytes(int64_t B, int64_t H, int64_t D, int64_t cap, int32_t bits);

@@ -108,6 +108,16 @@ def load() -> C.CDLL:
     lib.zc_group_quantize.argtypes = [T4, P, I64, I32, I32, P, P, P, P, P]
     lib.zc_unpack.restype = C.c_int
     lib.zc_unpack.argtypes = [PK, I32, I32, P, P, P]
+    lib.zc_paged_tables.restype = C.c_int
+    lib.zc_paged_tables.argtypes = [P, P, I64, P, I64, I64, P, I64, P, I64, P, P, I64, P, P]
+    lib.zc_paged_store.restype = C.c_int
+    lib.zc_paged_store.argtypes = [T4, T4, P, T4, T4, P]
+    lib.zc_paged_load.restype = C.c_int
+    lib.zc_paged_load.argtypes = [T4, T4, P, I64, I64, P, T4, T4, P]
+    lib.zc_paged_attention_workspace.restype = SZ
+    lib.zc_paged_attention_workspace.argtypes = [I64, I64, I64, I64, I64]
+    lib.zc_paged_attention.restype = C.c_int
+    lib.zc_paged_attention.argtypes = [T4, T4, T4, P, I64, I64, P, P, I64, I32, I32, F, T4, P, P, SZ, P]
     lib.zc_arena_bytes.restype = SZ
     lib.zc_arena_bytes.argtypes = [I64, I64, I64, I64, I32]
     lib.zc_arena_slots.restype = I64
@@ -344,3 +354,55 @@ def zc_group_quantize(x: torch.Tensor, bits: int, group: int = 32, idx: Optional
     _check("zc_group_quantize", lib.zc_group_quantize(C.byref(tx), _ptr(idx), n, bits, group, _ptr(co), _ptr(sc), _ptr(ze),
                                                       _ptr(dq), _stream()))
     return co, sc, ze, dq
+
+
+def zc_paged_tables(q_len: torch.Tensor, kv_len: torch.Tensor, block_table: torch.Tensor, free_pages: torch.Tensor, page: int, T: int,
+                    n_free: Optional[torch.Tensor] = None, q_start: Optional[torch.Tensor] = None,
+                    slot_map: Optional[torch.Tensor] = None, n_taken: Optional[torch.Tensor] = None):
+    """One step's bookkeeping from the requests' lengths (int32 [R] each): new pages go into block_table [R, max_blocks];
+    returns (q_start [R + 1], slot_map [T], n_taken [1])."""
+    host = _native()
+    if q_start is None:
+        q_start = torch.empty(block_table.shape[0] + 1, dtype=torch.int32, device=block_table.device)
+    if slot_map is None:
+        slot_map = torch.empty(T, dtype=torch.int32, device=block_table.device)
+    elif slot_map.numel() != T:
+        raise ValueError("slot_map must have T elements")
+    if n_taken is None:
+        n_taken = torch.empty(1, dtype=torch.int32, device=block_table.device)
+    _check("zc_paged_tables", host.paged_tables(q_len, kv_len, block_table, free_pages, n_free, page, q_start, slot_map, n_taken))
+    return q_start, slot_map, n_taken
+
+
+def zc_paged_store(k: torch.Tensor, v: torch.Tensor, slot_map: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor) -> None:
+    """New tokens' k, v [T, Hkv, D] (or [1, Hkv, T, D]) to their slots of the pools [N, Hkv, page, D]."""
+    _check("zc_paged_store", _native().paged_store(k, v, slot_map, k_pages, v_pages))
+
+
+def zc_paged_load(k_pages: torch.Tensor, v_pages: torch.Tensor, block_table: torch.Tensor, kv_len: torch.Tensor, L: Optional[int] = None,
+                  k_out: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None):
+    """(k, v) [R, Hkv, L, D]: the tokens of every request; rows past kv_len are not written."""
+    host = _native()
+    if k_out is None or v_out is None:
+        if L is None:
+            L = block_table.shape[1] * k_pages.shape[2]
+        shape = (block_table.shape[0], k_pages.shape[1], L, k_pages.shape[3])
+        k_out = torch.empty(shape, dtype=k_pages.dtype, device=k_pages.device) if k_out is None else k_out
+        v_out = torch.empty(shape, dtype=v_pages.dtype, device=v_pages.device) if v_out is None else v_out
+    _check("zc_paged_load", host.paged_load(k_pages, v_pages, block_table, kv_len, k_out, v_out))
+    return k_out, v_out
+
+
+def zc_paged_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, block_table: torch.Tensor, q_start: torch.Tensor,
+                       kv_len: torch.Tensor, window: int = 0, sinks: int = 0, sm_scale: float = 0.0,
+                       out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None):
+    """q [T, Hq, D] (or [1, Hq, T, D]): a step's new tokens, request after request -> (out like q, lse [Hq, T]).
+    Rows behind the last request are not written."""
+    host = _native()
+    if out is None:
+        out = torch.empty_like(q)
+    if lse is None:
+        T, Hq = (q.shape[0], q.shape[1]) if q.dim() == 3 else (q.shape[2], q.shape[1])
+        lse = torch.empty(Hq, T, dtype=torch.float32, device=q.device)
+    _check("zc_paged_attention", host.paged_attention(q, k_pages, v_pages, block_table, q_start, kv_len, window, sinks, sm_scale, out, lse))
+    return out, lse

@@ -17,6 +17,7 @@
 #include <vector>
 
 #include <ATen/ATen.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -27,13 +28,14 @@ namespace {
 // ---- entry points, in the order of kNames ---------------------------------------------------
 enum Fn {
   kProbe, kAccumulated, kPrefill, kSelect, kQuantize, kQuantizeKV, kDecode, kDecodeStatic, kProbs, kRows, kDequantize,
-  kProbeWs, kQuantizeWs, kQuantizeKVWs, kDecodeWs, kFnCount
+  kPagedTables, kPagedStore, kPagedLoad, kPagedAttention,
+  kProbeWs, kQuantizeWs, kQuantizeKVWs, kDecodeWs, kPagedAttentionWs, kFnCount
 };
 const char* const kNames[kFnCount] = {
     "zc_probe_saliency", "zc_probe_accumulated", "zc_prefill_attention", "zc_select_salient", "zc_quantize_pack",
     "zc_quantize_pack_kv", "zc_decode_attention", "zc_decode_attention_static", "zc_decode_probs", "zc_rows_saliency",
-    "zc_dequantize_cache", "zc_probe_saliency_workspace", "zc_quantize_pack_workspace", "zc_quantize_pack_kv_workspace",
-    "zc_decode_attention_workspace"};
+    "zc_dequantize_cache", "zc_paged_tables", "zc_paged_store", "zc_paged_load", "zc_paged_attention", "zc_probe_saliency_workspace", "zc_quantize_pack_workspace", "zc_quantize_pack_kv_workspace",
+    "zc_decode_attention_workspace", "zc_paged_attention_workspace"};
 void* g_fn[kFnCount];
 
 #define ZC_FN(id, name) reinterpret_cast<decltype(&name)>(g_fn[id])
@@ -109,7 +111,7 @@ struct Packed {
 // it was captured: the graph holds its address, and it is kept.  (So a stream holds less than one and a
 // half times its largest request, and what its graphs were captured with.)  All of this runs
 // under the interpreter lock.
-enum Kind { kScratchProbe, kScratchQuantize, kScratchQuantizeKV, kScratchDecode };
+enum Kind { kScratchProbe, kScratchQuantize, kScratchQuantizeKV, kScratchDecode, kScratchPaged };
 struct Scratch { at::Tensor t; void* ptr = nullptr; size_t bytes = 0; bool captured = false; };
 std::map<std::tuple<int, int, void*>, Scratch>* g_scratch;
 std::vector<at::Tensor>* g_captured;      // replaced buffers that graphs may hold
@@ -329,6 +331,129 @@ PyObject* rows_saliency(PyObject*, Args a, Py_ssize_t n) {
   });
 }
 
+// ---- the paged cache: what a call's tensors are is checked here (lengths and tables come from the caller's own bookkeeping) ----
+[[noreturn]] void refuse(const char* what, const char* why) {
+  PyErr_Format(PyExc_ValueError, "%s %s", what, why);
+  throw Bad();
+}
+void on_device(const at::Tensor& t, const char* what) {
+  if (!t.is_cuda()) refuse(what, "must be on the GPU");
+  if (t.device().index() != c10::hip::current_device()) refuse(what, "must be on the current device");
+}
+// int32, contiguous, of `n` elements (any number: -1); null for None.
+int32_t* ints(PyObject* o, const char* what, int64_t n = -1) {
+  if (o == Py_None) return nullptr;
+  const at::Tensor& t = tensor_of(o);
+  on_device(t, what);
+  if (t.scalar_type() != at::kInt || !t.is_contiguous()) refuse(what, "must be a contiguous int32 tensor");
+  if (n >= 0 && t.numel() != n) refuse(what, "has another number of elements than the requests or rows ask for");
+  return static_cast<int32_t*>(t.data_ptr());
+}
+struct Table { int32_t* ptr; int64_t R, row, cols; };
+Table table_of(PyObject* o) {
+  const at::Tensor& t = tensor_of(o);
+  on_device(t, "block_table");
+  if (t.scalar_type() != at::kInt || t.dim() != 2 || (t.size(1) > 1 && t.stride(1) != 1)) refuse("block_table", "must be an int32 [R, max_blocks] tensor with rows that lie together");
+  Table r = {static_cast<int32_t*>(t.data_ptr()), t.size(0), t.stride(0), t.size(1)};
+  if (r.R < 2 || r.row < r.cols) {
+    if (r.R > 1) refuse("block_table", "has rows that overlap");
+    r.row = r.cols;
+  }
+  return r;
+}
+zc_tensor4 pool(PyObject* o, const char* what) {
+  const zc_tensor4 r = describe(o);
+  on_device(tensor_of(o), what);
+  return r;
+}
+// Rows of a step's tokens: [T, H, D], or [1, H, T, D].
+zc_tensor4 tokens(PyObject* o, const char* what) {
+  const at::Tensor& t = tensor_of(o);
+  zc_tensor4 r = describe(o, true);
+  on_device(t, what);
+  if (t.dim() == 3) {
+    r.B = 1; r.H = t.size(1); r.L = t.size(0);
+    r.sB = 0; r.sH = t.stride(1); r.sL = t.stride(0);
+  }
+  if (r.L <= 1) r.sL = r.D;                // (the stride of an axis of one element says nothing)
+  if (r.H == 1) r.sH = 0;
+  if (r.B == 1) r.sB = 0;
+  return r;
+}
+int32_t int32_of(PyObject* o) {
+  const int64_t v = int_of(o);
+  return v > INT32_MAX ? INT32_MAX : v < INT32_MIN ? INT32_MIN : (int32_t)v;
+}
+
+// (q_len, kv_len, block_table, free_pages, n_free, page, q_start, slot_map, n_taken)
+PyObject* paged_tables(PyObject*, Args a, Py_ssize_t n) {
+  return guarded(kPagedTables, n, 9, [&]() -> int {
+    const Table t = table_of(a[2]);
+    const auto *q = ints(a[0], "q_len", t.R), *kv = ints(a[1], "kv_len", t.R);
+    const auto* free = ints(a[3], "free_pages");
+    const int64_t F = tensor_of(a[3]).numel(), T = tensor_of(a[7]).numel(), page = int_of(a[5]);
+    const auto* n_free = ints(a[4], "n_free", 1);
+    auto *start = ints(a[6], "q_start", t.R + 1), *slots = ints(a[7], "slot_map"), *taken = ints(a[8], "n_taken", 1);
+    const hipStream_t st = current_stream();
+    const auto fn = ZC_FN(kPagedTables, zc_paged_tables);
+    return unlocked([&] { return fn(q, kv, t.R, t.ptr, t.row, t.cols, free, F, n_free, page, start, slots, T, taken, st); });
+  });
+}
+
+// (k, v, slot_map, k_pages, v_pages)
+PyObject* paged_store(PyObject*, Args a, Py_ssize_t n) {
+  return guarded(kPagedStore, n, 5, [&]() -> int {
+    const zc_tensor4 k = tokens(a[0], "k"), v = tokens(a[1], "v"), kp = pool(a[3], "k_pages"), vp = pool(a[4], "v_pages");
+    const auto* slots = ints(a[2], "slot_map", k.L);
+    const hipStream_t st = current_stream();
+    const auto fn = ZC_FN(kPagedStore, zc_paged_store);
+    return unlocked([&] { return fn(&k, &v, slots, &kp, &vp, st); });
+  });
+}
+
+// (k_pages, v_pages, block_table, kv_len, k_out, v_out)
+PyObject* paged_load(PyObject*, Args a, Py_ssize_t n) {
+  return guarded(kPagedLoad, n, 6, [&]() -> int {
+    const zc_tensor4 kp = pool(a[0], "k_pages"), vp = pool(a[1], "v_pages"), k = pool(a[4], "k_out"), v = pool(a[5], "v_out");
+    const Table t = table_of(a[2]);
+    const auto* kv = ints(a[3], "kv_len", t.R);
+    if (k.B != t.R || v.B != t.R) refuse("k_out and v_out", "must have a batch element for each row of block_table");
+    const hipStream_t st = current_stream();
+    const auto fn = ZC_FN(kPagedLoad, zc_paged_load);
+    return unlocked([&] { return fn(&kp, &vp, t.ptr, t.row, t.cols, kv, &k, &v, st); });
+  });
+}
+
+// (q, k_pages, v_pages, block_table, q_start, kv_len, window, sinks, sm_scale, out, lse)
+PyObject* paged_attention(PyObject*, Args a, Py_ssize_t n) {
+  return guarded(kPagedAttention, n, 11, [&]() -> int {
+    const zc_tensor4 q = tokens(a[0], "q"), kp = pool(a[1], "k_pages"), vp = pool(a[2], "v_pages"), o = tokens(a[9], "out");
+    const Table t = table_of(a[3]);
+    const auto *start = ints(a[4], "q_start", t.R + 1), *kv = ints(a[5], "kv_len", t.R);
+    const int32_t window = int32_of(a[6]), sinks = int32_of(a[7]);
+    const float scale = float_of(a[8]);
+    float* lse = nullptr;
+    if (a[10] != Py_None) {
+      const at::Tensor& l = tensor_of(a[10]);
+      on_device(l, "lse");
+      if (l.scalar_type() != at::kFloat || !l.is_contiguous() || l.numel() != q.H * q.L) refuse("lse", "must be a contiguous float32 [Hq, T] tensor");
+      lse = static_cast<float*>(l.data_ptr());
+    }
+    const hipStream_t st = current_stream();
+    const size_t need = ZC_FN(kPagedAttentionWs, zc_paged_attention_workspace)(t.R, q.L, q.H, kp.H, q.D);
+    void* wp = nullptr;
+    size_t wn = 0;
+    Scratch ws;
+    if (need) {
+      ws = scratch(need, tensor_of(a[0]), kScratchPaged, st);
+      wp = ws.ptr;
+      wn = ws.bytes;
+    }
+    const auto fn = ZC_FN(kPagedAttention, zc_paged_attention);
+    return unlocked([&] { return fn(&q, &kp, &vp, t.ptr, t.row, t.cols, start, kv, t.R, window, sinks, scale, &o, lse, wp, wn, st); });
+  });
+}
+
 // (packed, out)
 PyObject* dequantize(PyObject*, Args a, Py_ssize_t n) {
   return guarded(kDequantize, n, 2, [&]() -> int {
@@ -370,6 +495,10 @@ PyMethodDef kMethods[] = {
     ZC_METHOD("probs", probs),
     ZC_METHOD("rows_saliency", rows_saliency),
     ZC_METHOD("dequantize", dequantize),
+    ZC_METHOD("paged_tables", paged_tables),
+    ZC_METHOD("paged_store", paged_store),
+    ZC_METHOD("paged_load", paged_load),
+    ZC_METHOD("paged_attention", paged_attention),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_zc_host", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,521 @@
+// zc_paged_attention: attention of a step's new tokens - one a request or a chunk - over keys and values in pages.
+//
+// The rows of a request and a KV head are its new tokens times the G query heads of the group, token after token: a block
+// of them reads a key once for all its rows, whatever their number, so single tokens and chunks are the same work.
+//   logits  D[key][row]     = sum_c K[key][c] Q[row][c]            (A = K block, B = Q rows in registers)
+//   output  D[channel][row] = sum_key Vt[channel][key] P[row][key]  (A = V block transposed, B = P)
+// Both results put a row in a lane (column r = lane & 31): its running maximum, sum and rescaling are lane-local, and the
+// weights that a lane has computed are, converted in place, the B operand of the second product.
+//
+// A unit of work is a block of rows and a part of the key tiles it sees.  The host knows neither lengths nor how the
+// rows are spread over requests; every wave finds its unit from the lengths alone (find_unit), so nothing has to be
+// prepared, and what is long is split by the same rule in every wave.
+#include <limits.h>
+
+#include "mfma_tiles.hpp"
+#include "paged_args.hpp"
+
+namespace zc {
+
+struct PagedArgs {
+  const uint8_t *q, *k, *v;
+  uint8_t* o;
+  int64_t q_sH, q_sT, o_sH, o_sT;               // bytes
+  int64_t k_sB, k_sH, v_sB, v_sH;               // bytes
+  uint32_t k_row, v_row;                        // bytes from a token to the next
+  const int32_t *table, *q_start, *kv_len;
+  int64_t row;                                  // of the table, in entries
+  int cols, shift, n_pages, cap;                // blocks of the table; page size; pages; tokens a row of the table has room for
+  int R, T, Hkv, G, window, sinks;
+  float scale_log2;
+  float* lse;                                   // [Hq, T] or null
+  int target;                                   // units a head's rows are split into, about; 0: nothing is split
+  int units;                                    // of a head, at most
+  float *part_o, *part_ml;                      // of split units: [unit][row][D], [unit][row][2] (reference, sum)
+};
+
+constexpr float kLowestLogit = -3.40282347e38f; // where a reference starts: finite, so that weights of -inf are 0 whatever came before
+
+template <int DT>
+__device__ inline uint32_t pack_two(float lo, float hi) {
+  typedef float f2 __attribute__((ext_vector_type(2)));
+  if constexpr (DT == ZC_F16) {
+    typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{lo, hi}, h2));
+  } else {
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{lo, hi}, b2));
+  }
+}
+
+// ---- the work of a wave ---------------------------------------------------------------------------
+struct Unit {
+  int r, qs, nq, kv;            // request, its first row, new tokens, tokens
+  int i0, rows;                 // first (token, head) row of the block, how many
+  int p0, p1;                   // positions of its first and last row
+  int first, sink_tiles;        // tile t is t of the first sink_tiles, then first + t - sink_tiles
+  int t_lo, t_hi;               // tiles of this unit
+  int part, parts;              // which of the parts of the block's tiles
+  int index;                    // of the block's first unit among the head's
+};
+
+struct Request { int qs, nq, kv; };
+__device__ inline Request request(const PagedArgs& a, int r) {
+  Request x = {0, 0, 0};
+  if (r < a.R) {
+    x.qs = min(max(a.q_start[r], 0), a.T);
+    x.nq = max(min(a.q_start[r + 1], a.T) - x.qs, 0);
+    x.kv = min(max(a.kv_len[r], 0), a.cap);
+  }
+  return x;
+}
+
+template <int RB>
+__device__ inline int row_blocks(const PagedArgs& a, const Request& x) { return (int)(((uint32_t)x.nq * a.G + RB - 1) / RB); }
+
+// Key tiles that a block of the request's rows sees, at most.
+template <int RB, int KT>
+__device__ inline int key_tiles(const PagedArgs& a, const Request& x) {
+  if (x.nq == 0) return 0;
+  const int all = (x.kv + KT - 1) / KT;
+  if (!a.window) return all;
+  // (RB rows are of RB / G + 2 tokens at most)
+  return min(all, (a.window + RB / a.G + 2 + KT - 2) / KT + 1 + (a.sinks + KT - 1) / KT);
+}
+
+__device__ inline int64_t wave_sum64(int64_t v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor((long long)v, o);
+  return v;
+}
+
+// The unit with index u of a head, BLOCKS: the row block with index u.  LEAST tiles at least make a part.
+template <int RB, int KT, int LEAST, bool BLOCKS>
+__device__ inline bool find_unit(const PagedArgs& a, int u, Unit& x) {
+  const int lane = threadIdx.x & 63;
+  const Request head = request(a, lane);
+  int per = INT_MAX;                                        // tiles of a part, at most
+  if (a.target) {
+    int64_t all = (int64_t)row_blocks<RB>(a, head) * key_tiles<RB, KT>(a, head);
+    for (int r0 = 64; r0 < a.R; r0 += 64) {
+      const Request t = request(a, r0 + lane);
+      all += (int64_t)row_blocks<RB>(a, t) * key_tiles<RB, KT>(a, t);
+    }
+    all = wave_sum64(all);
+    const int64_t each = (all + a.target - 1) / a.target;
+    per = each < LEAST ? LEAST : each > INT_MAX / 2 ? INT_MAX / 2 : (int)each;
+    per = __builtin_amdgcn_readfirstlane(per);
+  }
+  int units = 0, blocks = 0;
+  for (int r0 = 0; r0 < a.R; r0 += 64) {
+    const Request t = r0 ? request(a, r0 + lane) : head;
+    const int nb = row_blocks<RB>(a, t), nt = key_tiles<RB, KT>(a, t);
+    const int parts = nt <= per ? 1 : (nt - 1) / per + 1;
+    const int cu = wave_inclusive_sum(nb * parts), cb = BLOCKS ? wave_inclusive_sum(nb) : 0;
+    const uint64_t here = __builtin_amdgcn_ballot_w64(BLOCKS ? u < blocks + cb : u < units + cu);
+    if (here) {
+      const int l = __builtin_ctzll(here);
+      const auto of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
+      x.r = r0 + l;
+      x.qs = of(t.qs); x.nq = of(t.nq); x.kv = of(t.kv);
+      const int n = of(nb);
+      x.parts = of(parts);
+      const int first_unit = units + of(cu) - n * x.parts;
+      int b;
+      if constexpr (BLOCKS) {
+        b = u - (blocks + of(cb) - n);
+        x.part = 0;
+      } else {
+        const int rest = u - first_unit;
+        b = rest / x.parts;
+        x.part = rest - b * x.parts;
+      }
+      x.index = first_unit + b * x.parts;
+      b = n - 1 - b;                                        // (a chunk's last rows see the most keys: first)
+      const int all_rows = x.nq * a.G;
+      x.i0 = b * RB;
+      x.rows = min(RB, all_rows - x.i0);
+      x.p0 = x.kv - x.nq + x.i0 / a.G;
+      x.p1 = x.kv - x.nq + (x.i0 + x.rows - 1) / a.G;
+      const int low = a.window ? max(0, x.p0 - a.window + 1) : 0;
+      x.first = low / KT;
+      x.sink_tiles = min((min(a.sinks, low) + KT - 1) / KT, x.first);
+      const int tiles = x.p1 < 0 ? 0 : x.sink_tiles + x.p1 / KT + 1 - x.first;
+      const int q = tiles / x.parts, rem = tiles - q * x.parts;
+      x.t_lo = x.part * q + min(x.part, rem);
+      x.t_hi = x.t_lo + q + (x.part < rem ? 1 : 0);
+      return true;
+    }
+    units += __builtin_amdgcn_readlane(cu, 63);
+    if constexpr (BLOCKS) blocks += __builtin_amdgcn_readlane(cb, 63);
+  }
+  return false;
+}
+
+__device__ inline int tile_of(const Unit& x, int t) { return t < x.sink_tiles ? t : x.first + t - x.sink_tiles; }
+
+// The page of 16 keys from key0 on, -1 where there is none.
+__device__ inline int page_of(const PagedArgs& a, const Unit& x, int key0) {
+  typedef __attribute__((address_space(4))) const int32_t* scalar;
+  const int col = key0 >> a.shift;
+  if (col >= a.cols) return -1;
+  return ((scalar)(uintptr_t)(a.table + x.r * a.row))[col];
+}
+// Of 16 keys from key0 on, how many a unit reads: none of a missing page, of those that no row's window reaches, past the end.
+// What is not read arrives as zeros.
+__device__ inline int keys_read(const PagedArgs& a, const Unit& x, int key0, int id) {
+  int n = max(x.kv - key0, 0);
+  asm("" : "+s"(n));                                        // (both bounds at once would be one vector instruction, and what follows too)
+  n = min(n, 16);
+  if ((uint32_t)id >= (uint32_t)a.n_pages) n = 0;
+  if (a.window && key0 + 15 <= max(x.p0, 0) - a.window && key0 >= a.sinks) n = 0;
+  return n;
+}
+__device__ inline __amdgpu_buffer_rsrc_t keys_at(const PagedArgs& a, const uint8_t* head, int64_t sB, uint32_t row, int key0, int id, int n) {
+  const int64_t at = (int64_t)(n ? id : 0) * sB + (int64_t)(key0 & ((1 << a.shift) - 1)) * row;
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(head + at), 0, n * row, kBufFlags);
+}
+
+// Chunk slot permutation of a V row of 16-bit types: the transposing load reads 64 bytes of four consecutive keys per
+// half-wave; these land in different banks.
+template <int DT, int D>
+__device__ inline int v_slot(int key) {
+  if constexpr (DT == ZC_F32) return 0;
+  return D == 128 ? 4 * (key & 3) ^ (key & 2) : 2 * (key & 2) ^ 2 * (key & 1);
+}
+
+// ---- blocks of 32 rows: single tokens, short chunks, fp32 ---------------------------------------------
+// NW waves share the keys of 32 rows, a wave every NW-th 32 keys, in a place of its own in LDS for one K and one V block: a
+// block's K is requested when the one before has been multiplied, its V likewise, so that a wave has one of them in flight
+// at any time and waits for nobody.
+constexpr int kRowsLeast = 4;   // blocks of 32 keys that make a part: one a wave
+template <int DT, int D, int NW>
+__global__ __launch_bounds__(64 * NW, DT == ZC_F32 && D == 128 ? 1 : 2) void k_paged_rows(PagedArgs a) {
+  using T = Tile<DT, D>;
+  constexpr int BLK = 32 * T::ROWB;              // bytes of a block
+  constexpr int NT = BLK / 1024;                 // transfers of a block
+  constexpr int PG = 16 / T::RPI;                // of 16 keys
+  constexpr int CT = D / 32;
+  static_assert(NW * 2 * BLK >= NW * CT * 4 * 64 * 16 && CT * 4 % NW == 0, "the waves' outputs fit where their keys were");
+  __shared__ __align__(1024) uint8_t mem[NW * 2 * BLK];
+  __shared__ float sum[NW][2][64];
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+  const int hk = blockIdx.x % a.Hkv;
+  Unit x;
+  if (!find_unit<32, 32, kRowsLeast, false>(a, blockIdx.x / a.Hkv, x)) return;
+  const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, kh = lane >> 5;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const uint8_t* kb = a.k + hk * a.k_sH;
+  const uint8_t* vb = a.v + hk * a.v_sH;
+  const uint32_t mem_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)&mem[0];
+  const uint32_t k_lds = mem_lds + w * 2 * BLK, v_lds = k_lds + BLK;
+
+  int kvoff[PG], vvoff[PG];
+#pragma unroll
+  for (int j = 0; j < PG; ++j) {
+    const int row = j * T::RPI + lane / T::CPR;
+    kvoff[j] = (int)(row * a.k_row) + (((lane % T::CPR) ^ T::swz(row)) << 4);
+    vvoff[j] = (int)(row * a.v_row) + (((lane % T::CPR) ^ v_slot<DT, D>(row)) << 4);
+  }
+  struct Ids { int id[2], n[2], key0; };
+  auto pages = [&](int t) {
+    Ids s;
+    s.key0 = tile_of(x, t) * 32;
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      s.id[g] = page_of(a, x, s.key0 + 16 * g);
+      s.n[g] = keys_read(a, x, s.key0 + 16 * g, s.id[g]);
+    }
+    return s;
+  };
+  auto issue = [&](const Ids& s, const uint8_t* head, int64_t sB, uint32_t row, uint32_t lds, const int (&voff)[PG]) {
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      const auto rs = keys_at(a, head, sB, row, s.key0 + 16 * g, s.id[g], s.n[g]);
+#pragma unroll
+      for (int j = 0; j < PG; ++j) dma16<0>(lds + g * 16 * T::ROWB + j * 1024, rs, voff[j], 0);
+    }
+  };
+
+  int t = x.t_lo + w;
+  Ids at;
+  if (t < x.t_hi) {
+    at = pages(t);
+    issue(at, kb, a.k_sB, a.k_row, k_lds, kvoff);
+    issue(at, vb, a.v_sB, a.v_row, v_lds, vvoff);
+  }
+
+  // this lane's row, straight into operand registers
+  const bool mine = r < x.rows;
+  const int i = x.i0 + r, j = i / a.G;
+  const int64_t hq = hk * a.G + (i - j * a.G), tok = x.qs + j;
+  const int pos = mine ? x.kv - x.nq + j : -1;
+  u32x4 qf[T::NKC];
+#pragma unroll
+  for (int kc = 0; kc < T::NKC; ++kc) qf[kc] = u32x4{0, 0, 0, 0};
+  if (mine) {
+    const uint8_t* qr = a.q + hq * a.q_sH + tok * a.q_sT + kh * 16;
+#pragma unroll
+    for (int kc = 0; kc < T::NKC; ++kc) qf[kc] = *reinterpret_cast<const u32x4*>(qr + kc * 32);
+  }
+
+  typedef __attribute__((address_space(3))) const uint8_t* lds_ptr;
+  const uint32_t kaddr = k_lds + T::slot(r, kh);          // chunk 2 kc + kh sits at kaddr ^ (32 kc)
+  const int vkey = 4 * kh + ((lane & 15) >> 2);
+  const int vsub = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+  uint32_t vaddr[CT];
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    if constexpr (DT == ZC_F32) vaddr[ct] = v_lds + 4 * kh * T::ROWB + (32 * ct + r) * 4;
+    else vaddr[ct] = v_lds + vkey * T::ROWB + (((4 * ct + vsub) ^ v_slot<DT, D>(vkey)) << 4) + (lane & 1) * 8;
+  }
+
+  v16f oacc[CT];
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) oacc[ct] = v16f{};
+  float m = kLowestLogit, l = 0.f;   // running maximum (log2 units), this half-wave's share of the sum
+
+  for (; t < x.t_hi; t += NW) {
+    const bool more = t + NW < x.t_hi;
+    const int key0 = at.key0;
+    if (more) at = pages(t + NW);
+    wait_vmem<NT>();                                       // K is there (V was requested after it)
+    v16f s = {};
+#pragma unroll
+    for (int kc = 0; kc < T::NKC; ++kc) {
+      const u32x4 kf = *(__attribute__((address_space(3))) const u32x4*)(lds_ptr)(uintptr_t)(kaddr ^ (32 * kc));
+      mma_chunk<DT>(s, kf, qf[kc]);
+    }
+    dma_reuse_fence();
+    if (more) issue(at, kb, a.k_sB, a.k_row, k_lds, kvoff);
+    if (key0 + 31 > x.p0 || (a.window && key0 <= x.p1 - a.window && key0 + 31 >= a.sinks)) {
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        const int key = key0 + acc_row(v, kh);
+        if (key > pos || (a.window && key <= pos - a.window && key >= a.sinks)) s[v] = -INFINITY;
+      }
+    }
+    // (the maximum is taken over the raw products - the scale is not negative - and the scale enters with the subtraction)
+    float tmax = s[0];
+#pragma unroll
+    for (int v = 1; v < 16; ++v) tmax = fmaxf(tmax, s[v]);
+    tmax = fmaxf(tmax, __shfl_xor(tmax, 32));
+    const float m_new = fmaxf(m, tmax * a.scale_log2);
+    if (__builtin_amdgcn_ballot_w64(m_new > m)) {
+      const float alpha = __builtin_amdgcn_exp2f(m - m_new);
+      l *= alpha;
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) oacc[ct][e] *= alpha;
+      m = m_new;
+    }
+    float psum = 0.f;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], a.scale_log2, -m));
+      psum += s[v];
+    }
+    l += psum;
+    if (more) wait_vmem<NT>();
+    else wait_vmem<0>();                                   // V is there
+    if constexpr (DT == ZC_F32) {
+#pragma unroll
+      for (int v = 0; v < 16; ++v)
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+          const float vf = *(__attribute__((address_space(3))) const float*)((lds_ptr)(uintptr_t)vaddr[ct] + acc_row(v, 0) * T::ROWB);
+          oacc[ct] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, s[v], oacc[ct], 0, 0, 0);
+        }
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        u32x4 pb;
+        pb.x = pack_two<DT>(s[8 * h], s[8 * h + 1]);
+        pb.y = pack_two<DT>(s[8 * h + 2], s[8 * h + 3]);
+        pb.z = pack_two<DT>(s[8 * h + 4], s[8 * h + 5]);
+        pb.w = pack_two<DT>(s[8 * h + 6], s[8 * h + 7]);
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+          const lds_ptr base = (lds_ptr)(uintptr_t)vaddr[ct] + 16 * h * T::ROWB;
+          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)base);
+          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(base + 8 * T::ROWB));
+          const uint2 l2 = __builtin_bit_cast(uint2, lo), h2 = __builtin_bit_cast(uint2, hi);
+          u32x4 vf;
+          vf.x = l2.x; vf.y = l2.y; vf.z = h2.x; vf.w = h2.y;
+          mma_chunk<DT>(oacc[ct], vf, pb);
+        }
+      }
+    }
+    dma_reuse_fence();
+    if (more) issue(at, vb, a.v_sB, a.v_row, v_lds, vvoff);
+  }
+
+  // ---- join the waves: all outputs to LDS, each wave finishes an equal part of the channels ----
+  // (a wave without keys has m = kLowestLogit, l = 0 and zeros)
+  constexpr int PART = CT * 4 / NW;                        // groups of four channels of a lane
+  float4* stage = reinterpret_cast<float4*>(mem);
+  const float l_wave = l + __shfl_xor(l, 32);
+  __syncthreads();                                         // (every wave is done with its blocks)
+  if (mine) {
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+      for (int v4 = 0; v4 < 4; ++v4)
+        stage[((w * CT + ct) * 4 + v4) * 64 + lane] = make_float4(oacc[ct][4 * v4], oacc[ct][4 * v4 + 1], oacc[ct][4 * v4 + 2], oacc[ct][4 * v4 + 3]);
+  }
+  sum[w][0][lane] = m;
+  sum[w][1][lane] = l_wave;
+  __syncthreads();
+  if (!mine) return;
+  float M = kLowestLogit, l_tot = 0.f, f[NW];
+#pragma unroll
+  for (int v = 0; v < NW; ++v) { f[v] = sum[v][0][lane]; M = fmaxf(M, f[v]); }
+#pragma unroll
+  for (int v = 0; v < NW; ++v) {
+    f[v] = __builtin_amdgcn_exp2f(f[v] - M);
+    l_tot = fmaf(sum[v][1][lane], f[v], l_tot);
+  }
+  const bool whole = x.parts == 1;
+  const int64_t prow = ((int64_t)blockIdx.x * 32 + r);
+  const float inv = !whole ? 1.f : l_tot == 0.f ? 0.f : 1.f / l_tot;
+  uint8_t* orow = a.o + hq * a.o_sH + tok * a.o_sT;
+#pragma unroll
+  for (int u = 0; u < PART; ++u) {
+    const int part = w * PART + u;                         // group part % 4 of channel tile part / 4
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int v = 0; v < NW; ++v) {
+      const float4 p = stage[((v * CT * 4) + part) * 64 + lane];
+      o.x = fmaf(p.x, f[v], o.x); o.y = fmaf(p.y, f[v], o.y); o.z = fmaf(p.z, f[v], o.z); o.w = fmaf(p.w, f[v], o.w);
+    }
+    const int c = 32 * (part >> 2) + 8 * (part & 3) + 4 * kh;
+    o.x *= inv; o.y *= inv; o.z *= inv; o.w *= inv;
+    if (!whole) *reinterpret_cast<float4*>(a.part_o + prow * D + c) = o;
+    else if constexpr (DT == ZC_F32) *reinterpret_cast<float4*>(orow + c * 4) = o;
+    else *reinterpret_cast<uint2*>(orow + c * 2) = make_uint2(pack_two<DT>(o.x, o.y), pack_two<DT>(o.z, o.w));
+  }
+  if (w == 0 && kh == 0) {
+    if (!whole) *reinterpret_cast<float2*>(a.part_ml + prow * 2) = make_float2(M, l_tot);
+    else if (a.lse) a.lse[hq * a.T + tok] = l_tot == 0.f ? -INFINITY : (M + log2f(l_tot)) * kLn2;
+  }
+}
+
+// ---- the join of split blocks ---------------------------------------------------------------------------
+// A workgroup per row block; D / 4 threads take a row.
+template <int DT, int D, int RB, int KT, int LEAST>
+__global__ __launch_bounds__(256) void k_paged_join(PagedArgs a) {
+  const int hk = blockIdx.x % a.Hkv;
+  Unit x;
+  if (!find_unit<RB, KT, LEAST, true>(a, blockIdx.x / a.Hkv, x) || x.parts == 1 || x.index + x.parts > a.units) return;
+  constexpr int TPR = D / 4;
+  const int c = threadIdx.x % TPR * 4;
+  for (int row = threadIdx.x / TPR; row < x.rows; row += 256 / TPR) {
+    float M = kLowestLogit;
+    for (int s = 0; s < x.parts; ++s) M = fmaxf(M, a.part_ml[(((int64_t)(x.index + s) * a.Hkv + hk) * RB + row) * 2]);
+    float l = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int s = 0; s < x.parts; ++s) {
+      const int64_t p = ((int64_t)(x.index + s) * a.Hkv + hk) * RB + row;
+      const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + p * 2);
+      const float4 t = *reinterpret_cast<const float4*>(a.part_o + p * D + c);
+      const float f = __builtin_amdgcn_exp2f(ml.x - M);
+      l = fmaf(ml.y, f, l);
+      o.x = fmaf(t.x, f, o.x); o.y = fmaf(t.y, f, o.y); o.z = fmaf(t.z, f, o.z); o.w = fmaf(t.w, f, o.w);
+    }
+    const int i = x.i0 + row, j = i / a.G;
+    const int64_t hq = hk * a.G + (i - j * a.G), tok = x.qs + j;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    uint8_t* orow = a.o + hq * a.o_sH + tok * a.o_sT;
+    if constexpr (DT == ZC_F32) *reinterpret_cast<float4*>(orow + c * 4) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+    else *reinterpret_cast<uint2*>(orow + c * 2) = make_uint2(pack_two<DT>(o.x * inv, o.y * inv), pack_two<DT>(o.z * inv, o.w * inv));
+    if (a.lse && c == 0) a.lse[hq * a.T + tok] = l == 0.f ? -INFINITY : (M + log2f(l)) * kLn2;
+  }
+}
+
+// ---- host ---------------------------------------------------------------------------------------------
+// How a call's rows are cut: units that splitting aims at (0: nothing is split) and row blocks, at most, of a head.
+struct Cut { int64_t target, blocks; };
+constexpr int64_t kPlaces = 512;               // workgroups the chip holds at a time
+
+static Cut cut_of(int64_t R, int64_t T, int64_t G, int64_t Hkv, int rows) {
+  Cut c;
+  c.blocks = T * G / rows + (R < T ? R : T);   // (a request has one block that is not full)
+  c.target = c.blocks * Hkv > 2 * kPlaces ? 0 : ceil_div64(kPlaces, Hkv);
+  return c;
+}
+
+template <int DT, int D>
+static int launch_paged(PagedArgs& a, const Cut& cut, hipStream_t st) {
+  const dim3 units((unsigned)((cut.target + cut.blocks) * a.Hkv)), blocks((unsigned)(cut.blocks * a.Hkv));
+  hipLaunchKernelGGL((k_paged_rows<DT, D, 4>), units, dim3(256), 0, st, a);
+  ZC_LAUNCH_CHECK();
+  if (cut.target) {
+    hipLaunchKernelGGL((k_paged_join<DT, D, 32, 32, kRowsLeast>), blocks, dim3(256), 0, st, a);
+    ZC_LAUNCH_CHECK();
+  }
+  return ZC_OK;
+}
+
+}  // namespace zc
+
+using namespace zc;
+
+extern "C" size_t zc_paged_attention_workspace(int64_t R, int64_t T, int64_t Hq, int64_t Hkv, int64_t D) {
+  if (R <= 0 || T <= 0 || Hkv <= 0 || Hq < Hkv || Hq % Hkv || D <= 0) return 0;
+  const Cut c = cut_of(R, T, Hq / Hkv, Hkv, 32);
+  return c.target ? (size_t)(c.target + c.blocks) * Hkv * 32 * (D + 2) * sizeof(float) : 0;
+}
+
+extern "C" int zc_paged_attention(const zc_tensor4* q, const zc_tensor4* k_pages, const zc_tensor4* v_pages, const int32_t* block_table,
+                                  int64_t row_stride, int64_t max_blocks, const int32_t* q_start, const int32_t* kv_len, int64_t R,
+                                  int32_t window, int32_t sinks, float sm_scale, const zc_tensor4* out, float* lse,
+                                  void* ws, size_t ws_bytes, void* stream) {
+  int rc = zc_validate_pages(k_pages, v_pages);
+  if (rc) return rc;
+  rc = zc_validate_heads(q, k_pages);
+  if (rc) return rc;
+  rc = zc_validate_heads(out, k_pages);
+  if (rc) return rc;
+  if (q->H != out->H || q->L != out->L || q->H % k_pages->H) return ZC_ERR_INVALID_ARG;
+  if (R < 0 || window < 0 || sinks < 0 || !(sm_scale >= 0.f) || sm_scale > 3.4e38f) return ZC_ERR_INVALID_ARG;
+  if (max_blocks < 0 || row_stride < max_blocks) return ZC_ERR_INVALID_ARG;
+  if (q->L == 0 || R == 0) return ZC_OK;
+  if (!q_start || !kv_len || (max_blocks > 0 && !block_table)) return ZC_ERR_INVALID_ARG;
+  for (const void* p : {(const void*)block_table, (const void*)q_start, (const void*)kv_len, (const void*)lse})
+    if (reinterpret_cast<uintptr_t>(p) & 3) return ZC_ERR_INVALID_ARG;
+  const int64_t T = q->L, Hkv = k_pages->H, G = q->H / Hkv;
+  if (R >= (1 << 24) || max_blocks > 0x7fffffff || T > 0x7fffffff / q->H || q->H > 65535) return ZC_ERR_UNSUPPORTED;
+  const Cut cut = cut_of(R, T, G, Hkv, 32);
+  if ((cut.target + cut.blocks) * Hkv > 0xffffff) return ZC_ERR_UNSUPPORTED;
+  const size_t need = zc_paged_attention_workspace(R, T, q->H, Hkv, q->D);
+  if (need && (!ws || ws_bytes < need || (reinterpret_cast<uintptr_t>(ws) & 15))) return ZC_ERR_WORKSPACE;
+
+  const int64_t eb = elem_bytes(q->dtype), page = k_pages->L;
+  const int64_t room = max_blocks > 0x7fff0000 / page ? 0x7fff0000 : max_blocks * page;
+  PagedArgs a;
+  a.q = (const uint8_t*)q->ptr; a.k = (const uint8_t*)k_pages->ptr; a.v = (const uint8_t*)v_pages->ptr; a.o = (uint8_t*)out->ptr;
+  a.q_sH = q->sH * eb; a.q_sT = q->sL * eb; a.o_sH = out->sH * eb; a.o_sT = out->sL * eb;
+  a.k_sB = k_pages->sB * eb; a.k_sH = k_pages->sH * eb; a.v_sB = v_pages->sB * eb; a.v_sH = v_pages->sH * eb;
+  a.k_row = (uint32_t)(k_pages->sL * eb); a.v_row = (uint32_t)(v_pages->sL * eb);
+  a.table = block_table; a.q_start = q_start; a.kv_len = kv_len; a.row = row_stride;
+  a.cols = (int)max_blocks; a.shift = __builtin_ctzll((unsigned long long)page); a.n_pages = (int)k_pages->B; a.cap = (int)room;
+  a.R = (int)R; a.T = (int)T; a.Hkv = (int)Hkv; a.G = (int)G;
+  a.window = window >= room ? 0 : window;          // (every row sees all it could)
+  a.sinks = sinks > room ? (int)room : sinks;
+  a.scale_log2 = (sm_scale == 0.f ? 1.0f / sqrtf((float)q->D) : sm_scale) * kLog2e;
+  a.lse = lse;
+  a.target = (int)cut.target;
+  a.units = (int)(cut.target + cut.blocks);
+  const int64_t parts = (cut.target + cut.blocks) * Hkv;
+  a.part_o = (float*)ws;
+  a.part_ml = need ? (float*)ws + parts * 32 * q->D : nullptr;
+  hipStream_t st = (hipStream_t)stream;
+#define ZC_PA(DT) (q->D == 128 ? launch_paged<DT, 128>(a, cut, st) : launch_paged<DT, 64>(a, cut, st))
+  if (q->dtype == ZC_F32) rc = ZC_PA(ZC_F32);
+  else if (q->dtype == ZC_F16) rc = ZC_PA(ZC_F16);
+  else rc = ZC_PA(ZC_BF16);
+#undef ZC_PA
+  return rc;
+}
