@@ -11,6 +11,7 @@
 // rows are spread over requests; every wave finds its unit from the lengths alone (find_unit), so nothing has to be
 // prepared, and what is long is split by the same rule in every wave.
 #include <limits.h>
+#include <type_traits>
 
 #include "mfma_tiles.hpp"
 #include "paged_args.hpp"
@@ -290,10 +291,11 @@ __global__ __launch_bounds__(64 * NW, DT == ZC_F32 && D == 128 ? 1 : 2) void k_p
     dma_reuse_fence();
     if (more) issue(at, kb, a.k_sB, a.k_row, k_lds, kvoff);
     if (key0 + 31 > x.p0 || (a.window && key0 <= x.p1 - a.window && key0 + 31 >= a.sinks)) {
+      const int low = a.window && pos >= 0 ? pos - a.window : -1;          // keys up to it are seen as sinks only
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
         const int key = key0 + acc_row(v, kh);
-        if (key > pos || (a.window && key <= pos - a.window && key >= a.sinks)) s[v] = -INFINITY;
+        if ((key > pos) | ((key <= low) & (key >= a.sinks))) s[v] = -INFINITY;
       }
     }
     // (the maximum is taken over the raw products - the scale is not negative - and the scale enters with the subtraction)
@@ -402,6 +404,271 @@ __global__ __launch_bounds__(64 * NW, DT == ZC_F32 && D == 128 ? 1 : 2) void k_p
   }
 }
 
+// ---- blocks of 128 rows, 16-bit types: chunks ------------------------------------------------------------
+// Four waves of 32 rows each; 64-key tiles of K and V stream through LDS for all of them, two waves on a SIMD.  Keys go by
+// halves of a tile, and no wave multiplies a half that lies behind its last row.  A wave moves 16 keys of a tile, which
+// lie in one page: its address is scalar work, and a page that ends inside a tile costs nothing.
+//
+// Bound by the matrix cores: a half is 16 matrix instructions of 32 cycles (128 channels) and about 300 cycles of vector
+// instructions, so the two have to run at the same time: the logits of half h + 1 are multiplied while the exponentials of
+// half h are taken, and the operands of each product are requested one phase before.
+constexpr int kTilesLeast = 4;  // tiles of 64 keys that make a part
+template <int DT, int D>
+__global__ __launch_bounds__(256, 2) void k_paged_tiles(PagedArgs a) {
+  using T = Tile<DT, D>;
+  constexpr int KEYS = 64, RB = 128;
+  constexpr int TILE_B = KEYS * T::ROWB;
+  constexpr int NI = 16 / T::RPI;                // transfers per wave, tile and tensor
+  constexpr int CT = D / 32;                     // 32-channel tiles of the output
+  constexpr int EPS = 16 / T::NKC;               // logits per slice
+  constexpr int VS = T::NKC / 4;                 // the slice that requests the first V operand
+  __shared__ __align__(1024) uint8_t Ks[2][TILE_B];
+  __shared__ __align__(1024) uint8_t Vs[2][TILE_B];
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+  const int hk = blockIdx.x % a.Hkv;
+  Unit x;
+  if (!find_unit<RB, KEYS, kTilesLeast, false>(a, blockIdx.x / a.Hkv, x)) return;
+  const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, kh = lane >> 5;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const uint8_t* kb = a.k + hk * a.k_sH;
+  const uint8_t* vb = a.v + hk * a.v_sH;
+  const uint32_t ks_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)&Ks[0][0] + w * 16 * T::ROWB;
+  const uint32_t vs_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)&Vs[0][0] + w * 16 * T::ROWB;
+
+  // this wave's rows, and the halves of this unit that they see: all up to the last row's
+  const int wi = x.i0 + 32 * w, wrows = min(max(x.rows - 32 * w, 0), 32);
+  const int wp0 = x.kv - x.nq + wi / a.G, wp1 = wrows > 0 ? x.kv - x.nq + (wi + wrows - 1) / a.G : -1;
+  const int ntiles = x.t_hi - x.t_lo;
+  int nh = 0;
+  if (wp1 >= 0) {
+    const int t1 = wp1 / KEYS - x.first + x.sink_tiles - x.t_lo;          // the tile of the last row's own token
+    nh = t1 < 0 ? 0 : t1 >= ntiles ? 2 * ntiles : 2 * t1 + ((wp1 & 32) ? 2 : 1);
+  }
+
+  // A lane's place in transfer jj: row jj * RPI + lane / CPR of 16, its chunks swizzled by the row (the swizzles repeat after 16
+  // rows).  The parts are put together at every transfer: kept, they would be eight registers of a loop that has none to spare.
+  int krow = (lane / T::CPR) * (int)a.k_row, kchunk = ((lane % T::CPR) ^ T::swz(lane / T::CPR)) << 4;
+  int vplace = (lane / T::CPR) * (int)a.v_row + (((lane % T::CPR) ^ v_slot<DT, D>(lane / T::CPR)) << 4);
+  static_assert(T::RPI % 4 == 0 && T::SW * T::RP256 == 16, "what a transfer's first row adds to the swizzles");
+  struct Group { int key0, id; };
+  auto group = [&](int t) {
+    Group g;
+    g.key0 = tile_of(x, x.t_lo + t) * KEYS + 16 * w;
+    g.id = page_of(a, x, g.key0);
+    return g;
+  };
+  auto k_issue = [&](int t, const Group& g) {
+    const auto rs = keys_at(a, kb, a.k_sB, a.k_row, g.key0, g.id, keys_read(a, x, g.key0, g.id));
+#pragma unroll
+    for (int jj = 0; jj < NI; ++jj) {
+      asm volatile("" : "+v"(krow), "+v"(kchunk));
+      dma16<0>(ks_lds + (t & 1) * TILE_B + jj * 1024, rs, krow + jj * T::RPI * (int)a.k_row + (kchunk ^ (T::swz(jj * T::RPI) << 4)), 0);
+    }
+  };
+  auto v_issue = [&](int t, const Group& g) {
+    const auto rs = keys_at(a, vb, a.v_sB, a.v_row, g.key0, g.id, keys_read(a, x, g.key0, g.id));
+#pragma unroll
+    for (int jj = 0; jj < NI; ++jj) {
+      asm volatile("" : "+v"(vplace));
+      dma16<0>(vs_lds + (t & 1) * TILE_B + jj * 1024, rs, vplace + jj * T::RPI * (int)a.v_row, 0);
+    }
+  };
+  Group gv = {0, -1}, gk = {0, -1};              // of V(t + 1) and K(t + 2)
+  if (ntiles > 0) {
+    const Group g = group(0);
+    gv = group(1);
+    gk = group(2);
+    k_issue(0, g);
+    v_issue(0, g);
+    if (ntiles > 1) k_issue(1, gv);
+  }
+
+  // this lane's row, straight into operand registers
+  const int pos = r < wrows ? x.kv - x.nq + (wi + r) / a.G : INT_MIN;
+  u32x4 qf[T::NKC];
+#pragma unroll
+  for (int kc = 0; kc < T::NKC; ++kc) qf[kc] = u32x4{0, 0, 0, 0};
+  if (r < wrows) {
+    const int j = (wi + r) / a.G;
+    const uint8_t* qr = a.q + (hk * a.G + (wi + r - j * a.G)) * a.q_sH + (int64_t)(x.qs + j) * a.q_sT + kh * 16;
+#pragma unroll
+    for (int kc = 0; kc < T::NKC; ++kc) qf[kc] = *reinterpret_cast<const u32x4*>(qr + kc * 32);
+  }
+
+  // ---- operands from LDS -----------------------------------------------------------------
+  struct KFrag { u32x4 x[T::NKC]; };
+  // (LDS addresses: one register per lane and chunk pattern, tile and half in the offset of
+  // the instruction; the empty assembly keeps the compiler from holding a register for each)
+  typedef __attribute__((address_space(3))) const uint8_t* lds_ptr;
+  uint32_t kaddr = ks_lds - w * 16 * T::ROWB + T::slot(r, kh);           // chunk 2 kc + kh sits at kaddr ^ (32 kc)
+  asm volatile("" : "+v"(kaddr));
+  auto k_read = [&](int half, KFrag& f) {
+#pragma unroll
+    for (int kc = 0; kc < T::NKC; ++kc)
+      f.x[kc] = *(__attribute__((address_space(3))) const u32x4*)((lds_ptr)(uintptr_t)(kaddr ^ (32 * kc)) + half * 32 * T::ROWB);
+  };
+  // The transposing load: in every 16 lanes, lanes 4 i .. 4 i + 3 name the 16 channels of key i, and lane c receives channel
+  // c of the four keys.  A lane's 8 k-indices of operand chunk s are the keys its logit accumulators 8 s .. 8 s + 7 stand for.
+  const int vkey = 4 * kh + ((lane & 15) >> 2);
+  const int vsub = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+  uint32_t vaddr[CT];
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    vaddr[ct] = vs_lds - w * 16 * T::ROWB + vkey * T::ROWB + (((4 * ct + vsub) ^ v_slot<DT, D>(vkey)) << 4) + (lane & 1) * 8;
+    asm volatile("" : "+v"(vaddr[ct]));
+  }
+  auto v_read = [&](int half, int s, int ct, u32x4& f) {
+    const lds_ptr base = (lds_ptr)(uintptr_t)vaddr[ct] + (half * 32 + 16 * s) * T::ROWB;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)base);
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(base + 8 * T::ROWB));
+    const uint2 l2 = __builtin_bit_cast(uint2, lo), h2 = __builtin_bit_cast(uint2, hi);
+    f.x = l2.x; f.y = l2.y; f.z = h2.x; f.w = h2.y;
+  };
+
+  v16f oacc[CT];
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) oacc[ct] = v16f{};
+  float m = kLowestLogit, l = 0.f;   // running maximum (log2 units), this half-wave's share of the sum
+  KFrag kf;
+  v16f s0, s1;
+
+  // Largest logit (log2 units) of a half in either half-wave, over the raw products (the scale is not negative).
+  auto half_max = [&](const v16f& sc) {
+    float t = sc[0];
+#pragma unroll
+    for (int v = 1; v < 16; ++v) t = fmaxf(t, sc[v]);
+    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(t), __float_as_uint(t), false, false);
+    return fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * a.scale_log2;
+  };
+  float tmax = 0.f;                                  // of the half whose weights are taken next
+
+  // One half, of keys key0 on: weights of the logits sc, output += V^T P; unless it is the wave's LAST, the logits of the half
+  // after it (operands in kf) meanwhile, their maximum, and the request of the operands of the half after that.
+  auto step = [&](auto last_c, int half, int key0, v16f& sc, v16f& sn) {
+    constexpr bool LAST = decltype(last_c)::value;
+    u32x4 vf[2][CT];
+    if (key0 + 31 > wp0 || (a.window && key0 <= wp1 - a.window && key0 + 31 >= a.sinks)) {
+      const int low = a.window && pos >= 0 ? pos - a.window : -1;          // keys up to it are seen as sinks only
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        const int key = key0 + acc_row(v, kh);
+        if ((key > pos) | ((key <= low) & (key >= a.sinks))) sc[v] = -INFINITY;
+      }
+      tmax = half_max(sc);
+    }
+    const float m_new = fmaxf(m, tmax);
+    if (__builtin_amdgcn_ballot_w64(m_new > m)) {
+      const float alpha = __builtin_amdgcn_exp2f(m - m_new);
+      l *= alpha;
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) oacc[ct][e] *= alpha;
+      m = m_new;
+    }
+    uint32_t pw[8];                                  // the weights, two to a word
+    float psum = 0.f;
+    const float nm = -m;
+    if constexpr (!LAST) sn = v16f{};
+#pragma unroll
+    for (int kc = 0; kc < T::NKC; ++kc) {
+      if constexpr (!LAST) mma_chunk<DT>(sn, kf.x[kc], qf[kc]);
+      if (kc >= VS && kc < VS + CT) v_read(half, 0, kc - VS, vf[0][kc - VS]);     // (into registers kf has left)
+#pragma unroll
+      for (int e = kc * EPS; e < (kc + 1) * EPS; e += 2) {
+        const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[e], a.scale_log2, nm));
+        const float p1 = __builtin_amdgcn_exp2f(fmaf(sc[e + 1], a.scale_log2, nm));
+        psum += p0;
+        psum += p1;
+        pw[e >> 1] = pack_two<DT>(p0, p1);
+      }
+    }
+    l += psum;
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) v_read(half, 1, ct, vf[1][ct]);
+    if constexpr (!LAST) k_read(half, kf);
+    u32x4 pb[2];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) { pb[s].x = pw[4 * s]; pb[s].y = pw[4 * s + 1]; pb[s].z = pw[4 * s + 2]; pb[s].w = pw[4 * s + 3]; }
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) mma_chunk<DT>(oacc[ct], vf[s][ct], pb[s]);
+    if constexpr (!LAST) tmax = half_max(sn);        // (beside the second product, which leaves the vector units idle)
+  };
+  // Tile t's barrier: K(t + 1) and V(t) are complete in LDS, and nobody still reads K(t) (its second half was requested
+  // before) or V(t - 1), whose buffers are filled next.
+  auto top = [&](int t) {
+    wait_all_loads();
+    __syncthreads();
+    if (t + 1 < ntiles) v_issue(t + 1, gv);
+    if (t + 2 < ntiles) k_issue(t + 2, gk);
+    gv = gk;
+    gk = group(t + 3);
+  };
+  int turn = TILE_B;
+  auto next_buffers = [&]() {                        // tile t + 1: V from the other buffer, K (of t + 2) too
+    kaddr -= turn;
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) vaddr[ct] += turn;
+    turn = -turn;
+  };
+  if (ntiles > 0) {
+    wait_all_loads();
+    __syncthreads();
+    k_read(0, kf);
+    s0 = v16f{};
+#pragma unroll
+    for (int kc = 0; kc < T::NKC; ++kc) mma_chunk<DT>(s0, kf.x[kc], qf[kc]);
+    k_read(1, kf);
+    kaddr += TILE_B;                                 // the K operands of a step are read one tile ahead
+    tmax = half_max(s0);
+  }
+  const int t_full = nh > 0 ? (nh - 1) / 2 : 0;      // tiles of whose halves none is the wave's last
+  int t = 0;
+  for (; t < t_full; ++t) {
+    const int key0 = tile_of(x, x.t_lo + t) * KEYS;
+    top(t);
+    step(std::false_type{}, 0, key0, s0, s1);
+    step(std::false_type{}, 1, key0 + 32, s1, s0);
+    next_buffers();
+  }
+  if (nh > 0) {                                      // the tile of the last (t < ntiles: the wave has rows)
+    const int key0 = tile_of(x, x.t_lo + t) * KEYS;
+    top(t++);
+    if (nh & 1) {
+      step(std::true_type{}, 0, key0, s0, s1);
+    } else {
+      step(std::false_type{}, 0, key0, s0, s1);
+      step(std::true_type{}, 1, key0 + 32, s1, s0);
+    }
+  }
+  for (; t < ntiles; ++t) top(t);                    // the other waves' tiles: their transfers and barriers
+
+  // ---- normalise and store: lane = row, accumulator v of tile ct = channel 32 ct + acc_row(v, kh) ----
+  const float l_tot = l + __shfl_xor(l, 32);
+  if (pos == INT_MIN) return;
+  const int j = pos - (x.kv - x.nq);
+  const bool whole = x.parts == 1;
+  const float inv = !whole ? 1.f : l_tot == 0.f ? 0.f : 1.f / l_tot;
+  const int64_t prow = (int64_t)blockIdx.x * RB + 32 * w + r, hq = hk * a.G + (wi + r - j * a.G), tok = x.qs + j;
+  uint8_t* orow = a.o + hq * a.o_sH + tok * a.o_sT;
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+    for (int v4 = 0; v4 < 4; ++v4) {
+      const int c = 32 * ct + acc_row(4 * v4, kh);        // four consecutive channels
+      const float4 o = make_float4(oacc[ct][4 * v4] * inv, oacc[ct][4 * v4 + 1] * inv, oacc[ct][4 * v4 + 2] * inv, oacc[ct][4 * v4 + 3] * inv);
+      if (!whole) *reinterpret_cast<float4*>(a.part_o + prow * D + c) = o;
+      else *reinterpret_cast<uint2*>(orow + c * 2) = make_uint2(pack_two<DT>(o.x, o.y), pack_two<DT>(o.z, o.w));
+    }
+  if (kh == 0) {
+    if (!whole) *reinterpret_cast<float2*>(a.part_ml + prow * 2) = make_float2(m, l_tot);
+    else if (a.lse) a.lse[hq * a.T + tok] = l_tot == 0.f ? -INFINITY : (m + log2f(l_tot)) * kLn2;
+  }
+}
+
 // ---- the join of split blocks ---------------------------------------------------------------------------
 // A workgroup per row block; D / 4 threads take a row.
 template <int DT, int D, int RB, int KT, int LEAST>
@@ -435,26 +702,37 @@ __global__ __launch_bounds__(256) void k_paged_join(PagedArgs a) {
 }
 
 // ---- host ---------------------------------------------------------------------------------------------
-// How a call's rows are cut: units that splitting aims at (0: nothing is split) and row blocks, at most, of a head.
-struct Cut { int64_t target, blocks; };
+// How a call's rows are cut: rows of a block, units of a head that splitting aims at (0: nothing is split), row blocks of a head, at most.
+struct Cut { int64_t rows, target, blocks; };
 constexpr int64_t kPlaces = 512;               // workgroups the chip holds at a time
 
-static Cut cut_of(int64_t R, int64_t T, int64_t G, int64_t Hkv, int rows) {
+static Cut cut_of(int64_t R, int64_t T, int64_t G, int64_t Hkv, int dtype) {
   Cut c;
-  c.blocks = T * G / rows + (R < T ? R : T);   // (a request has one block that is not full)
+  c.rows = dtype != ZC_F32 && T * G > 48 * R ? 128 : 32;
+  c.blocks = T * G / c.rows + (R < T ? R : T);   // (a request has one block that is not full)
   c.target = c.blocks * Hkv > 2 * kPlaces ? 0 : ceil_div64(kPlaces, Hkv);
   return c;
+}
+static size_t workspace_of(const Cut& c, int64_t Hkv, int64_t D) {
+  return c.target ? (size_t)(c.target + c.blocks) * Hkv * c.rows * (D + 2) * sizeof(float) : 0;
 }
 
 template <int DT, int D>
 static int launch_paged(PagedArgs& a, const Cut& cut, hipStream_t st) {
-  const dim3 units((unsigned)((cut.target + cut.blocks) * a.Hkv)), blocks((unsigned)(cut.blocks * a.Hkv));
+  const dim3 units((unsigned)(a.units * a.Hkv)), blocks((unsigned)(cut.blocks * a.Hkv));
+  if constexpr (DT != ZC_F32) {
+    if (cut.rows == 128) {
+      hipLaunchKernelGGL((k_paged_tiles<DT, D>), units, dim3(256), 0, st, a);
+      ZC_LAUNCH_CHECK();
+      if (cut.target) hipLaunchKernelGGL((k_paged_join<DT, D, 128, 64, kTilesLeast>), blocks, dim3(256), 0, st, a);
+      ZC_LAUNCH_CHECK();
+      return ZC_OK;
+    }
+  }
   hipLaunchKernelGGL((k_paged_rows<DT, D, 4>), units, dim3(256), 0, st, a);
   ZC_LAUNCH_CHECK();
-  if (cut.target) {
-    hipLaunchKernelGGL((k_paged_join<DT, D, 32, 32, kRowsLeast>), blocks, dim3(256), 0, st, a);
-    ZC_LAUNCH_CHECK();
-  }
+  if (cut.target) hipLaunchKernelGGL((k_paged_join<DT, D, 32, 32, kRowsLeast>), blocks, dim3(256), 0, st, a);
+  ZC_LAUNCH_CHECK();
   return ZC_OK;
 }
 
@@ -462,10 +740,11 @@ static int launch_paged(PagedArgs& a, const Cut& cut, hipStream_t st) {
 
 using namespace zc;
 
+// (the larger of what fp32 and 16-bit calls take: the types' blocks differ)
 extern "C" size_t zc_paged_attention_workspace(int64_t R, int64_t T, int64_t Hq, int64_t Hkv, int64_t D) {
   if (R <= 0 || T <= 0 || Hkv <= 0 || Hq < Hkv || Hq % Hkv || D <= 0) return 0;
-  const Cut c = cut_of(R, T, Hq / Hkv, Hkv, 32);
-  return c.target ? (size_t)(c.target + c.blocks) * Hkv * 32 * (D + 2) * sizeof(float) : 0;
+  const size_t x = workspace_of(cut_of(R, T, Hq / Hkv, Hkv, ZC_F32), Hkv, D), y = workspace_of(cut_of(R, T, Hq / Hkv, Hkv, ZC_F16), Hkv, D);
+  return x > y ? x : y;
 }
 
 extern "C" int zc_paged_attention(const zc_tensor4* q, const zc_tensor4* k_pages, const zc_tensor4* v_pages, const int32_t* block_table,
@@ -487,7 +766,7 @@ extern "C" int zc_paged_attention(const zc_tensor4* q, const zc_tensor4* k_pages
     if (reinterpret_cast<uintptr_t>(p) & 3) return ZC_ERR_INVALID_ARG;
   const int64_t T = q->L, Hkv = k_pages->H, G = q->H / Hkv;
   if (R >= (1 << 24) || max_blocks > 0x7fffffff || T > 0x7fffffff / q->H || q->H > 65535) return ZC_ERR_UNSUPPORTED;
-  const Cut cut = cut_of(R, T, G, Hkv, 32);
+  const Cut cut = cut_of(R, T, G, Hkv, q->dtype);
   if ((cut.target + cut.blocks) * Hkv > 0xffffff) return ZC_ERR_UNSUPPORTED;
   const size_t need = zc_paged_attention_workspace(R, T, q->H, Hkv, q->D);
   if (need && (!ws || ws_bytes < need || (reinterpret_cast<uintptr_t>(ws) & 15))) return ZC_ERR_WORKSPACE;
@@ -510,7 +789,7 @@ extern "C" int zc_paged_attention(const zc_tensor4* q, const zc_tensor4* k_pages
   a.units = (int)(cut.target + cut.blocks);
   const int64_t parts = (cut.target + cut.blocks) * Hkv;
   a.part_o = (float*)ws;
-  a.part_ml = need ? (float*)ws + parts * 32 * q->D : nullptr;
+  a.part_ml = need ? (float*)ws + parts * cut.rows * q->D : nullptr;
   hipStream_t st = (hipStream_t)stream;
 #define ZC_PA(DT) (q->D == 128 ? launch_paged<DT, 128>(a, cut, st) : launch_paged<DT, 64>(a, cut, st))
   if (q->dtype == ZC_F32) rc = ZC_PA(ZC_F32);
