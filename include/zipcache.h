@@ -377,7 +377,7 @@ int zc_paged_load(const zc_tensor4* k_pages, const zc_tensor4* v_pages, const in
  * pos = kv_len[r] - nq + j (its keys and values are in the pages already) and sees the tokens i <= pos,
  * with window > 0 only those with i > pos - window or i < sinks:
  *   out[h, t, :] = sum_i softmax_i(q[h, t] . k[h/G, i] * sm_scale) v[h/G, i, :]
- * q, out [1, Hq, T, D] of the pools' type, Hq a multiple of Hkv (any group); sm_scale == 0 means
+ * q, out [1, Hq, T, D] of the pools' type, Hq / Hkv whole and at most 4096; sm_scale == 0 means
  * 1/sqrt(D), a negative one is refused.  lse (device float [Hq, T], optional) receives the natural-log
  * normalisers (for zc_probe_saliency's lse_ext).  A row that sees no token (kv_len < nq), or only logits of
  * -inf, has zeros for its output and -inf for its normaliser.  A request may have no new tokens.

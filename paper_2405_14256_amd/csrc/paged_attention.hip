@@ -30,8 +30,11 @@ struct PagedArgs {
   int R, T, Hkv, G, window, sinks;
   float scale_log2;
   float* lse;                                   // [Hq, T] or null
-  int target;                                   // units a head's rows are split into, about; 0: nothing is split
-  int units;                                    // of a head, at most
+  int target, units;                            // units a head's rows are split into, about (0: nothing is split); at most
+  uint32_t over_G;                              // ceil(2^32 / G)
+  int reach;                                    // tiles that a block of rows sees under the window, at most
+  int slot;                                     // rows of a unit's partial results
+  int coarse;                                   // tiles are added up in steps of 2^coarse (sums stay within 32 bits)
   float *part_o, *part_ml;                      // of split units: [unit][row][D], [unit][row][2] (reference, sum)
 };
 
@@ -50,101 +53,114 @@ __device__ inline uint32_t pack_two(float lo, float hi) {
 }
 
 // ---- the work of a wave ---------------------------------------------------------------------------
+// Key tiles are of 64 keys.  A request of few rows goes in blocks of 32 rows whose keys four waves share, any other (of 16-bit
+// types) in blocks of 128, 32 a wave: with one token a request the first way has four waves at work where the second has one,
+// and the first waits for no barrier; with many rows the second reads a key once for four times as many.
+constexpr int kTile = 64;
+template <int DT> struct Blocks {
+  static constexpr int kMany = DT == ZC_F32 ? 32 : 128;                   // rows of a block, of many rows
+  __device__ static bool few(int rows) { return DT == ZC_F32 || rows <= 32; }
+};
+
 struct Unit {
   int r, qs, nq, kv;            // request, its first row, new tokens, tokens
-  int i0, rows;                 // first (token, head) row of the block, how many
+  bool few;
+  int j0, g0, rows;             // token and head of the block's first row, its rows
   int p0, p1;                   // positions of its first and last row
   int first, sink_tiles;        // tile t is t of the first sink_tiles, then first + t - sink_tiles
   int t_lo, t_hi;               // tiles of this unit
-  int part, parts;              // which of the parts of the block's tiles
+  int parts;                    // that the block's tiles are divided into
   int index;                    // of the block's first unit among the head's
 };
+
+// Row r of a block: its token (after the block's first) and head.
+struct Row { int j, g; };
+__device__ inline Row row_at(const PagedArgs& a, const Unit& x, int r) {
+  const int v = x.g0 + r, j = a.G == 1 ? v : (int)__umulhi((uint32_t)v, a.over_G);    // (exact while v G < 2^32)
+  return {x.j0 + j, v - j * a.G};
+}
 
 struct Request { int qs, nq, kv; };
 __device__ inline Request request(const PagedArgs& a, int r) {
   Request x = {0, 0, 0};
   if (r < a.R) {
-    x.qs = min(max(a.q_start[r], 0), a.T);
-    x.nq = max(min(a.q_start[r + 1], a.T) - x.qs, 0);
-    x.kv = min(max(a.kv_len[r], 0), a.cap);
+    const int s = a.q_start[r], e = a.q_start[r + 1], kv = a.kv_len[r];
+    x.qs = min(max(s, 0), a.T);
+    x.nq = max(min(e, a.T) - x.qs, 0);
+    x.kv = min(max(kv, 0), a.cap);
   }
   return x;
 }
 
-template <int RB>
-__device__ inline int row_blocks(const PagedArgs& a, const Request& x) { return (int)(((uint32_t)x.nq * a.G + RB - 1) / RB); }
-
-// Key tiles that a block of the request's rows sees, at most.
-template <int RB, int KT>
-__device__ inline int key_tiles(const PagedArgs& a, const Request& x) {
-  if (x.nq == 0) return 0;
-  const int all = (x.kv + KT - 1) / KT;
-  if (!a.window) return all;
-  // (RB rows are of RB / G + 2 tokens at most)
-  return min(all, (a.window + RB / a.G + 2 + KT - 2) / KT + 1 + (a.sinks + KT - 1) / KT);
-}
-
-__device__ inline int64_t wave_sum64(int64_t v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor((long long)v, o);
-  return v;
-}
-
-// The unit with index u of a head, BLOCKS: the row block with index u.  LEAST tiles at least make a part.
-template <int RB, int KT, int LEAST, bool BLOCKS>
+// The unit with index u of a head; BLOCKS: the row block with index u.
+template <int DT, bool BLOCKS>
 __device__ inline bool find_unit(const PagedArgs& a, int u, Unit& x) {
+  using B = Blocks<DT>;
   const int lane = threadIdx.x & 63;
+  struct Size { int blocks, tiles, least; };               // row blocks; tiles that one sees, at most, and that make a part
+  auto size = [&](const Request& t) {
+    const int rows = t.nq * a.G;
+    Size s;
+    s.blocks = B::few(rows) ? (rows + 31) / 32 : (rows + B::kMany - 1) / B::kMany;
+    s.tiles = min((t.kv + kTile - 1) / kTile, a.reach);
+    s.least = B::few(rows) ? 2 : 4;                        // (32 keys a wave)
+    return s;
+  };
   const Request head = request(a, lane);
-  int per = INT_MAX;                                        // tiles of a part, at most
+  int per = INT_MAX;                                       // tiles of a part, at most
   if (a.target) {
-    int64_t all = (int64_t)row_blocks<RB>(a, head) * key_tiles<RB, KT>(a, head);
-    for (int r0 = 64; r0 < a.R; r0 += 64) {
-      const Request t = request(a, r0 + lane);
-      all += (int64_t)row_blocks<RB>(a, t) * key_tiles<RB, KT>(a, t);
-    }
-    all = wave_sum64(all);
-    const int64_t each = (all + a.target - 1) / a.target;
-    per = each < LEAST ? LEAST : each > INT_MAX / 2 ? INT_MAX / 2 : (int)each;
-    per = __builtin_amdgcn_readfirstlane(per);
+    auto work = [&](const Request& t) {
+      const Size s = size(t);
+      return s.blocks * ((s.tiles + (1 << a.coarse) - 1) >> a.coarse);
+    };
+    int all = work(head);
+    for (int r0 = 64; r0 < a.R; r0 += 64) all += work(request(a, r0 + lane));
+    all = __builtin_amdgcn_readlane(wave_inclusive_sum(all), 63);
+    per = (int)(((uint32_t)all + a.target - 1) / (uint32_t)a.target) << a.coarse;
   }
   int units = 0, blocks = 0;
   for (int r0 = 0; r0 < a.R; r0 += 64) {
     const Request t = r0 ? request(a, r0 + lane) : head;
-    const int nb = row_blocks<RB>(a, t), nt = key_tiles<RB, KT>(a, t);
-    const int parts = nt <= per ? 1 : (nt - 1) / per + 1;
-    const int cu = wave_inclusive_sum(nb * parts), cb = BLOCKS ? wave_inclusive_sum(nb) : 0;
+    const Size s = size(t);
+    const int most = max(per, s.least);
+    const int parts = s.tiles <= most ? 1 : (int)((uint32_t)(s.tiles - 1) / (uint32_t)most) + 1;
+    const int cu = wave_inclusive_sum(s.blocks * parts), cb = BLOCKS ? wave_inclusive_sum(s.blocks) : 0;
     const uint64_t here = __builtin_amdgcn_ballot_w64(BLOCKS ? u < blocks + cb : u < units + cu);
     if (here) {
       const int l = __builtin_ctzll(here);
       const auto of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
       x.r = r0 + l;
       x.qs = of(t.qs); x.nq = of(t.nq); x.kv = of(t.kv);
-      const int n = of(nb);
+      const int n = of(s.blocks), all_rows = x.nq * a.G;
+      x.few = B::few(all_rows);
       x.parts = of(parts);
       const int first_unit = units + of(cu) - n * x.parts;
-      int b;
+      int b, part = 0;
       if constexpr (BLOCKS) {
         b = u - (blocks + of(cb) - n);
-        x.part = 0;
       } else {
-        const int rest = u - first_unit;
-        b = rest / x.parts;
-        x.part = rest - b * x.parts;
+        b = x.parts == 1 ? u - first_unit : (int)((uint32_t)(u - first_unit) / (uint32_t)x.parts);
+        part = u - first_unit - b * x.parts;
       }
       x.index = first_unit + b * x.parts;
-      b = n - 1 - b;                                        // (a chunk's last rows see the most keys: first)
-      const int all_rows = x.nq * a.G;
-      x.i0 = b * RB;
-      x.rows = min(RB, all_rows - x.i0);
-      x.p0 = x.kv - x.nq + x.i0 / a.G;
-      x.p1 = x.kv - x.nq + (x.i0 + x.rows - 1) / a.G;
+      b = n - 1 - b;                                       // (a chunk's last rows see the most keys: first)
+      const int rb = x.few ? 32 : B::kMany, i0 = b * rb;
+      x.j0 = i0 == 0 ? 0 : (int)((uint32_t)i0 / (uint32_t)a.G);
+      x.g0 = i0 - x.j0 * a.G;
+      x.rows = min(rb, all_rows - i0);
+      x.p0 = x.kv - x.nq + x.j0;
+      x.p1 = x.kv - x.nq + row_at(a, x, x.rows - 1).j;
       const int low = a.window ? max(0, x.p0 - a.window + 1) : 0;
-      x.first = low / KT;
-      x.sink_tiles = min((min(a.sinks, low) + KT - 1) / KT, x.first);
-      const int tiles = x.p1 < 0 ? 0 : x.sink_tiles + x.p1 / KT + 1 - x.first;
-      const int q = tiles / x.parts, rem = tiles - q * x.parts;
-      x.t_lo = x.part * q + min(x.part, rem);
-      x.t_hi = x.t_lo + q + (x.part < rem ? 1 : 0);
+      x.first = low / kTile;
+      x.sink_tiles = min((min(a.sinks, low) + kTile - 1) / kTile, x.first);
+      const int tiles = x.p1 < 0 ? 0 : x.sink_tiles + x.p1 / kTile + 1 - x.first;
+      x.t_lo = 0;
+      x.t_hi = tiles;
+      if (x.parts > 1) {
+        const int q = (int)((uint32_t)tiles / (uint32_t)x.parts), rem = tiles - q * x.parts;
+        x.t_lo = part * q + min(part, rem);
+        x.t_hi = x.t_lo + q + (part < rem ? 1 : 0);
+      }
       return true;
     }
     units += __builtin_amdgcn_readlane(cu, 63);
@@ -154,6 +170,7 @@ __device__ inline bool find_unit(const PagedArgs& a, int u, Unit& x) {
 }
 
 __device__ inline int tile_of(const Unit& x, int t) { return t < x.sink_tiles ? t : x.first + t - x.sink_tiles; }
+__device__ inline int unit_of_grid() { return blockIdx.y + 65535 * blockIdx.z; }
 
 // The page of 16 keys from key0 on, -1 where there is none.
 __device__ inline int page_of(const PagedArgs& a, const Unit& x, int key0) {
@@ -185,31 +202,34 @@ __device__ inline int v_slot(int key) {
   return D == 128 ? 4 * (key & 3) ^ (key & 2) : 2 * (key & 2) ^ 2 * (key & 1);
 }
 
+// First row of the partial results of a head's unit.
+__device__ inline int64_t part_row(const PagedArgs& a, int hk, int unit) { return ((int64_t)hk * a.units + unit) * a.slot; }
+
 // ---- blocks of 32 rows: single tokens, short chunks, fp32 ---------------------------------------------
-// NW waves share the keys of 32 rows, a wave every NW-th 32 keys, in a place of its own in LDS for one K and one V block: a
+// Four waves share the keys of 32 rows, a wave every fourth 32 keys, in a place of its own in LDS for one K and one V block: a
 // block's K is requested when the one before has been multiplied, its V likewise, so that a wave has one of them in flight
 // at any time and waits for nobody.
-constexpr int kRowsLeast = 4;   // blocks of 32 keys that make a part: one a wave
-template <int DT, int D, int NW>
-__global__ __launch_bounds__(64 * NW, DT == ZC_F32 && D == 128 ? 1 : 2) void k_paged_rows(PagedArgs a) {
+template <int DT, int D>
+struct RowsMemory {
+  static constexpr int kBlock = 32 * Tile<DT, D>::ROWB;                   // bytes of a block of keys or values
+  static constexpr int kBytes = 8 * kBlock;
+};
+template <int DT, int D>
+__device__ __forceinline__ void attend_rows(const PagedArgs& a, const Unit& x, int hk, uint8_t* mem, float (*sum)[2][64]) {
   using T = Tile<DT, D>;
-  constexpr int BLK = 32 * T::ROWB;              // bytes of a block
+  constexpr int NW = 4;
+  constexpr int BLK = RowsMemory<DT, D>::kBlock;
   constexpr int NT = BLK / 1024;                 // transfers of a block
   constexpr int PG = 16 / T::RPI;                // of 16 keys
   constexpr int CT = D / 32;
   static_assert(NW * 2 * BLK >= NW * CT * 4 * 64 * 16 && CT * 4 % NW == 0, "the waves' outputs fit where their keys were");
-  __shared__ __align__(1024) uint8_t mem[NW * 2 * BLK];
-  __shared__ float sum[NW][2][64];
   typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-  const int hk = blockIdx.x % a.Hkv;
-  Unit x;
-  if (!find_unit<32, 32, kRowsLeast, false>(a, blockIdx.x / a.Hkv, x)) return;
   const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, kh = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const uint8_t* kb = a.k + hk * a.k_sH;
   const uint8_t* vb = a.v + hk * a.v_sH;
-  const uint32_t mem_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)&mem[0];
+  const uint32_t mem_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)mem;
   const uint32_t k_lds = mem_lds + w * 2 * BLK, v_lds = k_lds + BLK;
 
   int kvoff[PG], vvoff[PG];
@@ -220,9 +240,9 @@ __global__ __launch_bounds__(64 * NW, DT == ZC_F32 && D == 128 ? 1 : 2) void k_p
     vvoff[j] = (int)(row * a.v_row) + (((lane % T::CPR) ^ v_slot<DT, D>(row)) << 4);
   }
   struct Ids { int id[2], n[2], key0; };
-  auto pages = [&](int t) {
+  auto pages = [&](int b) {                      // of the unit's block b of 32 keys, two to a tile
     Ids s;
-    s.key0 = tile_of(x, t) * 32;
+    s.key0 = tile_of(x, x.t_lo + (b >> 1)) * kTile + 32 * (b & 1);
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
       s.id[g] = page_of(a, x, s.key0 + 16 * g);
@@ -239,9 +259,12 @@ __global__ __launch_bounds__(64 * NW, DT == ZC_F32 && D == 128 ? 1 : 2) void k_p
     }
   };
 
-  int t = x.t_lo + w;
+  // (the tile of the last row's own token may have one block only)
+  int blocks = 2 * (x.t_hi - x.t_lo);
+  if (blocks > 0 && tile_of(x, x.t_hi - 1) * kTile + 32 > x.p1) --blocks;
+  int t = w;
   Ids at;
-  if (t < x.t_hi) {
+  if (t < blocks) {
     at = pages(t);
     issue(at, kb, a.k_sB, a.k_row, k_lds, kvoff);
     issue(at, vb, a.v_sB, a.v_row, v_lds, vvoff);
@@ -249,9 +272,9 @@ __global__ __launch_bounds__(64 * NW, DT == ZC_F32 && D == 128 ? 1 : 2) void k_p
 
   // this lane's row, straight into operand registers
   const bool mine = r < x.rows;
-  const int i = x.i0 + r, j = i / a.G;
-  const int64_t hq = hk * a.G + (i - j * a.G), tok = x.qs + j;
-  const int pos = mine ? x.kv - x.nq + j : -1;
+  const Row me = row_at(a, x, r);
+  const int64_t hq = hk * a.G + me.g, tok = x.qs + me.j;
+  const int pos = mine ? x.kv - x.nq + me.j : -1;
   u32x4 qf[T::NKC];
 #pragma unroll
   for (int kc = 0; kc < T::NKC; ++kc) qf[kc] = u32x4{0, 0, 0, 0};
@@ -277,8 +300,8 @@ __global__ __launch_bounds__(64 * NW, DT == ZC_F32 && D == 128 ? 1 : 2) void k_p
   for (int ct = 0; ct < CT; ++ct) oacc[ct] = v16f{};
   float m = kLowestLogit, l = 0.f;   // running maximum (log2 units), this half-wave's share of the sum
 
-  for (; t < x.t_hi; t += NW) {
-    const bool more = t + NW < x.t_hi;
+  for (; t < blocks; t += NW) {
+    const bool more = t + NW < blocks;
     const int key0 = at.key0;
     if (more) at = pages(t + NW);
     wait_vmem<NT>();                                       // K is there (V was requested after it)
@@ -380,7 +403,7 @@ __global__ __launch_bounds__(64 * NW, DT == ZC_F32 && D == 128 ? 1 : 2) void k_p
     l_tot = fmaf(sum[v][1][lane], f[v], l_tot);
   }
   const bool whole = x.parts == 1;
-  const int64_t prow = ((int64_t)blockIdx.x * 32 + r);
+  const int64_t prow = part_row(a, hk, unit_of_grid()) + r;
   const float inv = !whole ? 1.f : l_tot == 0.f ? 0.f : 1.f / l_tot;
   uint8_t* orow = a.o + hq * a.o_sH + tok * a.o_sT;
 #pragma unroll
@@ -412,33 +435,28 @@ __global__ __launch_bounds__(64 * NW, DT == ZC_F32 && D == 128 ? 1 : 2) void k_p
 // Bound by the matrix cores: a half is 16 matrix instructions of 32 cycles (128 channels) and about 300 cycles of vector
 // instructions, so the two have to run at the same time: the logits of half h + 1 are multiplied while the exponentials of
 // half h are taken, and the operands of each product are requested one phase before.
-constexpr int kTilesLeast = 4;  // tiles of 64 keys that make a part
 template <int DT, int D>
-__global__ __launch_bounds__(256, 2) void k_paged_tiles(PagedArgs a) {
+__device__ __forceinline__ void attend_tiles(const PagedArgs& a, const Unit& x, int hk, uint8_t* mem) {
   using T = Tile<DT, D>;
-  constexpr int KEYS = 64, RB = 128;
+  constexpr int KEYS = kTile;
   constexpr int TILE_B = KEYS * T::ROWB;
   constexpr int NI = 16 / T::RPI;                // transfers per wave, tile and tensor
   constexpr int CT = D / 32;                     // 32-channel tiles of the output
   constexpr int EPS = 16 / T::NKC;               // logits per slice
   constexpr int VS = T::NKC / 4;                 // the slice that requests the first V operand
-  __shared__ __align__(1024) uint8_t Ks[2][TILE_B];
-  __shared__ __align__(1024) uint8_t Vs[2][TILE_B];
+  static_assert(RowsMemory<DT, D>::kBytes == 4 * TILE_B, "two K tiles, two V tiles");
   typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-  const int hk = blockIdx.x % a.Hkv;
-  Unit x;
-  if (!find_unit<RB, KEYS, kTilesLeast, false>(a, blockIdx.x / a.Hkv, x)) return;
   const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, kh = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const uint8_t* kb = a.k + hk * a.k_sH;
   const uint8_t* vb = a.v + hk * a.v_sH;
-  const uint32_t ks_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)&Ks[0][0] + w * 16 * T::ROWB;
-  const uint32_t vs_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)&Vs[0][0] + w * 16 * T::ROWB;
+  const uint32_t ks_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)mem + w * 16 * T::ROWB;
+  const uint32_t vs_lds = ks_lds + 2 * TILE_B;
 
   // this wave's rows, and the halves of this unit that they see: all up to the last row's
-  const int wi = x.i0 + 32 * w, wrows = min(max(x.rows - 32 * w, 0), 32);
-  const int wp0 = x.kv - x.nq + wi / a.G, wp1 = wrows > 0 ? x.kv - x.nq + (wi + wrows - 1) / a.G : -1;
+  const int wrows = min(max(x.rows - 32 * w, 0), 32);
+  const int wp0 = x.kv - x.nq + row_at(a, x, 32 * w).j, wp1 = wrows > 0 ? x.kv - x.nq + row_at(a, x, 32 * w + wrows - 1).j : -1;
   const int ntiles = x.t_hi - x.t_lo;
   int nh = 0;
   if (wp1 >= 0) {
@@ -485,13 +503,13 @@ __global__ __launch_bounds__(256, 2) void k_paged_tiles(PagedArgs a) {
   }
 
   // this lane's row, straight into operand registers
-  const int pos = r < wrows ? x.kv - x.nq + (wi + r) / a.G : INT_MIN;
+  const int pos = r < wrows ? x.kv - x.nq + row_at(a, x, 32 * w + r).j : INT_MIN;
   u32x4 qf[T::NKC];
 #pragma unroll
   for (int kc = 0; kc < T::NKC; ++kc) qf[kc] = u32x4{0, 0, 0, 0};
   if (r < wrows) {
-    const int j = (wi + r) / a.G;
-    const uint8_t* qr = a.q + (hk * a.G + (wi + r - j * a.G)) * a.q_sH + (int64_t)(x.qs + j) * a.q_sT + kh * 16;
+    const Row me = row_at(a, x, 32 * w + r);
+    const uint8_t* qr = a.q + (hk * a.G + me.g) * a.q_sH + (int64_t)(x.qs + me.j) * a.q_sT + kh * 16;
 #pragma unroll
     for (int kc = 0; kc < T::NKC; ++kc) qf[kc] = *reinterpret_cast<const u32x4*>(qr + kc * 32);
   }
@@ -649,10 +667,10 @@ __global__ __launch_bounds__(256, 2) void k_paged_tiles(PagedArgs a) {
   // ---- normalise and store: lane = row, accumulator v of tile ct = channel 32 ct + acc_row(v, kh) ----
   const float l_tot = l + __shfl_xor(l, 32);
   if (pos == INT_MIN) return;
-  const int j = pos - (x.kv - x.nq);
+  const Row me = row_at(a, x, 32 * w + r);
   const bool whole = x.parts == 1;
   const float inv = !whole ? 1.f : l_tot == 0.f ? 0.f : 1.f / l_tot;
-  const int64_t prow = (int64_t)blockIdx.x * RB + 32 * w + r, hq = hk * a.G + (wi + r - j * a.G), tok = x.qs + j;
+  const int64_t prow = part_row(a, hk, unit_of_grid()) + 32 * w + r, hq = hk * a.G + me.g, tok = x.qs + me.j;
   uint8_t* orow = a.o + hq * a.o_sH + tok * a.o_sT;
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct)
@@ -669,70 +687,128 @@ __global__ __launch_bounds__(256, 2) void k_paged_tiles(PagedArgs a) {
   }
 }
 
-// ---- the join of split blocks ---------------------------------------------------------------------------
-// A workgroup per row block; D / 4 threads take a row.
-template <int DT, int D, int RB, int KT, int LEAST>
-__global__ __launch_bounds__(256) void k_paged_join(PagedArgs a) {
-  const int hk = blockIdx.x % a.Hkv;
+// Four channels of a row whose parts are together: reference M, sum l, weighted values o.
+template <int DT>
+__device__ inline void store_row(const PagedArgs& a, const Unit& x, int hk, int row, int c, float M, float l, float4 o) {
+  const Row me = row_at(a, x, row);
+  const int64_t hq = hk * a.G + me.g, tok = x.qs + me.j;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  uint8_t* orow = a.o + hq * a.o_sH + tok * a.o_sT;
+  if constexpr (DT == ZC_F32) *reinterpret_cast<float4*>(orow + c * 4) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+  else *reinterpret_cast<uint2*>(orow + c * 2) = make_uint2(pack_two<DT>(o.x * inv, o.y * inv), pack_two<DT>(o.z * inv, o.w * inv));
+  if (a.lse && c == 0) a.lse[hq * a.T + tok] = l == 0.f ? -INFINITY : (M + log2f(l)) * kLn2;
+}
+
+template <int DT, int D>
+__global__ __launch_bounds__(256, DT == ZC_F32 && D == 128 ? 1 : 2) void k_paged_attention(PagedArgs a) {
+  __shared__ __align__(1024) uint8_t mem[RowsMemory<DT, D>::kBytes];
+  __shared__ float sum[4][2][64];
+  const int hk = blockIdx.x;
   Unit x;
-  if (!find_unit<RB, KT, LEAST, true>(a, blockIdx.x / a.Hkv, x) || x.parts == 1 || x.index + x.parts > a.units) return;
-  constexpr int TPR = D / 4;
-  const int c = threadIdx.x % TPR * 4;
-  for (int row = threadIdx.x / TPR; row < x.rows; row += 256 / TPR) {
-    float M = kLowestLogit;
-    for (int s = 0; s < x.parts; ++s) M = fmaxf(M, a.part_ml[(((int64_t)(x.index + s) * a.Hkv + hk) * RB + row) * 2]);
-    float l = 0.f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int s = 0; s < x.parts; ++s) {
-      const int64_t p = ((int64_t)(x.index + s) * a.Hkv + hk) * RB + row;
-      const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + p * 2);
-      const float4 t = *reinterpret_cast<const float4*>(a.part_o + p * D + c);
-      const float f = __builtin_amdgcn_exp2f(ml.x - M);
-      l = fmaf(ml.y, f, l);
-      o.x = fmaf(t.x, f, o.x); o.y = fmaf(t.y, f, o.y); o.z = fmaf(t.z, f, o.z); o.w = fmaf(t.w, f, o.w);
+  if (!find_unit<DT, false>(a, unit_of_grid(), x)) return;
+  if constexpr (DT != ZC_F32) {
+    if (!x.few) {
+      attend_tiles<DT, D>(a, x, hk, mem);
+      return;
     }
-    const int i = x.i0 + row, j = i / a.G;
-    const int64_t hq = hk * a.G + (i - j * a.G), tok = x.qs + j;
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    uint8_t* orow = a.o + hq * a.o_sH + tok * a.o_sT;
-    if constexpr (DT == ZC_F32) *reinterpret_cast<float4*>(orow + c * 4) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-    else *reinterpret_cast<uint2*>(orow + c * 2) = make_uint2(pack_two<DT>(o.x * inv, o.y * inv), pack_two<DT>(o.z * inv, o.w * inv));
-    if (a.lse && c == 0) a.lse[hq * a.T + tok] = l == 0.f ? -INFINITY : (M + log2f(l)) * kLn2;
   }
+  attend_rows<DT, D>(a, x, hk, mem, sum);
+}
+
+// ---- the join of split blocks ---------------------------------------------------------------------------
+// A workgroup per row block.  D / 4 threads take a row; where rows are few, several such groups share a row's parts and
+// join what they have in LDS.  Bound by two trips to memory.
+constexpr int kJoinThreads = 512;
+template <int DT, int D>
+__global__ __launch_bounds__(kJoinThreads) void k_paged_join(PagedArgs a) {
+  constexpr int TPR = D / 4, GROUPS = kJoinThreads / TPR;
+  __shared__ __align__(16) float so[GROUPS][D];
+  __shared__ float2 sml[GROUPS];
+  const int hk = blockIdx.x;
+  Unit x;
+  if (!find_unit<DT, true>(a, unit_of_grid(), x) || x.parts == 1 || x.index + x.parts > a.units) return;
+  const int grp = threadIdx.x / TPR, c = threadIdx.x % TPR * 4;
+  int ways = 1;                                            // groups to a row
+  while (2 * ways * x.rows <= GROUPS && 2 * ways <= x.parts) ways *= 2;
+  const int way = grp & (ways - 1), at_once = GROUPS / ways;
+  const int64_t first = part_row(a, hk, x.index);
+  for (int row = grp / ways; row < x.rows; row += at_once) {
+    float M = kLowestLogit, l = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    constexpr int U = 4;                                   // parts requested at a time
+    for (int s0 = way; s0 < x.parts; s0 += U * ways) {
+      float2 ml[U];
+      float4 t[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int s = s0 + u * ways;
+        const int64_t p = first + (int64_t)(s < x.parts ? s : s0) * a.slot + row;
+        ml[u] = *reinterpret_cast<const float2*>(a.part_ml + p * 2);
+        t[u] = *reinterpret_cast<const float4*>(a.part_o + p * D + c);
+        if (s >= x.parts) ml[u] = make_float2(kLowestLogit, 0.f);
+      }
+      float top = M;
+#pragma unroll
+      for (int u = 0; u < U; ++u) top = fmaxf(top, ml[u].x);
+      const float f0 = __builtin_amdgcn_exp2f(M - top);
+      M = top;
+      l *= f0; o.x *= f0; o.y *= f0; o.z *= f0; o.w *= f0;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const float f = s0 + u * ways < x.parts ? __builtin_amdgcn_exp2f(ml[u].x - M) : 0.f;
+        l = fmaf(ml[u].y, f, l);
+        o.x = fmaf(t[u].x, f, o.x); o.y = fmaf(t[u].y, f, o.y); o.z = fmaf(t[u].z, f, o.z); o.w = fmaf(t[u].w, f, o.w);
+      }
+    }
+    if (ways > 1) {                                        // (all rows at once: every thread comes here once, or none of its wave's row)
+      if (c == 0) sml[grp] = make_float2(M, l);
+      *reinterpret_cast<float4*>(&so[grp][c]) = o;
+    } else {
+      store_row<DT>(a, x, hk, row, c, M, l, o);
+    }
+  }
+  if (ways == 1) return;
+  __syncthreads();
+  if (way != 0 || grp / ways >= x.rows) return;
+  float M = kLowestLogit, l = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int v = 0; v < ways; ++v) M = fmaxf(M, sml[grp + v].x);
+  for (int v = 0; v < ways; ++v) {
+    const float2 ml = sml[grp + v];
+    const float4 t = *reinterpret_cast<const float4*>(&so[grp + v][c]);
+    const float f = __builtin_amdgcn_exp2f(ml.x - M);
+    l = fmaf(ml.y, f, l);
+    o.x = fmaf(t.x, f, o.x); o.y = fmaf(t.y, f, o.y); o.z = fmaf(t.z, f, o.z); o.w = fmaf(t.w, f, o.w);
+  }
+  store_row<DT>(a, x, hk, grp / ways, c, M, l, o);
 }
 
 // ---- host ---------------------------------------------------------------------------------------------
-// How a call's rows are cut: rows of a block, units of a head that splitting aims at (0: nothing is split), row blocks of a head, at most.
-struct Cut { int64_t rows, target, blocks; };
+// How a call's rows are cut: row blocks of a head, at most; units of a head that splitting aims at (0: nothing is split); rows of a
+// unit's partial results.
+struct Cut { int64_t blocks, target, slot; };
 constexpr int64_t kPlaces = 512;               // workgroups the chip holds at a time
 
 static Cut cut_of(int64_t R, int64_t T, int64_t G, int64_t Hkv, int dtype) {
   Cut c;
-  c.rows = dtype != ZC_F32 && T * G > 48 * R ? 128 : 32;
-  c.blocks = T * G / c.rows + (R < T ? R : T);   // (a request has one block that is not full)
+  c.slot = dtype == ZC_F32 || T * G <= 32 ? 32 : 128;
+  c.blocks = T * G / c.slot + (R < T ? R : T);   // (a request has one block that is not full)
   c.target = c.blocks * Hkv > 2 * kPlaces ? 0 : ceil_div64(kPlaces, Hkv);
   return c;
 }
 static size_t workspace_of(const Cut& c, int64_t Hkv, int64_t D) {
-  return c.target ? (size_t)(c.target + c.blocks) * Hkv * c.rows * (D + 2) * sizeof(float) : 0;
+  return c.target ? (size_t)(c.target + c.blocks) * Hkv * c.slot * (D + 2) * sizeof(float) : 0;
 }
 
 template <int DT, int D>
-static int launch_paged(PagedArgs& a, const Cut& cut, hipStream_t st) {
-  const dim3 units((unsigned)(a.units * a.Hkv)), blocks((unsigned)(cut.blocks * a.Hkv));
-  if constexpr (DT != ZC_F32) {
-    if (cut.rows == 128) {
-      hipLaunchKernelGGL((k_paged_tiles<DT, D>), units, dim3(256), 0, st, a);
-      ZC_LAUNCH_CHECK();
-      if (cut.target) hipLaunchKernelGGL((k_paged_join<DT, D, 128, 64, kTilesLeast>), blocks, dim3(256), 0, st, a);
-      ZC_LAUNCH_CHECK();
-      return ZC_OK;
-    }
+static int launch_paged(PagedArgs& a, int64_t blocks, hipStream_t st) {
+  const auto grid = [&](int64_t n) { return dim3((unsigned)a.Hkv, (unsigned)(n < 65535 ? n : 65535), (unsigned)ceil_div64(n, 65535)); };
+  hipLaunchKernelGGL((k_paged_attention<DT, D>), grid(a.units), dim3(256), 0, st, a);
+  ZC_LAUNCH_CHECK();
+  if (a.target) {
+    hipLaunchKernelGGL((k_paged_join<DT, D>), grid(blocks), dim3(kJoinThreads), 0, st, a);
+    ZC_LAUNCH_CHECK();
   }
-  hipLaunchKernelGGL((k_paged_rows<DT, D, 4>), units, dim3(256), 0, st, a);
-  ZC_LAUNCH_CHECK();
-  if (cut.target) hipLaunchKernelGGL((k_paged_join<DT, D, 32, 32, kRowsLeast>), blocks, dim3(256), 0, st, a);
-  ZC_LAUNCH_CHECK();
   return ZC_OK;
 }
 
@@ -765,8 +841,8 @@ extern "C" int zc_paged_attention(const zc_tensor4* q, const zc_tensor4* k_pages
   for (const void* p : {(const void*)block_table, (const void*)q_start, (const void*)kv_len, (const void*)lse})
     if (reinterpret_cast<uintptr_t>(p) & 3) return ZC_ERR_INVALID_ARG;
   const int64_t T = q->L, Hkv = k_pages->H, G = q->H / Hkv;
-  if (R >= (1 << 24) || max_blocks > 0x7fffffff || T > 0x7fffffff / q->H || q->H > 65535) return ZC_ERR_UNSUPPORTED;
-  const Cut cut = cut_of(R, T, G, Hkv, q->dtype);
+  if (R >= (1 << 24) || max_blocks > 0x7fffffff || T > 0x7fffffff / q->H || q->H > 65535 || G > 4096) return ZC_ERR_UNSUPPORTED;
+  Cut cut = cut_of(R, T, G, Hkv, q->dtype);
   if ((cut.target + cut.blocks) * Hkv > 0xffffff) return ZC_ERR_UNSUPPORTED;
   const size_t need = zc_paged_attention_workspace(R, T, q->H, Hkv, q->D);
   if (need && (!ws || ws_bytes < need || (reinterpret_cast<uintptr_t>(ws) & 15))) return ZC_ERR_WORKSPACE;
@@ -785,13 +861,20 @@ extern "C" int zc_paged_attention(const zc_tensor4* q, const zc_tensor4* k_pages
   a.sinks = sinks > room ? (int)room : sinks;
   a.scale_log2 = (sm_scale == 0.f ? 1.0f / sqrtf((float)q->D) : sm_scale) * kLog2e;
   a.lse = lse;
+  if (room <= 2 * kTile) cut.target = 0;           // (no row has enough keys to be split)
   a.target = (int)cut.target;
   a.units = (int)(cut.target + cut.blocks);
+  a.slot = (int)cut.slot;
+  a.over_G = G == 1 ? 0 : (uint32_t)(((1ull << 32) + G - 1) / G);
+  // (a block's rows are of slot / G + 2 tokens at most)
+  a.reach = a.window ? (int)((a.window + cut.slot / G + 2 + kTile - 2) / kTile + 1 + (a.sinks + kTile - 1) / kTile) : 0x7fffffff;
+  a.coarse = 0;
+  while ((cut.blocks * (room / kTile + 1)) >> a.coarse > 0x3fffffff) ++a.coarse;
   const int64_t parts = (cut.target + cut.blocks) * Hkv;
   a.part_o = (float*)ws;
-  a.part_ml = need ? (float*)ws + parts * cut.rows * q->D : nullptr;
+  a.part_ml = need ? (float*)ws + parts * cut.slot * q->D : nullptr;
   hipStream_t st = (hipStream_t)stream;
-#define ZC_PA(DT) (q->D == 128 ? launch_paged<DT, 128>(a, cut, st) : launch_paged<DT, 64>(a, cut, st))
+#define ZC_PA(DT) (q->D == 128 ? launch_paged<DT, 128>(a, cut.blocks, st) : launch_paged<DT, 64>(a, cut.blocks, st))
   if (q->dtype == ZC_F32) rc = ZC_PA(ZC_F32);
   else if (q->dtype == ZC_F16) rc = ZC_PA(ZC_F16);
   else rc = ZC_PA(ZC_BF16);
