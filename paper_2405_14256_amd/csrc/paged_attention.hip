@@ -35,7 +35,8 @@ struct PagedArgs {
   int reach;                                    // tiles that a block of rows sees under the window, at most
   int slot;                                     // rows of a unit's partial results
   int coarse;                                   // tiles are added up in steps of 2^coarse (sums stay within 32 bits)
-  float *part_o, *part_ml;                      // of split units: [unit][row][D], [unit][row][2] (reference, sum)
+  float *part_o, *part_ml;                      // of split units: [head][unit][row][D], [head][unit][row][2] (reference, sum)
+  int4* todo;                                   // [head][unit]: what the join has to do from this unit on, x = 0: nothing
 };
 
 constexpr float kLowestLogit = -3.40282347e38f; // where a reference starts: finite, so that weights of -inf are 0 whatever came before
@@ -69,16 +70,16 @@ struct Unit {
   int p0, p1;                   // positions of its first and last row
   int first, sink_tiles;        // tile t is t of the first sink_tiles, then first + t - sink_tiles
   int t_lo, t_hi;               // tiles of this unit
-  int parts;                    // that the block's tiles are divided into
-  int index;                    // of the block's first unit among the head's
+  int part, parts;              // which of the parts that the block's tiles are divided into
 };
 
 // Row r of a block: its token (after the block's first) and head.
 struct Row { int j, g; };
-__device__ inline Row row_at(const PagedArgs& a, const Unit& x, int r) {
-  const int v = x.g0 + r, j = a.G == 1 ? v : (int)__umulhi((uint32_t)v, a.over_G);    // (exact while v G < 2^32)
-  return {x.j0 + j, v - j * a.G};
+__device__ inline Row row_at(const PagedArgs& a, int j0, int g0, int r) {
+  const int v = g0 + r, j = a.G == 1 ? v : (int)__umulhi((uint32_t)v, a.over_G);    // (exact while v G < 2^32)
+  return {j0 + j, v - j * a.G};
 }
+__device__ inline Row row_at(const PagedArgs& a, const Unit& x, int r) { return row_at(a, x.j0, x.g0, r); }
 
 struct Request { int qs, nq, kv; };
 __device__ inline Request request(const PagedArgs& a, int r) {
@@ -92,8 +93,8 @@ __device__ inline Request request(const PagedArgs& a, int r) {
   return x;
 }
 
-// The unit with index u of a head; BLOCKS: the row block with index u.
-template <int DT, bool BLOCKS>
+// The unit with index u of a head.
+template <int DT>
 __device__ inline bool find_unit(const PagedArgs& a, int u, Unit& x) {
   using B = Blocks<DT>;
   const int lane = threadIdx.x & 63;
@@ -118,14 +119,14 @@ __device__ inline bool find_unit(const PagedArgs& a, int u, Unit& x) {
     all = __builtin_amdgcn_readlane(wave_inclusive_sum(all), 63);
     per = (int)(((uint32_t)all + a.target - 1) / (uint32_t)a.target) << a.coarse;
   }
-  int units = 0, blocks = 0;
+  int units = 0;
   for (int r0 = 0; r0 < a.R; r0 += 64) {
     const Request t = r0 ? request(a, r0 + lane) : head;
     const Size s = size(t);
     const int most = max(per, s.least);
     const int parts = s.tiles <= most ? 1 : (int)((uint32_t)(s.tiles - 1) / (uint32_t)most) + 1;
-    const int cu = wave_inclusive_sum(s.blocks * parts), cb = BLOCKS ? wave_inclusive_sum(s.blocks) : 0;
-    const uint64_t here = __builtin_amdgcn_ballot_w64(BLOCKS ? u < blocks + cb : u < units + cu);
+    const int cu = wave_inclusive_sum(s.blocks * parts);
+    const uint64_t here = __builtin_amdgcn_ballot_w64(u < units + cu);
     if (here) {
       const int l = __builtin_ctzll(here);
       const auto of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
@@ -134,15 +135,9 @@ __device__ inline bool find_unit(const PagedArgs& a, int u, Unit& x) {
       const int n = of(s.blocks), all_rows = x.nq * a.G;
       x.few = B::few(all_rows);
       x.parts = of(parts);
-      const int first_unit = units + of(cu) - n * x.parts;
-      int b, part = 0;
-      if constexpr (BLOCKS) {
-        b = u - (blocks + of(cb) - n);
-      } else {
-        b = x.parts == 1 ? u - first_unit : (int)((uint32_t)(u - first_unit) / (uint32_t)x.parts);
-        part = u - first_unit - b * x.parts;
-      }
-      x.index = first_unit + b * x.parts;
+      const int rest = u - (units + of(cu) - n * x.parts);
+      int b = x.parts == 1 ? rest : (int)((uint32_t)rest / (uint32_t)x.parts);
+      x.part = rest - b * x.parts;
       b = n - 1 - b;                                       // (a chunk's last rows see the most keys: first)
       const int rb = x.few ? 32 : B::kMany, i0 = b * rb;
       x.j0 = i0 == 0 ? 0 : (int)((uint32_t)i0 / (uint32_t)a.G);
@@ -158,13 +153,12 @@ __device__ inline bool find_unit(const PagedArgs& a, int u, Unit& x) {
       x.t_hi = tiles;
       if (x.parts > 1) {
         const int q = (int)((uint32_t)tiles / (uint32_t)x.parts), rem = tiles - q * x.parts;
-        x.t_lo = part * q + min(part, rem);
-        x.t_hi = x.t_lo + q + (part < rem ? 1 : 0);
+        x.t_lo = x.part * q + min(x.part, rem);
+        x.t_hi = x.t_lo + q + (x.part < rem ? 1 : 0);
       }
       return true;
     }
     units += __builtin_amdgcn_readlane(cu, 63);
-    if constexpr (BLOCKS) blocks += __builtin_amdgcn_readlane(cb, 63);
   }
   return false;
 }
@@ -183,7 +177,7 @@ __device__ inline int page_of(const PagedArgs& a, const Unit& x, int key0) {
 // What is not read arrives as zeros.
 __device__ inline int keys_read(const PagedArgs& a, const Unit& x, int key0, int id) {
   int n = max(x.kv - key0, 0);
-  asm("" : "+s"(n));                                        // (both bounds at once would be one vector instruction, and what follows too)
+  asm("" : "+s"(n));                                       // (both bounds at once would be a vector instruction, and what follows too)
   n = min(n, 16);
   if ((uint32_t)id >= (uint32_t)a.n_pages) n = 0;
   if (a.window && key0 + 15 <= max(x.p0, 0) - a.window && key0 >= a.sinks) n = 0;
@@ -193,6 +187,26 @@ __device__ inline __amdgpu_buffer_rsrc_t keys_at(const PagedArgs& a, const uint8
   const int64_t at = (int64_t)(n ? id : 0) * sB + (int64_t)(key0 & ((1 << a.shift) - 1)) * row;
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(head + at), 0, n * row, kBufFlags);
 }
+
+// 16 keys to LDS in N transfers of 1024 bytes, to consecutive places.  The descriptor changes with every page, and the compiler may have
+// brought a part of it (or the place) from a vector register the instruction before: a memory instruction must not read
+// such a scalar register for five wait states, and does not see that it does inside an assembly block.
+#define ZC_KEYS_NEXT(v) "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tbuffer_load_dwordx4 " v ", %1, 0 offen lds\n\t"
+#define ZC_KEYS_FIRST "s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %1, 0 offen lds\n\t"
+template <int N>
+__device__ inline void move_keys(uint32_t lds, __amdgpu_buffer_rsrc_t rs, const int (&v)[N]) {
+  static_assert(N == 2 || N == 4 || N == 8, "16 rows of 128, 256 or 512 bytes");
+  if constexpr (N == 2)
+    asm volatile(ZC_KEYS_FIRST ZC_KEYS_NEXT("%3") :: "s"(lds), "s"(rs), "v"(v[0]), "v"(v[1]) : "memory", "scc");
+  else if constexpr (N == 4)
+    asm volatile(ZC_KEYS_FIRST ZC_KEYS_NEXT("%3") ZC_KEYS_NEXT("%4") ZC_KEYS_NEXT("%5")
+                 :: "s"(lds), "s"(rs), "v"(v[0]), "v"(v[1]), "v"(v[2]), "v"(v[3]) : "memory", "scc");
+  else
+    asm volatile(ZC_KEYS_FIRST ZC_KEYS_NEXT("%3") ZC_KEYS_NEXT("%4") ZC_KEYS_NEXT("%5") ZC_KEYS_NEXT("%6") ZC_KEYS_NEXT("%7") ZC_KEYS_NEXT("%8") ZC_KEYS_NEXT("%9")
+                 :: "s"(lds), "s"(rs), "v"(v[0]), "v"(v[1]), "v"(v[2]), "v"(v[3]), "v"(v[4]), "v"(v[5]), "v"(v[6]), "v"(v[7]) : "memory", "scc");
+}
+#undef ZC_KEYS_NEXT
+#undef ZC_KEYS_FIRST
 
 // Chunk slot permutation of a V row of 16-bit types: the transposing load reads 64 bytes of four consecutive keys per
 // half-wave; these land in different banks.
@@ -254,8 +268,7 @@ __device__ __forceinline__ void attend_rows(const PagedArgs& a, const Unit& x, i
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
       const auto rs = keys_at(a, head, sB, row, s.key0 + 16 * g, s.id[g], s.n[g]);
-#pragma unroll
-      for (int j = 0; j < PG; ++j) dma16<0>(lds + g * 16 * T::ROWB + j * 1024, rs, voff[j], 0);
+      move_keys<PG>(lds + g * 16 * T::ROWB, rs, voff);
     }
   };
 
@@ -478,19 +491,19 @@ __device__ __forceinline__ void attend_tiles(const PagedArgs& a, const Unit& x, 
   };
   auto k_issue = [&](int t, const Group& g) {
     const auto rs = keys_at(a, kb, a.k_sB, a.k_row, g.key0, g.id, keys_read(a, x, g.key0, g.id));
+    int v[NI];
+    asm volatile("" : "+v"(krow), "+v"(kchunk));
 #pragma unroll
-    for (int jj = 0; jj < NI; ++jj) {
-      asm volatile("" : "+v"(krow), "+v"(kchunk));
-      dma16<0>(ks_lds + (t & 1) * TILE_B + jj * 1024, rs, krow + jj * T::RPI * (int)a.k_row + (kchunk ^ (T::swz(jj * T::RPI) << 4)), 0);
-    }
+    for (int jj = 0; jj < NI; ++jj) v[jj] = krow + jj * T::RPI * (int)a.k_row + (kchunk ^ (T::swz(jj * T::RPI) << 4));
+    move_keys<NI>(ks_lds + (t & 1) * TILE_B, rs, v);
   };
   auto v_issue = [&](int t, const Group& g) {
     const auto rs = keys_at(a, vb, a.v_sB, a.v_row, g.key0, g.id, keys_read(a, x, g.key0, g.id));
+    int v[NI];
+    asm volatile("" : "+v"(vplace));
 #pragma unroll
-    for (int jj = 0; jj < NI; ++jj) {
-      asm volatile("" : "+v"(vplace));
-      dma16<0>(vs_lds + (t & 1) * TILE_B + jj * 1024, rs, vplace + jj * T::RPI * (int)a.v_row, 0);
-    }
+    for (int jj = 0; jj < NI; ++jj) v[jj] = vplace + jj * T::RPI * (int)a.v_row;
+    move_keys<NI>(vs_lds + (t & 1) * TILE_B, rs, v);
   };
   Group gv = {0, -1}, gk = {0, -1};              // of V(t + 1) and K(t + 2)
   if (ntiles > 0) {
@@ -689,9 +702,9 @@ __device__ __forceinline__ void attend_tiles(const PagedArgs& a, const Unit& x, 
 
 // Four channels of a row whose parts are together: reference M, sum l, weighted values o.
 template <int DT>
-__device__ inline void store_row(const PagedArgs& a, const Unit& x, int hk, int row, int c, float M, float l, float4 o) {
-  const Row me = row_at(a, x, row);
-  const int64_t hq = hk * a.G + me.g, tok = x.qs + me.j;
+__device__ inline void store_row(const PagedArgs& a, int tok0, int g0, int hk, int row, int c, float M, float l, float4 o) {
+  const Row me = row_at(a, tok0, g0, row);
+  const int64_t hq = hk * a.G + me.g, tok = me.j;
   const float inv = l == 0.f ? 0.f : 1.f / l;
   uint8_t* orow = a.o + hq * a.o_sH + tok * a.o_sT;
   if constexpr (DT == ZC_F32) *reinterpret_cast<float4*>(orow + c * 4) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
@@ -705,7 +718,10 @@ __global__ __launch_bounds__(256, DT == ZC_F32 && D == 128 ? 1 : 2) void k_paged
   __shared__ float sum[4][2][64];
   const int hk = blockIdx.x;
   Unit x;
-  if (!find_unit<DT, false>(a, unit_of_grid(), x)) return;
+  const bool any = find_unit<DT>(a, unit_of_grid(), x);
+  if (a.target && threadIdx.x == 0)
+    a.todo[(int64_t)hk * a.units + unit_of_grid()] = any && x.part == 0 && x.parts > 1 ? make_int4(x.parts, x.rows, x.qs + x.j0, x.g0) : make_int4(0, 0, 0, 0);
+  if (!any) return;
   if constexpr (DT != ZC_F32) {
     if (!x.few) {
       attend_tiles<DT, D>(a, x, hk, mem);
@@ -716,36 +732,37 @@ __global__ __launch_bounds__(256, DT == ZC_F32 && D == 128 ? 1 : 2) void k_paged
 }
 
 // ---- the join of split blocks ---------------------------------------------------------------------------
-// A workgroup per row block.  D / 4 threads take a row; where rows are few, several such groups share a row's parts and
+// A workgroup per unit, of which those that a split block begins with have something to do.  D / 4 threads take a row; where rows are few, several such groups share a row's parts and
 // join what they have in LDS.  Bound by two trips to memory.
-constexpr int kJoinThreads = 512;
+constexpr int kJoinThreads = 256;
 template <int DT, int D>
 __global__ __launch_bounds__(kJoinThreads) void k_paged_join(PagedArgs a) {
   constexpr int TPR = D / 4, GROUPS = kJoinThreads / TPR;
   __shared__ __align__(16) float so[GROUPS][D];
   __shared__ float2 sml[GROUPS];
   const int hk = blockIdx.x;
-  Unit x;
-  if (!find_unit<DT, true>(a, unit_of_grid(), x) || x.parts == 1 || x.index + x.parts > a.units) return;
+  const int4 todo = a.todo[(int64_t)hk * a.units + unit_of_grid()];
+  const int parts = todo.x, rows = todo.y;
+  if (parts == 0 || unit_of_grid() + parts > a.units) return;
   const int grp = threadIdx.x / TPR, c = threadIdx.x % TPR * 4;
   int ways = 1;                                            // groups to a row
-  while (2 * ways * x.rows <= GROUPS && 2 * ways <= x.parts) ways *= 2;
+  while (2 * ways * rows <= GROUPS && 2 * ways <= parts) ways *= 2;
   const int way = grp & (ways - 1), at_once = GROUPS / ways;
-  const int64_t first = part_row(a, hk, x.index);
-  for (int row = grp / ways; row < x.rows; row += at_once) {
+  const int64_t first = part_row(a, hk, unit_of_grid());
+  for (int row = grp / ways; row < rows; row += at_once) {
     float M = kLowestLogit, l = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     constexpr int U = 4;                                   // parts requested at a time
-    for (int s0 = way; s0 < x.parts; s0 += U * ways) {
+    for (int s0 = way; s0 < parts; s0 += U * ways) {
       float2 ml[U];
       float4 t[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int s = s0 + u * ways;
-        const int64_t p = first + (int64_t)(s < x.parts ? s : s0) * a.slot + row;
+        const int64_t p = first + (int64_t)(s < parts ? s : s0) * a.slot + row;
         ml[u] = *reinterpret_cast<const float2*>(a.part_ml + p * 2);
         t[u] = *reinterpret_cast<const float4*>(a.part_o + p * D + c);
-        if (s >= x.parts) ml[u] = make_float2(kLowestLogit, 0.f);
+        if (s >= parts) ml[u] = make_float2(kLowestLogit, 0.f);
       }
       float top = M;
 #pragma unroll
@@ -755,7 +772,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_paged_join(PagedArgs a) {
       l *= f0; o.x *= f0; o.y *= f0; o.z *= f0; o.w *= f0;
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const float f = s0 + u * ways < x.parts ? __builtin_amdgcn_exp2f(ml[u].x - M) : 0.f;
+        const float f = s0 + u * ways < parts ? __builtin_amdgcn_exp2f(ml[u].x - M) : 0.f;
         l = fmaf(ml[u].y, f, l);
         o.x = fmaf(t[u].x, f, o.x); o.y = fmaf(t[u].y, f, o.y); o.z = fmaf(t[u].z, f, o.z); o.w = fmaf(t[u].w, f, o.w);
       }
@@ -764,12 +781,12 @@ __global__ __launch_bounds__(kJoinThreads) void k_paged_join(PagedArgs a) {
       if (c == 0) sml[grp] = make_float2(M, l);
       *reinterpret_cast<float4*>(&so[grp][c]) = o;
     } else {
-      store_row<DT>(a, x, hk, row, c, M, l, o);
+      store_row<DT>(a, todo.z, todo.w, hk, row, c, M, l, o);
     }
   }
   if (ways == 1) return;
   __syncthreads();
-  if (way != 0 || grp / ways >= x.rows) return;
+  if (way != 0 || grp / ways >= rows) return;
   float M = kLowestLogit, l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int v = 0; v < ways; ++v) M = fmaxf(M, sml[grp + v].x);
@@ -780,7 +797,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_paged_join(PagedArgs a) {
     l = fmaf(ml.y, f, l);
     o.x = fmaf(t.x, f, o.x); o.y = fmaf(t.y, f, o.y); o.z = fmaf(t.z, f, o.z); o.w = fmaf(t.w, f, o.w);
   }
-  store_row<DT>(a, x, hk, grp / ways, c, M, l, o);
+  store_row<DT>(a, todo.z, todo.w, hk, grp / ways, c, M, l, o);
 }
 
 // ---- host ---------------------------------------------------------------------------------------------
@@ -797,16 +814,16 @@ static Cut cut_of(int64_t R, int64_t T, int64_t G, int64_t Hkv, int dtype) {
   return c;
 }
 static size_t workspace_of(const Cut& c, int64_t Hkv, int64_t D) {
-  return c.target ? (size_t)(c.target + c.blocks) * Hkv * c.slot * (D + 2) * sizeof(float) : 0;
+  return c.target ? (size_t)(c.target + c.blocks) * Hkv * (c.slot * (D + 2) * sizeof(float) + sizeof(int4)) : 0;
 }
 
 template <int DT, int D>
-static int launch_paged(PagedArgs& a, int64_t blocks, hipStream_t st) {
+static int launch_paged(PagedArgs& a, hipStream_t st) {
   const auto grid = [&](int64_t n) { return dim3((unsigned)a.Hkv, (unsigned)(n < 65535 ? n : 65535), (unsigned)ceil_div64(n, 65535)); };
   hipLaunchKernelGGL((k_paged_attention<DT, D>), grid(a.units), dim3(256), 0, st, a);
   ZC_LAUNCH_CHECK();
   if (a.target) {
-    hipLaunchKernelGGL((k_paged_join<DT, D>), grid(blocks), dim3(kJoinThreads), 0, st, a);
+    hipLaunchKernelGGL((k_paged_join<DT, D>), grid(a.units), dim3(kJoinThreads), 0, st, a);
     ZC_LAUNCH_CHECK();
   }
   return ZC_OK;
@@ -871,10 +888,11 @@ extern "C" int zc_paged_attention(const zc_tensor4* q, const zc_tensor4* k_pages
   a.coarse = 0;
   while ((cut.blocks * (room / kTile + 1)) >> a.coarse > 0x3fffffff) ++a.coarse;
   const int64_t parts = (cut.target + cut.blocks) * Hkv;
-  a.part_o = (float*)ws;
-  a.part_ml = need ? (float*)ws + parts * cut.slot * q->D : nullptr;
+  a.todo = (int4*)ws;
+  a.part_o = need ? (float*)((int4*)ws + parts) : nullptr;
+  a.part_ml = need ? a.part_o + parts * cut.slot * q->D : nullptr;
   hipStream_t st = (hipStream_t)stream;
-#define ZC_PA(DT) (q->D == 128 ? launch_paged<DT, 128>(a, cut.blocks, st) : launch_paged<DT, 64>(a, cut.blocks, st))
+#define ZC_PA(DT) (q->D == 128 ? launch_paged<DT, 128>(a, st) : launch_paged<DT, 64>(a, st))
   if (q->dtype == ZC_F32) rc = ZC_PA(ZC_F32);
   else if (q->dtype == ZC_F16) rc = ZC_PA(ZC_F16);
   else rc = ZC_PA(ZC_BF16);
