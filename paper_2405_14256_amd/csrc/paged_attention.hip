@@ -166,12 +166,10 @@ __device__ inline bool find_unit(const PagedArgs& a, int u, Unit& x) {
 __device__ inline int tile_of(const Unit& x, int t) { return t < x.sink_tiles ? t : x.first + t - x.sink_tiles; }
 __device__ inline int unit_of_grid() { return blockIdx.y + 65535 * blockIdx.z; }
 
-// The page of 16 keys from key0 on, -1 where there is none.
+// The page of 16 keys from key0 on (past the table: any, no key is read).
 __device__ inline int page_of(const PagedArgs& a, const Unit& x, int key0) {
   typedef __attribute__((address_space(4))) const int32_t* scalar;
-  const int col = key0 >> a.shift;
-  if (col >= a.cols) return -1;
-  return ((scalar)(uintptr_t)(a.table + x.r * a.row))[col];
+  return ((scalar)(uintptr_t)(a.table + x.r * a.row))[min(key0 >> a.shift, a.cols - 1)];
 }
 // Of 16 keys from key0 on, how many a unit reads: none of a missing page, of those that no row's window reaches, past the end.
 // What is not read arrives as zeros.
@@ -313,6 +311,7 @@ __device__ __forceinline__ void attend_rows(const PagedArgs& a, const Unit& x, i
   for (int ct = 0; ct < CT; ++ct) oacc[ct] = v16f{};
   float m = kLowestLogit, l = 0.f;   // running maximum (log2 units), this half-wave's share of the sum
 
+  wait_all_loads();                              // (the rows and the first blocks: the compiler would wait for the rows in the loop, and so for the next blocks)
   for (; t < blocks; t += NW) {
     const bool more = t + NW < blocks;
     const int key0 = at.key0;
@@ -448,6 +447,10 @@ __device__ __forceinline__ void attend_rows(const PagedArgs& a, const Unit& x, i
 // Bound by the matrix cores: a half is 16 matrix instructions of 32 cycles (128 channels) and about 300 cycles of vector
 // instructions, so the two have to run at the same time: the logits of half h + 1 are multiplied while the exponentials of
 // half h are taken, and the operands of each product are requested one phase before.
+//
+// Of 64 channels three tiles of K and V fit (three workgroups a CU either way), and they are requested two tiles ahead: a
+// tile is worth 0.2 us of matrix instructions there, less than a trip to memory.
+template <int D> constexpr int kStages = D == 64 ? 3 : 2;
 template <int DT, int D>
 __device__ __forceinline__ void attend_tiles(const PagedArgs& a, const Unit& x, int hk, uint8_t* mem) {
   using T = Tile<DT, D>;
@@ -457,7 +460,7 @@ __device__ __forceinline__ void attend_tiles(const PagedArgs& a, const Unit& x, 
   constexpr int CT = D / 32;                     // 32-channel tiles of the output
   constexpr int EPS = 16 / T::NKC;               // logits per slice
   constexpr int VS = T::NKC / 4;                 // the slice that requests the first V operand
-  static_assert(RowsMemory<DT, D>::kBytes == 4 * TILE_B, "two K tiles, two V tiles");
+  constexpr int STAGES = kStages<D>, AHEAD = STAGES - 1;       // tiles of K and of V in LDS; how far ahead they are requested
   typedef short s16x4 __attribute__((ext_vector_type(4)));
 
   const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, kh = lane >> 5;
@@ -465,7 +468,7 @@ __device__ __forceinline__ void attend_tiles(const PagedArgs& a, const Unit& x, 
   const uint8_t* kb = a.k + hk * a.k_sH;
   const uint8_t* vb = a.v + hk * a.v_sH;
   const uint32_t ks_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)mem + w * 16 * T::ROWB;
-  const uint32_t vs_lds = ks_lds + 2 * TILE_B;
+  const uint32_t vs_lds = ks_lds + STAGES * TILE_B;
 
   // this wave's rows, and the halves of this unit that they see: all up to the last row's
   const int wrows = min(max(x.rows - 32 * w, 0), 32);
@@ -489,30 +492,34 @@ __device__ __forceinline__ void attend_tiles(const PagedArgs& a, const Unit& x, 
     g.id = page_of(a, x, g.key0);
     return g;
   };
-  auto k_issue = [&](int t, const Group& g) {
+  auto k_issue = [&](int place, const Group& g) {
     const auto rs = keys_at(a, kb, a.k_sB, a.k_row, g.key0, g.id, keys_read(a, x, g.key0, g.id));
     int v[NI];
     asm volatile("" : "+v"(krow), "+v"(kchunk));
 #pragma unroll
     for (int jj = 0; jj < NI; ++jj) v[jj] = krow + jj * T::RPI * (int)a.k_row + (kchunk ^ (T::swz(jj * T::RPI) << 4));
-    move_keys<NI>(ks_lds + (t & 1) * TILE_B, rs, v);
+    move_keys<NI>(ks_lds + place * TILE_B, rs, v);
   };
-  auto v_issue = [&](int t, const Group& g) {
+  auto v_issue = [&](int place, const Group& g) {
     const auto rs = keys_at(a, vb, a.v_sB, a.v_row, g.key0, g.id, keys_read(a, x, g.key0, g.id));
     int v[NI];
     asm volatile("" : "+v"(vplace));
 #pragma unroll
     for (int jj = 0; jj < NI; ++jj) v[jj] = vplace + jj * T::RPI * (int)a.v_row;
-    move_keys<NI>(vs_lds + (t & 1) * TILE_B, rs, v);
+    move_keys<NI>(vs_lds + place * TILE_B, rs, v);
   };
-  Group gv = {0, -1}, gk = {0, -1};              // of V(t + 1) and K(t + 2)
+  Group gv = {0, -1}, gk = {0, -1};              // of V(t + AHEAD) and K(t + AHEAD + 1), t the next tile
   if (ntiles > 0) {
-    const Group g = group(0);
-    gv = group(1);
-    gk = group(2);
-    k_issue(0, g);
-    v_issue(0, g);
-    if (ntiles > 1) k_issue(1, gv);
+    gv = group(0);
+    k_issue(0, gv);
+#pragma unroll
+    for (int t = 0; t < AHEAD; ++t) {
+      gk = group(t + 1);
+      if (t < ntiles) v_issue(t, gv);
+      if (t + 1 < ntiles) k_issue((t + 1) % STAGES, gk);
+      gv = gk;
+    }
+    gk = group(AHEAD + 1);
   }
 
   // this lane's row, straight into operand registers
@@ -629,24 +636,31 @@ __device__ __forceinline__ void attend_tiles(const PagedArgs& a, const Unit& x, 
     if constexpr (!LAST) tmax = half_max(sn);        // (beside the second product, which leaves the vector units idle)
   };
   // Tile t's barrier: K(t + 1) and V(t) are complete in LDS, and nobody still reads K(t) (its second half was requested
-  // before) or V(t - 1), whose buffers are filled next.
+  // before) or V(t - 1), whose places are filled next.  The page of a later tile is asked for in front of the barrier, and
+  // had behind it: a scalar load on the way makes the waits for operands from LDS waits for all of them.
+  int place = AHEAD % STAGES;                        // of V(t + AHEAD); K(t + AHEAD + 1) goes where K(t) was
   auto top = [&](int t) {
-    wait_all_loads();
+    const Group gn = group(t + AHEAD + 2);
+    if (AHEAD > 1 && t + AHEAD < ntiles) wait_vmem<(AHEAD - 1) * 2 * NI>();
+    else wait_all_loads();
     __syncthreads();
-    if (t + 1 < ntiles) v_issue(t + 1, gv);
-    if (t + 2 < ntiles) k_issue(t + 2, gk);
+    asm volatile("" :: "s"(gn.id));
+    if (t + AHEAD < ntiles) v_issue(place, gv);
+    place = place + 1 == STAGES ? 0 : place + 1;
+    if (t + AHEAD + 1 < ntiles) k_issue(place, gk);
     gv = gk;
-    gk = group(t + 3);
+    gk = gn;
   };
-  int turn = TILE_B;
-  auto next_buffers = [&]() {                        // tile t + 1: V from the other buffer, K (of t + 2) too
-    kaddr -= turn;
+  int read_place = 0;                                // of V(t); K(t + 1) is in the next
+  auto next_buffers = [&]() {                        // tile t + 1
+    const int next = read_place + 1 == STAGES ? 0 : read_place + 1, after = next + 1 == STAGES ? 0 : next + 1;
+    kaddr += (after - next) * TILE_B;
 #pragma unroll
-    for (int ct = 0; ct < CT; ++ct) vaddr[ct] += turn;
-    turn = -turn;
+    for (int ct = 0; ct < CT; ++ct) vaddr[ct] += (next - read_place) * TILE_B;
+    read_place = next;
   };
+  wait_all_loads();                                  // (on every way to the loop: the compiler would wait for the rows in it, and so for the next tiles)
   if (ntiles > 0) {
-    wait_all_loads();
     __syncthreads();
     k_read(0, kf);
     s0 = v16f{};
@@ -714,7 +728,9 @@ __device__ inline void store_row(const PagedArgs& a, int tok0, int g0, int hk, i
 
 template <int DT, int D>
 __global__ __launch_bounds__(256, DT == ZC_F32 && D == 128 ? 1 : 2) void k_paged_attention(PagedArgs a) {
-  __shared__ __align__(1024) uint8_t mem[RowsMemory<DT, D>::kBytes];
+  constexpr int kBytes = DT == ZC_F32 ? RowsMemory<DT, D>::kBytes : kStages<D> * 2 * kTile * Tile<DT, D>::ROWB;
+  static_assert(kBytes >= RowsMemory<DT, D>::kBytes, "blocks of few rows find room");
+  __shared__ __align__(1024) uint8_t mem[kBytes];
   __shared__ float sum[4][2][64];
   const int hk = blockIdx.x;
   Unit x;
@@ -732,27 +748,27 @@ __global__ __launch_bounds__(256, DT == ZC_F32 && D == 128 ? 1 : 2) void k_paged
 }
 
 // ---- the join of split blocks ---------------------------------------------------------------------------
-// A workgroup per unit, of which those that a split block begins with have something to do.  D / 4 threads take a row; where rows are few, several such groups share a row's parts and
-// join what they have in LDS.  Bound by two trips to memory.
+// A workgroup per unit; those of a unit that a split block begins with join it, 32 rows each (the grid's third axis: which).  D / 4 threads take a row; where rows are few, several such groups share a row's parts and join what
+// they have in LDS.  Bound by two trips to memory.
 constexpr int kJoinThreads = 256;
 template <int DT, int D>
 __global__ __launch_bounds__(kJoinThreads) void k_paged_join(PagedArgs a) {
   constexpr int TPR = D / 4, GROUPS = kJoinThreads / TPR;
   __shared__ __align__(16) float so[GROUPS][D];
   __shared__ float2 sml[GROUPS];
-  const int hk = blockIdx.x;
-  const int4 todo = a.todo[(int64_t)hk * a.units + unit_of_grid()];
-  const int parts = todo.x, rows = todo.y;
-  if (parts == 0 || unit_of_grid() + parts > a.units) return;
+  const int hk = blockIdx.x, unit = blockIdx.y, row0 = blockIdx.z * 32;
+  const int4 todo = a.todo[(int64_t)hk * a.units + unit];
+  const int parts = todo.x, rows = min(todo.y, row0 + 32);
+  if (parts == 0 || rows <= row0 || unit + parts > a.units) return;
   const int grp = threadIdx.x / TPR, c = threadIdx.x % TPR * 4;
-  int ways = 1;                                            // groups to a row
-  while (2 * ways * rows <= GROUPS && 2 * ways <= parts) ways *= 2;
+  int ways = 1;                                          // groups to a row
+  while (2 * ways * (rows - row0) <= GROUPS && 2 * ways <= parts) ways *= 2;
   const int way = grp & (ways - 1), at_once = GROUPS / ways;
-  const int64_t first = part_row(a, hk, unit_of_grid());
-  for (int row = grp / ways; row < rows; row += at_once) {
+  const int64_t first = part_row(a, hk, unit);
+  for (int row = row0 + grp / ways; row < rows; row += at_once) {
     float M = kLowestLogit, l = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    constexpr int U = 4;                                   // parts requested at a time
+    constexpr int U = 4;                                 // parts requested at a time
     for (int s0 = way; s0 < parts; s0 += U * ways) {
       float2 ml[U];
       float4 t[U];
@@ -762,7 +778,6 @@ __global__ __launch_bounds__(kJoinThreads) void k_paged_join(PagedArgs a) {
         const int64_t p = first + (int64_t)(s < parts ? s : s0) * a.slot + row;
         ml[u] = *reinterpret_cast<const float2*>(a.part_ml + p * 2);
         t[u] = *reinterpret_cast<const float4*>(a.part_o + p * D + c);
-        if (s >= parts) ml[u] = make_float2(kLowestLogit, 0.f);
       }
       float top = M;
 #pragma unroll
@@ -777,7 +792,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_paged_join(PagedArgs a) {
         o.x = fmaf(t[u].x, f, o.x); o.y = fmaf(t[u].y, f, o.y); o.z = fmaf(t[u].z, f, o.z); o.w = fmaf(t[u].w, f, o.w);
       }
     }
-    if (ways > 1) {                                        // (all rows at once: every thread comes here once, or none of its wave's row)
+    if (ways > 1) {                                      // (all rows at once: a thread comes here once at most)
       if (c == 0) sml[grp] = make_float2(M, l);
       *reinterpret_cast<float4*>(&so[grp][c]) = o;
     } else {
@@ -786,18 +801,19 @@ __global__ __launch_bounds__(kJoinThreads) void k_paged_join(PagedArgs a) {
   }
   if (ways == 1) return;
   __syncthreads();
-  if (way != 0 || grp / ways >= rows) return;
-  float M = kLowestLogit, l = 0.f;
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int v = 0; v < ways; ++v) M = fmaxf(M, sml[grp + v].x);
-  for (int v = 0; v < ways; ++v) {
-    const float2 ml = sml[grp + v];
-    const float4 t = *reinterpret_cast<const float4*>(&so[grp + v][c]);
-    const float f = __builtin_amdgcn_exp2f(ml.x - M);
-    l = fmaf(ml.y, f, l);
-    o.x = fmaf(t.x, f, o.x); o.y = fmaf(t.y, f, o.y); o.z = fmaf(t.z, f, o.z); o.w = fmaf(t.w, f, o.w);
+  if (way == 0 && row0 + grp / ways < rows) {
+    float M = kLowestLogit, l = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int v = 0; v < ways; ++v) M = fmaxf(M, sml[grp + v].x);
+    for (int v = 0; v < ways; ++v) {
+      const float2 ml = sml[grp + v];
+      const float4 t = *reinterpret_cast<const float4*>(&so[grp + v][c]);
+      const float f = __builtin_amdgcn_exp2f(ml.x - M);
+      l = fmaf(ml.y, f, l);
+      o.x = fmaf(t.x, f, o.x); o.y = fmaf(t.y, f, o.y); o.z = fmaf(t.z, f, o.z); o.w = fmaf(t.w, f, o.w);
+    }
+    store_row<DT>(a, todo.z, todo.w, hk, row0 + grp / ways, c, M, l, o);
   }
-  store_row<DT>(a, todo.z, todo.w, hk, grp / ways, c, M, l, o);
 }
 
 // ---- host ---------------------------------------------------------------------------------------------
@@ -823,7 +839,8 @@ static int launch_paged(PagedArgs& a, hipStream_t st) {
   hipLaunchKernelGGL((k_paged_attention<DT, D>), grid(a.units), dim3(256), 0, st, a);
   ZC_LAUNCH_CHECK();
   if (a.target) {
-    hipLaunchKernelGGL((k_paged_join<DT, D>), grid(a.units), dim3(kJoinThreads), 0, st, a);
+    const dim3 joins((unsigned)a.Hkv, (unsigned)a.units, (unsigned)(a.slot / 32));     // (units: at most 1536)
+    hipLaunchKernelGGL((k_paged_join<DT, D>), joins, dim3(kJoinThreads), 0, st, a);
     ZC_LAUNCH_CHECK();
   }
   return ZC_OK;
