@@ -11,6 +11,7 @@
 // rows are spread over requests; every wave finds its unit from the lengths alone (find_unit), so nothing has to be
 // prepared, and what is long is split by the same rule in every wave.
 #include <limits.h>
+#include <stdint.h>
 #include <type_traits>
 
 #include "mfma_tiles.hpp"
@@ -510,16 +511,17 @@ __device__ __forceinline__ void attend_tiles(const PagedArgs& a, const Unit& x, 
   };
   Group gv = {0, -1}, gk = {0, -1};              // of V(t + AHEAD) and K(t + AHEAD + 1), t the next tile
   if (ntiles > 0) {
-    gv = group(0);
-    k_issue(0, gv);
+    Group g[AHEAD + 2];                          // (all pages are asked for before the first is used)
+#pragma unroll
+    for (int t = 0; t < AHEAD + 2; ++t) g[t] = group(t);
+    k_issue(0, g[0]);
 #pragma unroll
     for (int t = 0; t < AHEAD; ++t) {
-      gk = group(t + 1);
-      if (t < ntiles) v_issue(t, gv);
-      if (t + 1 < ntiles) k_issue((t + 1) % STAGES, gk);
-      gv = gk;
+      if (t < ntiles) v_issue(t, g[t]);
+      if (t + 1 < ntiles) k_issue((t + 1) % STAGES, g[t + 1]);
     }
-    gk = group(AHEAD + 1);
+    gv = g[AHEAD];
+    gk = g[AHEAD + 1];
   }
 
   // this lane's row, straight into operand registers
@@ -820,13 +822,70 @@ __global__ __launch_bounds__(kJoinThreads) void k_paged_join(PagedArgs a) {
 // How a call's rows are cut: row blocks of a head, at most; units of a head that splitting aims at (0: nothing is split); rows of a
 // unit's partial results.
 struct Cut { int64_t blocks, target, slot; };
-constexpr int64_t kPlaces = 512;               // workgroups the chip holds at a time
+constexpr int64_t kUnits = 2560;               // of all heads, that splitting aims at, at most
+constexpr int64_t kMostUnits = 4096;           // and that there may be (their partial results, 128 rows of 128 channels: 272 MB)
 
-static Cut cut_of(int64_t R, int64_t T, int64_t G, int64_t Hkv, int dtype) {
+// Whether rows see too few keys, or the chip has too much to do without, for parts of them to be worth a second launch.  us, split
+// and whole, tables of as many tiles as the keys fill: bf16, 32 heads over 8 of 128 channels, one token each, 1 request of 256 keys 8.4 and 6.9,
+// of 512 8.5 and 9.2; 16 of 512 14.0 and 10.6, of 1024 18.5 and 15.0, 24 of 100 to 4096 28 and 43; 64 of 300 to 600 33 and 26; 2 chunks of 500 tokens 28.3
+// and 18.7, of 1000 45.2 and 41.7; fp32, 16 heads over 4, 4 requests of 256 keys of 64 channels 9.4 and 9.0, of 128 12.5 and 14.0.
+static bool whole(int64_t blocks, int64_t tiles, int dtype, int64_t D) {
+  if (dtype == ZC_F32) return tiles <= (D == 64 ? 4 : 2);
+  return tiles <= (blocks >= 128 ? 16 : blocks >= 64 ? 10 : 6);
+}
+
+// Parts of every one of n row blocks that see `tiles` tiles each.  The chip runs them in rounds of what it holds, the last of which is
+// shorter where CUs are left with one workgroup or none; a part costs the way of its rows' results through memory.  Of blocks
+// that fill the chip two parts at most: parts of one block read different keys at a time, which the L2s then hold fewer of.
+// us at 1, 2, 3 and 4 parts, bf16, 32 heads over 8 of 128 channels: 2048 tokens over 32768 (512 blocks) 1120, 1139, 1151 and 1182, 2500 (632) 1526,
+// 1353, 1418 and 1408; 1200 over 8192 (304) 220, 217, 197 and 201; 512 over 8192 (128) 163, 98, 102 and 90; 40 heads, 2048 over 16384 (640) 794, 790, 866
+// and 881; fp16 of 64 channels, 20 tokens and 4 chunks of 250 to 500 over up to 4001 (202) 52, 37, 33.5 and 38.
+static int64_t parts_of(int64_t n, int64_t tiles, int dtype, int64_t D) {
+  // workgroups at a time; us of a tile in each of them; us that a part's results take of the memory's time
+  struct Kind { int64_t places; double tile, part; int least; };
+  const Kind k = dtype == ZC_F32 ? (D == 64 ? Kind{512, 3.3, 0.0033, 2} : Kind{256, 2.2, 0.0065, 2})
+                                 : (D == 64 ? Kind{768, 1.7, 0.013, 4} : Kind{512, 2.0, 0.026, 4});
+  const int64_t most = n >= k.places ? 2 : 256;
+  int64_t best = 1;
+  double least = 0.0;
+  for (int64_t p = 1; p <= most && (p == 1 || (p * n <= kUnits && k.least * p <= tiles)); ++p) {
+    const int64_t rounds = p * n / k.places;
+    const double last = (double)(p * n % k.places) / (double)k.places;
+    const double all = (double)rounds + (last == 0.0 ? 0.0 : last <= 0.5 ? 0.57 : 0.95);
+    const double t = all * (double)tiles * k.tile / (double)p + (p > 1 ? 3.0 + (double)(p * n) * k.part : 0.0);
+    if (p == 1) least = 0.95 * t;
+    else if (t < least) { least = t; best = p; }
+  }
+  return best;
+}
+
+// keys: a request's, at most; INT64_MAX: as many as cost the most workspace.
+static Cut cut_of(int64_t R, int64_t T, int64_t G, int64_t Hkv, int dtype, int64_t D, int64_t keys, int64_t window, int64_t sinks) {
   Cut c;
   c.slot = dtype == ZC_F32 || T * G <= 32 ? 32 : 128;
   c.blocks = T * G / c.slot + (R < T ? R : T);   // (a request has one block that is not full)
-  c.target = c.blocks * Hkv > 2 * kPlaces ? 0 : ceil_div64(kPlaces, Hkv);
+  const bool few = T * G <= 32 * R;
+  const int64_t n = few ? c.blocks * Hkv : ceil_div64(T * G, c.slot) * Hkv;
+  if (few ? n > 1024 : n > kUnits / 2 || c.blocks * Hkv + kUnits > kMostUnits) { c.target = 0; return c; }
+  if (keys == INT64_MAX) {
+    c.target = ceil_div64(few ? 512 : kUnits, Hkv);
+    return c;
+  }
+  if (window && window + sinks < keys) keys = window + sinks;
+  const int64_t tiles = ceil_div64(keys, kTile);
+  if (whole(n, tiles, dtype, D)) {
+    c.target = 0;
+  } else if (few) {
+    // Single tokens: two workgroups a CU, whatever the lengths.  us at 256, 512, 768 and 1024 units: 8 requests of 8192 keys (32 heads
+    // over 8 of 128 channels, bf16) 52.4, 53.0, 54.6 and 56.0; 1 of 32768 32.9, 33.3, 36.0 and 39.1; 4 of 20000 to 32768 105, 81, 82 and 84;
+    // 64 of 64 to 8192 110, 104.9, 101.5 and 102.9; 3 of 1000 to 9000, 16 heads, fp32 104, 72, 83 and 89.
+    c.target = ceil_div64(512, Hkv);
+  } else {
+    // (blocks of a prompt that begins with this step see half of its keys on average, the longest go first: rounds even out)
+    const int64_t past = keys > 2 * T ? keys - 2 * T : 0;
+    const int64_t p = parts_of(n, n < 512 ? tiles : ceil_div64(past, kTile), dtype, D);
+    c.target = p > 1 ? ceil_div64(p * n, Hkv) : 0;
+  }
   return c;
 }
 static size_t workspace_of(const Cut& c, int64_t Hkv, int64_t D) {
@@ -839,7 +898,7 @@ static int launch_paged(PagedArgs& a, hipStream_t st) {
   hipLaunchKernelGGL((k_paged_attention<DT, D>), grid(a.units), dim3(256), 0, st, a);
   ZC_LAUNCH_CHECK();
   if (a.target) {
-    const dim3 joins((unsigned)a.Hkv, (unsigned)a.units, (unsigned)(a.slot / 32));     // (units: at most 1536)
+    const dim3 joins((unsigned)a.Hkv, (unsigned)a.units, (unsigned)(a.slot / 32));     // (units: at most kMostUnits)
     hipLaunchKernelGGL((k_paged_join<DT, D>), joins, dim3(kJoinThreads), 0, st, a);
     ZC_LAUNCH_CHECK();
   }
@@ -853,7 +912,9 @@ using namespace zc;
 // (the larger of what fp32 and 16-bit calls take: the types' blocks differ)
 extern "C" size_t zc_paged_attention_workspace(int64_t R, int64_t T, int64_t Hq, int64_t Hkv, int64_t D) {
   if (R <= 0 || T <= 0 || Hkv <= 0 || Hq < Hkv || Hq % Hkv || D <= 0) return 0;
-  const size_t x = workspace_of(cut_of(R, T, Hq / Hkv, Hkv, ZC_F32), Hkv, D), y = workspace_of(cut_of(R, T, Hq / Hkv, Hkv, ZC_F16), Hkv, D);
+  const int64_t G = Hq / Hkv;
+  const size_t x = workspace_of(cut_of(R, T, G, Hkv, ZC_F32, D, INT64_MAX, 0, 0), Hkv, D);
+  const size_t y = workspace_of(cut_of(R, T, G, Hkv, ZC_F16, D, INT64_MAX, 0, 0), Hkv, D);
   return x > y ? x : y;
 }
 
@@ -876,13 +937,16 @@ extern "C" int zc_paged_attention(const zc_tensor4* q, const zc_tensor4* k_pages
     if (reinterpret_cast<uintptr_t>(p) & 3) return ZC_ERR_INVALID_ARG;
   const int64_t T = q->L, Hkv = k_pages->H, G = q->H / Hkv;
   if (R >= (1 << 24) || max_blocks > 0x7fffffff || T > 0x7fffffff / q->H || q->H > 65535 || G > 4096) return ZC_ERR_UNSUPPORTED;
-  Cut cut = cut_of(R, T, G, Hkv, q->dtype);
+  const int64_t page = k_pages->L, room = max_blocks > 0x7fff0000 / page ? 0x7fff0000 : max_blocks * page;
+  if (window >= room) window = 0;                    // (every row sees all it could)
+  if (sinks > room) sinks = (int32_t)room;
+  const Cut cut = cut_of(R, T, G, Hkv, q->dtype, q->D, room, window, sinks);
   if ((cut.target + cut.blocks) * Hkv > 0xffffff) return ZC_ERR_UNSUPPORTED;
   const size_t need = zc_paged_attention_workspace(R, T, q->H, Hkv, q->D);
+  if (workspace_of(cut, Hkv, q->D) > need) return ZC_ERR_WORKSPACE;     // (never: the size is that of the finest cut)
   if (need && (!ws || ws_bytes < need || (reinterpret_cast<uintptr_t>(ws) & 15))) return ZC_ERR_WORKSPACE;
 
-  const int64_t eb = elem_bytes(q->dtype), page = k_pages->L;
-  const int64_t room = max_blocks > 0x7fff0000 / page ? 0x7fff0000 : max_blocks * page;
+  const int64_t eb = elem_bytes(q->dtype);
   PagedArgs a;
   a.q = (const uint8_t*)q->ptr; a.k = (const uint8_t*)k_pages->ptr; a.v = (const uint8_t*)v_pages->ptr; a.o = (uint8_t*)out->ptr;
   a.q_sH = q->sH * eb; a.q_sT = q->sL * eb; a.o_sH = out->sH * eb; a.o_sT = out->sL * eb;
@@ -891,11 +955,10 @@ extern "C" int zc_paged_attention(const zc_tensor4* q, const zc_tensor4* k_pages
   a.table = block_table; a.q_start = q_start; a.kv_len = kv_len; a.row = row_stride;
   a.cols = (int)max_blocks; a.shift = __builtin_ctzll((unsigned long long)page); a.n_pages = (int)k_pages->B; a.cap = (int)room;
   a.R = (int)R; a.T = (int)T; a.Hkv = (int)Hkv; a.G = (int)G;
-  a.window = window >= room ? 0 : window;          // (every row sees all it could)
-  a.sinks = sinks > room ? (int)room : sinks;
+  a.window = window;
+  a.sinks = sinks;
   a.scale_log2 = (sm_scale == 0.f ? 1.0f / sqrtf((float)q->D) : sm_scale) * kLog2e;
   a.lse = lse;
-  if (room <= 2 * kTile) cut.target = 0;           // (no row has enough keys to be split)
   a.target = (int)cut.target;
   a.units = (int)(cut.target + cut.blocks);
   a.slot = (int)cut.slot;
@@ -906,8 +969,8 @@ extern "C" int zc_paged_attention(const zc_tensor4* q, const zc_tensor4* k_pages
   while ((cut.blocks * (room / kTile + 1)) >> a.coarse > 0x3fffffff) ++a.coarse;
   const int64_t parts = (cut.target + cut.blocks) * Hkv;
   a.todo = (int4*)ws;
-  a.part_o = need ? (float*)((int4*)ws + parts) : nullptr;
-  a.part_ml = need ? a.part_o + parts * cut.slot * q->D : nullptr;
+  a.part_o = cut.target ? (float*)((int4*)ws + parts) : nullptr;
+  a.part_ml = cut.target ? a.part_o + parts * cut.slot * q->D : nullptr;
   hipStream_t st = (hipStream_t)stream;
 #define ZC_PA(DT) (q->D == 128 ? launch_paged<DT, 128>(a, st) : launch_paged<DT, 64>(a, st))
   if (q->dtype == ZC_F32) rc = ZC_PA(ZC_F32);
