@@ -361,16 +361,8 @@ def zc_paged_tables(q_len: torch.Tensor, kv_len: torch.Tensor, block_table: torc
                     slot_map: Optional[torch.Tensor] = None, n_taken: Optional[torch.Tensor] = None):
     """One step's bookkeeping from the requests' lengths (int32 [R] each): new pages go into block_table [R, max_blocks];
     returns (q_start [R + 1], slot_map [T], n_taken [1])."""
-    host = _native()
-    if q_start is None:
-        q_start = torch.empty(block_table.shape[0] + 1, dtype=torch.int32, device=block_table.device)
-    if slot_map is None:
-        slot_map = torch.empty(T, dtype=torch.int32, device=block_table.device)
-    elif slot_map.numel() != T:
-        raise ValueError("slot_map must have T elements")
-    if n_taken is None:
-        n_taken = torch.empty(1, dtype=torch.int32, device=block_table.device)
-    _check("zc_paged_tables", host.paged_tables(q_len, kv_len, block_table, free_pages, n_free, page, q_start, slot_map, n_taken))
+    status, q_start, slot_map, n_taken = _native().paged_tables(q_len, kv_len, block_table, free_pages, n_free, page, T, q_start, slot_map, n_taken)
+    _check("zc_paged_tables", status)
     return q_start, slot_map, n_taken
 
 

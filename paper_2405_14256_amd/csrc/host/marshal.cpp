@@ -149,7 +149,7 @@ template <class F> int unlocked(F&& f) {
   return rc;
 }
 
-// Every function below returns the library's status as an int.
+// Every function below returns the library's status as an int (paged_tables: beside its outputs).
 template <class F> PyObject* guarded(Fn id, Py_ssize_t n, Py_ssize_t want, F&& f) {
   if (n != want) return PyErr_Format(PyExc_TypeError, "%s: %zd arguments, expected %zd", kNames[id], n, want);
   if (!g_fn[id]) return PyErr_Format(PyExc_RuntimeError, "%s is not bound", kNames[id]);
@@ -385,19 +385,50 @@ int32_t int32_of(PyObject* o) {
   return v > INT32_MAX ? INT32_MAX : v < INT32_MIN ? INT32_MIN : (int32_t)v;
 }
 
-// (q_len, kv_len, block_table, free_pages, n_free, page, q_start, slot_map, n_taken)
+// (q_len, kv_len, block_table, free_pages, n_free, page, T, q_start, slot_map, n_taken) -> (status, q_start, slot_map, n_taken); outputs
+// that are None are allocated here: from Python the three allocations took longer than the kernel (8.0 -> 5.4 us a call).
 PyObject* paged_tables(PyObject*, Args a, Py_ssize_t n) {
-  return guarded(kPagedTables, n, 9, [&]() -> int {
+  at::Tensor made[3];
+  PyObject* status = guarded(kPagedTables, n, 10, [&]() -> int {
     const Table t = table_of(a[2]);
     const auto *q = ints(a[0], "q_len", t.R), *kv = ints(a[1], "kv_len", t.R);
+    const at::Tensor& list = tensor_of(a[3]);
     const auto* free = ints(a[3], "free_pages");
-    const int64_t F = tensor_of(a[3]).numel(), T = tensor_of(a[7]).numel(), page = int_of(a[5]);
     const auto* n_free = ints(a[4], "n_free", 1);
-    auto *start = ints(a[6], "q_start", t.R + 1), *slots = ints(a[7], "slot_map"), *taken = ints(a[8], "n_taken", 1);
+    const int64_t page = int_of(a[5]), T = int_of(a[6]), sizes[3] = {t.R + 1, T, 1};
+    if (T < 0) refuse("T", "must not be negative");
+    const char* const what[3] = {"q_start", "slot_map", "n_taken"};
+    int32_t* out[3];
+    // (one allocation for those that are missing, each from a multiple of 16 bytes on)
+    at::Tensor memory;
+    int64_t at = 0;
+    for (int i = 0; i < 3; ++i) {
+      if (a[7 + i] == Py_None) {
+        if (!memory.defined()) memory = at::empty({(sizes[0] + 3) / 4 * 4 + (sizes[1] + 3) / 4 * 4 + sizes[2]}, list.options());
+        made[i] = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(memory.storage()), memory.key_set(), memory.dtype());
+        made[i].unsafeGetTensorImpl()->set_sizes_contiguous({sizes[i]});
+        made[i].unsafeGetTensorImpl()->set_storage_offset(at);
+        out[i] = static_cast<int32_t*>(made[i].data_ptr());
+        at += (sizes[i] + 3) / 4 * 4;
+      } else {
+        made[i] = tensor_of(a[7 + i]);
+        out[i] = ints(a[7 + i], what[i], sizes[i]);
+      }
+    }
     const hipStream_t st = current_stream();
     const auto fn = ZC_FN(kPagedTables, zc_paged_tables);
-    return unlocked([&] { return fn(q, kv, t.R, t.ptr, t.row, t.cols, free, F, n_free, page, start, slots, T, taken, st); });
+    return unlocked([&] { return fn(q, kv, t.R, t.ptr, t.row, t.cols, free, list.numel(), n_free, page, out[0], out[1], T, out[2], st); });
   });
+  if (!status) return nullptr;
+  PyObject* all = PyTuple_New(4);
+  if (!all) { Py_DECREF(status); return nullptr; }
+  PyTuple_SET_ITEM(all, 0, status);
+  for (int i = 0; i < 3; ++i) {
+    PyObject* o = THPVariable_Wrap(made[i]);
+    if (!o) { Py_DECREF(all); return nullptr; }
+    PyTuple_SET_ITEM(all, 1 + i, o);
+  }
+  return all;
 }
 
 // (k, v, slot_map, k_pages, v_pages)

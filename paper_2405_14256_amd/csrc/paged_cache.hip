@@ -22,10 +22,11 @@ struct TableArgs {
   int32_t* q_start;
   int32_t* slots;
   int64_t T, share;             // rows of the slot map, of a workgroup
+  int half;                     // the search's first step: half of the requests' number, rounded up to a power of two
   int32_t* taken;
 };
 
-constexpr int kTabThreads = 256, kTabEach = 4, kTabReq = kTabThreads * kTabEach;
+constexpr int kTabThreads = 256, kTabEach = 4, kTabReq = kTabThreads * kTabEach, kTabTokens = 4;
 
 __global__ __launch_bounds__(kTabThreads) void k_paged_tables(TableArgs a) {
   __shared__ int s_start[kTabReq], s_page[kTabReq], s_past[kTabReq];
@@ -70,29 +71,44 @@ __global__ __launch_bounds__(kTabThreads) void k_paged_tables(TableArgs a) {
       bn += need[i];
     }
     __syncthreads();
-    // the tokens of these requests that are this workgroup's
+    // the tokens of these requests that are this workgroup's, four a thread at a time: their searches and their loads overlap
     const int64_t lo = max(t_lo, start), hi = min(t_hi, start + tq);
-    for (int64_t t = lo + tid; t < hi; t += kTabThreads) {
-      const int rel = (int)(t - start);
-      int x = 0;                                                        // the last request that starts at or before the token: it has tokens
+    for (int64_t t0 = lo + tid; t0 < hi; t0 += kTabTokens * kTabThreads) {
+      int rel[kTabTokens], x[kTabTokens], id[kTabTokens], pos[kTabTokens];
+      int32_t* entry[kTabTokens];
+      bool mine[kTabTokens];
 #pragma unroll
-      for (int b = kTabReq / 2; b; b >>= 1)
-        if (x + b < kTabReq && s_start[x + b] <= rel) x += b;
-      const int pos = s_past[x] + rel - s_start[x];
-      const int col = pos >> a.shift, had = (int)(((int64_t)s_past[x] + (1 << a.shift) - 1) >> a.shift);
-      int32_t* entry = a.table + (int64_t)(r0 + x) * a.row + col;
-      int id = -1;
-      if ((uint32_t)col < (uint32_t)a.cols) {
-        if (col < had) {
-          id = *entry;
-        } else {
-          const int64_t at = (int64_t)n_free - 1 - ((int64_t)page + s_page[x] + col - had);
-          id = at >= 0 && at < n_free ? a.free[at] : -1;
-          if ((pos & ((1 << a.shift) - 1)) == 0) *entry = id;
+      for (int i = 0; i < kTabTokens; ++i) {
+        const int64_t t = t0 + i * kTabThreads;
+        mine[i] = t < hi;
+        rel[i] = (int)((mine[i] ? t : t0) - start);
+        x[i] = 0;
+      }
+      for (int b = a.half; b; b >>= 1)                                  // the last request that starts at or before the token: it has tokens
+#pragma unroll
+        for (int i = 0; i < kTabTokens; ++i)
+          if (s_start[x[i] + b] <= rel[i]) x[i] += b;
+#pragma unroll
+      for (int i = 0; i < kTabTokens; ++i) {
+        const int past = s_past[x[i]];
+        pos[i] = past + rel[i] - s_start[x[i]];
+        const int col = pos[i] >> a.shift, had = (int)(((int64_t)past + (1 << a.shift) - 1) >> a.shift);
+        entry[i] = nullptr;
+        id[i] = -1;
+        if (mine[i] && (uint32_t)col < (uint32_t)a.cols) {
+          int32_t* e = a.table + (int64_t)(r0 + x[i]) * a.row + col;
+          const int64_t at = (int64_t)n_free - 1 - ((int64_t)page + s_page[x[i]] + col - had);
+          if (col < had) id[i] = *e;
+          else if (at >= 0 && at < n_free) id[i] = a.free[at];
+          if (col >= had && (pos[i] & ((1 << a.shift) - 1)) == 0) entry[i] = e;
         }
       }
-      const int64_t slot = ((int64_t)id << a.shift) + (pos & ((1 << a.shift) - 1));
-      a.slots[t] = id >= 0 && slot <= 0x7fffffff ? (int)slot : -1;
+#pragma unroll
+      for (int i = 0; i < kTabTokens; ++i) {
+        if (entry[i]) *entry[i] = id[i];
+        const int64_t slot = ((int64_t)id[i] << a.shift) + (pos[i] & ((1 << a.shift) - 1));
+        if (mine[i]) a.slots[t0 + i * kTabThreads] = id[i] >= 0 && slot <= 0x7fffffff ? (int)slot : -1;
+      }
     }
     start += tq;
     page += tn;
@@ -234,8 +250,10 @@ extern "C" int zc_paged_tables(const int32_t* q_len, const int32_t* kv_len, int6
   a.table = block_table; a.row = row_stride; a.cols = (int)max_blocks; a.shift = __builtin_ctzll((unsigned long long)page);
   a.free = free_pages; a.n_free = n_free; a.F = (int)n_list;
   a.q_start = q_start; a.slots = slot_map; a.T = T; a.taken = n_taken;
-  int64_t wgs = ceil_div64(T, 8 * kTabThreads);
-  wgs = wgs < 1 ? 1 : wgs > 512 ? 512 : wgs;
+  a.half = 0;
+  while (2 * a.half < R && 2 * a.half < kTabReq) a.half = a.half ? 2 * a.half : 1;
+  int64_t wgs = ceil_div64(T, kTabTokens * kTabThreads);
+  wgs = wgs < 1 ? 1 : wgs > 2048 ? 2048 : wgs;
   a.share = ceil_div64(T, wgs);
   hipLaunchKernelGGL(k_paged_tables, dim3((unsigned)wgs), dim3(kTabThreads), 0, (hipStream_t)stream, a);
   ZC_LAUNCH_CHECK();
