@@ -349,6 +349,14 @@ int32_t* ints(PyObject* o, const char* what, int64_t n = -1) {
   if (n >= 0 && t.numel() != n) refuse(what, "has another number of elements than the requests or rows ask for");
   return static_cast<int32_t*>(t.data_ptr());
 }
+bool capturing(hipStream_t stream) {
+  hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(stream, &status) != hipSuccess) {
+    (void)hipGetLastError();
+    return false;                          // (the default stream beside a capture)
+  }
+  return status != hipStreamCaptureStatusNone;
+}
 struct Table { int32_t* ptr; int64_t R, row, cols; };
 Table table_of(PyObject* o) {
   const at::Tensor& t = tensor_of(o);
@@ -474,8 +482,14 @@ PyObject* paged_attention(PyObject*, Args a, Py_ssize_t n) {
     const size_t need = ZC_FN(kPagedAttentionWs, zc_paged_attention_workspace)(t.R, q.L, q.H, kp.H, q.D);
     void* wp = nullptr;
     size_t wn = 0;
+    // (a captured call takes memory of its graph, given back behind it in the order of the capture: graphs share nothing, whatever
+    // stream they were captured on and whatever streams replay them)
     Scratch ws;
-    if (need) {
+    if (need && capturing(st)) {
+      ws.t = at::empty({(int64_t)need}, tensor_of(a[0]).options().dtype(at::kByte));
+      wp = ws.t.data_ptr();
+      wn = need;
+    } else if (need) {
       ws = scratch(need, tensor_of(a[0]), kScratchPaged, st);
       wp = ws.ptr;
       wn = ws.bytes;

@@ -368,6 +368,36 @@ def test_a_captured_step_replays_with_other_lengths():
     assert int(n_free) == len(spare) - sum(-(-(n + steps) // page) - -(-n // page) for n in first)
 
 
+def test_graphs_captured_on_one_stream_replay_side_by_side():
+    """Two graphs whose calls are split and joined through workspaces: each has its own."""
+    ps = [plain.Pages([1, 1], [6000, 300], 8, 2, 128, BF, seed=20 + i) for i in range(2)]
+    want = [_attend(p) for p in ps]
+    side = torch.cuda.Stream()
+    graphs, outs = [], []
+    for p in ps:
+        o, n = torch.zeros_like(p.q), torch.zeros(8, p.T, dtype=torch.float32, device=DEV)
+        side.wait_stream(torch.cuda.current_stream())
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            for _ in range(20):
+                zb.zc_paged_attention(p.q, p.kp, p.vp, p.table, p.q_start, p.kv, out=o, lse=n)
+        graphs.append(g)
+        outs.append((o, n))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in ps]
+    for _ in range(5):
+        for (o, n) in outs:
+            o.zero_()
+            n.zero_()
+        torch.cuda.synchronize()
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+        torch.cuda.synchronize()
+        for (o, n), (wo, wn) in zip(outs, want):
+            assert torch.equal(o, wo) and torch.equal(n, wn)
+
+
 # ---- together -----------------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("dtype", [BF, FL])
