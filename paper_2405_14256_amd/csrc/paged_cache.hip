@@ -120,6 +120,11 @@ __global__ __launch_bounds__(kTabThreads) void k_paged_tables(TableArgs a) {
   }
 }
 
+// 16 bytes that pass through once: stored without taking a place in the caches.
+typedef uint32_t piece16 __attribute__((ext_vector_type(4)));
+__device__ inline void put(uint8_t* to, piece16 x) { __builtin_nontemporal_store(x, reinterpret_cast<piece16*>(to)); }
+__device__ inline piece16 get(const uint8_t* from) { return *reinterpret_cast<const piece16*>(from); }
+
 // ---- zc_paged_store -------------------------------------------------------------------------------
 struct StoreArgs {
   const uint8_t *k, *v;
@@ -133,7 +138,8 @@ struct StoreArgs {
 };
 
 // A thread copies one 16-byte piece of UNROLL tokens: pieces of a token are consecutive threads, keys and then values.
-// Bound by memory; the loads of all tokens are issued before the first store.
+// Bound by memory; the loads of all tokens are issued before the first store.  8066 tokens of 40 heads of 128 channels, fp16,
+// pages of 32: 62 us (5.3 TB/s; 73 with stores through the caches, 105 with eight tokens a thread); 64 tokens 2.0 us.
 template <int UNROLL>
 __global__ __launch_bounds__(256) void k_paged_store(StoreArgs a) {
   const int piece = blockIdx.y * 256 + threadIdx.x % a.wide, first = threadIdx.x / a.wide;
@@ -146,7 +152,7 @@ __global__ __launch_bounds__(256) void k_paged_store(StoreArgs a) {
   uint8_t* dst = (value ? a.vp + h * a.vp_sH : a.kp + h * a.kp_sH) + c;
   const int64_t src_t = value ? a.v_sL : a.k_sL, dst_b = value ? a.vp_sB : a.kp_sB, dst_t = value ? a.vp_sL : a.kp_sL;
   const int64_t t0 = (int64_t)blockIdx.x * a.tokens * UNROLL + first;
-  uint4 x[UNROLL];
+  piece16 x[UNROLL];
   int slot[UNROLL];
 #pragma unroll
   for (int u = 0; u < UNROLL; ++u) {
@@ -155,11 +161,11 @@ __global__ __launch_bounds__(256) void k_paged_store(StoreArgs a) {
   }
 #pragma unroll
   for (int u = 0; u < UNROLL; ++u)
-    if (slot[u] >= 0 && slot[u] < a.slots_n) x[u] = *reinterpret_cast<const uint4*>(src + (t0 + (int64_t)u * a.tokens) * src_t);
+    if (slot[u] >= 0 && slot[u] < a.slots_n) x[u] = get(src + (t0 + (int64_t)u * a.tokens) * src_t);
 #pragma unroll
   for (int u = 0; u < UNROLL; ++u)
     if (slot[u] >= 0 && slot[u] < a.slots_n)
-      *reinterpret_cast<uint4*>(dst + (slot[u] >> a.shift) * dst_b + (slot[u] & ((1 << a.shift) - 1)) * dst_t) = x[u];
+      put(dst + (slot[u] >> a.shift) * dst_b + (slot[u] & ((1 << a.shift) - 1)) * dst_t, x[u]);
 }
 
 // ---- zc_paged_load --------------------------------------------------------------------------------
@@ -173,7 +179,8 @@ struct LoadArgs {
   int64_t kp_sB, kp_sH, kp_sL, vp_sB, vp_sH, vp_sL;
 };
 
-// A workgroup copies 256 * UNROLL pieces of one head of one request.  Bound by memory.
+// A workgroup copies 256 * UNROLL pieces of one head of one request.  Bound by memory: 16 requests of 3500 to 4096 tokens, 40 heads
+// of 128 channels, fp16, 435 us (5.7 TB/s; 467 with stores through the caches), one of 4096 tokens, 8 heads, bf16, 6.3 us.
 template <int UNROLL>
 __global__ __launch_bounds__(256) void k_paged_load(LoadArgs a) {
   const int r = blockIdx.z >> 1, h = blockIdx.y;
@@ -185,7 +192,7 @@ __global__ __launch_bounds__(256) void k_paged_load(LoadArgs a) {
   uint8_t* dst = (value ? a.v + r * a.v_sB + h * a.v_sH : a.k + r * a.k_sB + h * a.k_sH) + c;
   const int64_t src_b = value ? a.vp_sB : a.kp_sB, src_t = value ? a.vp_sL : a.kp_sL, dst_t = value ? a.v_sL : a.k_sL;
   int id[UNROLL];
-  uint4 x[UNROLL];
+  piece16 x[UNROLL];
 #pragma unroll
   for (int u = 0; u < UNROLL; ++u) {
     const int i = i0 + u * rows, col = i >> a.shift;
@@ -193,12 +200,12 @@ __global__ __launch_bounds__(256) void k_paged_load(LoadArgs a) {
   }
 #pragma unroll
   for (int u = 0; u < UNROLL; ++u) {
-    x[u] = make_uint4(0, 0, 0, 0);
-    if (id[u] >= 0 && id[u] < a.n_pages) x[u] = *reinterpret_cast<const uint4*>(src + id[u] * src_b + ((i0 + u * rows) & ((1 << a.shift) - 1)) * src_t);
+    x[u] = piece16{0, 0, 0, 0};
+    if (id[u] >= 0 && id[u] < a.n_pages) x[u] = get(src + id[u] * src_b + ((i0 + u * rows) & ((1 << a.shift) - 1)) * src_t);
   }
 #pragma unroll
   for (int u = 0; u < UNROLL; ++u)
-    if (i0 + u * rows < n) *reinterpret_cast<uint4*>(dst + (i0 + u * rows) * dst_t) = x[u];
+    if (i0 + u * rows < n) put(dst + (i0 + u * rows) * dst_t, x[u]);
 }
 
 }  // namespace zc
@@ -325,8 +332,8 @@ extern "C" int zc_paged_load(const zc_tensor4* k_pages, const zc_tensor4* v_page
   const int rows = 256 >> a.cpr;
   const bool many = ceil_div64(a.L, rows) * k->H * k->B * 2 >= 4096;
   hipStream_t st = (hipStream_t)stream;
-  const dim3 grid((unsigned)ceil_div64(a.L, many ? 4 * rows : rows), (unsigned)k->H, (unsigned)(2 * k->B));
-  if (many) hipLaunchKernelGGL(k_paged_load<4>, grid, dim3(256), 0, st, a);
+  const dim3 grid((unsigned)ceil_div64(a.L, many ? 2 * rows : rows), (unsigned)k->H, (unsigned)(2 * k->B));
+  if (many) hipLaunchKernelGGL(k_paged_load<2>, grid, dim3(256), 0, st, a);
   else hipLaunchKernelGGL(k_paged_load<1>, grid, dim3(256), 0, st, a);
   ZC_LAUNCH_CHECK();
   return ZC_OK;
