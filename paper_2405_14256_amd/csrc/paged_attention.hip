@@ -275,12 +275,7 @@ __device__ __forceinline__ void attend_rows(const PagedArgs& a, const Unit& x, i
   int blocks = 2 * (x.t_hi - x.t_lo);
   if (blocks > 0 && tile_of(x, x.t_hi - 1) * kTile + 32 > x.p1) --blocks;
   int t = w;
-  Ids at;
-  if (t < blocks) {
-    at = pages(t);
-    issue(at, kb, a.k_sB, a.k_row, k_lds, kvoff);
-    issue(at, vb, a.v_sB, a.v_row, v_lds, vvoff);
-  }
+  Ids at = pages(t);                             // (of no block of the unit: any page, and nothing is requested)
 
   // this lane's row, straight into operand registers
   const bool mine = r < x.rows;
@@ -294,6 +289,10 @@ __device__ __forceinline__ void attend_rows(const PagedArgs& a, const Unit& x, i
     const uint8_t* qr = a.q + hq * a.q_sH + tok * a.q_sT + kh * 16;
 #pragma unroll
     for (int kc = 0; kc < T::NKC; ++kc) qf[kc] = *reinterpret_cast<const u32x4*>(qr + kc * 32);
+  }
+  if (t < blocks) {
+    issue(at, kb, a.k_sB, a.k_row, k_lds, kvoff);
+    issue(at, vb, a.v_sB, a.v_row, v_lds, vvoff);
   }
 
   typedef __attribute__((address_space(3))) const uint8_t* lds_ptr;
@@ -509,20 +508,9 @@ __device__ __forceinline__ void attend_tiles(const PagedArgs& a, const Unit& x, 
     for (int jj = 0; jj < NI; ++jj) v[jj] = vplace + jj * T::RPI * (int)a.v_row;
     move_keys<NI>(vs_lds + place * TILE_B, rs, v);
   };
-  Group gv = {0, -1}, gk = {0, -1};              // of V(t + AHEAD) and K(t + AHEAD + 1), t the next tile
-  if (ntiles > 0) {
-    Group g[AHEAD + 2];                          // (all pages are asked for before the first is used)
+  Group g[AHEAD + 2];                            // (all pages are asked for before the first is used; of tiles that are not the unit's: any)
 #pragma unroll
-    for (int t = 0; t < AHEAD + 2; ++t) g[t] = group(t);
-    k_issue(0, g[0]);
-#pragma unroll
-    for (int t = 0; t < AHEAD; ++t) {
-      if (t < ntiles) v_issue(t, g[t]);
-      if (t + 1 < ntiles) k_issue((t + 1) % STAGES, g[t + 1]);
-    }
-    gv = g[AHEAD];
-    gk = g[AHEAD + 1];
-  }
+  for (int t = 0; t < AHEAD + 2; ++t) g[t] = group(t);
 
   // this lane's row, straight into operand registers
   const int pos = r < wrows ? x.kv - x.nq + row_at(a, x, 32 * w + r).j : INT_MIN;
@@ -535,6 +523,15 @@ __device__ __forceinline__ void attend_tiles(const PagedArgs& a, const Unit& x, 
 #pragma unroll
     for (int kc = 0; kc < T::NKC; ++kc) qf[kc] = *reinterpret_cast<const u32x4*>(qr + kc * 32);
   }
+  if (ntiles > 0) {
+    k_issue(0, g[0]);
+#pragma unroll
+    for (int t = 0; t < AHEAD; ++t) {
+      if (t < ntiles) v_issue(t, g[t]);
+      if (t + 1 < ntiles) k_issue((t + 1) % STAGES, g[t + 1]);
+    }
+  }
+  Group gv = g[AHEAD], gk = g[AHEAD + 1];        // of V(t + AHEAD) and K(t + AHEAD + 1), t the next tile
 
   // ---- operands from LDS -----------------------------------------------------------------
   struct KFrag { u32x4 x[T::NKC]; };
@@ -952,8 +949,9 @@ extern "C" int zc_paged_attention(const zc_tensor4* q, const zc_tensor4* k_pages
   a.q_sH = q->sH * eb; a.q_sT = q->sL * eb; a.o_sH = out->sH * eb; a.o_sT = out->sL * eb;
   a.k_sB = k_pages->sB * eb; a.k_sH = k_pages->sH * eb; a.v_sB = v_pages->sB * eb; a.v_sH = v_pages->sH * eb;
   a.k_row = (uint32_t)(k_pages->sL * eb); a.v_row = (uint32_t)(v_pages->sL * eb);
-  a.table = block_table; a.q_start = q_start; a.kv_len = kv_len; a.row = row_stride;
-  a.cols = (int)max_blocks; a.shift = __builtin_ctzll((unsigned long long)page); a.n_pages = (int)k_pages->B; a.cap = (int)room;
+  // (a table without columns holds no token: any readable word stands for its pages)
+  a.table = max_blocks ? block_table : q_start; a.q_start = q_start; a.kv_len = kv_len; a.row = max_blocks ? row_stride : 0;
+  a.cols = max_blocks ? (int)max_blocks : 1; a.shift = __builtin_ctzll((unsigned long long)page); a.n_pages = (int)k_pages->B; a.cap = (int)room;
   a.R = (int)R; a.T = (int)T; a.Hkv = (int)Hkv; a.G = (int)G;
   a.window = window;
   a.sinks = sinks;

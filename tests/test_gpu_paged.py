@@ -300,6 +300,9 @@ def test_nothing_to_do():
     out = torch.full_like(p.q, 5.0)
     zb.zc_paged_attention(p.q, p.kp, p.vp, p.table[:0], torch.zeros(1, **I32), none, out=out)
     assert bool((out == 5.0).all())
+    out, lse = torch.full_like(p.q, 5.0), torch.full((4, 1), 5.0, dtype=torch.float32, device=DEV)
+    zb.zc_paged_attention(p.q, p.kp, p.vp, p.table[:, :0], p.q_start, p.kv, out=out, lse=lse)          # a table without room: no token is seen
+    assert bool((out == 0).all()) and bool((lse == -float("inf")).all())
     zb.zc_paged_store(p.q[:0, :2], p.q[:0, :2], none, p.kp, p.vp)
     k, v = zb.zc_paged_load(p.kp, p.vp, p.table[:0], none)
     assert k.shape == (0, 2, 16, 64)
