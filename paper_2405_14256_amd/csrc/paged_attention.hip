@@ -57,11 +57,14 @@ __device__ inline uint32_t pack_two(float lo, float hi) {
 // ---- the work of a wave ---------------------------------------------------------------------------
 // Key tiles are of 64 keys.  A request of few rows goes in blocks of 32 rows whose keys four waves share, any other (of 16-bit
 // types) in blocks of 128, 32 a wave: with one token a request the first way has four waves at work where the second has one,
-// and the first waits for no barrier; with many rows the second reads a key once for four times as many.
+// and the first waits for no barrier; with many rows the second reads a key once for four times as many.  us by 128 and by 32 rows,
+// 32 heads over 8 of 128 channels, bf16: 16 requests of 4096 tokens, 9 of them new (36 rows) 58.4 and 53.8, 16 (64) 60.4 and 55.0; 1 of 8192, 16 new 29.1
+// and 22.4; 8 of 200 to 500, 10 to 16 new 15.9 and 10.5; 4 of 4096, 32 new (128 rows) 29.1 and 30.3; of 64 channels, 2 of 1000 to 3000, 40 to 64 new
+// (one head a group) 16.7 and 14.6.
 constexpr int kTile = 64;
 template <int DT> struct Blocks {
   static constexpr int kMany = DT == ZC_F32 ? 32 : 128;                   // rows of a block, of many rows
-  __device__ static bool few(int rows) { return DT == ZC_F32 || rows <= 32; }
+  __device__ static bool few(int rows) { return DT == ZC_F32 || rows <= 64; }
 };
 
 struct Unit {
@@ -747,71 +750,71 @@ __global__ __launch_bounds__(256, DT == ZC_F32 && D == 128 ? 1 : 2) void k_paged
 }
 
 // ---- the join of split blocks ---------------------------------------------------------------------------
-// A workgroup per unit; those of a unit that a split block begins with join it, 32 rows each (the grid's third axis: which).  D / 4 threads take a row; where rows are few, several such groups share a row's parts and join what
-// they have in LDS.  Bound by two trips to memory.
-constexpr int kJoinThreads = 256;
+// Four workgroups per unit; those of a unit that a split block begins with join it, every fourth 256 / (D / 4) rows
+// each.  D / 4 threads take a row; where rows are few, several such groups share a row's parts and join what they have in LDS.  Bound by two trips to memory.
+constexpr int kJoinGroups = 4;
 template <int DT, int D>
-__global__ __launch_bounds__(kJoinThreads) void k_paged_join(PagedArgs a) {
-  constexpr int TPR = D / 4, GROUPS = kJoinThreads / TPR;
+__global__ __launch_bounds__(256) void k_paged_join(PagedArgs a) {
+  constexpr int TPR = D / 4, GROUPS = 256 / TPR;
   __shared__ __align__(16) float so[GROUPS][D];
   __shared__ float2 sml[GROUPS];
-  const int hk = blockIdx.x, unit = blockIdx.y, row0 = blockIdx.z * 32;
+  const int hk = blockIdx.x, unit = blockIdx.y;
   const int4 todo = a.todo[(int64_t)hk * a.units + unit];
-  const int parts = todo.x, rows = min(todo.y, row0 + 32);
-  if (parts == 0 || rows <= row0 || unit + parts > a.units) return;
+  const int parts = todo.x, rows = todo.y;
+  if (parts == 0 || unit + parts > a.units) return;
   const int grp = threadIdx.x / TPR, c = threadIdx.x % TPR * 4;
-  int ways = 1;                                          // groups to a row
-  while (2 * ways * (rows - row0) <= GROUPS && 2 * ways <= parts) ways *= 2;
-  const int way = grp & (ways - 1), at_once = GROUPS / ways;
   const int64_t first = part_row(a, hk, unit);
-  for (int row = row0 + grp / ways; row < rows; row += at_once) {
+  for (int row0 = blockIdx.z * GROUPS; row0 < rows; row0 += kJoinGroups * GROUPS) {
+    const int n = min(rows - row0, GROUPS);
+    int ways = 1;                                          // groups to a row
+    while (2 * ways * n <= GROUPS && 2 * ways <= parts) ways *= 2;
+    const int way = grp & (ways - 1), row = row0 + grp / ways;
+    const bool mine = row < row0 + n;
     float M = kLowestLogit, l = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    constexpr int U = 4;                                 // parts requested at a time
-    for (int s0 = way; s0 < parts; s0 += U * ways) {
-      float2 ml[U];
-      float4 t[U];
+    if (mine) {
+      constexpr int U = 4;                                 // parts requested at a time
+      for (int s0 = way; s0 < parts; s0 += U * ways) {
+        float2 ml[U];
+        float4 t[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int s = s0 + u * ways;
-        const int64_t p = first + (int64_t)(s < parts ? s : s0) * a.slot + row;
-        ml[u] = *reinterpret_cast<const float2*>(a.part_ml + p * 2);
-        t[u] = *reinterpret_cast<const float4*>(a.part_o + p * D + c);
-      }
-      float top = M;
+        for (int u = 0; u < U; ++u) {
+          const int s = s0 + u * ways;
+          const int64_t p = first + (int64_t)(s < parts ? s : s0) * a.slot + row;
+          ml[u] = *reinterpret_cast<const float2*>(a.part_ml + p * 2);
+          t[u] = *reinterpret_cast<const float4*>(a.part_o + p * D + c);
+        }
+        float top = M;
 #pragma unroll
-      for (int u = 0; u < U; ++u) top = fmaxf(top, ml[u].x);
-      const float f0 = __builtin_amdgcn_exp2f(M - top);
-      M = top;
-      l *= f0; o.x *= f0; o.y *= f0; o.z *= f0; o.w *= f0;
+        for (int u = 0; u < U; ++u) top = fmaxf(top, ml[u].x);
+        const float f0 = __builtin_amdgcn_exp2f(M - top);
+        M = top;
+        l *= f0; o.x *= f0; o.y *= f0; o.z *= f0; o.w *= f0;
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const float f = s0 + u * ways < parts ? __builtin_amdgcn_exp2f(ml[u].x - M) : 0.f;
-        l = fmaf(ml[u].y, f, l);
-        o.x = fmaf(t[u].x, f, o.x); o.y = fmaf(t[u].y, f, o.y); o.z = fmaf(t[u].z, f, o.z); o.w = fmaf(t[u].w, f, o.w);
+        for (int u = 0; u < U; ++u) {
+          const float f = s0 + u * ways < parts ? __builtin_amdgcn_exp2f(ml[u].x - M) : 0.f;
+          l = fmaf(ml[u].y, f, l);
+          o.x = fmaf(t[u].x, f, o.x); o.y = fmaf(t[u].y, f, o.y); o.z = fmaf(t[u].z, f, o.z); o.w = fmaf(t[u].w, f, o.w);
+        }
       }
     }
-    if (ways > 1) {                                      // (all rows at once: a thread comes here once at most)
+    if (ways > 1) {
       if (c == 0) sml[grp] = make_float2(M, l);
       *reinterpret_cast<float4*>(&so[grp][c]) = o;
-    } else {
-      store_row<DT>(a, todo.z, todo.w, hk, row, c, M, l, o);
+      __syncthreads();
+      if (mine && way == 0) {
+        for (int v = 1; v < ways; ++v) {
+          const float2 ml = sml[grp + v];
+          const float4 t = *reinterpret_cast<const float4*>(&so[grp + v][c]);
+          const float top = fmaxf(M, ml.x), f0 = __builtin_amdgcn_exp2f(M - top), f = __builtin_amdgcn_exp2f(ml.x - top);
+          M = top;
+          l = fmaf(ml.y, f, l * f0);
+          o.x = fmaf(t.x, f, o.x * f0); o.y = fmaf(t.y, f, o.y * f0); o.z = fmaf(t.z, f, o.z * f0); o.w = fmaf(t.w, f, o.w * f0);
+        }
+      }
+      __syncthreads();
     }
-  }
-  if (ways == 1) return;
-  __syncthreads();
-  if (way == 0 && row0 + grp / ways < rows) {
-    float M = kLowestLogit, l = 0.f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int v = 0; v < ways; ++v) M = fmaxf(M, sml[grp + v].x);
-    for (int v = 0; v < ways; ++v) {
-      const float2 ml = sml[grp + v];
-      const float4 t = *reinterpret_cast<const float4*>(&so[grp + v][c]);
-      const float f = __builtin_amdgcn_exp2f(ml.x - M);
-      l = fmaf(ml.y, f, l);
-      o.x = fmaf(t.x, f, o.x); o.y = fmaf(t.y, f, o.y); o.z = fmaf(t.z, f, o.z); o.w = fmaf(t.w, f, o.w);
-    }
-    store_row<DT>(a, todo.z, todo.w, hk, row0 + grp / ways, c, M, l, o);
+    if (mine && way == 0) store_row<DT>(a, todo.z, todo.w, hk, row, c, M, l, o);
   }
 }
 
@@ -859,9 +862,11 @@ static int64_t parts_of(int64_t n, int64_t tiles, int dtype, int64_t D) {
 // keys: a request's, at most; INT64_MAX: as many as cost the most workspace.
 static Cut cut_of(int64_t R, int64_t T, int64_t G, int64_t Hkv, int dtype, int64_t D, int64_t keys, int64_t window, int64_t sinks) {
   Cut c;
-  c.slot = dtype == ZC_F32 || T * G <= 32 ? 32 : 128;
-  c.blocks = T * G / c.slot + (R < T ? R : T);   // (a request has one block that is not full)
-  const bool few = T * G <= 32 * R;
+  c.slot = dtype == ZC_F32 || T * G <= 64 ? 32 : 128;
+  // (a request has one block that is not full; where blocks of 128 rows are the rule, one of 33 to 64 rows is two of 32)
+  const int64_t with = R < T ? R : T, two = T * G / 33;
+  c.blocks = T * G / c.slot + with + (c.slot == 32 ? 0 : two < with ? two : with);
+  const bool few = T * G <= 64 * R;
   const int64_t n = few ? c.blocks * Hkv : ceil_div64(T * G, c.slot) * Hkv;
   if (few ? n > 1024 : n > kUnits / 2 || c.blocks * Hkv + kUnits > kMostUnits) { c.target = 0; return c; }
   if (keys == INT64_MAX) {
@@ -875,8 +880,9 @@ static Cut cut_of(int64_t R, int64_t T, int64_t G, int64_t Hkv, int dtype, int64
   } else if (few) {
     // Single tokens: two workgroups a CU, whatever the lengths.  us at 256, 512, 768 and 1024 units: 8 requests of 8192 keys (32 heads
     // over 8 of 128 channels, bf16) 52.4, 53.0, 54.6 and 56.0; 1 of 32768 32.9, 33.3, 36.0 and 39.1; 4 of 20000 to 32768 105, 81, 82 and 84;
-    // 64 of 64 to 8192 110, 104.9, 101.5 and 102.9; 3 of 1000 to 9000, 16 heads, fp32 104, 72, 83 and 89.
-    c.target = ceil_div64(512, Hkv);
+    // 64 of 64 to 8192 110, 104.9, 101.5 and 102.9; 3 of 1000 to 9000, 16 heads, fp32 104, 72, 83 and 89.  One a CU where a request has two
+    // blocks, which read the same keys: 256 and 512 units, 16 new tokens of 4 requests of 4096 20.0 and 20.6, of 16 55.6 and 60.7, of one of 8192 15.8 and 19.5.
+    c.target = ceil_div64(T * G > 32 * R ? 256 : 512, Hkv);
   } else {
     // (blocks of a prompt that begins with this step see half of its keys on average, the longest go first: rounds even out)
     const int64_t past = keys > 2 * T ? keys - 2 * T : 0;
@@ -895,8 +901,8 @@ static int launch_paged(PagedArgs& a, hipStream_t st) {
   hipLaunchKernelGGL((k_paged_attention<DT, D>), grid(a.units), dim3(256), 0, st, a);
   ZC_LAUNCH_CHECK();
   if (a.target) {
-    const dim3 joins((unsigned)a.Hkv, (unsigned)a.units, (unsigned)(a.slot / 32));     // (units: at most kMostUnits)
-    hipLaunchKernelGGL((k_paged_join<DT, D>), joins, dim3(kJoinThreads), 0, st, a);
+    const dim3 joins((unsigned)a.Hkv, (unsigned)a.units, (unsigned)kJoinGroups);     // (units: at most kMostUnits)
+    hipLaunchKernelGGL((k_paged_join<DT, D>), joins, dim3(256), 0, st, a);
     ZC_LAUNCH_CHECK();
   }
   return ZC_OK;

@@ -196,6 +196,50 @@ def test_rows_that_see_nothing(dtype):
         assert bool((out[:q[0] - kv[0]] == 0).all()) and bool((lse[:, :q[0] - kv[0]] == -float("inf")).all())
 
 
+# a request's rows in one block, in two of 32 (33 to 64 rows), in blocks of 128 (fp32: always of 32); parts of their keys joined by a second
+# launch or not: new tokens, all tokens, query and KV heads, channels, page, window, sinks
+BLOCKS = [([8, 9, 16, 17, 1], [8, 900, 400, 3000, 2500], 8, 2, 128, 16, 0, 0), ([33, 64, 65, 32], [33, 2000, 1100, 5000], 3, 3, 64, 32, 0, 0),
+          ([512], [4000], 4, 2, 128, 64, 0, 0), ([200], [9000], 2, 1, 64, 16, 0, 0), ([130, 1, 7], [6000, 6000, 6000], 8, 4, 64, 128, 2500, 70),
+          ([40, 300], [5000, 4097], 6, 1, 128, 32, 3001, 4), ([0] * 100 + [3] + [0] * 40 + [90], [50] * 100 + [2600] + [0] * 40 + [700], 8, 2, 64, 16, 0, 0),
+          ([21] * 3, [4096] * 3, 12, 4, 64, 65536, 0, 0), ([1], [3000], 96, 1, 64, 16, 0, 0), ([5], [200], 70, 2, 128, 16, 50, 3)]
+
+
+@pytest.mark.parametrize("dtype", [BF, HF, FL])
+@pytest.mark.parametrize("case", range(len(BLOCKS)))
+def test_blocks_and_parts(case, dtype):
+    q, kv, Hq, Hkv, D, page, window, sinks = BLOCKS[case]
+    _run(q, kv, Hq, Hkv, D, dtype, window, sinks, page=page, by_head=case % 2 == 0, pad=case % 3)
+
+
+@pytest.mark.parametrize("seed", range(40))
+def test_any_lengths(seed):
+    rng = random.Random(1000 + seed)
+    dtype, D = rng.choice((BF, HF, FL)), rng.choice((64, 128))
+    Hkv, G = rng.choice((1, 2, 3, 5)), rng.choice((1, 2, 3, 4, 7, 8, 11))
+    R = rng.choice((1, 2, 5, 20, 70))
+    top = 5000 // R + 40
+    kv = [rng.randint(0, top) if rng.random() < 0.9 else rng.randint(0, 3) for _ in range(R)]
+    q = [min(n + rng.choice((0, 0, 0, 2)), rng.choice((0, 1, 1, rng.randint(1, 20), rng.randint(1, 200)))) for n in kv]
+    window, sinks = rng.choice(((0, 0), (0, 0), (rng.randint(1, 300), 0), (rng.randint(1, 2000), rng.randint(0, 99))))
+    if sum(q) == 0:
+        q[0], kv[0] = 1, max(kv[0], 1)
+    _run(q, kv, Hkv * G, Hkv, D, dtype, window, sinks, page=rng.choice((16, 32, 64, 256)), by_head=rng.random() < 0.5, pad=rng.choice((0, 5)))
+
+
+@pytest.mark.parametrize("dtype", [BF, HF, FL])
+@pytest.mark.parametrize("q,kv", [([1], [4000]), ([150], [4000])])
+def test_parts_without_a_logit_above_minus_infinity(q, kv, dtype):
+    """The first 2000 keys of 4000, more than one part of them, have logits of -inf: their parts weigh nothing."""
+    p = plain.Pages(q, kv, 4, 2, 64, dtype, seed=4)
+    p.q[..., 1] = 1.0
+    p.k[0][:, :2000, 1] = -float("inf")
+    p.write(0)
+    out, lse = _attend(p)
+    o, n, size, _ = p.want()
+    u = {BF: 2.0 ** -7, HF: 2.0 ** -10, FL: 2.0 ** -13}[dtype]                 # (the weights and the result; fp32: of logits of up to 2^3)
+    assert bool(((out.double() - o).abs() <= u * size + 1e-4).all()) and (lse.double() - n).abs().max().item() <= 1e-4
+
+
 @pytest.mark.parametrize("dtype", [BF, HF, FL])
 @pytest.mark.parametrize("q,kv", [([1], [300]), ([90], [300])])
 def test_keys_whose_logits_are_minus_infinity(q, kv, dtype):
