@@ -336,6 +336,12 @@ def test_a_long_request_beside_short_ones(dtype):
     _run([1, 1], [20000, 20000], 8, 2, 64, dtype, page=64, window=7000, sinks=100)
 
 
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_a_long_request_beside_a_chunk_that_fills_the_chip(dtype):
+    """The chunk's blocks are whole, the long request's is in parts."""
+    _run([900, 1, 1], [900, 300, 20000], 20, 20, 64, dtype, page=64)
+
+
 def test_nothing_to_do():
     p = plain.Pages([1], [5], 4, 2, 64, BF)
     none = torch.zeros(0, **I32)
