@@ -869,8 +869,16 @@ static Cut cut_of(int64_t R, int64_t T, int64_t G, int64_t Hkv, int dtype, int64
   const bool few = T * G <= 64 * R;
   const int64_t n = few ? c.blocks * Hkv : ceil_div64(T * G, c.slot) * Hkv;
   if (few ? n > 1024 : n > kUnits / 2 || c.blocks * Hkv + kUnits > kMostUnits) { c.target = 0; return c; }
+  // Single tokens: so many that, with the half part that a block has too much on average, they fill the chip once - two workgroups a CU -
+  // or twice where blocks are many.  us at 512 units and here: bf16, 32 heads over 8 of 128 channels, 64 requests of 64 to 8192 tokens 108.7 and 104.3,
+  // 24 of 100 to 4096 28.2 and 24.5, 6 of 500 to 16000 44.9 and 41.0, 12 of 4000 45.6 and 41.8, 16 under a window of 4096 57.5 and 52.6, 8 of
+  // 8192 53.4 both, 1 of 32768 33.5 both, 48 of 3000 108.5 and 112.0; fp16, 16 heads over 4, 20 of 700 to 20000 54.5 and 49.4.
+  // (1 of 32768 at 256, 768 and 1024 units 32.9, 36.0 and 39.1; 4 of 20000 to 32768 105, 82 and 84; 3 of 1000 to 9000, 16 heads, fp32 104, 83 and 89.)
+  // One a CU where requests have two blocks, which read the same keys: 256 and 512 units, 16 new tokens of 4 requests of 4096 20.0 and 20.6, of 16 55.6
+  // and 60.7, of one of 8192 15.8 and 19.5.
+  const int64_t all = with * Hkv, single = T * G > 32 * R ? 256 : (all > 320 ? 1024 : 512) - all / 2;
   if (keys == INT64_MAX) {
-    c.target = ceil_div64(few ? 512 : kUnits, Hkv);
+    c.target = ceil_div64(few ? single : kUnits, Hkv);
     return c;
   }
   if (window && window + sinks < keys) keys = window + sinks;
@@ -878,11 +886,7 @@ static Cut cut_of(int64_t R, int64_t T, int64_t G, int64_t Hkv, int dtype, int64
   if (whole(n, tiles, dtype, D)) {
     c.target = 0;
   } else if (few) {
-    // Single tokens: two workgroups a CU, whatever the lengths.  us at 256, 512, 768 and 1024 units: 8 requests of 8192 keys (32 heads
-    // over 8 of 128 channels, bf16) 52.4, 53.0, 54.6 and 56.0; 1 of 32768 32.9, 33.3, 36.0 and 39.1; 4 of 20000 to 32768 105, 81, 82 and 84;
-    // 64 of 64 to 8192 110, 104.9, 101.5 and 102.9; 3 of 1000 to 9000, 16 heads, fp32 104, 72, 83 and 89.  One a CU where a request has two
-    // blocks, which read the same keys: 256 and 512 units, 16 new tokens of 4 requests of 4096 20.0 and 20.6, of 16 55.6 and 60.7, of one of 8192 15.8 and 19.5.
-    c.target = ceil_div64(T * G > 32 * R ? 256 : 512, Hkv);
+    c.target = ceil_div64(single, Hkv);
   } else {
     // (blocks of a prompt that begins with this step see half of its keys on average, the longest go first: rounds even out)
     const int64_t past = keys > 2 * T ? keys - 2 * T : 0;
