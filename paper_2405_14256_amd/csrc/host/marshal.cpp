@@ -336,9 +336,11 @@ PyObject* rows_saliency(PyObject*, Args a, Py_ssize_t n) {
   PyErr_Format(PyExc_ValueError, "%s %s", what, why);
   throw Bad();
 }
+int g_device;                              // the current one, of the call that holds the interpreter lock (asked once a call)
 void on_device(const at::Tensor& t, const char* what) {
   if (!t.is_cuda()) refuse(what, "must be on the GPU");
-  if (t.device().index() != c10::hip::current_device()) refuse(what, "must be on the current device");
+  if (g_device < 0) g_device = c10::hip::current_device();
+  if (t.device().index() != g_device) refuse(what, "must be on the current device");
 }
 // int32, contiguous, of `n` elements (any number: -1); null for None.
 int32_t* ints(PyObject* o, const char* what, int64_t n = -1) {
@@ -398,6 +400,7 @@ int32_t int32_of(PyObject* o) {
 PyObject* paged_tables(PyObject*, Args a, Py_ssize_t n) {
   at::Tensor made[3];
   PyObject* status = guarded(kPagedTables, n, 10, [&]() -> int {
+    g_device = -1;
     const Table t = table_of(a[2]);
     const auto *q = ints(a[0], "q_len", t.R), *kv = ints(a[1], "kv_len", t.R);
     const at::Tensor& list = tensor_of(a[3]);
@@ -442,6 +445,7 @@ PyObject* paged_tables(PyObject*, Args a, Py_ssize_t n) {
 // (k, v, slot_map, k_pages, v_pages)
 PyObject* paged_store(PyObject*, Args a, Py_ssize_t n) {
   return guarded(kPagedStore, n, 5, [&]() -> int {
+    g_device = -1;
     const zc_tensor4 k = tokens(a[0], "k"), v = tokens(a[1], "v"), kp = pool(a[3], "k_pages"), vp = pool(a[4], "v_pages");
     const auto* slots = ints(a[2], "slot_map", k.L);
     const hipStream_t st = current_stream();
@@ -453,6 +457,7 @@ PyObject* paged_store(PyObject*, Args a, Py_ssize_t n) {
 // (k_pages, v_pages, block_table, kv_len, k_out, v_out)
 PyObject* paged_load(PyObject*, Args a, Py_ssize_t n) {
   return guarded(kPagedLoad, n, 6, [&]() -> int {
+    g_device = -1;
     const zc_tensor4 kp = pool(a[0], "k_pages"), vp = pool(a[1], "v_pages"), k = pool(a[4], "k_out"), v = pool(a[5], "v_out");
     const Table t = table_of(a[2]);
     const auto* kv = ints(a[3], "kv_len", t.R);
@@ -466,6 +471,7 @@ PyObject* paged_load(PyObject*, Args a, Py_ssize_t n) {
 // (q, k_pages, v_pages, block_table, q_start, kv_len, window, sinks, sm_scale, out, lse)
 PyObject* paged_attention(PyObject*, Args a, Py_ssize_t n) {
   return guarded(kPagedAttention, n, 11, [&]() -> int {
+    g_device = -1;
     const zc_tensor4 q = tokens(a[0], "q"), kp = pool(a[1], "k_pages"), vp = pool(a[2], "v_pages"), o = tokens(a[9], "out");
     const Table t = table_of(a[3]);
     const auto *start = ints(a[4], "q_start", t.R + 1), *kv = ints(a[5], "kv_len", t.R);
