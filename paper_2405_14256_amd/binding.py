@@ -377,7 +377,8 @@ def zc_paged_load(k_pages: torch.Tensor, v_pages: torch.Tensor, block_table: tor
     host = _native()
     if k_out is None or v_out is None:
         if L is None:
-            L = block_table.shape[1] * k_pages.shape[2]
+            given = k_out if k_out is not None else v_out
+            L = block_table.shape[1] * k_pages.shape[2] if given is None else given.shape[2]
         shape = (block_table.shape[0], k_pages.shape[1], L, k_pages.shape[3])
         k_out = torch.empty(shape, dtype=k_pages.dtype, device=k_pages.device) if k_out is None else k_out
         v_out = torch.empty(shape, dtype=v_pages.dtype, device=v_pages.device) if v_out is None else v_out
@@ -393,7 +394,7 @@ def zc_paged_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Te
     host = _native()
     if out is None:
         out = torch.empty_like(q)
-    if lse is None:
+    if lse is None and q.dim() in (3, 4):
         T, Hq = (q.shape[0], q.shape[1]) if q.dim() == 3 else (q.shape[2], q.shape[1])
         lse = torch.empty(Hq, T, dtype=torch.float32, device=q.device)
     _check("zc_paged_attention", host.paged_attention(q, k_pages, v_pages, block_table, q_start, kv_len, window, sinks, sm_scale, out, lse))

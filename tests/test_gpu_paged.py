@@ -451,6 +451,72 @@ def test_graphs_captured_on_one_stream_replay_side_by_side():
             assert torch.equal(o, wo) and torch.equal(n, wn)
 
 
+def test_calls_on_two_streams_at_once():
+    """Eager calls that are split and joined, on two streams without a wait between them: each stream has its own workspace."""
+    ps = [plain.Pages([1, 1, 30], [5000 + 900 * i, 40, 333], 8, 2, 128, HF, seed=30 + i) for i in range(2)]
+    want = [_attend(p) for p in ps]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in ps]
+    outs = [[(torch.zeros_like(p.q), torch.zeros(8, p.T, dtype=torch.float32, device=DEV)) for _ in range(20)] for p in ps]
+    torch.cuda.synchronize()
+    for i in range(20):
+        for p, s, o in zip(ps, streams, outs):
+            with torch.cuda.stream(s):
+                zb.zc_paged_attention(p.q, p.kp, p.vp, p.table, p.q_start, p.kv, out=o[i][0], lse=o[i][1])
+    torch.cuda.synchronize()
+    for (wo, wn), o in zip(want, outs):
+        assert all(torch.equal(x, wo) and torch.equal(y, wn) for x, y in o)
+
+
+def test_the_binding_refuses_what_does_not_fit():
+    p = plain.Pages([1, 2], [20, 30], 4, 2, 64, BF)
+    ok = (p.q, p.kp, p.vp, p.table, p.q_start, p.kv)
+
+    def attend(error, at, value, **kw):
+        args = list(ok)
+        args[at] = value
+        with pytest.raises(error):
+            zb.zc_paged_attention(*args, **kw)
+    attend(ValueError, 3, p.table.long())
+    attend(ValueError, 3, p.table.cpu())
+    attend(ValueError, 3, p.table[0])
+    attend(ValueError, 3, p.table.T.contiguous().T)
+    attend(ValueError, 3, p.table[:1].expand(2, -1))
+    attend(ValueError, 4, p.q_start.long())
+    attend(ValueError, 4, p.q_start[:2])
+    attend(ValueError, 5, p.kv.float())
+    attend(ValueError, 5, torch.cat([p.kv, p.kv]))
+    attend(ValueError, 5, torch.stack([p.kv, p.kv], 1)[:, 0])
+    attend(ValueError, 0, p.q.cpu())
+    attend(ValueError, 0, p.q, lse=torch.zeros(4, p.T, device=DEV, dtype=torch.float64))
+    attend(ValueError, 0, p.q, lse=torch.zeros(4, p.T + 1, device=DEV))
+    attend(zb.ZipCacheError, 0, p.q.half())
+    attend(zb.ZipCacheError, 0, p.q[:, :3])
+    attend(zb.ZipCacheError, 0, p.q, out=torch.zeros(p.T, 4, 64, device=DEV))
+    attend(zb.ZipCacheError, 0, p.q, window=-1)
+    attend(zb.ZipCacheError, 0, p.q, sm_scale=-1.0)
+    attend(AssertionError, 0, p.q[0])
+    attend(AssertionError, 1, p.kp[..., ::2])
+    with pytest.raises(zb.ZipCacheError):
+        zb.zc_paged_attention(p.q, p.kp[:, :, :8], p.vp[:, :, :8], p.table, p.q_start, p.kv)
+    slots = torch.zeros(3, **I32)
+    for s in (slots.long(), slots[:2], slots.cpu()):
+        with pytest.raises(ValueError):
+            zb.zc_paged_store(p.q[:, :2], p.q[:, :2], s, p.kp, p.vp)
+    with pytest.raises(ValueError):
+        zb.zc_paged_load(p.kp, p.vp, p.table, p.kv, k_out=torch.zeros(3, 2, 8, 64, dtype=BF, device=DEV), v_out=torch.zeros(3, 2, 8, 64, dtype=BF, device=DEV))
+    with pytest.raises(zb.ZipCacheError):
+        zb.zc_paged_load(p.kp, p.vp, p.table, p.kv, k_out=torch.zeros(2, 2, 8, 64, dtype=BF, device=DEV), v_out=torch.zeros(2, 2, 9, 64, dtype=BF, device=DEV))
+    one = torch.ones(2, **I32)
+    for kw in (dict(page=12), dict(page=8)):
+        with pytest.raises(zb.ZipCacheError):
+            zb.zc_paged_tables(one, one, p.table, one, T=2, **kw)
+    for kw in (dict(T=-1), dict(T=3, slot_map=one), dict(T=2, n_free=one), dict(T=2, q_start=one)):
+        with pytest.raises(ValueError):
+            zb.zc_paged_tables(one, one, p.table, one, page=16, **kw)
+    torch.cuda.synchronize()
+
+
 # ---- together -----------------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("dtype", [BF, FL])
