@@ -329,7 +329,8 @@ int zc_decode_attention_static(const zc_tensor4* q, const zc_packed* Kp, const z
  * Keys and values of many requests lie in pages of two pools (one for keys, one for values):
  * k_pages, v_pages [N, Hkv, page, D], `page` token rows to a page, a power of two from
  * ZC_PAGE_MIN to ZC_PAGE_MAX, any strides (a page may hold its heads one after the other or its
- * tokens).  N * page must stay below 2^31, the heads below 65536.  Request r's block table is row r
+ * tokens; a head's rows of one page span less than 2 GB, pages lie less than 4 GB apart).
+ * N * page must stay below 2^31, the heads below 65536.  Request r's block table is row r
  * of block_table (device int32 [R, max_blocks], rows row_stride elements apart): entry c is the page
  * of its tokens c * page .. c * page + page - 1.  A step's new tokens lie request after request in
  * tensors of T rows, q_start[r] .. q_start[r + 1] - 1 (device int32 [R + 1]) those of request r;

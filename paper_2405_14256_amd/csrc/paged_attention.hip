@@ -23,8 +23,8 @@ struct PagedArgs {
   const uint8_t *q, *k, *v;
   uint8_t* o;
   int64_t q_sH, q_sT, o_sH, o_sT;               // bytes
-  int64_t k_sB, k_sH, v_sB, v_sH;               // bytes
-  uint32_t k_row, v_row;                        // bytes from a token to the next
+  int64_t k_sH, v_sH;                           // bytes
+  uint32_t k_sB, v_sB, k_row, v_row;            // bytes from a page, a token to the next (a head's rows of a page: below 2 GB)
   const int32_t *table, *q_start, *kv_len;
   int64_t row;                                  // of the table, in entries
   int cols, shift, n_pages, cap;                // blocks of the table; page size; pages; tokens a row of the table has room for
@@ -75,6 +75,7 @@ struct Unit {
   int first, sink_tiles;        // tile t is t of the first sink_tiles, then first + t - sink_tiles
   int t_lo, t_hi;               // tiles of this unit
   int part, parts;              // which of the parts that the block's tiles are divided into
+  uint32_t behind;              // 16 keys from key0 on are behind every window of the block's if key0 - sinks, without sign, is less than this
 };
 
 // Row r of a block: its token (after the block's first) and head.
@@ -152,6 +153,8 @@ __device__ inline bool find_unit(const PagedArgs& a, int u, Unit& x) {
       const int low = a.window ? max(0, x.p0 - a.window + 1) : 0;
       x.first = low / kTile;
       x.sink_tiles = min((min(a.sinks, low) + kTile - 1) / kTile, x.first);
+      const int far = max(x.p0, 0) - a.window - 14;
+      x.behind = a.window && far > a.sinks ? far - a.sinks : 0;
       const int tiles = x.p1 < 0 ? 0 : x.sink_tiles + x.p1 / kTile + 1 - x.first;
       x.t_lo = 0;
       x.t_hi = tiles;
@@ -182,13 +185,27 @@ __device__ inline int keys_read(const PagedArgs& a, const Unit& x, int key0, int
   asm("" : "+s"(n));                                       // (both bounds at once would be a vector instruction, and what follows too)
   n = min(n, 16);
   if ((uint32_t)id >= (uint32_t)a.n_pages) n = 0;
-  if (a.window && key0 + 15 <= max(x.p0, 0) - a.window && key0 >= a.sinks) n = 0;
+  if ((uint32_t)(key0 - a.sinks) < x.behind) n = 0;
   return n;
 }
-__device__ inline __amdgpu_buffer_rsrc_t keys_at(const PagedArgs& a, const uint8_t* head, int64_t sB, uint32_t row, int key0, int id, int n) {
-  const int64_t at = (int64_t)(n ? id : 0) * sB + (int64_t)(key0 & ((1 << a.shift) - 1)) * row;
+// Where they are (of no keys: anywhere, nothing is read).
+__device__ inline __amdgpu_buffer_rsrc_t keys_at(const PagedArgs& a, const uint8_t* head, uint32_t sB, uint32_t row, int key0, int id, int n) {
+  const uint64_t at = (uint64_t)(uint32_t)id * sB + ((uint32_t)key0 & ((1u << a.shift) - 1)) * row;
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(head + at), 0, n * row, kBufFlags);
 }
+// The blocks of 32 keys that every row from position p0 to p1 sees whole: those from `low` on, `span` of them by their first key, and
+// those whose first key is below `sink`.
+struct Seen {
+  int low, sink;
+  uint32_t span;
+  __device__ Seen(const PagedArgs& a, int p0, int p1) {
+    low = a.window ? max(p1 - a.window + 1, 0) : 0;
+    const int end = max(p0, 0) - 30;                       // (of positions in front of the first key no block is seen)
+    span = max(end - low, 0);
+    sink = a.window ? min(a.sinks - 31, end) : 0;
+  }
+  __device__ bool whole(int key0) const { return (uint32_t)(key0 - low) < span || key0 < sink; }
+};
 
 // 16 keys to LDS in N transfers of 1024 bytes, to consecutive places.  The descriptor changes with every page, and the compiler may have
 // brought a part of it (or the place) from a vector register the instruction before: a memory instruction must not read
@@ -266,7 +283,7 @@ __device__ __forceinline__ void attend_rows(const PagedArgs& a, const Unit& x, i
     }
     return s;
   };
-  auto issue = [&](const Ids& s, const uint8_t* head, int64_t sB, uint32_t row, uint32_t lds, const int (&voff)[PG]) {
+  auto issue = [&](const Ids& s, const uint8_t* head, uint32_t sB, uint32_t row, uint32_t lds, const int (&voff)[PG]) {
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
       const auto rs = keys_at(a, head, sB, row, s.key0 + 16 * g, s.id[g], s.n[g]);
@@ -314,6 +331,7 @@ __device__ __forceinline__ void attend_rows(const PagedArgs& a, const Unit& x, i
   for (int ct = 0; ct < CT; ++ct) oacc[ct] = v16f{};
   float m = kLowestLogit, l = 0.f;   // running maximum (log2 units), this half-wave's share of the sum
 
+  const Seen seen(a, x.p0, x.p1);
   wait_all_loads();                              // (the rows and the first blocks: the compiler would wait for the rows in the loop, and so for the next blocks)
   for (; t < blocks; t += NW) {
     const bool more = t + NW < blocks;
@@ -328,7 +346,7 @@ __device__ __forceinline__ void attend_rows(const PagedArgs& a, const Unit& x, i
     }
     dma_reuse_fence();
     if (more) issue(at, kb, a.k_sB, a.k_row, k_lds, kvoff);
-    if (key0 + 31 > x.p0 || (a.window && key0 <= x.p1 - a.window && key0 + 31 >= a.sinks)) {
+    if (!seen.whole(key0)) {
       const int low = a.window && pos >= 0 ? pos - a.window : -1;          // keys up to it are seen as sinks only
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
@@ -477,6 +495,7 @@ __device__ __forceinline__ void attend_tiles(const PagedArgs& a, const Unit& x, 
   const int wrows = min(max(x.rows - 32 * w, 0), 32);
   const int wp0 = x.kv - x.nq + row_at(a, x, 32 * w).j, wp1 = wrows > 0 ? x.kv - x.nq + row_at(a, x, 32 * w + wrows - 1).j : -1;
   const int ntiles = x.t_hi - x.t_lo;
+  const Seen seen(a, wp0, wp1);
   int nh = 0;
   if (wp1 >= 0) {
     const int t1 = wp1 / KEYS - x.first + x.sink_tiles - x.t_lo;          // the tile of the last row's own token
@@ -488,15 +507,17 @@ __device__ __forceinline__ void attend_tiles(const PagedArgs& a, const Unit& x, 
   int krow = (lane / T::CPR) * (int)a.k_row, kchunk = ((lane % T::CPR) ^ T::swz(lane / T::CPR)) << 4;
   int vplace = (lane / T::CPR) * (int)a.v_row + (((lane % T::CPR) ^ v_slot<DT, D>(lane / T::CPR)) << 4);
   static_assert(T::RPI % 4 == 0 && T::SW * T::RP256 == 16, "what a transfer's first row adds to the swizzles");
-  struct Group { int key0, id; };
+  struct Group { int key0, id, n; };
   auto group = [&](int t) {
     Group g;
     g.key0 = tile_of(x, x.t_lo + t) * KEYS + 16 * w;
     g.id = page_of(a, x, g.key0);
+    g.n = 0;                                     // (found when its keys are requested, known when its values are)
     return g;
   };
-  auto k_issue = [&](int place, const Group& g) {
-    const auto rs = keys_at(a, kb, a.k_sB, a.k_row, g.key0, g.id, keys_read(a, x, g.key0, g.id));
+  auto k_issue = [&](int place, Group& g) {
+    g.n = keys_read(a, x, g.key0, g.id);
+    const auto rs = keys_at(a, kb, a.k_sB, a.k_row, g.key0, g.id, g.n);
     int v[NI];
     asm volatile("" : "+v"(krow), "+v"(kchunk));
 #pragma unroll
@@ -504,7 +525,7 @@ __device__ __forceinline__ void attend_tiles(const PagedArgs& a, const Unit& x, 
     move_keys<NI>(ks_lds + place * TILE_B, rs, v);
   };
   auto v_issue = [&](int place, const Group& g) {
-    const auto rs = keys_at(a, vb, a.v_sB, a.v_row, g.key0, g.id, keys_read(a, x, g.key0, g.id));
+    const auto rs = keys_at(a, vb, a.v_sB, a.v_row, g.key0, g.id, g.n);
     int v[NI];
     asm volatile("" : "+v"(vplace));
 #pragma unroll
@@ -588,7 +609,7 @@ __device__ __forceinline__ void attend_tiles(const PagedArgs& a, const Unit& x, 
   auto step = [&](auto last_c, int half, int key0, v16f& sc, v16f& sn) {
     constexpr bool LAST = decltype(last_c)::value;
     u32x4 vf[2][CT];
-    if (key0 + 31 > wp0 || (a.window && key0 <= wp1 - a.window && key0 + 31 >= a.sinks)) {
+    if (!seen.whole(key0)) {
       const int low = a.window && pos >= 0 ? pos - a.window : -1;          // keys up to it are seen as sinks only
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
@@ -961,7 +982,7 @@ extern "C" int zc_paged_attention(const zc_tensor4* q, const zc_tensor4* k_pages
   PagedArgs a;
   a.q = (const uint8_t*)q->ptr; a.k = (const uint8_t*)k_pages->ptr; a.v = (const uint8_t*)v_pages->ptr; a.o = (uint8_t*)out->ptr;
   a.q_sH = q->sH * eb; a.q_sT = q->sL * eb; a.o_sH = out->sH * eb; a.o_sT = out->sL * eb;
-  a.k_sB = k_pages->sB * eb; a.k_sH = k_pages->sH * eb; a.v_sB = v_pages->sB * eb; a.v_sH = v_pages->sH * eb;
+  a.k_sB = (uint32_t)(k_pages->sB * eb); a.k_sH = k_pages->sH * eb; a.v_sB = (uint32_t)(v_pages->sB * eb); a.v_sH = v_pages->sH * eb;
   a.k_row = (uint32_t)(k_pages->sL * eb); a.v_row = (uint32_t)(v_pages->sL * eb);
   // (a table without columns holds no token: any readable word stands for its pages)
   a.table = max_blocks ? block_table : q_start; a.q_start = q_start; a.kv_len = kv_len; a.row = max_blocks ? row_stride : 0;

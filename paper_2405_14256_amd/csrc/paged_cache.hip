@@ -222,7 +222,9 @@ int zc_validate_pages(const zc_tensor4* k, const zc_tensor4* v) {
   const int64_t eb = elem_bytes(k->dtype);
   if (k->B > 0x7fffffff / k->L || k->H > 65535) return ZC_ERR_UNSUPPORTED;
   if (k->sB < 0 || k->sH < 0 || v->sB < 0 || v->sH < 0) return ZC_ERR_INVALID_ARG;
-  if (k->sL > 0x7fffffff / (eb * 16) || v->sL > 0x7fffffff / (eb * 16)) return ZC_ERR_UNSUPPORTED;    // 16 rows: 32-bit offsets
+  // offsets inside a head's rows of a page, and from a page to the next, have 32 bits
+  for (const zc_tensor4* t : {k, v})
+    if (t->sL > 0x7fffffff / (eb * t->L) || t->sB > 0xffffffff / eb) return ZC_ERR_UNSUPPORTED;
   return ZC_OK;
 }
 

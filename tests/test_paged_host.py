@@ -54,6 +54,9 @@ def test_store_and_load_refuse_bad_arguments_before_launch():
         wide = _t4(**pages)
         wide.sL = 1 << 27
         assert call(kp=wide) == UNS                                                         # rows too far apart for 32-bit offsets
+        wide = _t4(**pages)
+        wide.sB = 1 << 31
+        assert call(vp=wide) == UNS                                                         # and pages
     # nothing to do is no error, and needs no memory
     assert store(k=_t4(ptr=None, L=0), v=_t4(ptr=None, L=0), slots=None) == 0
     assert load(k=_t4(ptr=None, B=0), v=_t4(ptr=None, B=0), table=None, kv=None) == 0
