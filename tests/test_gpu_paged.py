@@ -240,6 +240,23 @@ def test_parts_without_a_logit_above_minus_infinity(q, kv, dtype):
     assert bool(((out.double() - o).abs() <= u * size + 1e-4).all()) and (lse.double() - n).abs().max().item() <= 1e-4
 
 
+@pytest.mark.parametrize("q,kv,Hq,Hkv,D", [([1], [2529], 32, 4, 128), ([1, 1], [3900, 534], 12, 12, 64), ([40], [1500], 8, 2, 64)])
+def test_fp32_logits_of_outlier_channels(q, kv, Hq, Hkv, D):
+    """Six channels of the keys are 15 times the others: a logit's partial sums are large, and so are their roundings."""
+    p = plain.Pages(q, kv, Hq, Hkv, D, FL, seed=6)
+    for r in range(len(q)):
+        for h in range(Hkv):
+            p.k[r][h][:, torch.randperm(D, generator=torch.Generator().manual_seed(h))[:6].to(DEV)] *= 15.0
+        p.write(r)
+    out, lse = _attend(p)
+    o, n, _, _ = p.want()
+    # Relative to the result's 2-norm, the root of the summed squares, u = 2^-24, X the size of a logit (3.4 of 128 channels, 4.7 of 64): D
+    # products in four sums of half the size, each addition within u / sqrt 3 of it: X sqrt(D) / 2 u / sqrt 3 = 6.6e-7 (one sum: 1.3e-6); three
+    # additions u X = 2e-7; the scale's own rounding, of a few units of the exponent, 3.6e-7; the exponential 1.2e-7: 7.9e-7
+    assert ((out.double() - o).norm() / o.norm()).item() < 1e-6
+    assert ((lse.double() - n).norm() / n.norm()).item() < 1e-6
+
+
 @pytest.mark.parametrize("dtype", [BF, HF, FL])
 @pytest.mark.parametrize("q,kv", [([1], [300]), ([90], [300])])
 def test_keys_whose_logits_are_minus_infinity(q, kv, dtype):
