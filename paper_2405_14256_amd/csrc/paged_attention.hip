@@ -516,10 +516,17 @@ __device__ __forceinline__ void attend_tiles(const PagedArgs& a, const Unit& x, 
   int vplace = (lane / T::CPR) * (int)a.v_row + (((lane % T::CPR) ^ v_slot<DT, D>(lane / T::CPR)) << 4);
   static_assert(T::RPI % 4 == 0 && T::SW * T::RP256 == 16, "what a transfer's first row adds to the swizzles");
   struct Group { int key0, id, n; };
-  auto group = [&](int t) {
+  // The pages of this wave's keys of 64 tiles, one a lane (of tiles that are not the unit's: any).
+  int ids;
+  auto pages = [&](int t) {
+    const int key0 = tile_of(x, x.t_lo + t + lane) * KEYS + 16 * w;
+    ids = a.table[x.r * a.row + min(key0 >> a.shift, a.cols - 1)];
+  };
+  const int jump = x.first * KEYS + 16 * w;
+  auto group = [&](int t, int key0) {            // of tile t, after one with key0
     Group g;
-    g.key0 = tile_of(x, x.t_lo + t) * KEYS + 16 * w;
-    g.id = page_of(a, x, g.key0);
+    g.key0 = x.t_lo + t == x.sink_tiles ? jump : key0 + KEYS;
+    g.id = __builtin_amdgcn_readlane(ids, t & 63);
     g.n = 0;                                     // (found when its keys are requested, known when its values are)
     return g;
   };
@@ -540,9 +547,7 @@ __device__ __forceinline__ void attend_tiles(const PagedArgs& a, const Unit& x, 
     for (int jj = 0; jj < NI; ++jj) v[jj] = vplace + jj * T::RPI * (int)a.v_row;
     move_keys<NI>(vs_lds + place * TILE_B, rs, v);
   };
-  Group g[AHEAD + 2];                            // (all pages are asked for before the first is used; of tiles that are not the unit's: any)
-#pragma unroll
-  for (int t = 0; t < AHEAD + 2; ++t) g[t] = group(t);
+  pages(0);
 
   // this lane's row, straight into operand registers
   const int pos = r < wrows ? x.kv - x.nq + row_at(a, x, 32 * w + r).j : INT_MIN;
@@ -555,6 +560,9 @@ __device__ __forceinline__ void attend_tiles(const PagedArgs& a, const Unit& x, 
 #pragma unroll
     for (int kc = 0; kc < T::NKC; ++kc) qf[kc] = *reinterpret_cast<const u32x4*>(qr + kc * 32);
   }
+  Group g[AHEAD + 2];
+#pragma unroll
+  for (int t = 0; t < AHEAD + 2; ++t) g[t] = group(t, t ? g[t - 1].key0 : tile_of(x, x.t_lo) * KEYS + 16 * w - KEYS);
   if (ntiles > 0) {
     k_issue(0, g[0]);
 #pragma unroll
@@ -667,20 +675,21 @@ __device__ __forceinline__ void attend_tiles(const PagedArgs& a, const Unit& x, 
     if constexpr (!LAST) tmax = half_max(sn);        // (beside the second product, which leaves the vector units idle)
   };
   // Tile t's barrier: K(t + 1) and V(t) are complete in LDS, and nobody still reads K(t) (its second half was requested
-  // before) or V(t - 1), whose places are filled next.  The page of a later tile is asked for in front of the barrier, and
-  // had behind it: a scalar load on the way makes the waits for operands from LDS waits for all of them.
+  // before) or V(t - 1), whose places are filled next.
   int place = AHEAD % STAGES;                        // of V(t + AHEAD); K(t + AHEAD + 1) goes where K(t) was
   auto top = [&](int t) {
-    const Group gn = group(t + AHEAD + 2);
+    if (((t + AHEAD + 2) & 63) == 0) {
+      pages(t + AHEAD + 2);
+      wait_all_loads();                              // (here, not where they are used: that would be a wait in every tile)
+    }
     if (AHEAD > 1 && t + AHEAD < ntiles) wait_vmem<(AHEAD - 1) * 2 * NI>();
     else wait_all_loads();
     __syncthreads();
-    asm volatile("" :: "s"(gn.id));
     if (t + AHEAD < ntiles) v_issue(place, gv);
     place = place + 1 == STAGES ? 0 : place + 1;
     if (t + AHEAD + 1 < ntiles) k_issue(place, gk);
     gv = gk;
-    gk = gn;
+    gk = group(t + AHEAD + 2, gk.key0);
   };
   int read_place = 0;                                // of V(t); K(t + 1) is in the next
   auto next_buffers = [&]() {                        // tile t + 1
