@@ -178,10 +178,10 @@ __device__ inline int page_of(const PagedArgs& a, const Unit& x, int key0) {
   typedef __attribute__((address_space(4))) const int32_t* scalar;
   return ((scalar)(uintptr_t)(a.table + x.r * a.row))[min(key0 >> a.shift, a.cols - 1)];
 }
-// Of 16 keys from key0 on, how many a unit reads: none of a missing page, of those that no row's window reaches, past the end.
+// Of 16 keys from key0 on, how many a unit reads: none of a missing page, of those that no row's window reaches, from `end` on.
 // What is not read arrives as zeros.
-__device__ inline int keys_read(const PagedArgs& a, const Unit& x, int key0, int id) {
-  int n = max(x.kv - key0, 0);
+__device__ inline int keys_read(const PagedArgs& a, const Unit& x, int end, int key0, int id) {
+  int n = max(end - key0, 0);
   asm("" : "+s"(n));                                       // (both bounds at once would be a vector instruction, and what follows too)
   n = min(n, 16);
   if ((uint32_t)id >= (uint32_t)a.n_pages) n = 0;
@@ -204,7 +204,8 @@ struct Seen {
     span = max(end - low, 0);
     sink = a.window ? min(a.sinks - 31, end) : 0;
   }
-  __device__ bool whole(int key0) const { return (uint32_t)(key0 - low) < span || key0 < sink; }
+  // Blocks of 32 + more keys.
+  __device__ bool whole(int key0, int more = 0) const { return (uint32_t)(key0 - low) < (uint32_t)max((int)span - more, 0) || key0 < sink - more; }
 };
 
 // 16 keys to LDS in N transfers of 1024 bytes, to consecutive places.  The descriptor changes with every page, and the compiler may have
@@ -283,7 +284,7 @@ __device__ __forceinline__ void attend_rows(const PagedArgs& a, const Unit& x, i
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
       s.id[g] = page_of(a, x, s.key0 + 16 * g);
-      s.n[g] = keys_read(a, x, s.key0 + 16 * g, s.id[g]);
+      s.n[g] = keys_read(a, x, x.kv, s.key0 + 16 * g, s.id[g]);
     }
     return s;
   };
@@ -522,16 +523,23 @@ __device__ __forceinline__ void attend_tiles(const PagedArgs& a, const Unit& x, 
     const int key0 = tile_of(x, x.t_lo + t + lane) * KEYS + 16 * w;
     ids = a.table[x.r * a.row + min(key0 >> a.shift, a.cols - 1)];
   };
-  const int jump = x.first * KEYS + 16 * w;
-  auto group = [&](int t, int key0) {            // of tile t, after one with key0
+  const int turn = x.sink_tiles - x.t_lo;        // the tile behind the sinks'
+  auto next_key = [&](int t, int key0, int off) { return t == turn ? x.first * KEYS + off : key0 + KEYS; };     // of tile t, key0 that of the one before
+  auto group = [&](int t, int key0) {
     Group g;
-    g.key0 = x.t_lo + t == x.sink_tiles ? jump : key0 + KEYS;
+    g.key0 = next_key(t, key0, 16 * w);
     g.id = __builtin_amdgcn_readlane(ids, t & 63);
     g.n = 0;                                     // (found when its keys are requested, known when its values are)
     return g;
   };
+  // Keys behind the unit's last tile are requested as none, so that every tile has as many requests behind it.  16 keys
+  // from `all` to all + all_span are read whole if they have a page.
+  const int end = min(x.kv, (tile_of(x, x.t_hi - 1) + 1) * KEYS), all = x.behind ? (int)x.behind + a.sinks : 0;
+  const uint32_t all_span = max(end - 15 - all, 0);
   auto k_issue = [&](int place, Group& g) {
-    g.n = keys_read(a, x, g.key0, g.id);
+    g.n = 16;
+    if ((uint32_t)(g.key0 - all) >= all_span) g.n = keys_read(a, x, end, g.key0, g.id);
+    if ((uint32_t)g.id >= (uint32_t)a.n_pages) g.n = 0;
     const auto rs = keys_at(a, kb, a.k_sB, a.k_row, g.key0, g.id, g.n);
     int v[NI];
     asm volatile("" : "+v"(krow), "+v"(kchunk));
@@ -567,8 +575,8 @@ __device__ __forceinline__ void attend_tiles(const PagedArgs& a, const Unit& x, 
     k_issue(0, g[0]);
 #pragma unroll
     for (int t = 0; t < AHEAD; ++t) {
-      if (t < ntiles) v_issue(t, g[t]);
-      if (t + 1 < ntiles) k_issue((t + 1) % STAGES, g[t + 1]);
+      v_issue(t, g[t]);
+      k_issue((t + 1) % STAGES, g[t + 1]);
     }
   }
   Group gv = g[AHEAD], gk = g[AHEAD + 1];        // of V(t + AHEAD) and K(t + AHEAD + 1), t the next tile
@@ -622,10 +630,10 @@ __device__ __forceinline__ void attend_tiles(const PagedArgs& a, const Unit& x, 
 
   // One half, of keys key0 on: weights of the logits sc, output += V^T P; unless it is the wave's LAST, the logits of the half
   // after it (operands in kf) meanwhile, their maximum, and the request of the operands of the half after that.
-  auto step = [&](auto last_c, int half, int key0, v16f& sc, v16f& sn) {
+  auto step = [&](auto last_c, int half, int key0, bool seen_whole, v16f& sc, v16f& sn) {
     constexpr bool LAST = decltype(last_c)::value;
     u32x4 vf[2][CT];
-    if (!seen.whole(key0)) {
+    if (!seen_whole) {
       const int low = a.window && pos >= 0 ? pos - a.window : -1;          // keys up to it are seen as sinks only
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
@@ -682,12 +690,12 @@ __device__ __forceinline__ void attend_tiles(const PagedArgs& a, const Unit& x, 
       pages(t + AHEAD + 2);
       wait_all_loads();                              // (here, not where they are used: that would be a wait in every tile)
     }
-    if (AHEAD > 1 && t + AHEAD < ntiles) wait_vmem<(AHEAD - 1) * 2 * NI>();
+    if constexpr (AHEAD > 1) wait_vmem<(AHEAD - 1) * 2 * NI>();
     else wait_all_loads();
     __syncthreads();
-    if (t + AHEAD < ntiles) v_issue(place, gv);
+    v_issue(place, gv);
     place = place + 1 == STAGES ? 0 : place + 1;
-    if (t + AHEAD + 1 < ntiles) k_issue(place, gk);
+    k_issue(place, gk);
     gv = gk;
     gk = group(t + AHEAD + 2, gk.key0);
   };
@@ -711,25 +719,25 @@ __device__ __forceinline__ void attend_tiles(const PagedArgs& a, const Unit& x, 
     tmax = half_max(s0);
   }
   const int t_full = nh > 0 ? (nh - 1) / 2 : 0;      // tiles of whose halves none is the wave's last
-  int t = 0;
-  for (; t < t_full; ++t) {
-    const int key0 = tile_of(x, x.t_lo + t) * KEYS;
+  int t = 0, key0 = tile_of(x, x.t_lo) * KEYS;
+  for (; t < t_full; ++t, key0 = next_key(t, key0, 0)) {
+    const bool both = seen.whole(key0, 32);
     top(t);
-    step(std::false_type{}, 0, key0, s0, s1);
-    step(std::false_type{}, 1, key0 + 32, s1, s0);
+    step(std::false_type{}, 0, key0, both, s0, s1);
+    step(std::false_type{}, 1, key0 + 32, both, s1, s0);
     next_buffers();
   }
   if (nh > 0) {                                      // the tile of the last (t < ntiles: the wave has rows)
-    const int key0 = tile_of(x, x.t_lo + t) * KEYS;
     top(t++);
     if (nh & 1) {
-      step(std::true_type{}, 0, key0, s0, s1);
+      step(std::true_type{}, 0, key0, seen.whole(key0), s0, s1);
     } else {
-      step(std::false_type{}, 0, key0, s0, s1);
-      step(std::true_type{}, 1, key0 + 32, s1, s0);
+      step(std::false_type{}, 0, key0, seen.whole(key0), s0, s1);
+      step(std::true_type{}, 1, key0 + 32, seen.whole(key0 + 32), s1, s0);
     }
   }
   for (; t < ntiles; ++t) top(t);                    // the other waves' tiles: their transfers and barriers
+  wait_all_loads();                                  // (nothing is on its way to a workgroup's memory when it ends)
 
   // ---- normalise and store: lane = row, accumulator v of tile ct = channel 32 ct + acc_row(v, kh) ----
   const float l_tot = l + __shfl_xor(l, 32);
