@@ -243,6 +243,10 @@ __device__ inline int64_t part_row(const PagedArgs& a, int hk, int unit) { retur
 // Four waves share the keys of 32 rows, a wave every fourth 32 keys, in a place of its own in LDS for one K and one V block: a
 // block's K is requested when the one before has been multiplied, its V likewise, so that a wave has one of them in flight
 // at any time and waits for nobody.
+//
+// Bound by memory: 64 single tokens over 64 to 8192 tokens, 32 heads over 8 of 128 channels, bf16, 97 us (5.5 TB/s), the join 4 more; one over
+// 4096 by its chain of lengths, pages, keys and the waves' join, 6 us.  fp32 chunks by the matrix cores: 2048 over 8192, 16 heads over 4 of 64
+// channels 498 us, 121 TFLOP/s.
 template <int DT, int D>
 struct RowsMemory {
   static constexpr int kBlock = 32 * Tile<DT, D>::ROWB;                   // bytes of a block of keys or values
@@ -474,9 +478,11 @@ __device__ __forceinline__ void attend_rows(const PagedArgs& a, const Unit& x, i
 // halves of a tile, and no wave multiplies a half that lies behind its last row.  A wave moves 16 keys of a tile, which
 // lie in one page: its address is scalar work, and a page that ends inside a tile costs nothing.
 //
-// Bound by the matrix cores: a half is 16 matrix instructions of 32 cycles (128 channels) and about 300 cycles of vector
-// instructions, so the two have to run at the same time: the logits of half h + 1 are multiplied while the exponentials of
-// half h are taken, and the operands of each product are requested one phase before.
+// Bound by the matrix cores, the vector instructions beside them and the power both draw: a half is 16 matrix instructions of 32
+// cycles (128 channels) and about 600 cycles of vector instructions (16 of them exponentials at a quarter of the rate), so the two have
+// to run at the same time: the logits of half h + 1 are multiplied while the exponentials of half h are taken, and the operands of
+// each product are requested one phase before.  2048 tokens over 32768, 32 heads over 8 of 128 channels, bf16: 1013 to 1067 us by the card, 1.0 PFLOP/s,
+// matrix cores 52 % and vector issue 65 % busy at 1.79 GHz (blocks of 32 rows: 1610 us); 8192 over 16384, 16 heads over 4 of 64, 505 us, 0.82.
 //
 // Of 64 channels three tiles of K and V fit (three workgroups a CU either way), and they are requested two tiles ahead: a
 // tile is worth 0.2 us of matrix instructions there, less than a trip to memory.
@@ -797,7 +803,8 @@ __global__ __launch_bounds__(256, DT == ZC_F32 && D == 128 ? 1 : 2) void k_paged
 
 // ---- the join of split blocks ---------------------------------------------------------------------------
 // Four workgroups per unit; those of a unit that a split block begins with join it, every fourth 256 / (D / 4) rows
-// each.  D / 4 threads take a row; where rows are few, several such groups share a row's parts and join what they have in LDS.  Bound by two trips to memory.
+// each.  D / 4 threads take a row; where rows are few, several such groups share a row's parts and join what they have in LDS.  Bound by two trips to memory:
+// 3 us for one token over 4096 (32 heads of 128 channels), 4 for 64 of them, 6 for 4 chunks of 250 to 500 (16 heads of 64), a launch included.
 constexpr int kJoinGroups = 4;
 template <int DT, int D>
 __global__ __launch_bounds__(256) void k_paged_join(PagedArgs a) {
