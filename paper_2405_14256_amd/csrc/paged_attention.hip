@@ -62,9 +62,9 @@ __device__ inline uint32_t pack_two(float lo, float hi) {
 // and 22.4; 8 of 200 to 500, 10 to 16 new 15.9 and 10.5; 4 of 4096, 32 new (128 rows) 29.1 and 30.3; of 64 channels, 2 of 1000 to 3000, 40 to 64 new
 // (one head a group) 16.7 and 14.6.
 constexpr int kTile = 64;
-template <int DT> struct Blocks {
-  static constexpr int kMany = DT == ZC_F32 ? 32 : 128;                   // rows of a block, of many rows
-  __device__ static bool few(int rows) { return DT == ZC_F32 || rows <= 64; }
+template <int DT, bool FEW> struct Blocks {                              // FEW: of 32 rows whatever a request has
+  static constexpr int kMany = DT == ZC_F32 || FEW ? 32 : 128;            // rows of a block, of many rows
+  __device__ static bool few(int rows) { return DT == ZC_F32 || FEW || rows <= 64; }
 };
 
 struct Unit {
@@ -99,9 +99,9 @@ __device__ inline Request request(const PagedArgs& a, int r) {
 }
 
 // The unit with index u of a head.
-template <int DT>
+template <int DT, bool FEW>
 __device__ inline bool find_unit(const PagedArgs& a, int u, Unit& x) {
-  using B = Blocks<DT>;
+  using B = Blocks<DT, FEW>;
   const int lane = threadIdx.x & 63;
   struct Size { int blocks, tiles, least; };               // row blocks; tiles that one sees, at most, and that make a part
   auto size = [&](const Request& t) {
@@ -240,23 +240,22 @@ __device__ inline int v_slot(int key) {
 __device__ inline int64_t part_row(const PagedArgs& a, int hk, int unit) { return ((int64_t)hk * a.units + unit) * a.slot; }
 
 // ---- blocks of 32 rows: single tokens, short chunks, fp32 ---------------------------------------------
-// Four waves share the keys of 32 rows, a wave every fourth 32 keys, in a place of its own in LDS for one K and one V block: a
+// Four or eight waves share the keys of 32 rows, a wave every fourth or eighth 32 keys, in a place of its own in LDS for one K and one V block: a
 // block's K is requested when the one before has been multiplied, its V likewise, so that a wave has one of them in flight
 // at any time and waits for nobody.
 //
 // Bound by memory: 64 single tokens over 64 to 8192 tokens, 32 heads over 8 of 128 channels, bf16, 97 us (5.5 TB/s), the join 4 more; one over
 // 4096 by its chain of lengths, pages, keys and the waves' join, 6 us.  fp32 chunks by the matrix cores: 2048 over 8192, 16 heads over 4 of 64
 // channels 498 us, 121 TFLOP/s.
-template <int DT, int D>
+template <int DT, int D, int NW>
 struct RowsMemory {
   static constexpr int kBlock = 32 * Tile<DT, D>::ROWB;                   // bytes of a block of keys or values
-  static constexpr int kBytes = 8 * kBlock;
+  static constexpr int kBytes = 2 * NW * kBlock;
 };
-template <int DT, int D>
+template <int DT, int D, int NW>
 __device__ __forceinline__ void attend_rows(const PagedArgs& a, const Unit& x, int hk, uint8_t* mem, float (*sum)[2][64]) {
   using T = Tile<DT, D>;
-  constexpr int NW = 4;
-  constexpr int BLK = RowsMemory<DT, D>::kBlock;
+  constexpr int BLK = RowsMemory<DT, D, NW>::kBlock;
   constexpr int NT = BLK / 1024;                 // transfers of a block
   constexpr int PG = 16 / T::RPI;                // of 16 keys
   constexpr int CT = D / 32;
@@ -782,13 +781,13 @@ __device__ inline void store_row(const PagedArgs& a, int tok0, int g0, int hk, i
 
 template <int DT, int D>
 __global__ __launch_bounds__(256, DT == ZC_F32 && D == 128 ? 1 : 2) void k_paged_attention(PagedArgs a) {
-  constexpr int kBytes = DT == ZC_F32 ? RowsMemory<DT, D>::kBytes : kStages<D> * 2 * kTile * Tile<DT, D>::ROWB;
-  static_assert(kBytes >= RowsMemory<DT, D>::kBytes, "blocks of few rows find room");
+  constexpr int kBytes = DT == ZC_F32 ? RowsMemory<DT, D, 4>::kBytes : kStages<D> * 2 * kTile * Tile<DT, D>::ROWB;
+  static_assert(kBytes >= RowsMemory<DT, D, 4>::kBytes, "blocks of few rows find room");
   __shared__ __align__(1024) uint8_t mem[kBytes];
   __shared__ float sum[4][2][64];
   const int hk = blockIdx.x;
   Unit x;
-  const bool any = find_unit<DT>(a, unit_of_grid(), x);
+  const bool any = find_unit<DT, false>(a, unit_of_grid(), x);
   if (a.target && threadIdx.x == 0)
     a.todo[(int64_t)hk * a.units + unit_of_grid()] = any && x.part == 0 && x.parts > 1 ? make_int4(x.parts, x.rows, x.qs + x.j0, x.g0) : make_int4(0, 0, 0, 0);
   if (!any) return;
@@ -798,7 +797,16 @@ __global__ __launch_bounds__(256, DT == ZC_F32 && D == 128 ? 1 : 2) void k_paged
       return;
     }
   }
-  attend_rows<DT, D>(a, x, hk, mem, sum);
+  attend_rows<DT, D, 4>(a, x, hk, mem, sum);
+}
+
+// Eight waves, blocks of 32 rows that are not split (see wide below).
+template <int DT, int D>
+__global__ __launch_bounds__(512, 2) void k_paged_attention_wide(PagedArgs a) {
+  __shared__ __align__(1024) uint8_t mem[RowsMemory<DT, D, 8>::kBytes];
+  __shared__ float sum[8][2][64];
+  Unit x;
+  if (find_unit<DT, true>(a, unit_of_grid(), x)) attend_rows<DT, D, 8>(a, x, blockIdx.x, mem, sum);
 }
 
 // ---- the join of split blocks ---------------------------------------------------------------------------
@@ -874,7 +882,7 @@ __global__ __launch_bounds__(256) void k_paged_join(PagedArgs a) {
 // ---- host ---------------------------------------------------------------------------------------------
 // How a call's rows are cut: row blocks of a head, at most; units of a head that splitting aims at (0: nothing is split); rows of a
 // unit's partial results.
-struct Cut { int64_t blocks, target, slot; };
+struct Cut { int64_t blocks, target, slot; bool wide; };
 constexpr int64_t kUnits = 2560;               // of all heads, that splitting aims at, at most
 constexpr int64_t kMostUnits = 4096;           // and that there may be (their partial results, 128 rows of 128 channels: 272 MB)
 
@@ -886,6 +894,14 @@ static bool whole(int64_t blocks, int64_t tiles, int dtype, int64_t D) {
   if (dtype == ZC_F32) return tiles <= (D == 64 ? 4 : 2);
   return tiles <= (blocks >= 128 ? 16 : blocks >= 64 ? 10 : 6);
 }
+
+// Whether eight waves take a block (16-bit types, one block a request): fewer blocks than CUs, whose keys four waves would take by turns and which are
+// not worth a split for eight.  us of four waves, split where that is the rule, and of eight, 32 heads over 8 of 128 channels, bf16: 1 request of 512 keys 8.6
+// and 8.1, of 1024 8.5 and 11.1; 4 of 768 9.4 and 10.0; 8 of 1024 13.8 and 12.0; 12 of 51 to 1024 12.4 and 11.7, of 76 to 1536 12.5 and 14.3; 16 of 512 10.5 and 9.8, of 2048
+// 28.5 and 27.8, of 150 to 3000 18.2 and 22.7; 20 of 102 to 2048 20.0 and 19.3; 32 of 256 9.5 and 10.1.  16 heads over 4 of 64, fp16: 16 of 512 7.6 and 6.4, of 1024
+// 10.9 and 8.9; 32 of 2048 16.7 and 13.7, of 102 to 2048 12.3 and 12.5, of 204 to 4096 16.5 and 19.8; 60 of 2048 26.3 and 22.2.  In fp32 both
+// wait for the matrix cores: 2 of 512, 12 heads of 64, 9.7 and 13.4.
+static bool wide(int64_t n, int64_t tiles) { return n < 256 && tiles > 2 && tiles <= (n >= 128 ? 32 : n >= 64 ? 16 : 8); }
 
 // Parts of every one of n row blocks that see `tiles` tiles each.  The chip runs them in rounds of what it holds, the last of which is
 // shorter where CUs are left with one workgroup or none; a part costs the way of its rows' results through memory.  Of blocks
@@ -915,6 +931,7 @@ static int64_t parts_of(int64_t n, int64_t tiles, int dtype, int64_t D) {
 // keys: a request's, at most; INT64_MAX: as many as cost the most workspace.
 static Cut cut_of(int64_t R, int64_t T, int64_t G, int64_t Hkv, int dtype, int64_t D, int64_t keys, int64_t window, int64_t sinks) {
   Cut c;
+  c.wide = false;
   c.slot = dtype == ZC_F32 || T * G <= 64 ? 32 : 128;
   // (a request has one block that is not full; where blocks of 128 rows are the rule, one of 33 to 64 rows is two of 32)
   const int64_t with = R < T ? R : T, two = T * G / 33;
@@ -936,6 +953,12 @@ static Cut cut_of(int64_t R, int64_t T, int64_t G, int64_t Hkv, int dtype, int64
   }
   if (window && window + sinks < keys) keys = window + sinks;
   const int64_t tiles = ceil_div64(keys, kTile);
+  if (dtype != ZC_F32 && T * G <= 32 * R && wide(with * Hkv, tiles)) {
+    c.blocks = T * G / 32 + with;
+    c.target = 0;
+    c.wide = true;
+    return c;
+  }
   if (whole(n, tiles, dtype, D)) {
     c.target = 0;
   } else if (few) {
@@ -957,8 +980,15 @@ static size_t workspace_of(const Cut& c, int64_t Hkv, int64_t D) {
 }
 
 template <int DT, int D>
-static int launch_paged(PagedArgs& a, hipStream_t st) {
+static int launch_paged(PagedArgs& a, bool wide, hipStream_t st) {
   const auto grid = [&](int64_t n) { return dim3((unsigned)a.Hkv, (unsigned)(n < 65535 ? n : 65535), (unsigned)ceil_div64(n, 65535)); };
+  if constexpr (DT != ZC_F32) {
+    if (wide) {
+      hipLaunchKernelGGL((k_paged_attention_wide<DT, D>), grid(a.units), dim3(512), 0, st, a);
+      ZC_LAUNCH_CHECK();
+      return ZC_OK;
+    }
+  }
   hipLaunchKernelGGL((k_paged_attention<DT, D>), grid(a.units), dim3(256), 0, st, a);
   ZC_LAUNCH_CHECK();
   if (a.target) {
@@ -1037,7 +1067,7 @@ extern "C" int zc_paged_attention(const zc_tensor4* q, const zc_tensor4* k_pages
   a.part_o = cut.target ? (float*)((int4*)ws + parts) : nullptr;
   a.part_ml = cut.target ? a.part_o + parts * cut.slot * q->D : nullptr;
   hipStream_t st = (hipStream_t)stream;
-#define ZC_PA(DT) (q->D == 128 ? launch_paged<DT, 128>(a, st) : launch_paged<DT, 64>(a, st))
+#define ZC_PA(DT) (q->D == 128 ? launch_paged<DT, 128>(a, cut.wide, st) : launch_paged<DT, 64>(a, cut.wide, st))
   if (q->dtype == ZC_F32) rc = ZC_PA(ZC_F32);
   else if (q->dtype == ZC_F16) rc = ZC_PA(ZC_F16);
   else rc = ZC_PA(ZC_BF16);

@@ -240,6 +240,17 @@ def test_parts_without_a_logit_above_minus_infinity(q, kv, dtype):
     assert bool(((out.double() - o).abs() <= u * size + 1e-4).all()) and (lse.double() - n).abs().max().item() <= 1e-4
 
 
+# (few blocks of up to 32 rows over up to 2048 keys; the last two: more blocks than that, and a request of many rows among empty ones)
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("q,kv,Hq,Hkv,window,sinks", [
+    ([1], [129], 8, 8, 0, 0), ([1], [500], 32, 2, 0, 0), ([1, 0, 2, 1], [257, 90, 480, 0], 8, 2, 0, 0), ([1] * 20, [1 + 107 * i for i in range(20)], 16, 8, 0, 0),
+    ([1] * 9, [1000 - 111 * i for i in range(9)], 8, 8, 0, 0), ([1] * 12, [30 * i for i in range(12)], 16, 8, 100, 5), ([1] * 5, [900, 37, 64, 300, 1], 48, 16, 130, 0),
+    ([1] * 40, [25 * i + 1 for i in range(40)], 16, 8, 0, 0), ([0, 0, 100, 1], [10, 0, 400, 3], 4, 4, 0, 0)])
+def test_blocks_of_eight_waves(q, kv, Hq, Hkv, window, sinks, D, dtype):
+    _run(q, kv, Hq, Hkv, D, dtype, window, sinks, page=32, pad=2)
+
+
 @pytest.mark.parametrize("q,kv,Hq,Hkv,D", [([1], [2529], 32, 4, 128), ([1, 1], [3900, 534], 12, 12, 64), ([40], [1500], 8, 2, 64)])
 def test_fp32_logits_of_outlier_channels(q, kv, Hq, Hkv, D):
     """Six channels of the keys are 15 times the others: a logit's partial sums are large, and so are their roundings."""
