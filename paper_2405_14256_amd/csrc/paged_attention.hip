@@ -953,7 +953,7 @@ static Cut cut_of(int64_t R, int64_t T, int64_t G, int64_t Hkv, int dtype, int64
   }
   if (window && window + sinks < keys) keys = window + sinks;
   const int64_t tiles = ceil_div64(keys, kTile);
-  if (dtype != ZC_F32 && T * G <= 32 * R && wide(with * Hkv, tiles)) {
+  if (dtype != ZC_F32 && T * G <= 32 * with && wide(with * Hkv, tiles)) {
     c.blocks = T * G / 32 + with;
     c.target = 0;
     c.wide = true;
