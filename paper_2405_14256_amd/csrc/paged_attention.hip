@@ -895,13 +895,17 @@ static bool whole(int64_t blocks, int64_t tiles, int dtype, int64_t D) {
   return tiles <= (blocks >= 128 ? 16 : blocks >= 64 ? 10 : 6);
 }
 
-// Whether eight waves take a block (16-bit types, one block a request): fewer blocks than CUs, whose keys four waves would take by turns and which are
-// not worth a split for eight.  us of four waves, split where that is the rule, and of eight, 32 heads over 8 of 128 channels, bf16: 1 request of 512 keys 8.6
-// and 8.1, of 1024 8.5 and 11.1; 4 of 768 9.4 and 10.0; 8 of 1024 13.8 and 12.0; 12 of 51 to 1024 12.4 and 11.7, of 76 to 1536 12.5 and 14.3; 16 of 512 10.5 and 9.8, of 2048
-// 28.5 and 27.8, of 150 to 3000 18.2 and 22.7; 20 of 102 to 2048 20.0 and 19.3; 32 of 256 9.5 and 10.1.  16 heads over 4 of 64, fp16: 16 of 512 7.6 and 6.4, of 1024
-// 10.9 and 8.9; 32 of 2048 16.7 and 13.7, of 102 to 2048 12.3 and 12.5, of 204 to 4096 16.5 and 19.8; 60 of 2048 26.3 and 22.2.  In fp32 both
+// Whether eight waves take a block (16-bit types, one block a request): blocks that leave CUs idle and whose keys four waves would take by turns, or that
+// have 17 to 32 tiles each and fill the chip less than twice; a split and its join would cost more.  us of four waves, split where that is the rule, and of eight, 32
+// heads over 8 of 128 channels, bf16: 1 request of 512 keys 8.6 and 8.1, of 1024 8.5 and 11.1; 4 of 768 9.4 and 10.0; 8 of 1024 13.8 and 12.0; 12 of 51 to 1024 12.4 and 11.7, of 76
+// to 1536 12.5 and 14.3; 16 of 512 10.5 and 9.8, of 2048 28.5 and 27.8, of 150 to 3000 18.2 and 22.7; 20 of 102 to 2048 20.0 and 19.3; 32 of 256 9.5 and 10.1; 40 of 512 16.9
+// and 20.2, of 1600 56.7 and 52.3, of 102 to 2048 27.3 and 28.3; 60 of 2048 86.2 and 79.5.  16 heads over 4 of 64, fp16: 16 of 512 7.6 and 6.4, of 1024 10.9 and 8.9; 32 of 2048
+// 16.7 and 13.7, of 102 to 2048 12.3 and 12.5, of 204 to 4096 16.5 and 19.8; 60 of 2048 26.3 and 22.2; 80 of 1200 21.9 and 19.6, of 1024 16.6 and 17.1.  In fp32 both
 // wait for the matrix cores: 2 of 512, 12 heads of 64, 9.7 and 13.4.
-static bool wide(int64_t n, int64_t tiles) { return n < 256 && tiles > 2 && tiles <= (n >= 128 ? 32 : n >= 64 ? 16 : 8); }
+static bool wide(int64_t n, int64_t tiles) {
+  if (n < 256) return tiles > 2 && tiles <= (n >= 128 ? 32 : n >= 64 ? 16 : 8);
+  return n <= 512 && tiles > 16 && tiles <= 32;
+}
 
 // Parts of every one of n row blocks that see `tiles` tiles each.  The chip runs them in rounds of what it holds, the last of which is
 // shorter where CUs are left with one workgroup or none; a part costs the way of its rows' results through memory.  Of blocks
@@ -953,11 +957,19 @@ static Cut cut_of(int64_t R, int64_t T, int64_t G, int64_t Hkv, int dtype, int64
   }
   if (window && window + sinks < keys) keys = window + sinks;
   const int64_t tiles = ceil_div64(keys, kTile);
-  if (dtype != ZC_F32 && T * G <= 32 * with && wide(with * Hkv, tiles)) {
-    c.blocks = T * G / 32 + with;
-    c.target = 0;
-    c.wide = true;
-    return c;
+  if (dtype != ZC_F32 && T * G <= 32 * with) {
+    if (wide(with * Hkv, tiles)) {
+      c.blocks = T * G / 32 + with;
+      c.target = 0;
+      c.wide = true;
+      return c;
+    }
+    // (so many blocks need no split either, us split and not: 90 requests of 2048 tokens, 32 heads over 8 of 128 channels 127 and 116, of 102 to 2048 61.4 and 57.8, of
+    // 204 to 4096 92 and 112; 8 heads of 64 69 and 60, 36.7 and 35.5; 20 of 102 to 2048, 40 heads of 128 73.4 and 75.3, of 60 to 1200 44.3 and 39.8)
+    if (with * Hkv > 512 && tiles <= 32) {
+      c.target = 0;
+      return c;
+    }
   }
   if (whole(n, tiles, dtype, D)) {
     c.target = 0;

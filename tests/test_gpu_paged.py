@@ -240,13 +240,13 @@ def test_parts_without_a_logit_above_minus_infinity(q, kv, dtype):
     assert bool(((out.double() - o).abs() <= u * size + 1e-4).all()) and (lse.double() - n).abs().max().item() <= 1e-4
 
 
-# (few blocks of up to 32 rows over up to 2048 keys; the last two: more blocks than that, and a request of many rows among empty ones)
+# (blocks of up to 32 rows over up to 2048 keys; more than 512 of them have four waves; the last: a request of many rows among empty ones)
 @pytest.mark.parametrize("dtype", [BF, HF])
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("q,kv,Hq,Hkv,window,sinks", [
     ([1], [129], 8, 8, 0, 0), ([1], [500], 32, 2, 0, 0), ([1, 0, 2, 1], [257, 90, 480, 0], 8, 2, 0, 0), ([1] * 20, [1 + 107 * i for i in range(20)], 16, 8, 0, 0),
     ([1] * 9, [1000 - 111 * i for i in range(9)], 8, 8, 0, 0), ([1] * 12, [30 * i for i in range(12)], 16, 8, 100, 5), ([1] * 5, [900, 37, 64, 300, 1], 48, 16, 130, 0),
-    ([1] * 40, [25 * i + 1 for i in range(40)], 16, 8, 0, 0), ([0, 0, 100, 1], [10, 0, 400, 3], 4, 4, 0, 0)])
+    ([1] * 40, [25 * i + 1 for i in range(40)], 16, 8, 0, 0), ([1] * 66, [30 * i + 1 for i in range(66)], 4, 4, 0, 0), ([1] * 66, [17 * i for i in range(66)], 8, 8, 0, 0), ([0, 0, 100, 1], [10, 0, 400, 3], 4, 4, 0, 0)])
 def test_blocks_of_eight_waves(q, kv, Hq, Hkv, window, sinks, D, dtype):
     _run(q, kv, Hq, Hkv, D, dtype, window, sinks, page=32, pad=2)
 
