@@ -25,6 +25,9 @@
  *   - All work is enqueued on the given HIP stream (`stream` is a hipStream_t
  *     passed as void*; NULL is the default stream).  Calls never synchronise
  *     with the host and never read results back.
+ *   - A call may be several launches.  Calls that share a workspace (or the buffer of
+ *     zc_decode_attention_static) on one stream must therefore be issued one after the other:
+ *     host threads that share a stream need a lock around them, or workspaces of their own.
  *   - Every function returns a zc_status.  Arguments are validated on the host
  *     before anything is launched; a failed validation launches nothing and
  *     leaves outputs untouched.  A launch failure returns ZC_ERR_HIP.

@@ -13,7 +13,9 @@
 #include <Python.h>
 
 #include <map>
+#include <mutex>
 #include <tuple>
+#include <utility>
 #include <vector>
 
 #include <ATen/ATen.h>
@@ -110,15 +112,19 @@ struct Packed {
 // back to torch's allocator, which reuses it in the order of the stream - unless a call that used
 // it was captured: the graph holds its address, and it is kept.  (So a stream holds less than one and a
 // half times its largest request, and what its graphs were captured with.)  All of this runs
-// under the interpreter lock.
+// under the interpreter lock; the launches do not, and a call is several of them: two threads' calls on
+// one stream (by default all threads share one) would come between each other's.  So a call holds its buffer's mutex
+// while it launches, taken when the interpreter lock has been given up and given back before that is taken again.
 enum Kind { kScratchProbe, kScratchQuantize, kScratchQuantizeKV, kScratchDecode, kScratchPaged };
-struct Scratch { at::Tensor t; void* ptr = nullptr; size_t bytes = 0; bool captured = false; };
+struct Scratch { at::Tensor t; void* ptr = nullptr; size_t bytes = 0; bool captured = false; std::mutex* use = nullptr; };
 std::map<std::tuple<int, int, void*>, Scratch>* g_scratch;
 std::vector<at::Tensor>* g_captured;      // replaced buffers that graphs may hold
+std::mutex g_static;                      // of the library's own buffer, zc_decode_attention_static's
 
 // The reference keeps the buffer during the call, whose launch runs without the lock.
 Scratch scratch(size_t need, const at::Tensor& like, Kind kind, hipStream_t stream) {
   Scratch& s = (*g_scratch)[std::make_tuple((int)like.device().index(), (int)kind, (void*)stream)];
+  if (!s.use) s.use = new std::mutex;      // (as the buffers, until the process ends)
   if (!s.ptr || s.bytes < need) {
     size_t n = need < 256 ? 256 : need;
     if (s.ptr && n < s.bytes + s.bytes / 2) n = s.bytes + s.bytes / 2;
@@ -140,14 +146,18 @@ Scratch scratch(size_t need, const at::Tensor& like, Kind kind, hipStream_t stre
 
 hipStream_t current_stream() { return c10::hip::getCurrentHIPStream().stream(); }
 
-// Runs a launch without the interpreter lock (it may wait for room in the stream's queue).
-template <class F> int unlocked(F&& f) {
+// Runs a call's launches without the interpreter lock (they may wait for room in the stream's queue), one call of those that
+// share scratch memory (whose mutex is `use`, null: none) at a time.
+template <class F> int unlocked(std::mutex* use, F&& f) {
   int rc;
   Py_BEGIN_ALLOW_THREADS
+  if (use) use->lock();
   rc = f();
+  if (use) use->unlock();
   Py_END_ALLOW_THREADS
   return rc;
 }
+template <class F> int unlocked(F&& f) { return unlocked(nullptr, std::forward<F>(f)); }
 
 // Every function below returns the library's status as an int (paged_tables: beside its outputs).
 template <class F> PyObject* guarded(Fn id, Py_ssize_t n, Py_ssize_t want, F&& f) {
@@ -183,7 +193,7 @@ PyObject* probe(PyObject*, Args a, Py_ssize_t n) {
     void* wp = ws.ptr;
     const size_t wn = ws.bytes;
     const auto fn = ZC_FN(acc ? kAccumulated : kProbe, zc_probe_saliency);
-    return unlocked([&] { return fn(&q, &k, rows, posp, P, scale, lse, scores, per_head, wp, wn, st); });
+    return unlocked(ws.use, [&] { return fn(&q, &k, rows, posp, P, scale, lse, scores, per_head, wp, wn, st); });
   });
 }
 
@@ -240,7 +250,7 @@ PyObject* quantize(PyObject*, Args a, Py_ssize_t n) {
     void* wp = ws.ptr;
     const size_t wn = ws.bytes;
     const auto fn = ZC_FN(kQuantize, zc_quantize_pack);
-    return unlocked([&] { return fn(&x, l.sal, l.k, l.reg, l.n_reg, off, p.get(), wp, wn, st); });
+    return unlocked(ws.use, [&] { return fn(&x, l.sal, l.k, l.reg, l.n_reg, off, p.get(), wp, wn, st); });
   });
 }
 
@@ -257,7 +267,7 @@ PyObject* quantize_kv(PyObject*, Args a, Py_ssize_t n) {
     void* wp = ws.ptr;
     const size_t wn = ws.bytes;
     const auto fn = ZC_FN(kQuantizeKV, zc_quantize_pack_kv);
-    return unlocked([&] { return fn(&xk, &xv, l.sal, l.k, l.reg, l.n_reg, off, pk.get(), pv.get(), wp, wn, st); });
+    return unlocked(ws.use, [&] { return fn(&xk, &xv, l.sal, l.k, l.reg, l.n_reg, off, pk.get(), pv.get(), wp, wn, st); });
   });
 }
 
@@ -277,13 +287,13 @@ PyObject* decode(PyObject*, Args a, Py_ssize_t n) {
     const hipStream_t st = current_stream();
     if (use_static) {
       const auto fn = ZC_FN(kDecodeStatic, zc_decode_attention_static);
-      return unlocked([&] { return fn(&q, pk.get(), pv.get(), tkp, tvp, T, scale, out, lse, st); });
+      return unlocked(&g_static, [&] { return fn(&q, pk.get(), pv.get(), tkp, tvp, T, scale, out, lse, st); });
     }
     const Scratch ws = scratch(ZC_FN(kDecodeWs, zc_decode_attention_workspace)(q.B, q.H, q.D), tensor_of(a[1]), kScratchDecode, st);
     void* wp = ws.ptr;
     const size_t wn = ws.bytes;
     const auto fn = ZC_FN(kDecode, zc_decode_attention);
-    return unlocked([&] { return fn(&q, pk.get(), pv.get(), tkp, tvp, T, scale, out, lse, wp, wn, st); });
+    return unlocked(ws.use, [&] { return fn(&q, pk.get(), pv.get(), tkp, tvp, T, scale, out, lse, wp, wn, st); });
   });
 }
 
@@ -501,7 +511,7 @@ PyObject* paged_attention(PyObject*, Args a, Py_ssize_t n) {
       wn = ws.bytes;
     }
     const auto fn = ZC_FN(kPagedAttention, zc_paged_attention);
-    return unlocked([&] { return fn(&q, &kp, &vp, t.ptr, t.row, t.cols, start, kv, t.R, window, sinks, scale, &o, lse, wp, wn, st); });
+    return unlocked(ws.use, [&] { return fn(&q, &kp, &vp, t.ptr, t.row, t.cols, start, kv, t.R, window, sinks, scale, &o, lse, wp, wn, st); });
   });
 }
 
