@@ -19,6 +19,7 @@
 #include <vector>
 
 #include <ATen/ATen.h>
+#include <c10/hip/HIPCachingAllocator.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -361,13 +362,50 @@ int32_t* ints(PyObject* o, const char* what, int64_t n = -1) {
   if (n >= 0 && t.numel() != n) refuse(what, "has another number of elements than the requests or rows ask for");
   return static_cast<int32_t*>(t.data_ptr());
 }
-bool capturing(hipStream_t stream) {
+// The capture that a stream is in.
+struct Capture { bool on; unsigned long long id; };
+Capture capture_of(hipStream_t stream) {
   hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
-  if (hipStreamIsCapturing(stream, &status) != hipSuccess) {
+  unsigned long long id = 0;
+  if (hipStreamGetCaptureInfo(stream, &status, &id) != hipSuccess) {
     (void)hipGetLastError();
-    return false;                          // (the default stream beside a capture)
+    return {false, 0};                     // (the default stream beside a capture)
   }
-  return status != hipStreamCaptureStatusNone;
+  return {status != hipStreamCaptureStatusNone, id};
+}
+// Whether torch's allocator has this memory in the pool of a graph.
+bool of_a_graph(const at::Tensor& t) {
+  const auto at = reinterpret_cast<uintptr_t>(t.data_ptr());
+  try {
+    for (const auto& s : c10::hip::HIPCachingAllocator::snapshot().segments)
+      if (at >= (uintptr_t)s.address && at - (uintptr_t)s.address < s.total_size) return s.owner_private_pool_id != decltype(s.owner_private_pool_id){0, 0};
+  } catch (const std::exception&) {
+  }
+  return false;                            // (an allocator that does not say)
+}
+// Scratch memory of a captured call: graphs share none, whatever stream they were captured on and whatever streams replay them.  In a
+// capture that torch began it is the graph's, given back behind the call in the order of the capture.  In one that HIP alone
+// knows of, what is given back would be anybody's while the graph is still replayed: it is kept, a buffer per capture and stream.
+Scratch captured_scratch(size_t need, const at::Tensor& like, hipStream_t stream, unsigned long long id) {
+  static bool of_torch = false;            // the capture `of`: asked once for each
+  static unsigned long long of = 0;
+  static auto* kept = new std::map<std::tuple<int, void*, unsigned long long>, at::Tensor>;
+  const auto key = std::make_tuple((int)like.device().index(), (void*)stream, id);
+  Scratch s;
+  const auto have = kept->find(key);
+  if (have != kept->end() && have->second.numel() >= (int64_t)need) {
+    s.t = have->second;
+  } else {
+    s.t = at::empty({(int64_t)need}, like.options().dtype(at::kByte));
+    if (!of_torch || of != id) { of_torch = of_a_graph(s.t); of = id; }
+    if (!of_torch) {
+      if (have != kept->end()) g_captured->push_back(have->second);
+      (*kept)[key] = s.t;
+    }
+  }
+  s.ptr = s.t.data_ptr();
+  s.bytes = s.t.numel();
+  return s;
 }
 struct Table { int32_t* ptr; int64_t R, row, cols; };
 Table table_of(PyObject* o) {
@@ -496,20 +534,13 @@ PyObject* paged_attention(PyObject*, Args a, Py_ssize_t n) {
     }
     const hipStream_t st = current_stream();
     const size_t need = ZC_FN(kPagedAttentionWs, zc_paged_attention_workspace)(t.R, q.L, q.H, kp.H, q.D);
-    void* wp = nullptr;
-    size_t wn = 0;
-    // (a captured call takes memory of its graph, given back behind it in the order of the capture: graphs share nothing, whatever
-    // stream they were captured on and whatever streams replay them)
     Scratch ws;
-    if (need && capturing(st)) {
-      ws.t = at::empty({(int64_t)need}, tensor_of(a[0]).options().dtype(at::kByte));
-      wp = ws.t.data_ptr();
-      wn = need;
-    } else if (need) {
-      ws = scratch(need, tensor_of(a[0]), kScratchPaged, st);
-      wp = ws.ptr;
-      wn = ws.bytes;
+    if (need) {
+      const Capture c = capture_of(st);
+      ws = c.on ? captured_scratch(need, tensor_of(a[0]), st, c.id) : scratch(need, tensor_of(a[0]), kScratchPaged, st);
     }
+    void* wp = ws.ptr;
+    const size_t wn = ws.bytes;
     const auto fn = ZC_FN(kPagedAttention, zc_paged_attention);
     return unlocked(ws.use, [&] { return fn(&q, &kp, &vp, t.ptr, t.row, t.cols, start, kv, t.R, window, sinks, scale, &o, lse, wp, wn, st); });
   });
