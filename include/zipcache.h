@@ -339,7 +339,9 @@ int zc_decode_attention_static(const zc_tensor4* q, const zc_packed* Kp, const z
  * tensors of T rows, q_start[r] .. q_start[r + 1] - 1 (device int32 [R + 1]) those of request r;
  * kv_len[r] (device int32 [R]) counts all its tokens, the new ones, its last, included.  T may be
  * larger than q_start[R] (calls captured for the largest step): rows behind the last request are
- * neither read nor written.  R and T may be 0.  Unlike elsewhere, memory that no token of a call
+ * neither read nor written.  R and T may be 0.  What is written must not overlap itself - out, the tensors
+ * that zc_paged_load fills, the pools that zc_paged_store fills: the stride of an axis of more than one
+ * element is at least what the axes of smaller strides span; what is only read may have any.  Unlike elsewhere, memory that no token of a call
  * lies in or sees - slots past kv_len, pages behind every window, rows behind the last request -
  * may hold anything, NaN included; the values of a request's tokens must be finite.
  *

@@ -1,6 +1,8 @@
 // The paged full-precision cache around its attention: zc_paged_tables (block tables and slot maps of a step),
 // zc_paged_store (a step's new keys and values into their slots), zc_paged_load (requests' pages as [B, H, L, D]
 // tensors, which the compression reads).
+#include <algorithm>
+
 #include "paged_args.hpp"
 
 namespace zc {
@@ -239,6 +241,18 @@ int zc_validate_heads(const zc_tensor4* x, const zc_tensor4* pages) {
   if (x->B != 1 || x->dtype != pages->dtype || x->D != pages->D || x->sH < 0) return ZC_ERR_INVALID_ARG;
   return ZC_OK;
 }
+bool zc_rows_apart(const zc_tensor4* x) {
+  if (x->B == 0 || x->H == 0 || x->L == 0) return true;
+  struct Axis { int64_t n, stride; } axes[3] = {{x->B, x->sB}, {x->H, x->sH}, {x->L, x->sL}};
+  std::sort(axes, axes + 3, [](const Axis& a, const Axis& b) { return a.stride < b.stride; });
+  __int128 span = x->D;
+  for (const Axis& a : axes) {
+    if (a.n <= 1) continue;
+    if (a.stride < span) return false;
+    span += (__int128)(a.n - 1) * a.stride;
+  }
+  return true;
+}
 static int validate_rows(const zc_tensor4* x, const zc_tensor4* pages) {
   const int rc = zc_validate_heads(x, pages);
   return rc ? rc : x->H != pages->H ? ZC_ERR_INVALID_ARG : ZC_OK;
@@ -280,7 +294,7 @@ extern "C" int zc_paged_store(const zc_tensor4* k, const zc_tensor4* v, const in
   if (rc) return rc;
   if (k->L != v->L) return ZC_ERR_INVALID_ARG;
   if (k->L == 0) return ZC_OK;
-  if (!slot_map || (reinterpret_cast<uintptr_t>(slot_map) & 3)) return ZC_ERR_INVALID_ARG;
+  if (!slot_map || (reinterpret_cast<uintptr_t>(slot_map) & 3) || !zc_rows_apart(k_pages) || !zc_rows_apart(v_pages)) return ZC_ERR_INVALID_ARG;
   const int64_t eb = elem_bytes(k->dtype), rowb = k->D * eb;
   StoreArgs a;
   a.k = (const uint8_t*)k->ptr; a.v = (const uint8_t*)v->ptr; a.kp = (uint8_t*)k_pages->ptr; a.vp = (uint8_t*)v_pages->ptr;
@@ -315,7 +329,7 @@ extern "C" int zc_paged_load(const zc_tensor4* k_pages, const zc_tensor4* v_page
   rc = zc_validate_tensor(v);
   if (rc) return rc;
   if (k->dtype != k_pages->dtype || v->dtype != k->dtype || k->D != k_pages->D || v->D != k->D || k->H != k_pages->H || v->H != k->H ||
-      k->B != v->B || k->L != v->L || k->sB < 0 || k->sH < 0 || v->sB < 0 || v->sH < 0)
+      k->B != v->B || k->L != v->L || k->sB < 0 || k->sH < 0 || v->sB < 0 || v->sH < 0 || !zc_rows_apart(k) || !zc_rows_apart(v))
     return ZC_ERR_INVALID_ARG;
   if (max_blocks < 0 || row_stride < max_blocks) return ZC_ERR_INVALID_ARG;
   if (!kv_len || (reinterpret_cast<uintptr_t>(kv_len) & 3) || (max_blocks > 0 && !block_table) || (reinterpret_cast<uintptr_t>(block_table) & 3))

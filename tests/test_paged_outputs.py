@@ -1,0 +1,49 @@
+"""CPU-only checks of the paged cache's outputs: which strides are refused before anything is launched, and which are not."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2405_14256_amd import binding as zb
+from tests.test_paged_host import INV, UNS, WSP, _t4
+
+
+def _strided(t, **kw):
+    for name, value in kw.items():
+        setattr(t, name, value)
+    return t
+
+
+OVERLAPS = [dict(sH=0), dict(sB=0), dict(sH=128, sL=128), dict(sH=64 * 128 - 8), dict(sB=64 * 128, sH=64 * 128), dict(sL=8 * 120, sH=128)]
+APART = [dict(), dict(sL=8 * 128, sH=128), dict(sB=64 * 128, sH=10 * 64 * 128), dict(sL=256, sH=128 * 128, sB=8 * 128 * 128), dict(sL=17 * 128, sH=2 * 128, sB=64 * 17 * 128)]
+
+
+@pytest.mark.parametrize("strides", OVERLAPS)
+def test_outputs_whose_rows_overlap_are_refused(strides):
+    lib = zb.load()
+    x, pages, read = _t4(H=8, L=64), _t4(B=10), _t4(B=10, H=8)
+    wrong = _strided(_t4(B=10), **strides)
+    for kp, vp in ((wrong, pages), (pages, wrong)):
+        assert lib.zc_paged_store(C.byref(x), C.byref(x), 0x3000, C.byref(kp), C.byref(vp), None) == INV
+    for k, v in ((wrong, read), (read, wrong)):
+        assert lib.zc_paged_load(C.byref(pages), C.byref(pages), 0x3000, 4, 4, 0x4000, C.byref(k), C.byref(v), None) == INV
+    if "sB" in strides:                                                       # (a step's rows have one batch element)
+        return
+    q, out = _t4(H=8, L=64), _strided(_t4(H=8, L=64), sB=0, **strides)
+    assert lib.zc_paged_attention(C.byref(q), C.byref(pages), C.byref(pages), 0x3000, 4, 4, 0x4000, 0x5000, 3, 0, 0, 0.0, C.byref(out), 0x6000, 0x7000, 1 << 30,
+                                  None) == INV
+
+
+@pytest.mark.parametrize("strides", APART)
+def test_outputs_whose_rows_lie_apart_are_taken(strides):
+    """(without a GPU a call that passes its checks ends at its launch)"""
+    if torch.cuda.is_available():
+        pytest.skip("the addresses are no memory")
+    lib = zb.load()
+    x, read = _t4(H=8, L=64), _t4(B=10)
+    pages = _strided(_t4(B=10), **strides)
+    assert lib.zc_paged_store(C.byref(x), C.byref(x), 0x3000, C.byref(pages), C.byref(pages), None) not in (INV, UNS, 0)
+    assert lib.zc_paged_load(C.byref(read), C.byref(read), 0x3000, 4, 4, 0x4000, C.byref(pages), C.byref(pages), None) not in (INV, UNS, 0)
+    out, q = _strided(_t4(H=8, L=64), **{**strides, "sB": 0}), _strided(_t4(H=8, L=64), sH=0)          # (what is read may overlap)
+    assert lib.zc_paged_attention(C.byref(q), C.byref(read), C.byref(read), 0x3000, 4, 4, 0x4000, 0x5000, 3, 0, 0, 0.0, C.byref(out), 0x6000, 0x7000, 1 << 30,
+                                  None) not in (INV, UNS, WSP, 0)
