@@ -150,7 +150,7 @@ __device__ inline bool find_unit(const PagedArgs& a, int u, Unit& x) {
       x.rows = min(rb, all_rows - i0);
       x.p0 = x.kv - x.nq + x.j0;
       x.p1 = x.kv - x.nq + row_at(a, x, x.rows - 1).j;
-      const int low = a.window ? max(0, x.p0 - a.window + 1) : 0;
+      const int low = a.window ? max(0, max(x.p0, 0) - a.window + 1) : 0;      // (a difference of positions in front of the first token may pass 32 bits)
       x.first = low / kTile;
       x.sink_tiles = min((min(a.sinks, low) + kTile - 1) / kTile, x.first);
       const int far = max(x.p0, 0) - a.window - 14;
@@ -199,7 +199,7 @@ struct Seen {
   int low, sink;
   uint32_t span;
   __device__ Seen(const PagedArgs& a, int p0, int p1) {
-    low = a.window ? max(p1 - a.window + 1, 0) : 0;
+    low = a.window ? max(max(p1, 0) - a.window + 1, 0) : 0;
     const int end = max(p0, 0) - 30;                       // (of positions in front of the first key no block is seen)
     span = max(end - low, 0);
     sink = a.window ? min(a.sinks - 31, end) : 0;

@@ -1,0 +1,24 @@
+"""Paged attention at the ends of the ranges that its documentation allows."""
+import pytest
+import torch
+
+from paper_2405_14256_amd import binding as zb
+from tests import paged_plain as plain
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+BF, FL = torch.bfloat16, torch.float32
+
+
+@pytest.mark.parametrize("dtype", [BF, FL])
+def test_the_widest_window_over_rows_far_in_front_of_the_first_token(dtype):
+    """A table with room for 2^31 - 2^16 tokens, a window one shorter, and 70 000 new tokens of a request that has 100: a row's
+    position less the window passes 32 bits."""
+    p = plain.Pages([70000], [100], 1, 1, 64, dtype, page=65536, seed=60)
+    table = torch.full((1, 32767), -1, dtype=torch.int32, device=DEV)
+    table[:, :1] = p.table[:, :1]
+    window = 32767 * 65536 - 1
+    out, lse = torch.full_like(p.q, 5.0), torch.full((1, p.T), 5.0, dtype=torch.float32, device=DEV)
+    zb.zc_paged_attention(p.q, p.kp, p.vp, table, p.q_start, p.kv, window=window, sinks=4, out=out, lse=lse)
+    p.check(out, lse, window=window, sinks=4)
+    assert bool((out[:69900] == 0).all()) and bool((lse[:, :69900] == -float("inf")).all())
