@@ -1035,7 +1035,7 @@ extern "C" int zc_paged_attention(const zc_tensor4* q, const zc_tensor4* k_pages
   rc = zc_validate_heads(out, k_pages);
   if (rc) return rc;
   if (q->H != out->H || q->L != out->L || q->H % k_pages->H || !zc_rows_apart(out)) return ZC_ERR_INVALID_ARG;
-  if (R < 0 || window < 0 || sinks < 0 || !(sm_scale >= 0.f) || sm_scale > 3.4e38f) return ZC_ERR_INVALID_ARG;
+  if (R < 0 || window < 0 || sinks < 0 || !(sm_scale >= 0.f) || !(sm_scale * kLog2e <= -kLowestLogit)) return ZC_ERR_INVALID_ARG;
   if (max_blocks < 0 || row_stride < max_blocks) return ZC_ERR_INVALID_ARG;
   if (q->L == 0 || R == 0) return ZC_OK;
   if (!q_start || !kv_len || (max_blocks > 0 && !block_table)) return ZC_ERR_INVALID_ARG;

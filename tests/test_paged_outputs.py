@@ -1,4 +1,4 @@
-"""CPU-only checks of the paged cache's outputs: which strides are refused before anything is launched, and which are not."""
+"""CPU-only checks of the paged cache: which strides of outputs and which scales are refused before anything is launched, and which are not."""
 import ctypes as C
 
 import pytest
@@ -47,3 +47,12 @@ def test_outputs_whose_rows_lie_apart_are_taken(strides):
     out, q = _strided(_t4(H=8, L=64), **{**strides, "sB": 0}), _strided(_t4(H=8, L=64), sH=0)          # (what is read may overlap)
     assert lib.zc_paged_attention(C.byref(q), C.byref(read), C.byref(read), 0x3000, 4, 4, 0x4000, 0x5000, 3, 0, 0, 0.0, C.byref(out), 0x6000, 0x7000, 1 << 30,
                                   None) not in (INV, UNS, WSP, 0)
+
+
+@pytest.mark.parametrize("scale,taken", [(2.3e38, True), (2.4e38, False), (3.3e38, False), (float("inf"), False), (1e-45, True)])
+def test_scales_whose_logits_have_no_finite_factor_are_refused(scale, taken):
+    if torch.cuda.is_available():
+        pytest.skip("the addresses are no memory")
+    q, pages = _t4(H=8, L=64), _t4(B=10)
+    rc = zb.load().zc_paged_attention(C.byref(q), C.byref(pages), C.byref(pages), 0x3000, 4, 4, 0x4000, 0x5000, 3, 0, 0, scale, C.byref(q), 0x6000, 0x7000, 1 << 30, None)
+    assert rc not in (INV, UNS, WSP, 0) if taken else rc == INV
