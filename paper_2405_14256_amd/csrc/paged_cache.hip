@@ -348,8 +348,10 @@ extern "C" int zc_paged_load(const zc_tensor4* k_pages, const zc_tensor4* v_page
   a.vp_sB = v_pages->sB * eb; a.vp_sH = v_pages->sH * eb; a.vp_sL = v_pages->sL * eb;
   const int rows = 256 >> a.cpr;
   const bool many = ceil_div64(a.L, rows) * k->H * k->B * 2 >= 4096;
+  const int64_t wgs = ceil_div64(a.L, many ? 2 * rows : rows);
+  if (wgs > 0xffffff) return ZC_ERR_UNSUPPORTED;         // (a grid counts the threads of a dimension in 32 bits)
   hipStream_t st = (hipStream_t)stream;
-  const dim3 grid((unsigned)ceil_div64(a.L, many ? 2 * rows : rows), (unsigned)k->H, (unsigned)(2 * k->B));
+  const dim3 grid((unsigned)wgs, (unsigned)k->H, (unsigned)(2 * k->B));
   if (many) hipLaunchKernelGGL(k_paged_load<2>, grid, dim3(256), 0, st, a);
   else hipLaunchKernelGGL(k_paged_load<1>, grid, dim3(256), 0, st, a);
   ZC_LAUNCH_CHECK();

@@ -1,4 +1,4 @@
-"""CPU-only checks of the paged cache: which strides of outputs and which scales are refused before anything is launched, and which are not."""
+"""CPU-only checks of the paged cache: which strides of outputs, scales and sizes are refused before anything is launched, and which are not."""
 import ctypes as C
 
 import pytest
@@ -56,3 +56,13 @@ def test_scales_whose_logits_have_no_finite_factor_are_refused(scale, taken):
     q, pages = _t4(H=8, L=64), _t4(B=10)
     rc = zb.load().zc_paged_attention(C.byref(q), C.byref(pages), C.byref(pages), 0x3000, 4, 4, 0x4000, 0x5000, 3, 0, 0, scale, C.byref(q), 0x6000, 0x7000, 1 << 30, None)
     assert rc not in (INV, UNS, WSP, 0) if taken else rc == INV
+
+
+@pytest.mark.parametrize("L,dtype,taken", [(1 << 28, zb.ZC_F32, False), ((1 << 28) - 16, zb.ZC_F32, True), (1 << 28, zb.ZC_BF16, True)])
+def test_a_load_that_one_launch_cannot_count_is_refused(L, dtype, taken):
+    if torch.cuda.is_available():
+        pytest.skip("the addresses are no memory")
+    pages, k = _t4(B=10, dtype=dtype), _t4(B=1, H=1, L=L, dtype=dtype)
+    pages.H, pages.sH = 1, 0
+    rc = zb.load().zc_paged_load(C.byref(pages), C.byref(pages), 0x3000, 1 << 22, 1 << 22, 0x4000, C.byref(k), C.byref(k), None)
+    assert rc not in (INV, UNS, 0) if taken else rc == UNS
