@@ -360,7 +360,8 @@ int zc_decode_attention_static(const zc_tensor4* q, const zc_packed* Kp, const z
  * requests and the pages they need must number less than 2^31 each.
  *
  * zc_paged_store: k, v [1, Hkv, T, D] (any strides) to the slots of their tokens; a token whose slot is
- * outside [0, N * page) is left out.  Of two tokens with one slot either may stay.
+ * outside [0, N * page) is left out.  Of tokens with one slot every 16 bytes of the
+ * slot's rows are one token's, and not of all the same token's: zc_paged_tables gives no slot twice.
  *
  * zc_paged_load: k[r, h, i, :] and v[r, h, i, :] = token i of request r, for i < min(kv_len[r], k->L,
  * max_blocks * page); other rows are left as they are.  k, v [R, Hkv, L, D]: what zc_probe_saliency and

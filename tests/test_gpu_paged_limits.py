@@ -22,3 +22,18 @@ def test_the_widest_window_over_rows_far_in_front_of_the_first_token(dtype):
     zb.zc_paged_attention(p.q, p.kp, p.vp, table, p.q_start, p.kv, window=window, sinks=4, out=out, lse=lse)
     p.check(out, lse, window=window, sinks=4)
     assert bool((out[:69900] == 0).all()) and bool((lse[:, :69900] == -float("inf")).all())
+
+
+@pytest.mark.parametrize("T,H,D,dtype", [(2, 40, 128, BF), (300, 5, 64, FL), (9000, 8, 128, BF)])
+def test_tokens_with_one_slot_leave_pieces_of_theirs(T, H, D, dtype):
+    """Every 16 bytes of the slot's rows are one of the tokens', and nothing else is written."""
+    g = torch.Generator(device=DEV).manual_seed(T)
+    k, v = (torch.randn(T, H, D, generator=g, device=DEV).to(dtype) for _ in range(2))
+    kp, vp = (torch.full((3, H, 16, D), 7.0, dtype=dtype, device=DEV) for _ in range(2))
+    zb.zc_paged_store(k, v, torch.full((T,), 21, dtype=torch.int32, device=DEV), kp, vp)
+    n = 16 // dtype.itemsize
+    for pool, x in ((kp, k), (vp, v)):
+        got = pool[1, :, 5].reshape(H, D // n, n)
+        assert bool((x.reshape(T, H, D // n, n) == got).all(-1).any(0).all())
+        pool[1, :, 5] = 7.0
+        assert bool((pool == 7.0).all())
