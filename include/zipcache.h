@@ -358,6 +358,8 @@ int zc_decode_attention_static(const zc_tensor4* q, const zc_packed* Kp, const z
  * blocks past max_blocks, get no slot and no entry.  free_pages and n_free are not changed: subtract
  * *n_taken from *n_free before the next step, on the device if need be.  The new tokens of all
  * requests and the pages they need must number less than 2^31 each.
+ * A finished request's pages go back by writing its row's first ceil(kv_len / page) entries to free_pages behind the
+ * first *n_free and adding their number to *n_free (n_list must have room), in the order of the stream with the calls that read the pages.
  *
  * zc_paged_store: k, v [1, Hkv, T, D] (any strides) to the slots of their tokens; a token whose slot is
  * outside [0, N * page) is left out.  Of tokens with one slot every 16 bytes of the
@@ -392,9 +394,19 @@ int zc_paged_load(const zc_tensor4* k_pages, const zc_tensor4* v_pages, const in
  * second product rounded to the tensors' type.  Deterministic for equal lengths and shapes; a row's last bits may
  * depend on the other requests (long rows are split by what the whole call has to do, and joined in fp32).
  * Workspace: zc_paged_attention_workspace() bytes, 16-byte aligned, with any contents; calls that share one
- * must not run concurrently.  q_start must ascend within [0, T], kv_len be 0 to max_blocks * page (values outside are
+ * must not run concurrently.  It is what the finest split of R requests and T rows takes, whether this call is split or not: up to
+ * 273 MB of 128 channels (32 heads over 8: one token 9 MB, 64 requests of one 90, a chunk of 2048 206), none where R or T are too large
+ * for a split.  q_start must ascend within [0, T], kv_len be 0 to max_blocks * page (values outside are
  * taken for the nearest).
- * Limits: R < 2^24, T * Hq < 2^31. */
+ * The host knows neither q_start nor kv_len; how rows are split, and whether at all, follows from R, T, the heads, the window and the room
+ * of a table's row, max_blocks * page.  So a table much wider than its requests costs time (one token each of 12 requests of 1024
+ * tokens 12.5 us in 16 columns of 64 tokens, 16.0 in 64 or 256): pass as many columns as the longest request needs, where the caller knows
+ * it, with the row stride of the whole table.  A step of so many rows that their blocks fill the chip is not split, whatever its
+ * lengths: of single tokens with 32 heads over 8 from 113 requests on (109 of 500 tokens and one of 32768 76 us, 113 and one 315); and
+ * where T * Hq / Hkv is more than 64 R it is T that counts, not q_start[R]: one token over 32768 in a step captured for T = 1000
+ * 29 us, for T = 5120 251.
+ * Limits: R < 2^24, T * Hq < 2^31; a step has at most 2^24 - 1 blocks of all heads, units of split ones among them: T * Hq / 128 (fp32: / 32) + 2 min(R, T) Hkv
+ * + Hkv + 2560 below 2^24 is always enough. */
 size_t zc_paged_attention_workspace(int64_t R, int64_t T, int64_t Hq, int64_t Hkv, int64_t D);
 int zc_paged_attention(const zc_tensor4* q, const zc_tensor4* k_pages, const zc_tensor4* v_pages, const int32_t* block_table,
                        int64_t row_stride, int64_t max_blocks, const int32_t* q_start, const int32_t* kv_len, int64_t R,

@@ -390,7 +390,8 @@ def zc_paged_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Te
                        kv_len: torch.Tensor, window: int = 0, sinks: int = 0, sm_scale: float = 0.0,
                        out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None):
     """q [T, Hq, D] (or [1, Hq, T, D]): a step's new tokens, request after request -> (out like q, lse [Hq, T]).
-    Rows behind the last request are not written."""
+    Rows behind the last request are not written.  The launch is chosen by the table's room, not by kv_len: pass the
+    columns that the longest request needs (block_table[:, :n]) where that is known."""
     host = _native()
     if out is None:
         out = torch.empty_like(q)

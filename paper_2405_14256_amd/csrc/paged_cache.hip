@@ -183,7 +183,7 @@ struct LoadArgs {
 };
 
 // A workgroup copies 256 * UNROLL pieces of one head of one request.  Bound by memory: 16 requests of 3500 to 4096 tokens, 40 heads
-// of 128 channels, fp16, 435 us (5.7 TB/s; 467 with stores through the caches), one of 4096 tokens, 8 heads, bf16, 6.3 us.
+// of 128 channels, fp16, 438 us (5.6 TB/s; 467 with stores through the caches), one of 4096 tokens, 8 heads, bf16, 6.4 us.
 template <int UNROLL>
 __global__ __launch_bounds__(256) void k_paged_load(LoadArgs a) {
   const int r = blockIdx.z >> 1, h = blockIdx.y;

@@ -37,3 +37,27 @@ def test_tokens_with_one_slot_leave_pieces_of_theirs(T, H, D, dtype):
         assert bool((x.reshape(T, H, D // n, n) == got).all(-1).any(0).all())
         pool[1, :, 5] = 7.0
         assert bool((pool == 7.0).all())
+
+
+def test_pages_of_finished_requests_are_taken_again():
+    """A pool that holds three requests' pages, twelve requests one after the other: every finished one's pages go back."""
+    page, cols, N = 16, 5, 15
+    i32 = dict(dtype=torch.int32, device=DEV)
+    free, n_free = torch.arange(N, **i32), torch.tensor([N], **i32)
+    table = torch.full((3, cols), -1, **i32)
+    kv = [0, 0, 0]
+    for step in range(200):
+        r = step % 3
+        if kv[r] == 80 - 7 * r:                                               # finished
+            n = -(-kv[r] // page)
+            free.index_copy_(0, n_free + torch.arange(n, device=DEV), table[r, :n])
+            n_free += n
+            kv[r] = 0
+        new = [0, 0, 0]
+        new[r] = min(9, 80 - 7 * r - kv[r])
+        kv[r] += new[r]
+        _, slots, taken = zb.zc_paged_tables(torch.tensor(new, **i32), torch.tensor(kv, **i32), table, free, page, sum(new), n_free=n_free)
+        n_free -= taken
+        held = [int(x) for i in range(3) for x in table[i, :-(-kv[i] // page)]]
+        assert sorted(held + free[:int(n_free)].tolist()) == list(range(N))
+        assert slots.tolist() == [int(table[r, p // page]) * page + p % page for p in range(kv[r] - new[r], kv[r])]
