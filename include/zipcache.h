@@ -387,7 +387,7 @@ int zc_paged_load(const zc_tensor4* k_pages, const zc_tensor4* v_pages, const in
  * with window > 0 only those with i > pos - window or i < sinks:
  *   out[h, t, :] = sum_i softmax_i(q[h, t] . k[h/G, i] * sm_scale) v[h/G, i, :]
  * q, out [1, Hq, T, D] of the pools' type, Hq / Hkv whole and at most 4096; sm_scale == 0 means
- * 1/sqrt(D); a negative one is refused, and one of 2.3e38 or more (its product with log2(e) is no finite float).  lse (device float [Hq, T], optional) receives the natural-log
+ * 1/sqrt(D); a negative one is refused, and one above 2.35e38 (its product with log2(e) is no finite float).  lse (device float [Hq, T], optional) receives the natural-log
  * normalisers (for zc_probe_saliency's lse_ext).  A row that sees no token (kv_len < nq), or only logits of
  * -inf, has zeros for its output and -inf for its normaliser.  A request may have no new tokens.
  * fp32 tensors are multiplied on the fp32 matrix pipes; the probabilities of 16-bit tensors enter the

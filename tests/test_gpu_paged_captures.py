@@ -93,3 +93,47 @@ def test_a_capture_of_torch_s_holds_no_memory_behind_its_graph():
     for _ in range(5):
         capture()
     assert torch.cuda.memory_allocated() - before < need
+
+
+def test_captures_of_both_kinds_one_after_the_other():
+    """A graph of torch's, one of HIP's own, one of torch's again: what each has for a workspace is asked for each capture."""
+    hip = _hip()
+    p = plain.Pages([1], [6000], 8, 2, 128, BF, seed=54)
+    out, lse = torch.zeros_like(p.q), torch.zeros(8, 1, dtype=torch.float32, device=DEV)
+    side = torch.cuda.Stream()
+
+    def call():
+        zb.zc_paged_attention(p.q, p.kp, p.vp, p.table, p.q_start, p.kv, out=out, lse=lse)
+    need = zb.load().zc_paged_attention_workspace(1, 1, 8, 2, 128)
+    torch.cuda.synchronize()
+    replays, others, held = [], [], []
+    for kind in ("torch", "hip", "torch", "hip"):
+        if kind == "torch":
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=side):
+                call()
+            replays.append(g.replay)
+            held.append(g)
+        else:
+            graph, run = C.c_void_p(), C.c_void_p()
+            assert hip.hipStreamBeginCapture(side.cuda_stream, 2) == 0
+            with torch.cuda.stream(side):
+                call()
+            assert hip.hipStreamEndCapture(side.cuda_stream, C.byref(graph)) == 0
+            assert hip.hipGraphInstantiate(C.byref(run), graph, None, None, 0) == 0
+            replays.append(lambda run=run: hip.hipGraphLaunch(run, side.cuda_stream))
+            held.append((graph, run))
+        with torch.cuda.stream(side):
+            others += [torch.full((need,), 0x5A, dtype=torch.uint8, device=DEV) for _ in range(3)]
+        torch.cuda.synchronize()
+    for _ in range(3):
+        for replay in replays:
+            out.zero_()
+            lse.zero_()
+            torch.cuda.synchronize()
+            replay()
+            torch.cuda.synchronize()
+            p.check(out, lse)
+            assert all(bool((x == 0x5A).all()) for x in others)
+    for graph, run in (x for x in held if isinstance(x, tuple)):
+        assert hip.hipGraphExecDestroy(run) == 0 and hip.hipGraphDestroy(graph) == 0
