@@ -395,7 +395,7 @@ int zc_paged_load(const zc_tensor4* k_pages, const zc_tensor4* v_pages, const in
  * depend on the other requests (long rows are split by what the whole call has to do, and joined in fp32).
  * Workspace: zc_paged_attention_workspace() bytes, 16-byte aligned, with any contents; calls that share one
  * must not run concurrently.  It is what the finest split of R requests and T rows takes, whether this call is split or not: up to
- * 273 MB of 128 channels (32 heads over 8: one token 9 MB, 64 requests of one 90, a chunk of 2048 206), none where R or T are too large
+ * 280 MB of 128 channels (32 heads over 8: one token 9 MB, 64 requests of one 90, a chunk of 2048 206), none where R or T are too large
  * for a split.  q_start must ascend within [0, T], kv_len be 0 to max_blocks * page (values outside are
  * taken for the nearest).
  * The host knows neither q_start nor kv_len; how rows are split, and whether at all, follows from R, T, the heads, the window and the room
