@@ -413,6 +413,31 @@ int zc_paged_attention(const zc_tensor4* q, const zc_tensor4* k_pages, const zc_
                        int32_t window, int32_t sinks, float sm_scale, const zc_tensor4* out, float* lse,
                        void* ws, size_t ws_bytes, void* stream);
 
+/* ---- eviction by gathered weight -----------------------------------------------------------------
+ * Request r keeps min(kv_len[r], keep[r], most) of its kv_len[r] tokens (keep: device int32 [R], negative: 0; most: what the
+ * host knows of it): the `recent` newest; of what is left the `sinks` first; of the others those of the largest scores,
+ * every KV head its own, and of equal ones the first.  Where recent is more than a request keeps its newest tokens stay, and where sinks
+ * is more than what is then left the first of them.  scores (device float [N, Hkv, page], 16-byte aligned) has a token's score at its
+ * place in the pages; of NaN any may stay.  With `together` (not 0) all heads keep the same tokens, by the sum of their scores
+ * (of 64 bits, rounded once).
+ * What stays moves, in its order, to the first places of the request's pages: keys, values and scores; what lies behind it is left as it
+ * was.  new_len (device int32 [R], no memory of kv_len or keep) receives the numbers, kept (device int32 [R, Hkv, most], [R, 1, most]
+ * with `together`) the places that the tokens had, ascending; entries behind them are left as they were.
+ * Pages that a request then does not need, entries ceil(new_len / page) to ceil(kv_len / page) - 1 of its row, are written to free_pages
+ * (device int32 [n_list]) from *n_free on (device int32), request after request, what passes the list's end left out; *n_freed
+ * (device int32, may be NULL) is their number.  As in zc_paged_tables *n_free is not changed: add *n_freed to it, in the order of the stream.  block_table is
+ * not changed.  free_pages may be NULL.
+ * A request's pages must be its own: not another's, not twice in its row.  A token whose entry is no page has a score of 0 and zeros for
+ * its rows, a place without a page takes nothing, and among the pages that are left such an entry is written like any other: evict with the lengths
+ * that zc_paged_tables found pages for.  kv_len outside [0, max_blocks * page] is taken for the nearest.
+ * Deterministic.  R may be 0; R and 3 Hkv <= 65535.  Workspace: zc_paged_evict_workspace() bytes, 16-byte aligned, with any contents (0 without
+ * `together`, else 4 for every place of every row of the table); calls that share one must not run concurrently. */
+size_t zc_paged_evict_workspace(int64_t R, int64_t max_blocks, int64_t page, int32_t together);
+int zc_paged_evict(const zc_tensor4* k_pages, const zc_tensor4* v_pages, float* scores, const int32_t* block_table, int64_t row_stride,
+                   int64_t max_blocks, const int32_t* kv_len, const int32_t* keep, int64_t R, int64_t most, int32_t sinks, int32_t recent,
+                   int32_t together, int32_t* new_len, int32_t* kept, int32_t* free_pages, int64_t n_list, const int32_t* n_free,
+                   int32_t* n_freed, void* ws, size_t ws_bytes, void* stream);
+
 /* ---- helpers ------------------------------------------------------------------ */
 /* Bytes of one code arena of `cap` slots. */
 size_t zc_arena_bytes(int64_t B, int64_t H, int64_t D, int64_t cap, int32_t bits);

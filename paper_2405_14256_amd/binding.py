@@ -118,6 +118,10 @@ def load() -> C.CDLL:
     lib.zc_paged_attention_workspace.argtypes = [I64, I64, I64, I64, I64]
     lib.zc_paged_attention.restype = C.c_int
     lib.zc_paged_attention.argtypes = [T4, T4, T4, P, I64, I64, P, P, I64, I32, I32, F, T4, P, P, SZ, P]
+    lib.zc_paged_evict_workspace.restype = SZ
+    lib.zc_paged_evict_workspace.argtypes = [I64, I64, I64, I32]
+    lib.zc_paged_evict.restype = C.c_int
+    lib.zc_paged_evict.argtypes = [T4, T4, P, P, I64, I64, P, P, I64, I64, I32, I32, I32, P, P, P, I64, P, P, P, SZ, P]
     lib.zc_arena_bytes.restype = SZ
     lib.zc_arena_bytes.argtypes = [I64, I64, I64, I64, I32]
     lib.zc_arena_slots.restype = I64
@@ -400,3 +404,23 @@ def zc_paged_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Te
         lse = torch.empty(Hq, T, dtype=torch.float32, device=q.device)
     _check("zc_paged_attention", host.paged_attention(q, k_pages, v_pages, block_table, q_start, kv_len, window, sinks, sm_scale, out, lse))
     return out, lse
+
+
+def zc_paged_evict(k_pages: torch.Tensor, v_pages: torch.Tensor, scores: torch.Tensor, block_table: torch.Tensor, kv_len: torch.Tensor,
+                   keep: torch.Tensor, most: int, sinks: int = 0, recent: int = 0, together: bool = False,
+                   free_pages: Optional[torch.Tensor] = None, n_free: Optional[torch.Tensor] = None, new_len: Optional[torch.Tensor] = None,
+                   kept: Optional[torch.Tensor] = None, n_freed: Optional[torch.Tensor] = None):
+    """Of request r's kv_len[r] tokens keep[r] at most (and `most`, which the host knows) stay, by scores [N, Hkv, page]; keys, values and
+    scores move to the front of its pages.  Returns (new_len [R], kept [R, Hkv, most] - [R, 1, most] with `together` - and n_freed [1],
+    None without a list of free pages)."""
+    host = _native()
+    R, dev = block_table.shape[0], k_pages.device
+    if new_len is None:
+        new_len = torch.empty(R, dtype=torch.int32, device=dev)
+    if kept is None:
+        kept = torch.empty(R, 1 if together else k_pages.shape[1], max(most, 0), dtype=torch.int32, device=dev)
+    if n_freed is None and free_pages is not None:
+        n_freed = torch.empty(1, dtype=torch.int32, device=dev)
+    _check("zc_paged_evict", host.paged_evict(k_pages, v_pages, scores, block_table, kv_len, keep, most, sinks, recent, together, new_len, kept,
+                                              free_pages, n_free, n_freed))
+    return new_len, kept, n_freed

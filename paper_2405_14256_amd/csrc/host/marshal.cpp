@@ -31,14 +31,15 @@ namespace {
 // ---- entry points, in the order of kNames ---------------------------------------------------
 enum Fn {
   kProbe, kAccumulated, kPrefill, kSelect, kQuantize, kQuantizeKV, kDecode, kDecodeStatic, kProbs, kRows, kDequantize,
-  kPagedTables, kPagedStore, kPagedLoad, kPagedAttention,
-  kProbeWs, kQuantizeWs, kQuantizeKVWs, kDecodeWs, kPagedAttentionWs, kFnCount
+  kPagedTables, kPagedStore, kPagedLoad, kPagedAttention, kPagedEvict,
+  kProbeWs, kQuantizeWs, kQuantizeKVWs, kDecodeWs, kPagedAttentionWs, kPagedEvictWs, kFnCount
 };
 const char* const kNames[kFnCount] = {
     "zc_probe_saliency", "zc_probe_accumulated", "zc_prefill_attention", "zc_select_salient", "zc_quantize_pack",
     "zc_quantize_pack_kv", "zc_decode_attention", "zc_decode_attention_static", "zc_decode_probs", "zc_rows_saliency",
-    "zc_dequantize_cache", "zc_paged_tables", "zc_paged_store", "zc_paged_load", "zc_paged_attention", "zc_probe_saliency_workspace", "zc_quantize_pack_workspace", "zc_quantize_pack_kv_workspace",
-    "zc_decode_attention_workspace", "zc_paged_attention_workspace"};
+    "zc_dequantize_cache", "zc_paged_tables", "zc_paged_store", "zc_paged_load", "zc_paged_attention", "zc_paged_evict",
+    "zc_probe_saliency_workspace", "zc_quantize_pack_workspace", "zc_quantize_pack_kv_workspace", "zc_decode_attention_workspace",
+    "zc_paged_attention_workspace", "zc_paged_evict_workspace"};
 void* g_fn[kFnCount];
 
 #define ZC_FN(id, name) reinterpret_cast<decltype(&name)>(g_fn[id])
@@ -116,7 +117,7 @@ struct Packed {
 // under the interpreter lock; the launches do not, and a call is several of them: two threads' calls on
 // one stream (by default all threads share one) would come between each other's.  So a call holds its buffer's mutex
 // while it launches, taken when the interpreter lock has been given up and given back before that is taken again.
-enum Kind { kScratchProbe, kScratchQuantize, kScratchQuantizeKV, kScratchDecode, kScratchPaged };
+enum Kind { kScratchProbe, kScratchQuantize, kScratchQuantizeKV, kScratchDecode, kScratchPaged, kScratchEvict };
 struct Scratch { at::Tensor t; void* ptr = nullptr; size_t bytes = 0; bool captured = false; std::mutex* use = nullptr; };
 std::map<std::tuple<int, int, void*>, Scratch>* g_scratch;
 std::vector<at::Tensor>* g_captured;      // replaced buffers that graphs may hold
@@ -407,6 +408,12 @@ Scratch captured_scratch(size_t need, const at::Tensor& like, hipStream_t stream
   s.bytes = s.t.numel();
   return s;
 }
+// Of a call over the pages: its graph's, or its stream's.
+Scratch paged_scratch(size_t need, const at::Tensor& like, Kind kind, hipStream_t stream) {
+  if (!need) return {};
+  const Capture c = capture_of(stream);
+  return c.on ? captured_scratch(need, like, stream, c.id) : scratch(need, like, kind, stream);
+}
 struct Table { int32_t* ptr; int64_t R, row, cols; };
 Table table_of(PyObject* o) {
   const at::Tensor& t = tensor_of(o);
@@ -534,15 +541,50 @@ PyObject* paged_attention(PyObject*, Args a, Py_ssize_t n) {
     }
     const hipStream_t st = current_stream();
     const size_t need = ZC_FN(kPagedAttentionWs, zc_paged_attention_workspace)(t.R, q.L, q.H, kp.H, q.D);
-    Scratch ws;
-    if (need) {
-      const Capture c = capture_of(st);
-      ws = c.on ? captured_scratch(need, tensor_of(a[0]), st, c.id) : scratch(need, tensor_of(a[0]), kScratchPaged, st);
-    }
+    const Scratch ws = paged_scratch(need, tensor_of(a[0]), kScratchPaged, st);
     void* wp = ws.ptr;
     const size_t wn = ws.bytes;
     const auto fn = ZC_FN(kPagedAttention, zc_paged_attention);
     return unlocked(ws.use, [&] { return fn(&q, &kp, &vp, t.ptr, t.row, t.cols, start, kv, t.R, window, sinks, scale, &o, lse, wp, wn, st); });
+  });
+}
+
+// Gathered weights beside the pages: float32 [N, Hkv, page].
+float* scores_of(PyObject* o, const zc_tensor4& pages) {
+  const at::Tensor& t = tensor_of(o);
+  on_device(t, "scores");
+  if (t.scalar_type() != at::kFloat || !t.is_contiguous() || t.dim() != 3 || t.size(0) != pages.B || t.size(1) != pages.H || t.size(2) != pages.L)
+    refuse("scores", "must be a contiguous float32 [N, Hkv, page] tensor");
+  return static_cast<float*>(t.data_ptr());
+}
+
+// (k_pages, v_pages, scores, block_table, kv_len, keep, most, sinks, recent, together, new_len, kept, free_pages, n_free, n_freed)
+PyObject* paged_evict(PyObject*, Args a, Py_ssize_t n) {
+  return guarded(kPagedEvict, n, 15, [&]() -> int {
+    g_device = -1;
+    const zc_tensor4 kp = pool(a[0], "k_pages"), vp = pool(a[1], "v_pages");
+    float* scores = scores_of(a[2], kp);
+    const Table t = table_of(a[3]);
+    const auto *kv = ints(a[4], "kv_len", t.R), *keep = ints(a[5], "keep", t.R);
+    const int64_t most = int_of(a[6]);
+    const int32_t sinks = int32_of(a[7]), recent = int32_of(a[8]);
+    const int together = PyObject_IsTrue(a[9]);
+    if (together < 0) throw Bad();
+    if (most < 0) refuse("most", "must not be negative");
+    auto *len = ints(a[10], "new_len", t.R), *kept = ints(a[11], "kept", t.R * (together ? 1 : kp.H) * most);
+    int32_t* free = ints(a[12], "free_pages");
+    const int64_t list = free ? tensor_of(a[12]).numel() : 0;
+    const auto* n_free = ints(a[13], "n_free", 1);
+    auto* n_freed = ints(a[14], "n_freed", 1);
+    const hipStream_t st = current_stream();
+    const size_t need = ZC_FN(kPagedEvictWs, zc_paged_evict_workspace)(t.R, t.cols, kp.L, together);
+    const Scratch ws = paged_scratch(need, tensor_of(a[0]), kScratchEvict, st);
+    void* wp = ws.ptr;
+    const size_t wn = ws.bytes;
+    const auto fn = ZC_FN(kPagedEvict, zc_paged_evict);
+    return unlocked(ws.use, [&] {
+      return fn(&kp, &vp, scores, t.ptr, t.row, t.cols, kv, keep, t.R, most, sinks, recent, together, len, kept, free, list, n_free, n_freed, wp, wn, st);
+    });
   });
 }
 
@@ -591,6 +633,7 @@ PyMethodDef kMethods[] = {
     ZC_METHOD("paged_store", paged_store),
     ZC_METHOD("paged_load", paged_load),
     ZC_METHOD("paged_attention", paged_attention),
+    ZC_METHOD("paged_evict", paged_evict),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_zc_host", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
