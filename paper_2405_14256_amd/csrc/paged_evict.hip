@@ -3,8 +3,8 @@
 //
 // Two launches (three where all heads take one choice): who stays, as an ascending list for each request and head, with the
 // lengths and the pages that are left; then the rows, in place.  A token that stays never moves back: the i-th of the list lies at
-// list[i] >= i.  So a wave that takes some channels of a (request, head) for itself may go through the list from its start, reading
-// as far ahead as it likes, and needs no copy and no other wave: the place i that it fills was read by then, as the
+// list[i] >= i.  So a workgroup that takes some channels of a (request, head) for itself may go through the list from its start, reading
+// as far ahead as it likes, and needs no copy and no other workgroup: the place i that it fills was read by then, as the
 // token there, if it stays, is the i-th of the list or one before.
 #include "lds_dma.hpp"
 #include "paged_args.hpp"
@@ -12,8 +12,7 @@
 namespace zc {
 
 struct EvictArgs {
-  const uint8_t* from[2];                                // keys, values (the pools)
-  uint8_t* to[2];
+  uint8_t* pool[2];                                      // keys, values
   float* scores;                                         // [page][head][row]
   int64_t sB[2], sH[2], sL[2];                           // bytes
   const int32_t *table, *kv_len, *keep;
@@ -25,7 +24,7 @@ struct EvictArgs {
   const int32_t* n_free;
   int64_t n_list;
   const float* sums;                                     // [R, cap], of all heads (null: every head by its own scores)
-  int rowb, slice, lanes;                                // bytes of a row, of a wave's part of it; 16-byte pieces of that, as a shift
+  int rowb, slice, lanes;                                // bytes of a row, of a workgroup's part of it; 16-byte pieces of that, as a shift
 };
 
 __device__ inline int tokens_of(const EvictArgs& a, int r) { return min(max(a.kv_len[r], 0), a.cap); }
@@ -35,254 +34,285 @@ __device__ inline int stay_of(const EvictArgs& a, int r, int kv) {
 }
 
 // ---- one score of all heads ------------------------------------------------------------------------
-// A thread a token: sums in 64 bits, rounded once (sums of 32 bits in another order would rank tokens of nearly equal weight
+// A thread four tokens: sums in 64 bits, rounded once (sums of 32 bits in another order would rank tokens of nearly equal weight
 // differently).
-__global__ __launch_bounds__(256) void k_evict_sums(EvictArgs a, float* sums) {
-  const int r = blockIdx.y, i = blockIdx.x * 256 + threadIdx.x;
+__global__ __launch_bounds__(64) void k_evict_sums(EvictArgs a, float* sums) {
+  const int r = blockIdx.y, i = (blockIdx.x * 64 + threadIdx.x) * 4;
   const int kv = tokens_of(a, r);
   if (i >= kv || kv <= stay_of(a, r, kv)) return;
   const int id = a.table[r * a.row + (i >> a.shift)];
-  double sum = 0.0;
+  double sum[4] = {0.0, 0.0, 0.0, 0.0};
   if ((uint32_t)id < (uint32_t)a.n_pages) {
     const float* s = a.scores + ((int64_t)id * a.Hkv << a.shift) + (i & ((1 << a.shift) - 1));
-    for (int h = 0; h < a.Hkv; ++h) sum += (double)s[(int64_t)h << a.shift];
+    constexpr int U = 8;
+    for (int h0 = 0; h0 < a.Hkv; h0 += U) {
+      float4 x[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) x[u] = h0 + u < a.Hkv ? *reinterpret_cast<const float4*>(s + ((int64_t)(h0 + u) << a.shift)) : float4{};
+#pragma unroll
+      for (int u = 0; u < U; ++u) { sum[0] += x[u].x; sum[1] += x[u].y; sum[2] += x[u].z; sum[3] += x[u].w; }
+    }
   }
-  sums[(int64_t)r * a.cap + i] = (float)sum;
+  *reinterpret_cast<float4*>(sums + (int64_t)r * a.cap + i) = make_float4((float)sum[0], (float)sum[1], (float)sum[2], (float)sum[3]);
 }
 
 // ---- who stays ------------------------------------------------------------------------------------
 // A workgroup a list.  The smallest score that stays is found digit by digit (11, 11 and 10 bits of the scores' order-preserving images)
-// from histograms in LDS; then every thread counts what it has above and at that score, and a scan of the counts gives the places.
-// A thread has consecutive tokens, so the list comes out in order and of equal scores the first ones stay.
-constexpr int kPick = 1024, kEach = 8, kChunk = kPick * kEach, kBins = 2048;
+// from histograms in LDS, until every score with the digits so far stays; then every thread counts what it has above and at that score, and
+// a scan of the counts gives the places.  A thread has consecutive tokens, so the list comes out in order and of equal scores the
+// first ones stay.
+constexpr int kEach = 8, kBins = 2048;
 
-// This thread's scores of chunk c, as order-preserving images (0: no candidate).
-__device__ inline void images(const EvictArgs& a, int r, int h, int lo, int hi, int chunk, uint32_t (&x)[kEach]) {
-  const int i0 = chunk * kChunk + threadIdx.x * kEach;
-#pragma unroll
-  for (int e = 0; e < kEach; ++e) x[e] = 0;
-  if (i0 >= hi || i0 + kEach <= lo) return;
+// A thread's scores of eight tokens from i0 on, as order-preserving images.  id: the page of i0.
+struct Images { uint32_t x[kEach]; };
+__device__ inline Images images(const EvictArgs& a, int r, int h, int i0, int hi, int id) {
   float4 v[2] = {};
-  if (a.sums) {
-    const float* s = a.sums + (int64_t)r * a.cap + i0;   // (cap: whole pages)
+  const bool page = (uint32_t)id < (uint32_t)a.n_pages;
+  if (i0 < hi && (a.sums || page)) {
+    const float* s = a.sums ? a.sums + (int64_t)r * a.cap + i0       // (cap: whole pages)
+                            : a.scores + (((int64_t)id * a.Hkv + h) << a.shift) + (i0 & ((1 << a.shift) - 1));
     v[0] = reinterpret_cast<const float4*>(s)[0];
     v[1] = reinterpret_cast<const float4*>(s)[1];
-  } else {
-    const int id = a.table[r * a.row + (i0 >> a.shift)];
-    if ((uint32_t)id < (uint32_t)a.n_pages) {
-      const float* s = a.scores + (((int64_t)id * a.Hkv + h) << a.shift) + (i0 & ((1 << a.shift) - 1));
-      v[0] = reinterpret_cast<const float4*>(s)[0];
-      v[1] = reinterpret_cast<const float4*>(s)[1];
-    }
   }
+  Images m;
 #pragma unroll
-  for (int e = 0; e < kEach; ++e) {
-    const float f = (&v[e >> 2].x)[e & 3];
-    const int i = i0 + e;
-    if (i >= lo && i < hi) x[e] = float_key(f + 0.f);    // (-0 ties with 0)
-  }
+  for (int e = 0; e < kEach; ++e) m.x[e] = float_key((&v[e >> 2].x)[e & 3] + 0.f);      // (-0 ties with 0)
+  return m;
 }
+__device__ inline int page_of(const EvictArgs& a, int r, int i) { return a.cols ? a.table[r * a.row + min(i >> a.shift, a.cols - 1)] : -1; }
 
-// Inclusive sum over the workgroup.
-__device__ inline int block_inclusive_sum(int v, int* waves) {
-  const int w = threadIdx.x >> 6;
+// Sum over the threads in front, this one's included; waves: a place of its own for each use between two others' barriers.
+template <int NW>
+__device__ inline int block_inclusive_sum(int v, int* waves, int& total) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   v = wave_inclusive_sum(v);
+  if (lane == 63) waves[w] = v;
   __syncthreads();
-  if ((threadIdx.x & 63) == 63) waves[w] = v;
-  __syncthreads();
-  int before = 0;
-  for (int u = 0; u < w; ++u) before += waves[u];
-  return v + before;
+  const int upto = wave_inclusive_sum(lane < NW ? waves[lane] : 0);
+  total = __builtin_amdgcn_readlane(upto, NW - 1);
+  return v + (w ? __builtin_amdgcn_readlane(upto, w - 1) : 0);
 }
 
-__global__ __launch_bounds__(kPick) void k_evict_pick(EvictArgs a) {
-  __shared__ int bins[kBins];
-  __shared__ int waves[kPick / 64];
-  __shared__ int s_digit, s_above, s_total;
-  const int r = blockIdx.y, h = blockIdx.x, tid = threadIdx.x;
-  const int kv = tokens_of(a, r), stay = stay_of(a, r, kv);
+// Pages that requests leave: where each one's go in the list of free ones.  A workgroup a request.
+template <int THREADS>
+__device__ void give_back(const EvictArgs& a, int r, int kv, int stay, int (*waves)[THREADS / 64]) {
+  const int tid = threadIdx.x;
+  if (tid == 0) a.new_len[r] = stay;
+  if (!a.free_pages && !a.n_freed) return;
+  const auto pages = [&](int n) { return (int)(((int64_t)n + (1 << a.shift) - 1) >> a.shift); };
+  int before = 0, all = 0;                                 // of the requests in front of this one, and of all
+  for (int q = tid; q < a.R; q += THREADS) {
+    const int n = tokens_of(a, q), gone = pages(n) - pages(stay_of(a, q, n));
+    all += gone;
+    if (q < r) before += gone;
+  }
+  int total_before, total;
+  block_inclusive_sum<THREADS / 64>(before, waves[0], total_before);
+  block_inclusive_sum<THREADS / 64>(all, waves[1], total);
+  if (r == 0 && tid == 0 && a.n_freed) *a.n_freed = total;
+  if (!a.free_pages) return;
+  const int first = pages(stay), last = pages(kv);
+  const int64_t at = (int64_t)*a.n_free + total_before - first;
+  for (int c = first + tid; c < last; c += THREADS)
+    if (at + c >= 0 && at + c < a.n_list) a.free_pages[at + c] = a.table[r * a.row + c];
+}
 
-  if (h == 0) {
-    if (tid == 0) a.new_len[r] = stay;
-    if (a.free_pages || a.n_freed) {
-      // pages that the requests in front of this one leave, and all of them
-      int before = 0, all = 0;
-      for (int q = tid; q < a.R; q += kPick) {
-        const int n = tokens_of(a, q), left = stay_of(a, q, n);
-        const int gone = (int)(((int64_t)n + (1 << a.shift) - 1) >> a.shift) - (int)(((int64_t)left + (1 << a.shift) - 1) >> a.shift);
-        all += gone;
-        if (q < r) before += gone;
-      }
-      before = block_inclusive_sum(before, waves);
-      if (tid == kPick - 1) s_total = before;
-      all = block_inclusive_sum(all, waves);
-      if (r == 0 && tid == kPick - 1 && a.n_freed) *a.n_freed = all;
-      const int64_t at = a.free_pages ? (int64_t)*a.n_free + s_total : 0;
-      const int first = (int)(((int64_t)stay + (1 << a.shift) - 1) >> a.shift), last = (int)(((int64_t)kv + (1 << a.shift) - 1) >> a.shift);
-      for (int c = first + tid; c < last; c += kPick)
-        if (a.free_pages && at + c - first >= 0 && at + c - first < a.n_list) a.free_pages[at + c - first] = a.table[r * a.row + c];
-    }
+// HELD: chunks of kEach tokens a thread that it holds; scores behind them are read again in every sweep.
+template <int THREADS, int HELD>
+__global__ __launch_bounds__(THREADS) void k_evict_pick(EvictArgs a) {
+  constexpr int NW = THREADS / 64, CHUNK = THREADS * kEach, PER = kBins / THREADS;
+  __shared__ __align__(16) int bins[3][kBins];
+  __shared__ int waves[5][NW];
+  __shared__ int s_digit[3], s_above[3], s_count[3];
+  const int r = blockIdx.y, h = blockIdx.x, tid = threadIdx.x;
+  int id[HELD];
+#pragma unroll
+  for (int c = 0; c < HELD; ++c) id[c] = page_of(a, r, c * CHUNK + tid * kEach);
+  const int kv = tokens_of(a, r), stay = stay_of(a, r, kv);
+  if (h == a.heads) {                                      // (beside the heads')
+    give_back<THREADS>(a, r, kv, stay, waves);
+    return;
   }
   int32_t* list = a.kept + ((int64_t)r * a.heads + h) * a.most;
   if (stay == kv) {
-    for (int i = tid; i < kv; i += kPick) list[i] = i;
+    for (int i = tid; i < kv; i += THREADS) list[i] = i;
     return;
   }
   const int recent = min(a.recent, stay), sinks = min(a.sinks, stay - recent);
   const int lo = sinks, hi = kv - recent, need = stay - recent - sinks;     // candidates, and how many of them stay
-  const int chunks = (hi + kChunk - 1) / kChunk;
-  uint32_t x[kEach];
-  images(a, r, h, lo, hi, 0, x);
-
-  // the least image that stays (`least`) and how many of its equals do (`ties`)
-  uint32_t least = 0xffffffffu;
-  int ties = 0;
-  if (need > 0) {
-    uint32_t prefix = 0;
-    int rest = need;
-    int shift = 32;
-    for (int pass = 0; pass < 3; ++pass) {
-      const int bits = pass < 2 ? 11 : 10, above_shift = shift;
-      shift -= bits;
-      for (int b = tid; b < kBins; b += kPick) bins[b] = 0;
-      __syncthreads();
-      for (int c = 0; c < chunks; ++c) {
-        uint32_t y[kEach];
-        if (c == 0) {
+  const int chunks = (int)(((int64_t)hi + CHUNK - 1) / CHUNK);
+  for (int i = tid; i < sinks; i += THREADS) list[i] = i;
+  for (int i = tid; i < recent; i += THREADS) list[stay - recent + i] = kv - recent + i;
+  if (need == 0) return;
+  Images held[HELD];
 #pragma unroll
-          for (int e = 0; e < kEach; ++e) y[e] = x[e];
-        } else {
-          images(a, r, h, lo, hi, c, y);
-        }
-        const int i0 = c * kChunk + tid * kEach;
+  for (int c = 0; c < HELD; ++c) held[c] = images(a, r, h, c * CHUNK + tid * kEach, hi, id[c]);
+  // f(first token, images) of every chunk
+  const auto sweep = [&](auto&& f) {
 #pragma unroll
-        for (int e = 0; e < kEach; ++e) {
-          const bool in = i0 + e >= lo && i0 + e < hi && (pass == 0 || (y[e] >> above_shift) == prefix);
-          if (in) atomicAdd(&bins[(y[e] >> shift) & ((1u << bits) - 1)], 1);
-        }
-      }
-      __syncthreads();
-      // bins from the top: thread t has the two below the 2 t largest
-      const int n = 1 << bits, top = n - 1 - 2 * tid;
-      const int b0 = top >= 1 ? bins[top] : 0, b1 = top >= 1 ? bins[top - 1] : 0;
-      const int upto = block_inclusive_sum(b0 + b1, waves), before = upto - b0 - b1;
-      if (before < rest && upto >= rest) {
-        const bool second = before + b0 < rest;
-        s_digit = second ? top - 1 : top;
-        s_above = second ? before + b0 : before;
-      }
-      __syncthreads();
-      prefix = pass == 0 ? (uint32_t)s_digit : (prefix << bits) | (uint32_t)s_digit;
-      rest -= s_above;
-      __syncthreads();
+    for (int c = 0; c < HELD; ++c)
+      if (c < chunks) f(c * CHUNK + tid * kEach, held[c]);
+    for (int c = HELD; c < chunks; ++c) {
+      const int i0 = c * CHUNK + tid * kEach;
+      const Images m = images(a, r, h, i0, hi, page_of(a, r, i0));
+      f(i0, m);
     }
-    least = prefix;
-    ties = rest;
+  };
+  const auto candidate = [&](int i) { return i >= lo && i < hi; };
+
+#pragma unroll
+  for (int p = 0; p < 3; ++p)
+    for (int b = tid; b < kBins; b += THREADS) bins[p][b] = 0;
+  __syncthreads();
+  // What is above `least` stays, and the first `ties` of its equals.
+  uint32_t prefix = 0, least = 0;
+  int ties = need;
+#pragma unroll
+  for (int pass = 0; pass < 3; ++pass) {
+    const int bits = pass < 2 ? 11 : 10, shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+    sweep([&](int i0, const Images& m) {
+#pragma unroll
+      for (int e = 0; e < kEach; ++e)
+        if (candidate(i0 + e) && (pass == 0 || m.x[e] >> (shift + bits) == prefix)) atomicAdd(&bins[pass][(m.x[e] >> shift) & ((1 << bits) - 1)], 1);
+    });
+    __syncthreads();
+    // from the top: thread t has the PER bins below the PER t largest
+    const int top = (1 << bits) - 1 - PER * tid;
+    int n[PER], sum = 0, all;
+#pragma unroll
+    for (int b = 0; b < PER; ++b) {
+      n[b] = top - b >= 0 ? bins[pass][top - b] : 0;
+      sum += n[b];
+    }
+    int above = block_inclusive_sum<NW>(sum, waves[pass], all) - sum;
+    if (above < ties && above + sum >= ties) {
+      int b = 0;
+#pragma unroll
+      for (int v = 0; v < PER - 1; ++v)
+        if (b == v && above + n[v] < ties) { above += n[v]; ++b; }
+      int count = 0;
+#pragma unroll
+      for (int v = 0; v < PER; ++v) count = b == v ? n[v] : count;
+      s_digit[pass] = top - b;
+      s_above[pass] = above;
+      s_count[pass] = count;
+    }
+    __syncthreads();
+    prefix = pass == 0 ? (uint32_t)s_digit[pass] : prefix << bits | (uint32_t)s_digit[pass];
+    ties -= s_above[pass];
+    least = prefix << shift;
+    if (pass < 2 && s_count[pass] == ties && least > 0) {  // (all of them stay)
+      --least;
+      ties = 0;
+      break;
+    }
   }
 
-  // the list: first tokens, those of the candidates that stay, newest tokens
-  for (int i = tid; i < sinks; i += kPick) list[i] = i;
-  for (int i = tid; i < recent; i += kPick) list[stay - recent + i] = kv - recent + i;
-  if (need == 0) return;
-  int placed = sinks, equal = 0;                           // so far, of the chunks before
-  for (int c = 0; c < chunks; ++c) {
-    if (c) images(a, r, h, lo, hi, c, x);
-    const int i0 = c * kChunk + tid * kEach;
+  int placed = sinks, equal = 0;                           // of the chunks before
+  sweep([&](int i0, const Images& m) {
     int over = 0, same = 0;
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
-      const bool in = i0 + e >= lo && i0 + e < hi;
-      over += in && x[e] > least;
-      same += in && x[e] == least;
+      over += candidate(i0 + e) && m.x[e] > least;
+      same += candidate(i0 + e) && m.x[e] == least;
     }
-    const int same_upto = block_inclusive_sum(same, waves);
-    const int first_same = equal + same_upto - same;       // equals in front of this thread's
-    const int mine = over + min(max(ties - first_same, 0), same);
-    const int upto = block_inclusive_sum(mine, waves);
-    int at = placed + upto - mine, left = max(ties - first_same, 0);
+    int all_same, all_mine;
+    int left = max(ties - equal - (block_inclusive_sum<NW>(same, waves[3], all_same) - same), 0);      // equals that stay from this thread's first on
+    const int mine = over + min(left, same);
+    int at = placed + block_inclusive_sum<NW>(mine, waves[4], all_mine) - mine;
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
-      const bool in = i0 + e >= lo && i0 + e < hi;
-      const bool tie = in && x[e] == least && left > 0;
+      const bool tie = candidate(i0 + e) && m.x[e] == least && left > 0;
       left -= tie;
-      if (tie || (in && x[e] > least)) list[at++] = i0 + e;
+      if (tie || (candidate(i0 + e) && m.x[e] > least)) list[at++] = i0 + e;
     }
-    if (tid == kPick - 1) { s_digit = upto; s_above = same_upto; }
-    __syncthreads();
-    placed += s_digit;
-    equal += s_above;
-    __syncthreads();
-  }
+    equal += all_same;
+    placed += all_mine;
+  });
 }
 
 // ---- the rows -------------------------------------------------------------------------------------
 typedef uint32_t piece16 __attribute__((ext_vector_type(4)));
 
-// Where token i of request r lies, in a pool: page, row; page < 0: nowhere.
-__device__ inline int page_at(const EvictArgs& a, int r, int i) {
+// The slot of token i of request r (< 0: none).
+__device__ inline int slot_at(const EvictArgs& a, int r, int i) {
   const int id = a.table[r * a.row + (i >> a.shift)];
-  return (uint32_t)id < (uint32_t)a.n_pages ? id : -1;
+  return (uint32_t)id < (uint32_t)a.n_pages ? id << a.shift | (i & ((1 << a.shift) - 1)) : -1;
 }
 
-// A wave takes `slice` bytes of every row of a (request, head, tensor), the waves of a workgroup the slices side by side.
-constexpr int kMove = 8;                                  // rows a lane has on their way
-__global__ __launch_bounds__(512) void k_evict_move(EvictArgs a) {
-  const int r = blockIdx.z, lane = threadIdx.x & 63;
+// A workgroup takes `slice` bytes of every row of a (request, head, tensor), a row's by consecutive threads, kMove rows a thread at a time:
+// all of them are read before the first is stored.  Where the next ones lie is looked up meanwhile.
+constexpr int kMove = 4, kMoveThreads = 1024;
+struct Move { int src, dst; };                           // slots (src < 0: zeros, dst < 0: nothing to do)
+
+__global__ __launch_bounds__(kMoveThreads, 4) void k_evict_move(EvictArgs a) {
+  const int r = blockIdx.z;
   const int kv = tokens_of(a, r), stay = stay_of(a, r, kv);
   if (stay == kv) return;
-  const int head = blockIdx.y;                           // keys, values, scores of every head
-  const int what = head / a.Hkv, h = head - what * a.Hkv;
+  const int what = blockIdx.y / a.Hkv, h = blockIdx.y - what * a.Hkv;          // keys, values, scores of every head
+  if (what == 2 && blockIdx.x) return;
   const int32_t* list = a.kept + ((int64_t)r * a.heads + (a.heads > 1 ? h : 0)) * a.most;
-  const int inside = (1 << a.shift) - 1;
+  const int inside = (1 << a.shift) - 1, lanes = what == 2 ? 0 : a.lanes;
+  const int per = kMoveThreads >> lanes, first = threadIdx.x >> lanes;         // rows of a transfer
+  // Three steps of the way are under way at a time: the list's entries, their pages, the rows.
+  int next[kMove];
+  Move m[kMove], ahead[kMove];
+  const auto entries = [&](int i0) {
+#pragma unroll
+    for (int u = 0; u < kMove; ++u) {
+      const int i = i0 + per * u + first;
+      next[u] = i < stay ? list[i] : i;
+    }
+  };
+  const auto find = [&](int i0, Move (&x)[kMove]) {
+#pragma unroll
+    for (int u = 0; u < kMove; ++u) {
+      const int i = i0 + per * u + first;
+      x[u] = {-1, -1};
+      if (next[u] != i) x[u] = {slot_at(a, r, next[u]), slot_at(a, r, i)};
+    }
+  };
+  const int step = per * kMove;
+  entries(0);
+  find(0, m);
+  entries(step);
   if (what == 2) {
-    if (blockIdx.x || threadIdx.x >= 64) return;
-    for (int i0 = 0; i0 < stay; i0 += 64 * kMove) {
+    const auto at = [&](int slot) { return a.scores + (((int64_t)(slot >> a.shift) * a.Hkv + h) << a.shift) + (slot & inside); };
+    for (int i0 = 0; i0 < stay; i0 += step) {
       float x[kMove];
-      float* to[kMove];
+      find(i0 + step, ahead);
+#pragma unroll
+      for (int u = 0; u < kMove; ++u) x[u] = m[u].src >= 0 ? *at(m[u].src) : 0.f;
+      entries(i0 + 2 * step);
+      wait_vmem<0>();
+      __syncthreads();
 #pragma unroll
       for (int u = 0; u < kMove; ++u) {
-        const int i = i0 + 64 * u + lane;
-        to[u] = nullptr;
-        if (i < stay) {
-          const int from = list[i], src = page_at(a, r, from), dst = page_at(a, r, i);
-          x[u] = src >= 0 ? a.scores[(((int64_t)src * a.Hkv + h) << a.shift) + (from & inside)] : 0.f;
-          if (dst >= 0 && from != i) to[u] = a.scores + (((int64_t)dst * a.Hkv + h) << a.shift) + (i & inside);
-        }
+        if (m[u].dst >= 0) *at(m[u].dst) = x[u];
+        m[u] = ahead[u];
       }
-      wait_vmem<0>();
-#pragma unroll
-      for (int u = 0; u < kMove; ++u)
-        if (to[u]) *to[u] = x[u];
     }
     return;
   }
-  const int w = blockIdx.x * (blockDim.x >> 6) + (threadIdx.x >> 6);
-  if (w * a.slice >= a.rowb) return;
-  const int per = 64 >> a.lanes;                          // rows of a transfer
-  const int64_t c = w * a.slice + (lane & ((1 << a.lanes) - 1)) * 16 + h * a.sH[what];
-  const uint8_t* from_pool = a.from[what] + c;
-  uint8_t* to_pool = a.to[what] + c;
+  uint8_t* pool = a.pool[what] + blockIdx.x * a.slice + (threadIdx.x & ((1 << lanes) - 1)) * 16 + h * a.sH[what];
   const int64_t sB = a.sB[what], sL = a.sL[what];
-  for (int i0 = 0; i0 < stay; i0 += per * kMove) {
+  const auto at = [&](int slot) { return reinterpret_cast<piece16*>(pool + (slot >> a.shift) * sB + (slot & inside) * sL); };
+  for (int i0 = 0; i0 < stay; i0 += step) {
     piece16 x[kMove];
-    uint8_t* to[kMove];
+    find(i0 + step, ahead);
 #pragma unroll
     for (int u = 0; u < kMove; ++u) {
-      const int i = i0 + per * u + (lane >> a.lanes);
-      to[u] = nullptr;
       x[u] = piece16{0, 0, 0, 0};
-      if (i < stay) {
-        const int from = list[i], src = page_at(a, r, from), dst = page_at(a, r, i);
-        if (from != i && dst >= 0) {
-          to[u] = to_pool + dst * sB + (i & inside) * sL;
-          if (src >= 0) x[u] = *reinterpret_cast<const piece16*>(from_pool + src * sB + (from & inside) * sL);
-        }
-      }
+      if (m[u].src >= 0) x[u] = *at(m[u].src);
     }
+    entries(i0 + 2 * step);
     wait_vmem<0>();
+    __syncthreads();
 #pragma unroll
-    for (int u = 0; u < kMove; ++u)
-      if (to[u]) *reinterpret_cast<piece16*>(to[u]) = x[u];
+    for (int u = 0; u < kMove; ++u) {
+      if (m[u].dst >= 0) *at(m[u].dst) = x[u];
+      m[u] = ahead[u];
+    }
   }
 }
 
@@ -329,7 +359,7 @@ extern "C" int zc_paged_evict(const zc_tensor4* k_pages, const zc_tensor4* v_pag
   EvictArgs a;
   const zc_tensor4* pools[2] = {k_pages, v_pages};
   for (int i = 0; i < 2; ++i) {
-    a.from[i] = a.to[i] = (uint8_t*)pools[i]->ptr;
+    a.pool[i] = (uint8_t*)pools[i]->ptr;
     a.sB[i] = pools[i]->sB * eb; a.sH[i] = pools[i]->sH * eb; a.sL[i] = pools[i]->sL * eb;
   }
   a.scores = scores;
@@ -340,17 +370,24 @@ extern "C" int zc_paged_evict(const zc_tensor4* k_pages, const zc_tensor4* v_pag
   a.new_len = new_len; a.kept = kept; a.free_pages = free_pages; a.n_freed = n_freed; a.n_free = n_free; a.n_list = n_list;
   a.sums = nullptr;
   if (need) {
-    hipLaunchKernelGGL(k_evict_sums, dim3((unsigned)ceil_div64(a.cap, 256), (unsigned)R), dim3(256), 0, st, a, (float*)ws);
+    hipLaunchKernelGGL(k_evict_sums, dim3((unsigned)ceil_div64(a.cap, 256), (unsigned)R), dim3(64), 0, st, a, (float*)ws);
     ZC_LAUNCH_CHECK();
     a.sums = (const float*)ws;
   }
-  hipLaunchKernelGGL(k_evict_pick, dim3((unsigned)a.heads, (unsigned)R), dim3(kPick), 0, st, a);
+  const dim3 lists((unsigned)a.heads + 1, (unsigned)R);
+  if (a.cap <= 512 * kEach) hipLaunchKernelGGL((k_evict_pick<512, 1>), lists, dim3(512), 0, st, a);
+  else if (a.cap <= 1024 * kEach) hipLaunchKernelGGL((k_evict_pick<1024, 1>), lists, dim3(1024), 0, st, a);
+  else hipLaunchKernelGGL((k_evict_pick<1024, 2>), lists, dim3(1024), 0, st, a);
   ZC_LAUNCH_CHECK();
   a.rowb = (int)(k_pages->D * eb);
-  a.lanes = 2;
-  a.slice = 16 << a.lanes;
-  const int slices = a.rowb / a.slice, waves = slices < 8 ? slices : 8;
-  hipLaunchKernelGGL(k_evict_move, dim3((unsigned)ceil_div(slices, waves), (unsigned)(3 * H), (unsigned)R), dim3(64 * waves), 0, st, a);
+  const int64_t chains = R * H * 2;
+  // Rows are cut where that fills the chip and saves steps of the way through the list.  us of whole rows, of 128, 64 and 32 bytes, 8 heads, 256 bytes
+  // a row: one request of 4096, 1638 stay 39.0, 26.0, 22.8 and 21.9; 4 of up to 400, 256 stay 15.7, 15.7, 17.8 and 20.2; 15 of up to 8192, 2048 stay
+  // 79 whole, 81 of 128.
+  a.slice = a.rowb;
+  while (a.slice > 64 && chains * (a.rowb / a.slice) < 256 && most > kMove * kMoveThreads * 16 / a.slice) a.slice /= 2;
+  a.lanes = __builtin_ctz(a.slice / 16);
+  hipLaunchKernelGGL(k_evict_move, dim3((unsigned)(a.rowb / a.slice), (unsigned)(3 * H), (unsigned)R), dim3(kMoveThreads), 0, st, a);
   ZC_LAUNCH_CHECK();
   return ZC_OK;
 }
