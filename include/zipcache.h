@@ -413,6 +413,20 @@ int zc_paged_attention(const zc_tensor4* q, const zc_tensor4* k_pages, const zc_
                        int32_t window, int32_t sinks, float sm_scale, const zc_tensor4* out, float* lse,
                        void* ws, size_t ws_bytes, void* stream);
 
+/* ---- the weight that cached tokens gather (Eq. 7 over the pages, step by step) --------------------
+ * For every request with new tokens, every KV head h and every token i < kv_len[r] of it
+ *   scores[h, i] = (i < kv_len[r] - nq ? decay * scores[h, i] : 0) + sum over rows (new token, query head of h) that see i of exp(logit - lse[row])
+ * at the token's place in the pages: scores is device float [N, Hkv, page], 16-byte aligned.  A step's new tokens start from 0,
+ * whatever their places held, so nothing has to be cleared when a page is taken.  Other places are left as they are, a request's without new tokens too.
+ * q, q_start, kv_len, window, sinks, sm_scale and the rows' positions as in zc_paged_attention, lse (device float [Hq, T]) as it returns
+ * it, or zc_paged_shared_attention, whose softmax also went over a prefix.  A row of lse = -inf weighs nothing.  decay is 0 (what was there is not read) to 1.
+ * fp32 tensors are multiplied on the fp32 matrix pipes; weights and sums are fp32.  Deterministic, and a token's score depends on its own
+ * request's rows only.  A request's pages must be its own (not another's, not twice in its row); a token without a page has no score.
+ * T and R may be 0.  Needs no workspace.  R < 2^24, T * Hq < 2^31, Hq / Hkv <= 4096. */
+int zc_paged_scores(const zc_tensor4* q, const zc_tensor4* k_pages, const int32_t* block_table, int64_t row_stride, int64_t max_blocks,
+                    const int32_t* q_start, const int32_t* kv_len, int64_t R, int32_t window, int32_t sinks, float sm_scale,
+                    const float* lse, float decay, float* scores, void* stream);
+
 /* ---- eviction by gathered weight -----------------------------------------------------------------
  * Request r keeps min(kv_len[r], keep[r], most) of its kv_len[r] tokens (keep: device int32 [R], negative: 0; most: what the
  * host knows of it): the `recent` newest; of what is left the `sinks` first; of the others those of the largest scores,

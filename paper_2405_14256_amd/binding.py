@@ -118,6 +118,8 @@ def load() -> C.CDLL:
     lib.zc_paged_attention_workspace.argtypes = [I64, I64, I64, I64, I64]
     lib.zc_paged_attention.restype = C.c_int
     lib.zc_paged_attention.argtypes = [T4, T4, T4, P, I64, I64, P, P, I64, I32, I32, F, T4, P, P, SZ, P]
+    lib.zc_paged_scores.restype = C.c_int
+    lib.zc_paged_scores.argtypes = [T4, T4, P, I64, I64, P, P, I64, I32, I32, F, P, F, P, P]
     lib.zc_paged_evict_workspace.restype = SZ
     lib.zc_paged_evict_workspace.argtypes = [I64, I64, I64, I32]
     lib.zc_paged_evict.restype = C.c_int
@@ -404,6 +406,15 @@ def zc_paged_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Te
         lse = torch.empty(Hq, T, dtype=torch.float32, device=q.device)
     _check("zc_paged_attention", host.paged_attention(q, k_pages, v_pages, block_table, q_start, kv_len, window, sinks, sm_scale, out, lse))
     return out, lse
+
+
+def zc_paged_scores(q: torch.Tensor, k_pages: torch.Tensor, block_table: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor,
+                    lse: torch.Tensor, scores: torch.Tensor, window: int = 0, sinks: int = 0, sm_scale: float = 0.0,
+                    decay: float = 1.0) -> torch.Tensor:
+    """Adds a step's attention weights to the scores [N, Hkv, page] of the tokens they went to; q, lse [Hq, T] as in zc_paged_attention.
+    A step's new tokens start from 0 (whatever their places held), the others from decay times what they had."""
+    _check("zc_paged_scores", _native().paged_scores(q, k_pages, block_table, q_start, kv_len, lse, scores, window, sinks, sm_scale, decay))
+    return scores
 
 
 def zc_paged_evict(k_pages: torch.Tensor, v_pages: torch.Tensor, scores: torch.Tensor, block_table: torch.Tensor, kv_len: torch.Tensor,

@@ -31,13 +31,13 @@ namespace {
 // ---- entry points, in the order of kNames ---------------------------------------------------
 enum Fn {
   kProbe, kAccumulated, kPrefill, kSelect, kQuantize, kQuantizeKV, kDecode, kDecodeStatic, kProbs, kRows, kDequantize,
-  kPagedTables, kPagedStore, kPagedLoad, kPagedAttention, kPagedEvict,
+  kPagedTables, kPagedStore, kPagedLoad, kPagedAttention, kPagedScores, kPagedEvict,
   kProbeWs, kQuantizeWs, kQuantizeKVWs, kDecodeWs, kPagedAttentionWs, kPagedEvictWs, kFnCount
 };
 const char* const kNames[kFnCount] = {
     "zc_probe_saliency", "zc_probe_accumulated", "zc_prefill_attention", "zc_select_salient", "zc_quantize_pack",
     "zc_quantize_pack_kv", "zc_decode_attention", "zc_decode_attention_static", "zc_decode_probs", "zc_rows_saliency",
-    "zc_dequantize_cache", "zc_paged_tables", "zc_paged_store", "zc_paged_load", "zc_paged_attention", "zc_paged_evict",
+    "zc_dequantize_cache", "zc_paged_tables", "zc_paged_store", "zc_paged_load", "zc_paged_attention", "zc_paged_scores", "zc_paged_evict",
     "zc_probe_saliency_workspace", "zc_quantize_pack_workspace", "zc_quantize_pack_kv_workspace", "zc_decode_attention_workspace",
     "zc_paged_attention_workspace", "zc_paged_evict_workspace"};
 void* g_fn[kFnCount];
@@ -558,6 +558,26 @@ float* scores_of(PyObject* o, const zc_tensor4& pages) {
   return static_cast<float*>(t.data_ptr());
 }
 
+// (q, k_pages, block_table, q_start, kv_len, lse, scores, window, sinks, sm_scale, decay)
+PyObject* paged_scores(PyObject*, Args a, Py_ssize_t n) {
+  return guarded(kPagedScores, n, 11, [&]() -> int {
+    g_device = -1;
+    const zc_tensor4 q = tokens(a[0], "q"), kp = pool(a[1], "k_pages");
+    const Table t = table_of(a[2]);
+    const auto *start = ints(a[3], "q_start", t.R + 1), *kv = ints(a[4], "kv_len", t.R);
+    const at::Tensor& l = tensor_of(a[5]);
+    on_device(l, "lse");
+    if (l.scalar_type() != at::kFloat || !l.is_contiguous() || l.numel() != q.H * q.L) refuse("lse", "must be a contiguous float32 [Hq, T] tensor");
+    const auto* lse = static_cast<const float*>(l.data_ptr());
+    float* scores = scores_of(a[6], kp);
+    const int32_t window = int32_of(a[7]), sinks = int32_of(a[8]);
+    const float scale = float_of(a[9]), decay = float_of(a[10]);
+    const hipStream_t st = current_stream();
+    const auto fn = ZC_FN(kPagedScores, zc_paged_scores);
+    return unlocked([&] { return fn(&q, &kp, t.ptr, t.row, t.cols, start, kv, t.R, window, sinks, scale, lse, decay, scores, st); });
+  });
+}
+
 // (k_pages, v_pages, scores, block_table, kv_len, keep, most, sinks, recent, together, new_len, kept, free_pages, n_free, n_freed)
 PyObject* paged_evict(PyObject*, Args a, Py_ssize_t n) {
   return guarded(kPagedEvict, n, 15, [&]() -> int {
@@ -633,6 +653,7 @@ PyMethodDef kMethods[] = {
     ZC_METHOD("paged_store", paged_store),
     ZC_METHOD("paged_load", paged_load),
     ZC_METHOD("paged_attention", paged_attention),
+    ZC_METHOD("paged_scores", paged_scores),
     ZC_METHOD("paged_evict", paged_evict),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_zc_host", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};

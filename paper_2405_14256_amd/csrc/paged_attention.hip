@@ -19,8 +19,8 @@
 #include <stdint.h>
 #include <type_traits>
 
-#include "mfma_tiles.hpp"
 #include "paged_args.hpp"
+#include "paged_keys.hpp"
 
 namespace zc {
 
@@ -178,25 +178,10 @@ __device__ inline bool find_unit(const PagedArgs& a, int u, Unit& x) {
 __device__ inline int tile_of(const Unit& x, int t) { return t < x.sink_tiles ? t : x.first + t - x.sink_tiles; }
 __device__ inline int unit_of_grid() { return blockIdx.y + 65535 * blockIdx.z; }
 
-// The page of 16 keys from key0 on (past the table: any, no key is read).
-__device__ inline int page_of(const PagedArgs& a, const Unit& x, int key0) {
-  typedef __attribute__((address_space(4))) const int32_t* scalar;
-  return ((scalar)(uintptr_t)(a.table + x.r * a.row))[min(key0 >> a.shift, a.cols - 1)];
-}
-// Of 16 keys from key0 on, how many a unit reads: none of a missing page, of those that no row's window reaches, from `end` on.
-// What is not read arrives as zeros.
-__device__ inline int keys_read(const PagedArgs& a, const Unit& x, int end, int key0, int id) {
-  int n = max(end - key0, 0);
-  asm("" : "+s"(n));                                       // (both bounds at once would be a vector instruction, and what follows too)
-  n = min(n, 16);
-  if ((uint32_t)id >= (uint32_t)a.n_pages) n = 0;
-  if ((uint32_t)(key0 - a.sinks) < x.behind) n = 0;
-  return n;
-}
-// Where they are (of no keys: anywhere, nothing is read).
+__device__ inline int page_of(const PagedArgs& a, const Unit& x, int key0) { return page_of(a.table + x.r * a.row, a.cols, a.shift, key0); }
+__device__ inline int keys_read(const PagedArgs& a, const Unit& x, int end, int key0, int id) { return keys_read(a.n_pages, a.sinks, x.behind, end, key0, id); }
 __device__ inline __amdgpu_buffer_rsrc_t keys_at(const PagedArgs& a, const uint8_t* head, uint32_t sB, uint32_t row, int key0, int id, int n) {
-  const uint64_t at = (uint64_t)(uint32_t)id * sB + ((uint32_t)key0 & ((1u << a.shift) - 1)) * row;
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(head + at), 0, n * row, kBufFlags);
+  return keys_at(a.shift, head, sB, row, key0, id, n);
 }
 // The blocks of 32 keys that every row from position p0 to p1 sees whole: those from `low` on, `span` of them by their first key, and
 // those whose first key is below `sink`.
@@ -212,26 +197,6 @@ struct Seen {
   // Blocks of 32 + more keys.
   __device__ bool whole(int key0, int more = 0) const { return (uint32_t)(key0 - low) < (uint32_t)max((int)span - more, 0) || key0 < sink - more; }
 };
-
-// 16 keys to LDS in N transfers of 1024 bytes, to consecutive places.  The descriptor changes with every page, and the compiler may have
-// brought a part of it (or the place) from a vector register the instruction before: a memory instruction must not read
-// such a scalar register for five wait states, and does not see that it does inside an assembly block.
-#define ZC_KEYS_NEXT(v) "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tbuffer_load_dwordx4 " v ", %1, 0 offen lds\n\t"
-#define ZC_KEYS_FIRST "s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %1, 0 offen lds\n\t"
-template <int N>
-__device__ inline void move_keys(uint32_t lds, __amdgpu_buffer_rsrc_t rs, const int (&v)[N]) {
-  static_assert(N == 2 || N == 4 || N == 8, "16 rows of 128, 256 or 512 bytes");
-  if constexpr (N == 2)
-    asm volatile(ZC_KEYS_FIRST ZC_KEYS_NEXT("%3") :: "s"(lds), "s"(rs), "v"(v[0]), "v"(v[1]) : "memory", "scc");
-  else if constexpr (N == 4)
-    asm volatile(ZC_KEYS_FIRST ZC_KEYS_NEXT("%3") ZC_KEYS_NEXT("%4") ZC_KEYS_NEXT("%5")
-                 :: "s"(lds), "s"(rs), "v"(v[0]), "v"(v[1]), "v"(v[2]), "v"(v[3]) : "memory", "scc");
-  else
-    asm volatile(ZC_KEYS_FIRST ZC_KEYS_NEXT("%3") ZC_KEYS_NEXT("%4") ZC_KEYS_NEXT("%5") ZC_KEYS_NEXT("%6") ZC_KEYS_NEXT("%7") ZC_KEYS_NEXT("%8") ZC_KEYS_NEXT("%9")
-                 :: "s"(lds), "s"(rs), "v"(v[0]), "v"(v[1]), "v"(v[2]), "v"(v[3]), "v"(v[4]), "v"(v[5]), "v"(v[6]), "v"(v[7]) : "memory", "scc");
-}
-#undef ZC_KEYS_NEXT
-#undef ZC_KEYS_FIRST
 
 // Chunk slot permutation of a V row of 16-bit types: the transposing load reads 64 bytes of four consecutive keys per
 // half-wave; these land in different banks.

@@ -1,0 +1,418 @@
+// zc_paged_scores: the attention weight that every cached token gathers, carried on from step to step (Eq. 7 over the pages).
+//
+// The rows of a request and a KV head are its new tokens times the G query heads of the group, token after token.  Given their
+// normalisers the weight of a token is one sum over rows of exp(logit - lse), so a sweep over the keys is all there is:
+//   logits  D[row][key] = sum_c Q[row][c] K[key][c]        (A = Q rows, B = K block)
+// puts a key in a lane (column lane & 31) and its rows in the accumulators: the sum over rows is lane-local.  No result is split
+// over workgroups, so there are no partial sums, and the order of every sum is fixed.  Logits, weights and sums are fp32.
+//
+// A unit of work is a range of a request's key tiles.  As for the paged attention the host knows neither lengths nor how rows are spread over
+// requests: every wave finds its unit from the lengths.
+#include <limits.h>
+
+#include "paged_args.hpp"
+#include "paged_keys.hpp"
+
+namespace zc {
+
+struct ScoreArgs {
+  const uint8_t *q, *k;
+  int64_t q_sH, q_sT, k_sH;                     // bytes
+  uint32_t k_sB, k_row;                         // bytes from a page, a token to the next
+  const int32_t *table, *q_start, *kv_len;
+  int64_t row;                                  // of the table, in entries
+  int cols, shift, n_pages, cap;                // blocks of the table; page size; pages; tokens a row of the table has room for
+  int R, T, Hkv, G, window, sinks;
+  float scale_log2, decay;
+  const float* lse;                             // [Hq, T]
+  float* scores;                                // [page][head][row]
+  float target;                                 // units a head's keys are split into, about
+  uint32_t over_G;                              // ceil(2^32 / G)
+};
+
+// A request's keys go in tiles of 128: of up to 32 rows a wave takes every fourth 32 keys, of more the four waves share a tile.
+constexpr int kScoreTile = 128;
+
+struct Span {
+  int r, qs, nq, kv;            // request, its first row, new tokens, tokens
+  int first, sink_tiles;        // tile t is t of the first sink_tiles, then first + t - sink_tiles
+  int t_lo, t_hi;               // tiles of this unit
+  uint32_t behind;              // 16 keys from key0 on are behind every window if key0 - sinks, without sign, is less than this
+};
+__device__ inline int tile_of(const Span& x, int t) { return t < x.sink_tiles ? t : x.first + t - x.sink_tiles; }
+
+// Unit u of a head; false: there are fewer.
+__device__ inline bool find_span(const ScoreArgs& a, int u, Span& x) {
+  const int lane = threadIdx.x & 63;
+  struct Part { int qs, nq, kv, first, sink_tiles, tiles, passes; };           // passes: of 64 rows over a tile
+  const auto part = [&](int r) {
+    Part p = {0, 0, 0, 0, 0, 0, 1};
+    if (r >= a.R) return p;
+    const int s = a.q_start[r], e = a.q_start[r + 1], kv = a.kv_len[r];
+    p.qs = min(max(s, 0), a.T);
+    p.nq = max(min(e, a.T) - p.qs, 0);
+    p.kv = min(max(kv, 0), a.cap);
+    // (weights that fade change every token's score, seen or not)
+    const int p0 = max(p.kv - p.nq, 0), low = a.window && a.decay == 1.f ? max(0, p0 - a.window + 1) : 0;
+    p.first = low / kScoreTile;
+    p.sink_tiles = min((min(a.sinks, low) + kScoreTile - 1) / kScoreTile, p.first);
+    if (p.nq) p.tiles = p.sink_tiles + (p.kv + kScoreTile - 1) / kScoreTile - p.first;
+    p.passes = (int)(((int64_t)p.nq * a.G + 63) / 64);
+    return p;
+  };
+  const Part head = part(lane);
+  float all = (float)head.tiles * (float)head.passes;
+  for (int r0 = 64; r0 < a.R; r0 += 64) {
+    const Part p = part(r0 + lane);
+    all += (float)p.tiles * (float)p.passes;
+  }
+  const float per = wave_sum(all) / a.target;                                  // work of a unit
+  int units = 0;
+  for (int r0 = 0; r0 < a.R; r0 += 64) {
+    const Part p = r0 ? part(r0 + lane) : head;
+    const int each = max((int)fminf(ceilf(per / (float)max(p.passes, 1)), 1e9f), 1);     // tiles
+    const int parts = p.tiles ? (int)((uint32_t)(p.tiles - 1) / (uint32_t)each) + 1 : 0;
+    const int cu = wave_inclusive_sum(parts);
+    const uint64_t here = __builtin_amdgcn_ballot_w64(u < units + cu);
+    if (here) {
+      const int l = __builtin_ctzll(here);
+      const auto of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
+      const int n = of(parts), b = u - (units + of(cu) - n), tiles = of(p.tiles);
+      x.r = r0 + l;
+      x.qs = of(p.qs); x.nq = of(p.nq); x.kv = of(p.kv);
+      x.first = of(p.first); x.sink_tiles = of(p.sink_tiles);
+      const int q = (int)((uint32_t)tiles / (uint32_t)n), rem = tiles - q * n;
+      x.t_lo = b * q + min(b, rem);
+      x.t_hi = x.t_lo + q + (b < rem ? 1 : 0);
+      const int far = max(x.kv - x.nq, 0) - a.window - 14;
+      x.behind = a.window && far > a.sinks ? far - a.sinks : 0;
+      return true;
+    }
+    units += __builtin_amdgcn_readlane(cu, 63);
+  }
+  return false;
+}
+
+// Row v (of g0 on) of a unit: its token after j0, and head.
+__device__ inline int2 row_of(const ScoreArgs& a, int j0, int v) {
+  const int j = a.G == 1 ? v : (int)__umulhi((uint32_t)v, a.over_G);           // (exact while v G < 2^32)
+  return make_int2(j0 + j, v - j * a.G);
+}
+
+// A row's normaliser in log2 units; of one that sees nothing (-inf) so that its weights are 0.
+__device__ inline float norm_of(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }
+
+// The score of token `key` of request x.r and head hk (null: it has no page).
+__device__ inline float* score_at(const ScoreArgs& a, const Span& x, int hk, int key) {
+  const int id = a.table[x.r * a.row + (key >> a.shift)];
+  return (uint32_t)id < (uint32_t)a.n_pages ? a.scores + (((int64_t)id * a.Hkv + hk) << a.shift) + (key & ((1 << a.shift) - 1)) : nullptr;
+}
+
+// ---- up to 32 rows: single tokens ------------------------------------------------------------------
+// Bound by memory.  A wave has a place for two K blocks in LDS: one is multiplied, the next is on its way.
+template <int DT, int D> struct FewMemory { static constexpr int kBlock = 32 * Tile<DT, D>::ROWB, kBytes = 4 * 2 * kBlock; };
+template <int DT, int D>
+__device__ __forceinline__ void score_rows(const ScoreArgs& a, const Span& x, int hk, uint8_t* mem, float* norms) {
+  using T = Tile<DT, D>;
+  constexpr int BLK = FewMemory<DT, D>::kBlock, PG = 16 / T::RPI;
+  constexpr int SUMS = DT == ZC_F32 ? 4 : 1;     // accumulators of an fp32 logit: the roundings of one chain of D products are most of its error
+  const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, kh = lane >> 5;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const uint8_t* kb = a.k + hk * a.k_sH;
+  const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)mem + w * 2 * BLK;
+  const int32_t* table = a.table + x.r * a.row;
+
+  int voff[PG];
+#pragma unroll
+  for (int j = 0; j < PG; ++j) {
+    const int row = j * T::RPI + lane / T::CPR;
+    voff[j] = (int)(row * a.k_row) + (((lane % T::CPR) ^ T::swz(row)) << 4);
+  }
+  const int blocks = 4 * (x.t_hi - x.t_lo);
+  const auto key_of = [&](int b) { return tile_of(x, x.t_lo + (b >> 2)) * kScoreTile + 32 * (b & 3); };
+  // A block's keys are requested, and this lane's score so far.
+  float* to = nullptr;
+  float old = 0.f;
+  const auto issue = [&](int key0, int place) {
+    int id[2];
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      const int k16 = key0 + 16 * g;
+      id[g] = page_of(table, a.cols, a.shift, k16);
+      const int n = keys_read(a.n_pages, a.sinks, x.behind, x.kv, k16, id[g]);
+      move_keys<PG>(lds + place * BLK + g * 16 * T::ROWB, keys_at(a.shift, kb, a.k_sB, a.k_row, k16, id[g], n), voff);
+    }
+    const int key = key0 + r, mine = r < 16 ? id[0] : id[1];
+    to = nullptr;
+    old = 0.f;
+    if (kh == 0 && key < x.kv && (uint32_t)mine < (uint32_t)a.n_pages) {
+      to = a.scores + (((int64_t)mine * a.Hkv + hk) << a.shift) + (key & ((1 << a.shift) - 1));
+      if (key < x.kv - x.nq && a.decay != 0.f) old = *to;
+    }
+  };
+  int b = w, key0 = key_of(b);
+  if (b < blocks) issue(key0, 0);
+
+  // the rows, straight into operand registers; their normalisers
+  const int rows = x.nq * a.G;
+  const int2 me = row_of(a, 0, r);
+  u32x4 qf[T::NKC];
+#pragma unroll
+  for (int kc = 0; kc < T::NKC; ++kc) qf[kc] = u32x4{0, 0, 0, 0};
+  if (r < rows) {
+    const uint8_t* qr = a.q + (int64_t)(hk * a.G + me.y) * a.q_sH + (int64_t)(x.qs + me.x) * a.q_sT + kh * 16;
+#pragma unroll
+    for (int kc = 0; kc < T::NKC; ++kc) qf[kc] = *reinterpret_cast<const u32x4*>(qr + kc * 32);
+  }
+  __syncthreads();                               // (the unit before is done with the normalisers)
+  if (tid < 32) norms[tid] = tid < rows ? norm_of(a.lse[(int64_t)(hk * a.G + me.y) * a.T + x.qs + me.x]) : INFINITY;
+  __syncthreads();
+  float norm[16];
+  int pos[16];
+#pragma unroll
+  for (int v = 0; v < 16; ++v) {
+    norm[v] = norms[acc_row(v, kh)];
+    pos[v] = x.kv - x.nq + row_of(a, 0, acc_row(v, kh)).x;
+  }
+  typedef __attribute__((address_space(3))) const uint8_t* lds_ptr;
+  const uint32_t kaddr = lds + T::slot(r, kh);
+  const int p0 = x.kv - x.nq, p1 = x.kv - 1;
+  int place = 0;
+  wait_all_loads();
+  for (; b < blocks; b += 4, place ^= 1) {
+    const int key = key0 + r, next = b + 4 < blocks ? key_of(b + 4) : 0;
+    const int seen_from = p1 - a.window;                                       // keys above it are in every row's window
+    const bool whole = key0 + 31 <= p0 && (!a.window || key0 > seen_from || key0 + 31 < a.sinks);
+    const bool any = (uint32_t)(key0 - a.sinks) >= x.behind || (uint32_t)(key0 + 16 - a.sinks) >= x.behind;      // of the block's keys a row may see some
+    wait_vmem<0>();
+    wait_all_loads();
+    float* const put = to;
+    const float before = old;
+    if (b + 4 < blocks) issue(next, place ^ 1);
+    float sum = 0.f;
+    if (any) {
+      v16f acc[SUMS] = {};
+#pragma unroll
+      for (int kc = 0; kc < T::NKC; ++kc) {
+        const u32x4 kf = *(__attribute__((address_space(3))) const u32x4*)((lds_ptr)(uintptr_t)(kaddr ^ (32 * kc)) + place * BLK);
+        mma_chunk<DT>(acc[kc % SUMS], qf[kc], kf);
+      }
+#pragma unroll
+      for (int v4 = 0; v4 < 4; ++v4) {
+        if (8 * v4 >= rows) break;
+#pragma unroll
+        for (int v = 4 * v4; v < 4 * v4 + 4; ++v) {
+          float s = acc[0][v];
+          if constexpr (SUMS == 4) s = (acc[0][v] + acc[1][v]) + (acc[2][v] + acc[3][v]);
+          const float e = __builtin_amdgcn_exp2f(fmaf(s, a.scale_log2, -norm[v]));
+          const bool sees = whole || ((key <= pos[v]) & (!a.window || key > pos[v] - a.window || key < a.sinks));
+          sum += sees ? e : 0.f;
+        }
+      }
+      sum += __shfl_xor(sum, 32);
+    }
+    if (put) *put = fmaf(before, a.decay, sum);
+    key0 = next;
+  }
+}
+
+// ---- more rows: chunks -----------------------------------------------------------------------------
+// The waves take 64 of a tile's keys and 32 of 64 rows each: K operands stay in registers, rows stream through LDS.
+template <int DT, int D> struct ManyMemory { static constexpr int kTileB = 64 * Tile<DT, D>::ROWB, kBytes = 2 * kTileB; };
+template <int DT, int D>
+__device__ __forceinline__ void score_tiles(const ScoreArgs& a, const Span& x, int hk, uint8_t* mem, float (*norms)[64], int (*where)[64], float (*sums)[kScoreTile]) {
+  using T = Tile<DT, D>;
+  constexpr int TILE_B = ManyMemory<DT, D>::kTileB, NI = 64 / T::RPI / 4, PG = 16 / T::RPI;
+  constexpr int SUMS = DT == ZC_F32 ? 4 : 1;
+  const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, kh = lane >> 5;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6), rw = w >> 1, kw = w & 1;       // rows 32 rw on of 64, keys 64 kw on of 128
+  const uint8_t* kb = a.k + hk * a.k_sH;
+  const uint8_t* qb = a.q + (int64_t)hk * a.G * a.q_sH + (int64_t)x.qs * a.q_sT;
+  const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)mem;
+  const int32_t* table = a.table + x.r * a.row;
+  const int past = x.kv - x.nq;                  // position of the first row's token
+  const int64_t rows = (int64_t)x.nq * a.G;
+  typedef __attribute__((address_space(3))) const uint8_t* lds_ptr;
+  using lds_u32x4 = __attribute__((address_space(3))) const u32x4;
+
+  for (int t = x.t_lo; t < x.t_hi; ++t) {
+    const int key0 = tile_of(x, t) * kScoreTile;
+    // ---- K to registers, by way of both row buffers
+    int voff[PG];
+#pragma unroll
+    for (int j = 0; j < PG; ++j) {
+      const int row = j * T::RPI + lane / T::CPR;
+      voff[j] = (int)(row * a.k_row) + (((lane % T::CPR) ^ T::swz(row)) << 4);
+    }
+    __syncthreads();                             // (the tile before is done with LDS)
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      const int k16 = key0 + 32 * w + 16 * g, id = page_of(table, a.cols, a.shift, k16);
+      move_keys<PG>(lds + (32 * w + 16 * g) * T::ROWB, keys_at(a.shift, kb, a.k_sB, a.k_row, k16, id, keys_read(a.n_pages, a.sinks, x.behind, x.kv, k16, id)), voff);
+    }
+    float* to = nullptr;
+    float old = 0.f;
+    if (tid < kScoreTile && key0 + tid < x.kv) {
+      to = score_at(a, x, hk, key0 + tid);
+      if (to && key0 + tid < past && a.decay != 0.f) old = *to;
+    }
+    wait_vmem<0>();
+    wait_all_loads();
+    __syncthreads();
+    u32x4 kf[2][T::NKC];
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int kc = 0; kc < T::NKC; ++kc)
+        kf[n][kc] = *reinterpret_cast<lds_u32x4*>((lds_ptr)(uintptr_t)((lds + T::slot(r, kh)) ^ (32 * kc)) + (64 * kw + 32 * n) * T::ROWB);
+
+    // ---- rows that see some of these keys: up to the last row, or the last whose window reaches them
+    const int key1 = min(key0 + kScoreTile, x.kv) - 1;
+    int j_first = max(key0 - past, 0), j_end = x.nq;
+    if (a.window && key0 >= a.sinks) j_end = (int)min((int64_t)x.nq, (int64_t)key1 + a.window - past);
+    const int64_t i_first = (int64_t)j_first * a.G / 64 * 64, i_end = (int64_t)max(j_end, 0) * a.G;
+    int j0 = (int)(i_first / a.G), g0 = (int)(i_first - (int64_t)j0 * a.G);    // token and head of the tile's first row
+    const auto advance = [&](int& j, int& g) { const int2 n = row_of(a, j, g + 64); j = n.x; g = n.y; };
+    float norm;
+    int pos;
+    const auto issue = [&](int64_t i0, int j, int g, int buf) {
+      const int left = (int)min((int64_t)64, rows - i0);
+#pragma unroll
+      for (int jj = 0; jj < NI; ++jj) {
+        const int row = (w + 4 * jj) * T::RPI + lane / T::CPR;
+        const int2 me = row_of(a, j, g + min(row, left - 1));
+        gdma16(lds + buf * TILE_B + (w + 4 * jj) * 1024, qb + (int64_t)me.y * a.q_sH + (int64_t)me.x * a.q_sT + (((lane % T::CPR) ^ T::swz(row)) << 4));
+      }
+      if (tid < 64) {
+        const int2 me = row_of(a, j, g + min(tid, left - 1));
+        norm = tid < left ? norm_of(a.lse[(int64_t)(hk * a.G + me.y) * a.T + x.qs + me.x]) : INFINITY;
+        pos = past + me.x;
+      }
+    };
+    float sum[2] = {0.f, 0.f};
+    __syncthreads();                             // (K is in registers)
+    if (i_first < i_end) issue(i_first, j0, g0, 0);
+    int buf = 0;
+    for (int64_t i0 = i_first; i0 < i_end; i0 += 64, buf ^= 1) {
+      int jn = j0, gn = g0;
+      advance(jn, gn);
+      wait_vmem<0>();
+      wait_all_loads();
+      if (tid < 64) { norms[buf][tid] = norm; where[buf][tid] = pos; }
+      __syncthreads();                           // rows and normalisers are there, and nobody still reads the other buffer
+      if (i0 + 64 < i_end) issue(i0 + 64, jn, gn, buf ^ 1);
+      const uint32_t row = lds + buf * TILE_B + 32 * rw * T::ROWB + T::slot(r, kh);
+      const int pa = past + j0, pb = past + row_of(a, j0, g0 + 63).x;          // positions of the tile's first and last row
+      const bool whole = key0 + kScoreTile - 1 <= pa && (!a.window || key0 > pb - a.window || key0 + kScoreTile - 1 < a.sinks);
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        v16f acc[SUMS] = {};
+#pragma unroll
+        for (int kc = 0; kc < T::NKC; ++kc) {
+          const u32x4 qf = *reinterpret_cast<lds_u32x4*>((lds_ptr)(uintptr_t)(row ^ (32 * kc)));
+          mma_chunk<DT>(acc[kc % SUMS], qf, kf[n][kc]);
+        }
+        const int key = key0 + 64 * kw + 32 * n + r;
+#pragma unroll
+        for (int v4 = 0; v4 < 4; ++v4) {
+          const float4 nv = *reinterpret_cast<const float4*>(&norms[buf][32 * rw + 8 * v4 + 4 * kh]);
+          const int4 pv = *reinterpret_cast<const int4*>(&where[buf][32 * rw + 8 * v4 + 4 * kh]);
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const int v = 4 * v4 + u;
+            float s = acc[0][v];
+            if constexpr (SUMS == 4) s = (acc[0][v] + acc[1][v]) + (acc[2][v] + acc[3][v]);
+            const float e = __builtin_amdgcn_exp2f(fmaf(s, a.scale_log2, -(&nv.x)[u]));
+            if (whole) {
+              sum[n] += e;
+            } else {
+              const int p = (&pv.x)[u];
+              sum[n] += ((key <= p) & (!a.window || key > p - a.window || key < a.sinks)) ? e : 0.f;
+            }
+          }
+        }
+      }
+      j0 = jn;
+      g0 = gn;
+    }
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      sum[n] += __shfl_xor(sum[n], 32);
+      if (kh == 0) sums[rw][64 * kw + 32 * n + r] = sum[n];
+    }
+    __syncthreads();
+    if (to) *to = fmaf(old, a.decay, sums[0][tid] + sums[1][tid]);
+  }
+}
+
+template <int DT, int D>
+__global__ __launch_bounds__(256, DT == ZC_F32 && D == 128 ? 1 : 2) void k_paged_scores(ScoreArgs a) {
+  constexpr int kFew = FewMemory<DT, D>::kBytes, kMany = ManyMemory<DT, D>::kBytes;
+  __shared__ __align__(1024) uint8_t mem[kFew > kMany ? kFew : kMany];
+  __shared__ __align__(16) float norms[2][64];
+  __shared__ __align__(16) int where[2][64];
+  __shared__ float sums[2][kScoreTile];
+  Span x;
+  for (int u = blockIdx.y; find_span(a, u, x); u += gridDim.y) {
+    if ((int64_t)x.nq * a.G <= 32) score_rows<DT, D>(a, x, blockIdx.x, mem, norms[0]);
+    else score_tiles<DT, D>(a, x, blockIdx.x, mem, norms, where, sums);
+  }
+}
+
+template <int DT, int D>
+static int launch_scores(const ScoreArgs& a, int units, hipStream_t st) {
+  hipLaunchKernelGGL((k_paged_scores<DT, D>), dim3((unsigned)a.Hkv, (unsigned)units), dim3(256), 0, st, a);
+  ZC_LAUNCH_CHECK();
+  return ZC_OK;
+}
+
+}  // namespace zc
+
+using namespace zc;
+
+extern "C" int zc_paged_scores(const zc_tensor4* q, const zc_tensor4* k_pages, const int32_t* block_table, int64_t row_stride, int64_t max_blocks,
+                               const int32_t* q_start, const int32_t* kv_len, int64_t R, int32_t window, int32_t sinks, float sm_scale,
+                               const float* lse, float decay, float* scores, void* stream) {
+  int rc = zc_validate_pages(k_pages, k_pages);
+  if (rc) return rc;
+  rc = zc_validate_heads(q, k_pages);
+  if (rc) return rc;
+  if (q->H % k_pages->H) return ZC_ERR_INVALID_ARG;
+  if (R < 0 || window < 0 || sinks < 0 || !(sm_scale >= 0.f) || !(sm_scale * kLog2e <= 3.40282347e38f) || !(decay >= 0.f && decay <= 1.f))
+    return ZC_ERR_INVALID_ARG;
+  if (max_blocks < 0 || row_stride < max_blocks) return ZC_ERR_INVALID_ARG;
+  if (!scores || (reinterpret_cast<uintptr_t>(scores) & 15)) return ZC_ERR_INVALID_ARG;
+  if (q->L == 0 || R == 0 || max_blocks == 0) return ZC_OK;
+  if (!q_start || !kv_len || !lse || !block_table) return ZC_ERR_INVALID_ARG;
+  for (const void* p : {(const void*)block_table, (const void*)q_start, (const void*)kv_len, (const void*)lse})
+    if (reinterpret_cast<uintptr_t>(p) & 3) return ZC_ERR_INVALID_ARG;
+  const int64_t T = q->L, Hkv = k_pages->H, G = q->H / Hkv, page = k_pages->L;
+  if (R >= (1 << 24) || max_blocks > 0x7fffffff || T > 0x7fffffff / q->H || q->H > 65535 || G > 4096) return ZC_ERR_UNSUPPORTED;
+  const int64_t room = max_blocks > 0x7fff0000 / page ? 0x7fff0000 : max_blocks * page;
+  if (window >= room) window = 0;                    // (every row sees all it could)
+  if (sinks > room) sinks = (int32_t)room;
+  const int64_t eb = elem_bytes(q->dtype);
+  ScoreArgs a;
+  a.q = (const uint8_t*)q->ptr; a.k = (const uint8_t*)k_pages->ptr;
+  a.q_sH = q->sH * eb; a.q_sT = q->sL * eb; a.k_sH = k_pages->sH * eb;
+  a.k_sB = (uint32_t)(k_pages->sB * eb); a.k_row = (uint32_t)(k_pages->sL * eb);
+  a.table = block_table; a.q_start = q_start; a.kv_len = kv_len; a.row = row_stride;
+  a.cols = (int)max_blocks; a.shift = __builtin_ctzll((unsigned long long)page); a.n_pages = (int)k_pages->B; a.cap = (int)room;
+  a.R = (int)R; a.T = (int)T; a.Hkv = (int)Hkv; a.G = (int)G;
+  a.window = window; a.sinks = sinks;
+  a.scale_log2 = (sm_scale == 0.f ? 1.0f / sqrtf((float)q->D) : sm_scale) * kLog2e;
+  a.decay = decay;
+  a.lse = lse;
+  a.scores = scores;
+  a.over_G = G == 1 ? 0 : (uint32_t)(((1ull << 32) + G - 1) / G);
+  const int64_t target = ceil_div64(1024, Hkv), tiles = ceil_div64(room, kScoreTile), with = R < T ? R : T;
+  a.target = (float)target;
+  const int64_t most = tiles > 65535 / with ? 65535 : tiles * with, units = target + with < most ? target + with : most;
+  hipStream_t st = (hipStream_t)stream;
+#define ZC_PS(DT) (q->D == 128 ? launch_scores<DT, 128>(a, (int)units, st) : launch_scores<DT, 64>(a, (int)units, st))
+  if (q->dtype == ZC_F32) rc = ZC_PS(ZC_F32);
+  else if (q->dtype == ZC_F16) rc = ZC_PS(ZC_F16);
+  else rc = ZC_PS(ZC_BF16);
+#undef ZC_PS
+  return rc;
+}

@@ -1,0 +1,226 @@
+"""zc_paged_scores against float64: the weight that every cached token gathers."""
+import math
+import threading
+
+import pytest
+import torch
+
+from paper_2405_14256_amd import binding as zb
+from tests import paged_plain, scores_plain as plain
+
+pytestmark = pytest.mark.gpu
+BF, HF, FL = torch.bfloat16, torch.float16, torch.float32
+DEV = "cuda"
+
+
+class Step:
+    """Pages with scores beside them: random ones at the tokens that were there before, NaN anywhere else."""
+
+    def __init__(self, *a, window=0, sinks=0, sm_scale=0.0, decay=1.0, **kw):
+        p = self.p = paged_plain.Pages(*a, **kw)
+        self.kw = dict(window=window, sinks=sinks, sm_scale=sm_scale, decay=decay)
+        self.lse = plain.normalisers(p, window, sinks, sm_scale)
+        self.scores = torch.full((p.kp.shape[0], p.Hkv, p.page), math.nan, device=DEV)
+        g = torch.Generator(device=DEV).manual_seed(7)
+        for r, (nq, kv) in enumerate(zip(p.q_len, p.kv_len)):
+            n = kv if nq == 0 else max(kv - nq, 0)
+            self.write(r, torch.rand(p.Hkv, n, generator=g, device=DEV))
+
+    def places(self, r):
+        i = torch.arange(self.p.kv_len[r])
+        return self.p.table_host[r, i // self.p.page].long().to(DEV), (i % self.p.page).to(DEV)
+
+    def at(self, scores, r):
+        page, row = self.places(r)
+        return scores[page, :, row].T.clone(), (page, row)
+
+    def write(self, r, x):
+        page, row = self.places(r)
+        n = x.shape[1]
+        self.scores[page[:n], :, row[:n]] = x.T
+
+    def call(self, scores, **kw):
+        p = self.p
+        return zb.zc_paged_scores(kw.get("q", p.q), p.kp, p.table, p.q_start, p.kv, self.lse, scores, **self.kw)
+
+    def check(self, got, lse=None):
+        p, touched = self.p, torch.zeros_like(self.scores, dtype=torch.bool)
+        for r, nq in enumerate(p.q_len):
+            if nq == 0:
+                continue
+            old, (page, row) = self.at(self.scores, r)
+            want, off = plain.gathered(p, r, self.lse, old.nan_to_num(), **self.kw)
+            now, _ = self.at(got, r)
+            bad = ~((now.double() - want).abs() <= off)
+            assert not bool(bad.any()), f"request {r}: {int(bad.sum())} of {bad.numel()} off, first at {bad.nonzero()[0].tolist()}: " \
+                                        f"{now[bad][0].item()} for {want[bad][0].item()} +- {off[bad][0].item()}"
+            touched[page, :, row] = True
+        same = (got == self.scores) | (got.isnan() & self.scores.isnan())
+        assert bool((same | touched).all()), "a place of nobody's changed"
+
+    def run(self):
+        got = self.scores.clone()
+        self.call(got)
+        self.check(got)
+
+
+@pytest.mark.parametrize("dtype,D,Hq,Hkv,page,by_head", [(BF, 128, 8, 2, 16, True), (HF, 64, 4, 4, 32, False), (FL, 64, 6, 2, 64, True), (FL, 128, 4, 1, 16, False),
+                                                         (BF, 64, 8, 1, 128, True), (HF, 128, 3, 3, 16, True)])
+@pytest.mark.parametrize("window,sinks,decay", [(0, 0, 1.0), (40, 3, 1.0), (40, 3, 0.5), (0, 0, 0.0), (130, 70, 0.9)])
+def test_single_tokens_and_chunks(dtype, D, Hq, Hkv, page, by_head, window, sinks, decay):
+    Step([1, 70, 0, 1, 5, 300, 33], [900, 500, 40, 1, 5, 300, 700], Hq, Hkv, D, dtype, page, by_head, pad=5, window=window, sinks=sinks, decay=decay).run()
+
+
+@pytest.mark.parametrize("dtype", [BF, FL])
+@pytest.mark.parametrize("rows", [1, 7, 8, 9, 31, 32, 33, 63, 64, 65, 127, 128, 129])
+def test_numbers_of_rows(dtype, rows):
+    Step([rows], [300 + rows], 2, 2, 64, dtype, seed=rows).run()
+
+
+@pytest.mark.parametrize("kv", [1, 15, 16, 17, 31, 32, 33, 127, 128, 129, 255, 257, 4097])
+@pytest.mark.parametrize("nq", [1, 40])
+def test_numbers_of_keys(kv, nq):
+    Step([min(nq, kv)], [kv], 4, 2, 128, BF, seed=kv).run()
+
+
+@pytest.mark.parametrize("G,nq", [(32, 1), (33, 1), (33, 3), (40, 2), (100, 1), (3, 43)])
+def test_large_and_odd_groups(G, nq):
+    Step([nq, 0, nq], [200, 10, 90], 2 * G, 2, 64, HF).run()
+
+
+def test_rows_in_front_of_the_first_token_weigh_nothing():
+    for nq, kv in ((5, 3), (90, 40), (50, 0)):
+        Step([nq, 2], [kv, 30], 4, 2, 64, BF, pad=2).run()
+
+
+def test_many_requests():
+    n = [1 + (7 * i) % 90 for i in range(200)]
+    Step([0 if i % 7 == 3 else 1 if i % 3 else min(k, 20) for i, k in enumerate(n)], n, 4, 2, 64, BF, pad=3).run()
+    Step([1] * 150, [1 + (37 * i) % 500 for i in range(150)], 8, 2, 128, HF, page=32).run()
+
+
+def test_long_requests_among_short_ones():
+    Step([1, 1, 64, 1], [20000, 5, 9000, 300], 8, 2, 128, BF, page=64).run()
+    Step([500, 1], [6000, 7000], 4, 2, 64, FL, page=64, window=1000, sinks=10).run()
+
+
+@pytest.mark.parametrize("window,sinks", [(2 ** 31 - 1, 0), (1, 0), (1, 2 ** 31 - 1), (500, 1), (128, 128), (129, 127)])
+def test_windows(window, sinks):
+    Step([1, 200, 3], [700, 650, 700], 4, 2, 64, BF, window=window, sinks=sinks).run()
+
+
+def test_strides_of_the_rows():
+    s = Step([1, 60], [200, 300], 6, 2, 64, BF, pad=4)
+    wide = torch.full((s.p.T, 3, 6, 128), math.nan, dtype=BF, device=DEV)
+    q = wide[:, 1, :, 64:]
+    q.copy_(s.p.q)
+    for x in (q, q.permute(1, 0, 2)[None]):
+        got = s.scores.clone()
+        s.call(got, q=x)
+        s.check(got)
+
+
+def test_a_scale_of_the_callers():
+    Step([1, 40], [200, 300], 4, 2, 64, FL, sm_scale=0.3).run()
+
+
+def test_missing_pages_have_no_scores():
+    s = Step([1, 50], [300, 200], 4, 2, 64, BF)
+    want = s.scores.clone()
+    s.call(want)
+    lost = []
+    for r, c, bad in ((0, 3, -1), (0, 18, 10 ** 9), (1, 0, -2 ** 31), (1, 12, 2 ** 31 - 1)):
+        lost.append(int(s.p.table_host[r, c]))
+        s.p.table[r, c] = bad
+    got = s.scores.clone()
+    s.call(got)
+    torch.cuda.synchronize()
+    for n in lost:                                                         # what is behind a missing entry is not touched, the others' weights do not change
+        want[n] = s.scores[n]
+    assert torch.equal(got.nan_to_num(-1.0), want.nan_to_num(-1.0))
+
+
+def test_steps_that_hold_nothing():
+    s = Step([1], [40], 4, 2, 64, BF)
+    got, p = s.scores.clone(), s.p
+    i32 = dict(dtype=torch.int32, device=DEV)
+    zb.zc_paged_scores(p.q[:0], p.kp, p.table, torch.zeros(2, **i32), p.kv, s.lse[:, :0].contiguous(), got)
+    zb.zc_paged_scores(p.q, p.kp, p.table[:0], torch.zeros(1, **i32), p.kv[:0], s.lse, got)
+    zb.zc_paged_scores(p.q, p.kp, p.table[:, :0], p.q_start, p.kv, s.lse, got)
+    torch.cuda.synchronize()
+    assert torch.equal(got.nan_to_num(-1.0), s.scores.nan_to_num(-1.0))
+
+
+def test_lengths_outside_the_table_are_the_nearest():
+    s = Step([1, 3], [160, 48], 4, 2, 64, BF, spare=2)
+    want = s.scores.clone()
+    s.call(want)
+    s.p.kv = torch.tensor([10 ** 9, 48], dtype=torch.int32, device=DEV)     # (the first fills its row of the table)
+    got = s.scores.clone()
+    s.call(got)
+    assert torch.equal(got.nan_to_num(-1.0), want.nan_to_num(-1.0))
+
+
+def test_equal_calls_have_equal_results_and_graphs_replay():
+    steps = [Step([1, 100, 1], [3000, 700, 64], 8, 2, 128, BF, seed=1, decay=0.9), Step([1] * 20, [500 + 40 * i for i in range(20)], 8, 2, 64, HF, seed=2)]
+    want = []
+    for s in steps:
+        a, b = s.scores.clone(), s.scores.clone()
+        s.call(a)
+        s.check(a)
+        s.call(b)
+        assert torch.equal(a.nan_to_num(-1.0), b.nan_to_num(-1.0))
+        want.append(a)
+    now = [s.scores.clone() for s in steps]
+    g = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        for s, x in zip(steps, now):
+            s.call(x)
+    for _ in range(4):
+        for s, x in zip(steps, now):
+            x.copy_(s.scores)
+        g.replay()
+        eager = steps[1].scores.clone()
+        steps[1].call(eager)
+        torch.cuda.synchronize()
+        for x, y in zip(now, want):
+            assert torch.equal(x.nan_to_num(-1.0), y.nan_to_num(-1.0))
+        assert torch.equal(eager.nan_to_num(-1.0), want[1].nan_to_num(-1.0))
+
+
+def test_steps_add_up():
+    """Two tokens in one step and one after the other: the same weight."""
+    s = Step([2], [301], 4, 2, 64, FL, seed=5)
+    both = s.scores.clone()
+    s.call(both)
+    p, one = s.p, s.scores.clone()
+    i32 = dict(dtype=torch.int32, device=DEV)
+    for j in range(2):
+        zb.zc_paged_scores(p.q[j:j + 1], p.kp, p.table, torch.tensor([0, 1], **i32), torch.tensor([300 + j], **i32), s.lse[:, j:j + 1].contiguous(), one)
+    a, b = s.at(both, 0)[0].double(), s.at(one, 0)[0].double()
+    assert bool(((a - b).abs() <= 2.0 ** -21 * b + 1e-30).all())             # (sums in another order: four roundings each)
+
+
+def test_calls_on_two_streams_and_from_two_threads():
+    steps = [Step([1] * 12, [900 + 50 * i for i in range(12)], 8, 2, 128, BF, seed=s) for s in (3, 4)]
+    want = []
+    for s in steps:
+        x = s.scores.clone()
+        s.call(x)
+        want.append(x)
+    torch.cuda.synchronize()
+    out = [None, None]
+
+    def work(n):
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            out[n] = [steps[n].call(steps[n].scores.clone()) for _ in range(20)]
+        stream.synchronize()
+    threads = [threading.Thread(target=work, args=(n,)) for n in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    for results, y in zip(out, want):
+        assert all(torch.equal(x.nan_to_num(-1.0), y.nan_to_num(-1.0)) for x in results)
