@@ -413,6 +413,27 @@ int zc_paged_attention(const zc_tensor4* q, const zc_tensor4* k_pages, const zc_
                        int32_t window, int32_t sinks, float sm_scale, const zc_tensor4* out, float* lse,
                        void* ws, size_t ws_bytes, void* stream);
 
+/* ---- attention of a step's new tokens where groups of requests share a prefix ---------------------
+ * Prefix g's prefix_len[g] tokens (device int32 [P]) lie in the pages of row g of prefix_table (device int32 [P, prefix_max_blocks], rows
+ * prefix_row_stride elements apart), in the same pools and stored once.  Requests group_start[g] .. group_start[g + 1] - 1 (device int32 [P + 1],
+ * ascending within [0, R]) begin with it; those in front of group_start[0] and from group_start[P] on have none.  block_table, kv_len and q_start are, as in
+ * zc_paged_attention, of the requests' own tokens, which follow the prefix: a new token sees its whole prefix and its request's own tokens
+ * up to itself,
+ *   out[h, t, :] = sum_i softmax_i(q[h, t] . k[h/G, i] * sm_scale) v[h/G, i, :]   over i in both,
+ * and lse is the normaliser of both (zc_paged_scores takes it for the own tokens as it is).  The rows of requests with up to 64 of them
+ * (new tokens times Hq / Hkv) go through their prefix together, so that a key of it is read and multiplied once for all; a longer chunk fills
+ * blocks of its own.  There is no sliding window here: where one is wanted, put the prefix's pages into every request's own row.
+ * prefix_len outside [0, prefix_max_blocks * page] is taken for the nearest; pages that are none read as zeros.  A row that sees nothing has zeros for its
+ * output and -inf for its normaliser.  Types, shapes, strides, sm_scale and rounding as in zc_paged_attention; deterministic for equal lengths and
+ * shapes; a row's last bits may depend on the other requests.  P, R and T may be 0; P <= 1024, R < 2^24, T * Hq < 2^31; T * Hq / 64 (fp32: / 16) +
+ * 6 min(R, T) Hkv + 512 below 2^24 is always enough for the blocks of a step.  Workspace: zc_paged_shared_attention_workspace() bytes, 16-byte aligned, with any contents; calls that share one must
+ * not run concurrently. */
+size_t zc_paged_shared_attention_workspace(int64_t P, int64_t R, int64_t T, int64_t Hq, int64_t Hkv, int64_t D);
+int zc_paged_shared_attention(const zc_tensor4* q, const zc_tensor4* k_pages, const zc_tensor4* v_pages, const int32_t* prefix_table,
+                              int64_t prefix_row_stride, int64_t prefix_max_blocks, const int32_t* prefix_len, const int32_t* group_start, int64_t P,
+                              const int32_t* block_table, int64_t row_stride, int64_t max_blocks, const int32_t* q_start, const int32_t* kv_len,
+                              int64_t R, float sm_scale, const zc_tensor4* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+
 /* ---- the weight that cached tokens gather (Eq. 7 over the pages, step by step) --------------------
  * For every request with new tokens, every KV head h and every token i < kv_len[r] of it
  *   scores[h, i] = (i < kv_len[r] - nq ? decay * scores[h, i] : 0) + sum over rows (new token, query head of h) that see i of exp(logit - lse[row])

@@ -118,6 +118,10 @@ def load() -> C.CDLL:
     lib.zc_paged_attention_workspace.argtypes = [I64, I64, I64, I64, I64]
     lib.zc_paged_attention.restype = C.c_int
     lib.zc_paged_attention.argtypes = [T4, T4, T4, P, I64, I64, P, P, I64, I32, I32, F, T4, P, P, SZ, P]
+    lib.zc_paged_shared_attention_workspace.restype = SZ
+    lib.zc_paged_shared_attention_workspace.argtypes = [I64, I64, I64, I64, I64, I64]
+    lib.zc_paged_shared_attention.restype = C.c_int
+    lib.zc_paged_shared_attention.argtypes = [T4, T4, T4, P, I64, I64, P, P, I64, P, I64, I64, P, P, I64, F, T4, P, P, SZ, P]
     lib.zc_paged_scores.restype = C.c_int
     lib.zc_paged_scores.argtypes = [T4, T4, P, I64, I64, P, P, I64, I32, I32, F, P, F, P, P]
     lib.zc_paged_evict_workspace.restype = SZ
@@ -405,6 +409,22 @@ def zc_paged_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Te
         T, Hq = (q.shape[0], q.shape[1]) if q.dim() == 3 else (q.shape[2], q.shape[1])
         lse = torch.empty(Hq, T, dtype=torch.float32, device=q.device)
     _check("zc_paged_attention", host.paged_attention(q, k_pages, v_pages, block_table, q_start, kv_len, window, sinks, sm_scale, out, lse))
+    return out, lse
+
+
+def zc_paged_shared_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, prefix_table: torch.Tensor, prefix_len: torch.Tensor,
+                              group_start: torch.Tensor, block_table: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor,
+                              sm_scale: float = 0.0, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None):
+    """zc_paged_attention where requests group_start[g] .. group_start[g + 1] - 1 see, in front of their own kv_len tokens, the prefix_len[g]
+    tokens in the pages of prefix_table[g]: these are read and multiplied once for all of the group's rows -> (out like q, lse [Hq, T])."""
+    host = _native()
+    if out is None:
+        out = torch.empty_like(q)
+    if lse is None and q.dim() in (3, 4):
+        T, Hq = (q.shape[0], q.shape[1]) if q.dim() == 3 else (q.shape[2], q.shape[1])
+        lse = torch.empty(Hq, T, dtype=torch.float32, device=q.device)
+    _check("zc_paged_shared_attention", host.paged_shared(q, k_pages, v_pages, prefix_table, prefix_len, group_start, block_table, q_start, kv_len,
+                                                          sm_scale, out, lse))
     return out, lse
 
 

@@ -31,15 +31,16 @@ namespace {
 // ---- entry points, in the order of kNames ---------------------------------------------------
 enum Fn {
   kProbe, kAccumulated, kPrefill, kSelect, kQuantize, kQuantizeKV, kDecode, kDecodeStatic, kProbs, kRows, kDequantize,
-  kPagedTables, kPagedStore, kPagedLoad, kPagedAttention, kPagedScores, kPagedEvict,
-  kProbeWs, kQuantizeWs, kQuantizeKVWs, kDecodeWs, kPagedAttentionWs, kPagedEvictWs, kFnCount
+  kPagedTables, kPagedStore, kPagedLoad, kPagedAttention, kPagedShared, kPagedScores, kPagedEvict,
+  kProbeWs, kQuantizeWs, kQuantizeKVWs, kDecodeWs, kPagedAttentionWs, kPagedSharedWs, kPagedEvictWs, kFnCount
 };
 const char* const kNames[kFnCount] = {
     "zc_probe_saliency", "zc_probe_accumulated", "zc_prefill_attention", "zc_select_salient", "zc_quantize_pack",
     "zc_quantize_pack_kv", "zc_decode_attention", "zc_decode_attention_static", "zc_decode_probs", "zc_rows_saliency",
-    "zc_dequantize_cache", "zc_paged_tables", "zc_paged_store", "zc_paged_load", "zc_paged_attention", "zc_paged_scores", "zc_paged_evict",
+    "zc_dequantize_cache", "zc_paged_tables", "zc_paged_store", "zc_paged_load", "zc_paged_attention", "zc_paged_shared_attention",
+    "zc_paged_scores", "zc_paged_evict",
     "zc_probe_saliency_workspace", "zc_quantize_pack_workspace", "zc_quantize_pack_kv_workspace", "zc_decode_attention_workspace",
-    "zc_paged_attention_workspace", "zc_paged_evict_workspace"};
+    "zc_paged_attention_workspace", "zc_paged_shared_attention_workspace", "zc_paged_evict_workspace"};
 void* g_fn[kFnCount];
 
 #define ZC_FN(id, name) reinterpret_cast<decltype(&name)>(g_fn[id])
@@ -117,7 +118,7 @@ struct Packed {
 // under the interpreter lock; the launches do not, and a call is several of them: two threads' calls on
 // one stream (by default all threads share one) would come between each other's.  So a call holds its buffer's mutex
 // while it launches, taken when the interpreter lock has been given up and given back before that is taken again.
-enum Kind { kScratchProbe, kScratchQuantize, kScratchQuantizeKV, kScratchDecode, kScratchPaged, kScratchEvict };
+enum Kind { kScratchProbe, kScratchQuantize, kScratchQuantizeKV, kScratchDecode, kScratchPaged, kScratchShared, kScratchEvict };
 struct Scratch { at::Tensor t; void* ptr = nullptr; size_t bytes = 0; bool captured = false; std::mutex* use = nullptr; };
 std::map<std::tuple<int, int, void*>, Scratch>* g_scratch;
 std::vector<at::Tensor>* g_captured;      // replaced buffers that graphs may hold
@@ -415,13 +416,13 @@ Scratch paged_scratch(size_t need, const at::Tensor& like, Kind kind, hipStream_
   return c.on ? captured_scratch(need, like, stream, c.id) : scratch(need, like, kind, stream);
 }
 struct Table { int32_t* ptr; int64_t R, row, cols; };
-Table table_of(PyObject* o) {
+Table table_of(PyObject* o, const char* what = "block_table") {
   const at::Tensor& t = tensor_of(o);
-  on_device(t, "block_table");
-  if (t.scalar_type() != at::kInt || t.dim() != 2 || (t.size(1) > 1 && t.stride(1) != 1)) refuse("block_table", "must be an int32 [R, max_blocks] tensor with rows that lie together");
+  on_device(t, what);
+  if (t.scalar_type() != at::kInt || t.dim() != 2 || (t.size(1) > 1 && t.stride(1) != 1)) refuse(what, "must be an int32 [R, max_blocks] tensor with rows that lie together");
   Table r = {static_cast<int32_t*>(t.data_ptr()), t.size(0), t.stride(0), t.size(1)};
   if (r.R < 2 || r.row < r.cols) {
-    if (r.R > 1) refuse("block_table", "has rows that overlap");
+    if (r.R > 1) refuse(what, "has rows that overlap");
     r.row = r.cols;
   }
   return r;
@@ -549,6 +550,34 @@ PyObject* paged_attention(PyObject*, Args a, Py_ssize_t n) {
   });
 }
 
+// (q, k_pages, v_pages, prefix_table, prefix_len, group_start, block_table, q_start, kv_len, sm_scale, out, lse)
+PyObject* paged_shared(PyObject*, Args a, Py_ssize_t n) {
+  return guarded(kPagedShared, n, 12, [&]() -> int {
+    g_device = -1;
+    const zc_tensor4 q = tokens(a[0], "q"), kp = pool(a[1], "k_pages"), vp = pool(a[2], "v_pages"), o = tokens(a[10], "out");
+    const Table pre = table_of(a[3], "prefix_table"), t = table_of(a[6]);
+    const auto *len = ints(a[4], "prefix_len", pre.R), *groups = ints(a[5], "group_start", pre.R + 1);
+    const auto *start = ints(a[7], "q_start", t.R + 1), *kv = ints(a[8], "kv_len", t.R);
+    const float scale = float_of(a[9]);
+    float* lse = nullptr;
+    if (a[11] != Py_None) {
+      const at::Tensor& l = tensor_of(a[11]);
+      on_device(l, "lse");
+      if (l.scalar_type() != at::kFloat || !l.is_contiguous() || l.numel() != q.H * q.L) refuse("lse", "must be a contiguous float32 [Hq, T] tensor");
+      lse = static_cast<float*>(l.data_ptr());
+    }
+    const hipStream_t st = current_stream();
+    const size_t need = ZC_FN(kPagedSharedWs, zc_paged_shared_attention_workspace)(pre.R, t.R, q.L, q.H, kp.H, q.D);
+    const Scratch ws = paged_scratch(need, tensor_of(a[0]), kScratchShared, st);
+    void* wp = ws.ptr;
+    const size_t wn = ws.bytes;
+    const auto fn = ZC_FN(kPagedShared, zc_paged_shared_attention);
+    return unlocked(ws.use, [&] {
+      return fn(&q, &kp, &vp, pre.ptr, pre.row, pre.cols, len, groups, pre.R, t.ptr, t.row, t.cols, start, kv, t.R, scale, &o, lse, wp, wn, st);
+    });
+  });
+}
+
 // Gathered weights beside the pages: float32 [N, Hkv, page].
 float* scores_of(PyObject* o, const zc_tensor4& pages) {
   const at::Tensor& t = tensor_of(o);
@@ -653,6 +682,7 @@ PyMethodDef kMethods[] = {
     ZC_METHOD("paged_store", paged_store),
     ZC_METHOD("paged_load", paged_load),
     ZC_METHOD("paged_attention", paged_attention),
+    ZC_METHOD("paged_shared", paged_shared),
     ZC_METHOD("paged_scores", paged_scores),
     ZC_METHOD("paged_evict", paged_evict),
     {nullptr, nullptr, 0, nullptr}};

@@ -81,18 +81,6 @@ __device__ inline Images images(const EvictArgs& a, int r, int h, int i0, int hi
 }
 __device__ inline int page_of(const EvictArgs& a, int r, int i) { return a.cols ? a.table[r * a.row + min(i >> a.shift, a.cols - 1)] : -1; }
 
-// Sum over the threads in front, this one's included; waves: a place of its own for each use between two others' barriers.
-template <int NW>
-__device__ inline int block_inclusive_sum(int v, int* waves, int& total) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  v = wave_inclusive_sum(v);
-  if (lane == 63) waves[w] = v;
-  __syncthreads();
-  const int upto = wave_inclusive_sum(lane < NW ? waves[lane] : 0);
-  total = __builtin_amdgcn_readlane(upto, NW - 1);
-  return v + (w ? __builtin_amdgcn_readlane(upto, w - 1) : 0);
-}
-
 // Pages that requests leave: where each one's go in the list of free ones.  A workgroup a request.
 template <int THREADS>
 __device__ void give_back(const EvictArgs& a, int r, int kv, int stay, int (*waves)[THREADS / 64]) {

@@ -1,0 +1,470 @@
+// zc_paged_shared_attention: attention of a step's new tokens where groups of requests share a prefix, which lies in pages of its own.
+//
+// Rows (token, query head of the group) of requests that share a prefix see the same keys, so they go through it together, in blocks of 32 or 128
+// rows of many requests, each key read and multiplied once for all of them; every request's own keys follow, and a row's parts are joined
+// in fp32:
+//   m = max(m_p, m_o),  l = l_p e^(m_p - m) + l_o e^(m_o - m),  o = (o_p e^(m_p - m) + o_o e^(m_o - m)) / l
+// A request with more than 64 rows fills blocks of its own: these take the prefix and then its own keys without a join.
+//
+// Lengths and groups are known to the GPU only.  One workgroup plans the step (k_shared_plan): what every unit of work is - a block of rows,
+// a range of tiles of the prefix, one of the request's own - how far long ranges are split, and what is to be joined.
+#include "paged_attention_kernel.hpp"
+
+namespace zc {
+
+constexpr int kGroups = 1024;                   // prefixes of a step, at most
+constexpr int kSharedJoinGroups = 4;            // workgroups that join a block
+constexpr int kFewRows = 64;                    // of a request that goes through a prefix together with others, at most
+
+struct SharedArgs : PagedArgs {
+  const int32_t *pre_table, *pre_len, *group_start;
+  int64_t pre_row;                              // of the prefixes' table, in entries
+  int pre_cols, pre_cap, P;
+  int* counts;                                  // units, joins
+  int4* plan;                                   // [unit][4]
+  int4* joins;                                  // [block][2]
+  int* tokens;                                  // the tokens that go through a prefix together, group after group
+  int most_units, most_joins;                   // (units: partial results that there is room for)
+};
+
+struct SharedUnit {
+  static constexpr int kSegments = 2;
+  int segments;                 // ranges of keys: the prefix, the request's own
+  int qs, past, j0, g0, rows;   // the request's first row; tokens in front of its new ones; token and head of the block's first row, its rows
+  int last;                     // rows of several requests: the block's last place in the list of tokens; -1: of one
+  const int* tokens;
+  int part;                     // where its partial results go, -1: nothing to join
+  const int32_t* tables[2];
+  int columns[2], keys[2], from[2], to[2];
+  // the range in hand
+  const int32_t* table;
+  int cols, kv, t_lo, t_hi, p0, p1;
+  bool own;
+  static constexpr int first = 0, sink_tiles = 0;
+  static constexpr uint32_t behind = 0;
+  __device__ void enter(const PagedArgs& a, int s);
+};
+__device__ inline Row row_at(const PagedArgs& a, const SharedUnit& x, int r) {
+  Row me = row_at(a, x.j0, x.g0, r);
+  if (x.last >= 0) me.j = x.tokens[min(me.j, x.last)];
+  return me;
+}
+__device__ inline int position(const SharedUnit& x, int j) { return x.own ? x.past + j : x.kv - 1; }
+__device__ inline void SharedUnit::enter(const PagedArgs& a, int s) {
+  const int i = segments == 2 ? s : from[0] < to[0] ? 0 : 1;
+  own = i == 1;
+  table = own ? tables[1] : tables[0];
+  cols = own ? columns[1] : columns[0];
+  kv = own ? keys[1] : keys[0];
+  t_lo = own ? from[1] : from[0];
+  t_hi = own ? to[1] : to[0];
+  p0 = own ? past + j0 : kv - 1;
+  p1 = own ? past + row_at(a, j0, g0, rows - 1).j : kv - 1;
+}
+__device__ inline int tile_of(const SharedUnit&, int t) { return t; }
+__device__ inline const int32_t* table_row(const PagedArgs&, const SharedUnit& x) { return x.table; }
+__device__ inline int table_cols(const PagedArgs&, const SharedUnit& x) { return x.cols; }
+__device__ inline bool is_whole(const SharedUnit& x) { return x.part < 0; }
+__device__ inline int64_t part_of(const PagedArgs& a, const SharedUnit& x, int hk) { return part_row(a, hk, x.part); }
+
+// ---- the plan -------------------------------------------------------------------------------------
+// One workgroup, a thread a request or group at first, then a thread a unit.  Bound by its chain of lengths, rows and barriers.
+constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64;
+
+// What is planned for an entry, a request or a group.
+struct Blocks32 { int few, blocks; };
+__device__ inline Blocks32 blocks_of(int rows, int many) {
+  const bool few = rows <= kFewRows || many == 32;
+  return {few, few ? (rows + 31) / 32 : (rows + many - 1) / many};
+}
+
+__global__ __launch_bounds__(kPlanThreads) void k_shared_plan(SharedArgs a, int many) {
+  __shared__ int g_start[kGroups + 1], g_kv[kGroups], g_first[kGroups], g_end[kGroups], g_part[kGroups], g_parts[kGroups];
+  // of the entries in hand
+  __shared__ int s_unit[kPlanThreads], s_join[kPlanThreads], s_part[kPlanThreads], s_parts[kPlanThreads], s_blocks[kPlanThreads];
+  __shared__ int s_qs[kPlanThreads], s_nq[kPlanThreads], s_kv[kPlanThreads], s_group[kPlanThreads], s_place[kPlanThreads];
+  __shared__ int waves[4][kPlanWaves];
+  __shared__ unsigned long long s_work;
+  const int tid = threadIdx.x;
+  for (int e = tid; e <= a.P; e += kPlanThreads) {
+    g_start[e] = min(max(a.group_start[e], 0), a.R);
+    if (e < a.P) {
+      g_kv[e] = min(max(a.pre_len[e], 0), a.pre_cap);
+      g_first[e] = g_end[e] = 0;
+    }
+  }
+  if (tid == 0) s_work = 0;
+  struct Entry { int qs, nq, kv, group, pre, few, blocks, tiles, together; };
+  const auto entry = [&](int r) {                          // of request r (g_start and g_kv are there)
+    Entry x = {0, 0, 0, -1, 0, 0, 0, 0, 0};
+    if (r >= a.R) return x;
+    const int s = a.q_start[r], e = a.q_start[r + 1], kv = a.kv_len[r];
+    x.qs = min(max(s, 0), a.T);
+    x.nq = max(min(e, a.T) - x.qs, 0);
+    x.kv = min(max(kv, 0), a.cap);
+    int lo = 0, hi = a.P + 1;                              // how many groups begin at or in front of it
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if (g_start[mid] <= r) lo = mid + 1;
+      else hi = mid;
+    }
+    if (lo > 0 && lo <= a.P) {
+      x.group = lo - 1;
+      x.pre = g_kv[lo - 1];
+    }
+    const int rows = x.nq * a.G;
+    const Blocks32 b = blocks_of(rows, many);
+    x.few = b.few;
+    x.blocks = b.blocks;
+    x.together = rows <= kFewRows && x.pre > 0;
+    x.tiles = (x.kv + kTile - 1) / kTile + (x.together ? 0 : (x.pre + kTile - 1) / kTile);
+    return x;
+  };
+  __syncthreads();
+
+  // ---- rows that go through a prefix together; all work
+  int placed = 0;
+  unsigned long long work = 0;
+  for (int r0 = 0; r0 < a.R; r0 += kPlanThreads) {
+    const int r = r0 + tid;
+    const Entry x = entry(r);
+    const int n = x.together ? x.nq : 0;
+    int all;
+    const int upto = placed + block_inclusive_sum<kPlanWaves>(n, waves[(r0 / kPlanThreads) & 1], all), at = upto - n;
+    for (int j = 0; j < n; ++j)
+      if (at + j < a.T) a.tokens[at + j] = x.qs + j;
+    if (x.group >= 0) {
+      if (r == g_start[x.group]) g_first[x.group] = at;
+      if (r == g_start[x.group + 1] - 1) g_end[x.group] = upto;
+    }
+    work += (unsigned long long)x.blocks * x.tiles;
+    placed += all;
+  }
+  __syncthreads();
+  Blocks32 gb = {0, 0};
+  int g_tiles = 0;
+  if (tid < a.P) {
+    gb = blocks_of((g_end[tid] - g_first[tid]) * a.G, many);
+    g_tiles = (g_kv[tid] + kTile - 1) / kTile;
+    work += (unsigned long long)gb.blocks * g_tiles;
+  }
+  atomicAdd(&s_work, work);                                // (whole numbers: in any order)
+  __syncthreads();
+  const unsigned long long each = (s_work + a.target - 1) / a.target;
+  const int per = each < 1 ? 1 : each > 0x3fffffff ? 0x3fffffff : (int)each;    // tiles of a part, at most
+  const auto parts_of = [&](int tiles, int few) {
+    const int most = max(per, few ? 2 : 4);
+    return tiles <= most ? 1 : (tiles + most - 1) / most;
+  };
+  int units = 0, joins = 0, parts = 0;
+
+  // The entry of this workgroup's that a unit belongs to.
+  const auto owner = [&](int u, int n) {
+    int lo = 0, hi = n;                                    // the last that begins at or in front of it
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) / 2;
+      if (s_unit[mid] <= u) lo = mid;
+      else hi = mid;
+    }
+    return lo;
+  };
+  const auto put = [&](int u, int part, int4 w0, int4 w1, int4 w2, int4 w3) {
+    if (u >= a.most_units) return;                         // (never of lengths that ascend)
+    if (part >= a.units) w0.w = w2.z = w3.x = w3.y = w3.z = w3.w = 0;
+    int4* d = a.plan + (int64_t)u * 4;
+    d[0] = w0; d[1] = w1; d[2] = w2; d[3] = w3;
+  };
+
+  // ---- units of the prefixes
+  {
+    const int n = parts_of(g_tiles, gb.few), mine = gb.blocks * n;
+    int all;
+    const int before = block_inclusive_sum<kPlanWaves>(mine, waves[2], all) - mine;
+    s_unit[tid] = before;
+    s_parts[tid] = n;
+    if (tid < a.P) {
+      g_part[tid] = before;
+      g_parts[tid] = n;
+    }
+    __syncthreads();
+    for (int u = tid; u < all; u += kPlanThreads) {
+      const int e = owner(u, a.P), rest = u - s_unit[e], b = rest / s_parts[e], p = rest - b * s_parts[e];
+      const int rows = (g_end[e] - g_first[e]) * a.G, tiles = (g_kv[e] + kTile - 1) / kTile;
+      const Blocks32 k = blocks_of(rows, many);
+      const int rb = k.few ? 32 : many, i0 = b * rb, j = i0 / a.G, q = tiles / s_parts[e], rem = tiles - q * s_parts[e];
+      const int lo = p * q + min(p, rem), hi = lo + q + (p < rem ? 1 : 0);
+      put(u, u, make_int4(k.few, e, 0, u), make_int4(0, 0, 0, g_kv[e]), make_int4(g_first[e] + j, i0 - j * a.G, min(rb, rows - i0), g_end[e] - 1),
+          make_int4(lo, hi, 0, 0));
+    }
+    units = parts = all;
+  }
+
+  // ---- units of the requests, and what is joined
+  placed = 0;
+  for (int r0 = 0; r0 < a.R; r0 += kPlanThreads) {
+    const Entry x = entry(r0 + tid);
+    const int n = parts_of(x.tiles, x.few), apart = x.together || n > 1;
+    int all_units, all_joins, all_parts, all_placed;
+    __syncthreads();                                       // (the entries before are done with)
+    const int u1 = block_inclusive_sum<kPlanWaves>(x.blocks * n, waves[0], all_units);
+    const int j1 = block_inclusive_sum<kPlanWaves>(apart ? x.blocks : 0, waves[1], all_joins);
+    const int p1 = block_inclusive_sum<kPlanWaves>(apart ? x.blocks * n : 0, waves[2], all_parts);
+    const int t = x.together ? x.nq : 0, t1 = block_inclusive_sum<kPlanWaves>(t, waves[3], all_placed);
+    s_unit[tid] = u1 - x.blocks * n;
+    s_join[tid] = j1 - (apart ? x.blocks : 0);
+    s_part[tid] = apart ? p1 - x.blocks * n : -1;
+    s_parts[tid] = n;
+    s_blocks[tid] = x.blocks;
+    s_qs[tid] = x.qs; s_nq[tid] = x.nq; s_kv[tid] = x.kv;
+    s_group[tid] = x.group;
+    s_place[tid] = x.together ? placed + t1 - t : -1;      // of its first token
+    __syncthreads();
+    for (int u = tid; u < all_units; u += kPlanThreads) {
+      const int e = owner(u, kPlanThreads), n = s_parts[e], rest = u - s_unit[e], b0 = rest / n, p = rest - b0 * n;
+      const int b = s_blocks[e] - 1 - b0;                  // (a chunk's last rows see the most keys: first)
+      const int nq = s_nq[e], kv = s_kv[e], rows = nq * a.G, group = s_group[e], together = s_place[e] >= 0;
+      const Blocks32 k = blocks_of(rows, many);
+      const int rb = k.few ? 32 : many, i0 = b * rb, j0 = i0 / a.G, g0 = i0 - j0 * a.G, take = min(rb, rows - i0);
+      const int past = kv - nq, p1 = past + (i0 + take - 1) / a.G;
+      const int pre = group >= 0 ? g_kv[group] : 0, pre_tiles = together ? 0 : (pre + kTile - 1) / kTile, tiles = pre_tiles + (p1 < 0 ? 0 : p1 / kTile + 1);
+      const int q = tiles / n, rem = tiles - q * n, lo = p * q + min(p, rem), hi = lo + q + (p < rem ? 1 : 0);
+      const int part = s_part[e] >= 0 ? parts + s_part[e] + b0 * n + p : -1;
+      put(units + u, part, make_int4(k.few, group < 0 ? 0 : group, r0 + e, part), make_int4(s_qs[e], past, kv, pre), make_int4(j0, g0, take, -1),
+          make_int4(min(lo, pre_tiles), min(hi, pre_tiles), max(lo, pre_tiles) - pre_tiles, max(hi, pre_tiles) - pre_tiles));
+      const int join = joins + s_join[e] + b0;
+      if (p == 0 && part >= 0 && join < a.most_joins) {
+        int4 w = make_int4(g0, 0, 0, 0);
+        if (together) {
+          const bool big = !blocks_of((g_end[group] - g_first[group]) * a.G, many).few;
+          w = make_int4(g0, g_part[group], g_parts[group] << 1 | (big ? 1 : 0), (s_place[e] - g_first[group]) * a.G + i0);
+        }
+        a.joins[2 * join] = make_int4(part, n, take, s_qs[e] + j0);
+        a.joins[2 * join + 1] = w;
+      }
+    }
+    units += all_units;
+    joins += all_joins;
+    parts += all_parts;
+    placed += all_placed;
+  }
+  if (tid == 0) {
+    a.counts[0] = min(units, a.most_units);
+    a.counts[1] = min(joins, a.most_joins);
+  }
+}
+
+// ---- the units ------------------------------------------------------------------------------------
+template <int DT, int D>
+__global__ __launch_bounds__(256, DT == ZC_F32 && D == 128 ? 1 : 2) void k_shared_attention(SharedArgs a) {
+  constexpr int kBytes = DT == ZC_F32 ? RowsMemory<DT, D, 4>::kBytes : kStages<D> * 2 * kTile * Tile<DT, D>::ROWB;
+  static_assert(kBytes >= RowsMemory<DT, D, 4>::kBytes, "blocks of few rows find room");
+  __shared__ __align__(1024) uint8_t mem[kBytes];
+  __shared__ float sum[4][2][64];
+  typedef __attribute__((address_space(4))) const int* scalar;
+  const int u = unit_of_grid();
+  if (u >= ((scalar)(uintptr_t)a.counts)[0]) return;
+  const scalar d = (scalar)(uintptr_t)(a.plan + (int64_t)u * 4);
+  SharedUnit x;
+  const int group = d[1], r = d[2];
+  x.part = d[3];
+  x.qs = d[4]; x.past = d[5];
+  x.j0 = d[8]; x.g0 = d[9]; x.rows = d[10]; x.last = d[11];
+  x.tokens = a.tokens;
+  x.tables[0] = a.pre_table + group * a.pre_row; x.columns[0] = a.pre_cols; x.keys[0] = d[7]; x.from[0] = d[12]; x.to[0] = d[13];
+  x.tables[1] = a.table + r * a.row; x.columns[1] = a.cols; x.keys[1] = d[6]; x.from[1] = d[14]; x.to[1] = d[15];
+  x.segments = x.from[0] < x.to[0] && x.from[1] < x.to[1] ? 2 : 1;
+  if constexpr (DT != ZC_F32) {
+    if (!d[0]) {
+      attend_tiles<DT, D>(a, x, blockIdx.x, mem);
+      return;
+    }
+  }
+  attend_rows<DT, D, 4>(a, x, blockIdx.x, mem, sum);
+}
+
+// ---- the join -------------------------------------------------------------------------------------
+// As the paged attention's: four workgroups a block, D / 4 threads a row; a row's parts are its own request's and those of its place
+// among the rows that went through the prefix together.
+template <int DT, int D>
+__global__ __launch_bounds__(256) void k_shared_join(SharedArgs a) {
+  constexpr int TPR = D / 4, GROUPS = 256 / TPR;
+  __shared__ __align__(16) float so[GROUPS][D];
+  __shared__ float2 sml[GROUPS];
+  const int turn = (int)blockIdx.x / a.Hkv, hk = blockIdx.x - turn * a.Hkv, join = unit_of_grid();
+  if (join >= a.counts[1]) return;
+  const int4 w = a.joins[2 * join], v = a.joins[2 * join + 1];
+  const int first = w.x, own = w.y, rows = w.z, pre = v.z >> 1, shift = v.z & 1 ? 7 : 5, parts = own + pre;
+  if (first + own > a.units) return;
+  const int grp = threadIdx.x / TPR, c = threadIdx.x % TPR * 4;
+  for (int row0 = turn * GROUPS; row0 < rows; row0 += kSharedJoinGroups * GROUPS) {
+    const int n = min(rows - row0, GROUPS);
+    int ways = 1;                                          // groups to a row
+    while (2 * ways * n <= GROUPS && 2 * ways <= parts) ways *= 2;
+    const int way = grp & (ways - 1), row = row0 + grp / ways;
+    const bool mine = row < row0 + n;
+    const int i = v.w + row, pre0 = v.y + (i >> shift) * pre, pre_row = i & ((1 << shift) - 1);
+    float M = kLowestLogit, l = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (mine && (pre == 0 || pre0 + pre <= a.units)) {
+      constexpr int U = 4;                                 // parts requested at a time
+      for (int s0 = way; s0 < parts; s0 += U * ways) {
+        float2 ml[U];
+        float4 t[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int s = s0 + u * ways < parts ? s0 + u * ways : s0;
+          const int64_t p = s < pre ? part_row(a, hk, pre0 + s) + pre_row : part_row(a, hk, first + s - pre) + row;
+          ml[u] = *reinterpret_cast<const float2*>(a.part_ml + p * 2);
+          t[u] = *reinterpret_cast<const float4*>(a.part_o + p * D + c);
+        }
+        float top = M;
+#pragma unroll
+        for (int u = 0; u < U; ++u) top = fmaxf(top, ml[u].x);
+        const float f0 = __builtin_amdgcn_exp2f(M - top);
+        M = top;
+        l *= f0; o.x *= f0; o.y *= f0; o.z *= f0; o.w *= f0;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const float f = s0 + u * ways < parts ? __builtin_amdgcn_exp2f(ml[u].x - M) : 0.f;
+          l = fmaf(ml[u].y, f, l);
+          o.x = fmaf(t[u].x, f, o.x); o.y = fmaf(t[u].y, f, o.y); o.z = fmaf(t[u].z, f, o.z); o.w = fmaf(t[u].w, f, o.w);
+        }
+      }
+    }
+    if (ways > 1) {
+      if (c == 0) sml[grp] = make_float2(M, l);
+      *reinterpret_cast<float4*>(&so[grp][c]) = o;
+      __syncthreads();
+      if (mine && way == 0) {
+        for (int y = 1; y < ways; ++y) {
+          const float2 ml = sml[grp + y];
+          const float4 t = *reinterpret_cast<const float4*>(&so[grp + y][c]);
+          const float top = fmaxf(M, ml.x), f0 = __builtin_amdgcn_exp2f(M - top), f = __builtin_amdgcn_exp2f(ml.x - top);
+          M = top;
+          l = fmaf(ml.y, f, l * f0);
+          o.x = fmaf(t.x, f, o.x * f0); o.y = fmaf(t.y, f, o.y * f0); o.z = fmaf(t.z, f, o.z * f0); o.w = fmaf(t.w, f, o.w * f0);
+        }
+      }
+      __syncthreads();
+    }
+    if (mine && way == 0) store_row<DT>(a, w.w, v.x, hk, row, c, M, l, o);
+  }
+}
+
+// ---- host ---------------------------------------------------------------------------------------------
+// How large a step can get, of one head: units, partial results (of how many rows), joins.  (target: what splitting aims at.)
+struct Most { int64_t target, units, parts, joins, slot, bytes; };
+static Most most_of(int64_t P, int64_t R, int64_t T, int64_t G, int64_t Hkv, bool fp32, int64_t D) {
+  Most m;
+  const int64_t with = R < T ? R : T, rows = T * G, many = fp32 ? 32 : 128, groups = P < with ? P : with;
+  m.slot = fp32 || rows <= kFewRows ? 32 : 128;
+  m.target = ceil_div64(512, Hkv);
+  // (a request has one block that is not full; where blocks of 128 rows are the rule, one of 33 to 64 rows is two of 32)
+  const int64_t two = rows / 33 < with ? rows / 33 : with, blocks = rows / many + with + two;
+  const int64_t few = rows / 32 + with < 2 * with ? rows / 32 + with : 2 * with;
+  const int64_t together = rows < kFewRows * with ? rows : kFewRows * with, pre = together / many + 2 * groups;
+  // a block is cut into at most tiles / (all work / target) + 1 parts; one of many rows leaves none if it is not cut
+  m.units = m.target + blocks + pre;
+  m.parts = 2 * m.target + few + pre;
+  m.joins = blocks;
+  m.bytes = (int64_t)Hkv * m.parts * m.slot * (D + 2) * 4 + m.units * 64 + m.joins * 32 + align_up64(T * 4, 16) + 16;
+  return m;
+}
+
+template <int DT, int D>
+static int launch_shared(SharedArgs& a, hipStream_t st) {
+  hipLaunchKernelGGL(k_shared_plan, dim3(1), dim3(kPlanThreads), 0, st, a, DT == ZC_F32 ? 32 : 128);
+  ZC_LAUNCH_CHECK();
+  const auto grid = [](int64_t x, int64_t n) { return dim3((unsigned)x, (unsigned)(n < 65535 ? n : 65535), (unsigned)ceil_div64(n, 65535)); };
+  hipLaunchKernelGGL((k_shared_attention<DT, D>), grid(a.Hkv, a.most_units), dim3(256), 0, st, a);
+  ZC_LAUNCH_CHECK();
+  hipLaunchKernelGGL((k_shared_join<DT, D>), grid(a.Hkv * kSharedJoinGroups, a.most_joins), dim3(256), 0, st, a);
+  ZC_LAUNCH_CHECK();
+  return ZC_OK;
+}
+
+}  // namespace zc
+
+using namespace zc;
+
+// (the larger of what fp32 and 16-bit calls take, and of what a step without a prefix does)
+extern "C" size_t zc_paged_shared_attention_workspace(int64_t P, int64_t R, int64_t T, int64_t Hq, int64_t Hkv, int64_t D) {
+  if (P < 0 || R <= 0 || T <= 0 || Hkv <= 0 || Hq < Hkv || Hq % Hkv || D <= 0 || T > 0x7fffffff / Hq) return 0;
+  const size_t none = zc_paged_attention_workspace(R, T, Hq, Hkv, D);
+  if (P == 0) return none;
+  const size_t x = (size_t)most_of(P, R, T, Hq / Hkv, Hkv, true, D).bytes, y = (size_t)most_of(P, R, T, Hq / Hkv, Hkv, false, D).bytes;
+  const size_t more = x > y ? x : y;
+  return none > more ? none : more;
+}
+
+extern "C" int zc_paged_shared_attention(const zc_tensor4* q, const zc_tensor4* k_pages, const zc_tensor4* v_pages, const int32_t* prefix_table,
+                                         int64_t prefix_row_stride, int64_t prefix_max_blocks, const int32_t* prefix_len, const int32_t* group_start,
+                                         int64_t P, const int32_t* block_table, int64_t row_stride, int64_t max_blocks, const int32_t* q_start,
+                                         const int32_t* kv_len, int64_t R, float sm_scale, const zc_tensor4* out, float* lse, void* ws,
+                                         size_t ws_bytes, void* stream) {
+  int rc = zc_validate_pages(k_pages, v_pages);
+  if (rc) return rc;
+  rc = zc_validate_heads(q, k_pages);
+  if (rc) return rc;
+  rc = zc_validate_heads(out, k_pages);
+  if (rc) return rc;
+  if (q->H != out->H || q->L != out->L || q->H % k_pages->H || !zc_rows_apart(out)) return ZC_ERR_INVALID_ARG;
+  if (P < 0 || R < 0 || !(sm_scale >= 0.f) || !(sm_scale * kLog2e <= -kLowestLogit)) return ZC_ERR_INVALID_ARG;
+  if (max_blocks < 0 || row_stride < max_blocks || prefix_max_blocks < 0 || prefix_row_stride < prefix_max_blocks) return ZC_ERR_INVALID_ARG;
+  if (q->L == 0 || R == 0) return ZC_OK;
+  if (!q_start || !kv_len || (max_blocks > 0 && !block_table)) return ZC_ERR_INVALID_ARG;
+  if (P > 0 && (!prefix_len || !group_start || (prefix_max_blocks > 0 && !prefix_table))) return ZC_ERR_INVALID_ARG;
+  for (const void* p : {(const void*)block_table, (const void*)q_start, (const void*)kv_len, (const void*)lse, (const void*)prefix_table,
+                        (const void*)prefix_len, (const void*)group_start})
+    if (reinterpret_cast<uintptr_t>(p) & 3) return ZC_ERR_INVALID_ARG;
+  if (P > kGroups) return ZC_ERR_UNSUPPORTED;
+  if (P == 0 || prefix_max_blocks == 0)                  // no prefix has a token
+    return zc_paged_attention(q, k_pages, v_pages, block_table, row_stride, max_blocks, q_start, kv_len, R, 0, 0, sm_scale, out, lse, ws, ws_bytes, stream);
+  const int64_t T = q->L, Hkv = k_pages->H, G = q->H / Hkv;
+  if (R >= (1 << 24) || max_blocks > 0x7fffffff || prefix_max_blocks > 0x7fffffff || T > 0x7fffffff / q->H || q->H > 65535 || G > 4096)
+    return ZC_ERR_UNSUPPORTED;
+  const int64_t page = k_pages->L;
+  const auto room = [&](int64_t blocks) { return blocks > 0x7fff0000 / page ? 0x7fff0000 : blocks * page; };
+  const Most m = most_of(P, R, T, G, Hkv, q->dtype == ZC_F32, q->D);
+  if (m.units * Hkv > 0xffffff) return ZC_ERR_UNSUPPORTED;
+  const size_t need = zc_paged_shared_attention_workspace(P, R, T, q->H, Hkv, q->D);
+  if (!ws || ws_bytes < need || (reinterpret_cast<uintptr_t>(ws) & 15)) return ZC_ERR_WORKSPACE;
+
+  const int64_t eb = elem_bytes(q->dtype);
+  SharedArgs a;
+  a.q = (const uint8_t*)q->ptr; a.k = (const uint8_t*)k_pages->ptr; a.v = (const uint8_t*)v_pages->ptr; a.o = (uint8_t*)out->ptr;
+  a.q_sH = q->sH * eb; a.q_sT = q->sL * eb; a.o_sH = out->sH * eb; a.o_sT = out->sL * eb;
+  a.k_sB = (uint32_t)(k_pages->sB * eb); a.k_sH = k_pages->sH * eb; a.v_sB = (uint32_t)(v_pages->sB * eb); a.v_sH = v_pages->sH * eb;
+  a.k_row = (uint32_t)(k_pages->sL * eb); a.v_row = (uint32_t)(v_pages->sL * eb);
+  // (a table without columns holds no token: any readable word stands for its pages)
+  a.table = max_blocks ? block_table : q_start; a.q_start = q_start; a.kv_len = kv_len; a.row = max_blocks ? row_stride : 0;
+  a.cols = max_blocks ? (int)max_blocks : 1; a.shift = __builtin_ctzll((unsigned long long)page); a.n_pages = (int)k_pages->B; a.cap = (int)room(max_blocks);
+  a.R = (int)R; a.T = (int)T; a.Hkv = (int)Hkv; a.G = (int)G;
+  a.window = a.sinks = 0;
+  a.scale_log2 = (sm_scale == 0.f ? 1.0f / sqrtf((float)q->D) : sm_scale) * kLog2e;
+  a.lse = lse;
+  a.target = (int)m.target;
+  a.units = (int)m.parts;
+  a.over_G = G == 1 ? 0 : (uint32_t)(((1ull << 32) + G - 1) / G);
+  a.reach = 0x7fffffff;
+  a.slot = (int)m.slot;
+  a.coarse = 0;
+  a.todo = nullptr;
+  a.pre_table = prefix_table; a.pre_len = prefix_len; a.group_start = group_start; a.pre_row = prefix_row_stride;
+  a.pre_cols = (int)prefix_max_blocks; a.pre_cap = (int)room(prefix_max_blocks); a.P = (int)P;
+  a.most_units = (int)m.units; a.most_joins = (int)m.joins;
+  uint8_t* at = (uint8_t*)ws;
+  a.counts = (int*)at; at += 16;
+  a.plan = (int4*)at; at += m.units * 64;
+  a.joins = (int4*)at; at += m.joins * 32;
+  a.tokens = (int*)at; at += align_up64(T * 4, 16);
+  a.part_o = (float*)at;
+  a.part_ml = a.part_o + Hkv * m.parts * m.slot * q->D;
+  hipStream_t st = (hipStream_t)stream;
+#define ZC_SA(DT) (q->D == 128 ? launch_shared<DT, 128>(a, st) : launch_shared<DT, 64>(a, st))
+  if (q->dtype == ZC_F32) rc = ZC_SA(ZC_F32);
+  else if (q->dtype == ZC_F16) rc = ZC_SA(ZC_F16);
+  else rc = ZC_SA(ZC_BF16);
+#undef ZC_SA
+  return rc;
+}

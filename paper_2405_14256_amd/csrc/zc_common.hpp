@@ -139,6 +139,18 @@ __device__ inline int wave_inclusive_sum(int v) {
   return v;
 }
 
+// Sum over a workgroup's threads up to this one (NW waves) and over all; waves: LDS of NW words, another for uses with no barrier between.
+template <int NW>
+__device__ inline int block_inclusive_sum(int v, int* waves, int& total) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  v = wave_inclusive_sum(v);
+  if (lane == 63) waves[w] = v;
+  __syncthreads();
+  const int upto = wave_inclusive_sum(lane < NW ? waves[lane] : 0);
+  total = __builtin_amdgcn_readlane(upto, NW - 1);
+  return v + (w ? __builtin_amdgcn_readlane(upto, w - 1) : 0);
+}
+
 }  // namespace zc
 
 // Host-side validation shared by the entry points (defined in api.hip).
