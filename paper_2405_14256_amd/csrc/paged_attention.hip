@@ -8,8 +8,7 @@
 namespace zc {
 
 struct Unit {
-  static constexpr int kSegments = 1;
-  __device__ void enter(const PagedArgs&, int) {}
+  static constexpr int kFirst = 0;
   int r, qs, nq, kv;            // request, its first row, new tokens, tokens
   bool few;
   int j0, g0, rows;             // token and head of the block's first row, its rows
@@ -21,10 +20,25 @@ struct Unit {
 };
 
 __device__ inline Row row_at(const PagedArgs& a, const Unit& x, int r) { return row_at(a, x.j0, x.g0, r); }
+__device__ inline Row row_of(const PagedArgs& a, const Unit& x, int r) { return row_at(a, x, r); }
 __device__ inline int position(const Unit& x, int j) { return x.kv - x.nq + j; }
 __device__ inline int tile_of(const Unit& x, int t) { return t < x.sink_tiles ? t : x.first + t - x.sink_tiles; }
-__device__ inline const int32_t* table_row(const PagedArgs& a, const Unit& x) { return a.table + x.r * a.row; }
-__device__ inline int table_cols(const PagedArgs& a, const Unit&) { return a.cols; }
+__device__ inline int tile_at(const Unit& x, int pos) { return pos / kTile - x.first + x.sink_tiles; }
+__device__ inline const int32_t* entry_of(const PagedArgs& a, const Unit& x, int key0) { return a.table + x.r * a.row + min(key0 >> a.shift, a.cols - 1); }
+__device__ inline int keys_read(const PagedArgs& a, const Unit& x, int end, int key0, int id) { return keys_read(a.n_pages, a.sinks, x.behind, end, key0, id); }
+__device__ inline __amdgpu_buffer_rsrc_t keys_at(const PagedArgs& a, const Unit&, const uint8_t* head, uint32_t sB, uint32_t row, int key0, int id, int n) {
+  return keys_at(a.shift, head, sB, row, key0, id, n);
+}
+__device__ inline Seen seen_by(const PagedArgs& a, const Unit&, int p0, int p1) {
+  Seen s;
+  s.low = a.window ? max(max(p1, 0) - a.window + 1, 0) : 0;
+  const int end = max(p0, 0) - 30;                         // (of positions in front of the first key no block is seen)
+  s.span = max(end - s.low, 0);
+  s.sink = a.window ? min(a.sinks - 31, end) : 0;
+  return s;
+}
+__device__ inline int low_of(const PagedArgs& a, const Unit&, int pos) { return a.window && pos >= 0 ? pos - a.window : -1; }
+__device__ inline int sinks_of(const PagedArgs& a, const Unit&) { return a.sinks; }
 __device__ inline bool is_whole(const Unit& x) { return x.parts == 1; }
 __device__ inline int64_t part_of(const PagedArgs& a, const Unit&, int hk) { return part_row(a, hk, unit_of_grid()); }
 

@@ -13,12 +13,15 @@
 // 2.10e-4.  Weights as a rounded part and a remainder would take the second product twice.
 //
 // A unit of work is a block of rows and a part of the key tiles it sees, described by an X of the kernel's own:
-//   kSegments, segments     ranges of keys that lie behind different rows of tables, at most and of this unit: enter(a, s) fills in what follows
-//   rows, kv, p0, p1        rows of the block; tokens of the range; positions of the block's first and last row in it
-//   t_lo, t_hi, behind      tiles of this unit; 16 keys from key0 on are behind every window if key0 - sinks, without sign, is less
-//   qs                      token of a row: qs + row_at(a, x, r).j
-//   first, sink_tiles       tile t is t of the first sink_tiles, then first + t - sink_tiles
-// and by the functions row_at, position, tile_of, table_row, table_cols, is_whole (nothing to join) and part_of (where its partial results go).
+//   rows, kv, p0, p1        rows of the block; tokens; positions of the block's first and last row
+//   kFirst                  the least position of a row that sees a key
+//   t_lo, t_hi              tiles of this unit
+//   first, sink_tiles       tile t is of the keys behind those of tile t - 1, tile sink_tiles of those from first * kTile on
+//   qs                      token of a row: qs + row_of(a, x, r).j; where nothing is to be joined, and for its position, qs + row_at(a, x, r).j
+//   behind                  16 keys from key0 on are behind every window if key0 - sinks, without sign, is less
+// and by functions that are found by its type: row_at, row_of, position, tile_of and tile_at (tiles and their keys), entry_of, keys_read and keys_at
+// (where keys lie), seen_by, low_of and sinks_of (who sees them: keys up to low, from sinks on, are hidden), is_whole (nothing is to be joined), part_of (where
+// partial results go).
 #pragma once
 
 #include <limits.h>
@@ -86,24 +89,15 @@ __device__ inline Row row_at(const PagedArgs& a, int j0, int g0, int r) {
 }
 __device__ inline int unit_of_grid() { return blockIdx.y + 65535 * blockIdx.z; }
 
-template <class X> __device__ inline int page_of(const PagedArgs& a, const X& x, int key0) { return page_of(table_row(a, x), table_cols(a, x), a.shift, key0); }
-template <class X> __device__ inline int keys_read(const PagedArgs& a, const X& x, int end, int key0, int id) {
-  return keys_read(a.n_pages, a.sinks, x.behind, end, key0, id);
-}
-__device__ inline __amdgpu_buffer_rsrc_t keys_at(const PagedArgs& a, const uint8_t* head, uint32_t sB, uint32_t row, int key0, int id, int n) {
-  return keys_at(a.shift, head, sB, row, key0, id, n);
+// The page of 16 keys from key0 on (past the table: any, no key is read).
+template <class X> __device__ inline int page_of(const PagedArgs& a, const X& x, int key0) {
+  return *(__attribute__((address_space(4))) const int32_t*)(uintptr_t)entry_of(a, x, key0);
 }
 // The blocks of 32 keys that every row from position p0 to p1 sees whole: those from `low` on, `span` of them by their first key, and
 // those whose first key is below `sink`.
 struct Seen {
   int low, sink;
   uint32_t span;
-  __device__ Seen(const PagedArgs& a, int p0, int p1) {
-    low = a.window ? max(max(p1, 0) - a.window + 1, 0) : 0;
-    const int end = max(p0, 0) - 30;                       // (of positions in front of the first key no block is seen)
-    span = max(end - low, 0);
-    sink = a.window ? min(a.sinks - 31, end) : 0;
-  }
   // Blocks of 32 + more keys.
   __device__ bool whole(int key0, int more = 0) const { return (uint32_t)(key0 - low) < (uint32_t)max((int)span - more, 0) || key0 < sink - more; }
 };
@@ -133,7 +127,7 @@ struct RowsMemory {
   static constexpr int kBytes = 2 * NW * kBlock;
 };
 template <int DT, int D, int NW, class X>
-__device__ __forceinline__ void attend_rows(const PagedArgs& a, X x, int hk, uint8_t* mem, float (*sum)[2][64]) {
+__device__ __forceinline__ void attend_rows(const PagedArgs& a, const X& x, int hk, uint8_t* mem, float (*sum)[2][64]) {
   using T = Tile<DT, D>;
   constexpr int BLK = RowsMemory<DT, D, NW>::kBlock;
   constexpr int NT = BLK / 1024;                 // transfers of a block
@@ -174,17 +168,11 @@ __device__ __forceinline__ void attend_rows(const PagedArgs& a, X x, int hk, uin
   auto issue = [&](const Ids& s, const uint8_t* head, uint32_t sB, uint32_t row, uint32_t lds, const int (&voff)[PG]) {
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
-      const auto rs = keys_at(a, head, sB, row, s.key0 + 16 * g, s.id[g], s.n[g]);
+      const auto rs = keys_at(a, x, head, sB, row, s.key0 + 16 * g, s.id[g], s.n[g]);
       move_keys<PG>(lds + g * 16 * T::ROWB, rs, voff);
     }
   };
 
-  u32x4 qf[T::NKC];
-  v16f oacc[CT];
-  float m, l;                                    // running maximum (log2 units), this half-wave's share of the sum
-  int seg = 0;
-[[maybe_unused]] range:                          // (a loop around one range took the chunks' kernel of 64 channels from 161 registers to 194)
-  x.enter(a, seg);
   // (the tile of the last row's own token may have one block only)
   int blocks = 2 * (x.t_hi - x.t_lo);
   if (blocks > 0 && tile_of(x, x.t_hi - 1) * kTile + 32 > x.p1) --blocks;
@@ -196,11 +184,12 @@ __device__ __forceinline__ void attend_rows(const PagedArgs& a, X x, int hk, uin
   const Row me = row_at(a, x, r);
   const int64_t hq = hk * a.G + me.g, tok = x.qs + me.j;
   const int pos = mine ? position(x, me.j) : -1;
-  if (seg == 0)
+  u32x4 qf[T::NKC];
 #pragma unroll
-    for (int kc = 0; kc < T::NKC; ++kc) qf[kc] = u32x4{0, 0, 0, 0};
-  if (seg == 0 && mine) {
-    const uint8_t* qr = a.q + hq * a.q_sH + tok * a.q_sT + kh * 16;
+  for (int kc = 0; kc < T::NKC; ++kc) qf[kc] = u32x4{0, 0, 0, 0};
+  if (mine) {
+    const Row from = row_of(a, x, r);
+    const uint8_t* qr = a.q + (hk * a.G + from.g) * a.q_sH + (int64_t)(x.qs + from.j) * a.q_sT + kh * 16;
 #pragma unroll
     for (int kc = 0; kc < T::NKC; ++kc) qf[kc] = *reinterpret_cast<const u32x4*>(qr + kc * 32);
   }
@@ -220,14 +209,12 @@ __device__ __forceinline__ void attend_rows(const PagedArgs& a, X x, int hk, uin
     else vaddr[ct] = v_lds + vkey * T::ROWB + (((4 * ct + vsub) ^ v_slot<DT, D>(vkey)) << 4) + (lane & 1) * 8;
   }
 
-  if (seg == 0) {
+  v16f oacc[CT];
 #pragma unroll
-    for (int ct = 0; ct < CT; ++ct) oacc[ct] = v16f{};
-    m = kLowestLogit;
-    l = 0.f;
-  }
+  for (int ct = 0; ct < CT; ++ct) oacc[ct] = v16f{};
+  float m = kLowestLogit, l = 0.f;   // running maximum (log2 units), this half-wave's share of the sum
 
-  const Seen seen(a, x.p0, x.p1);
+  const Seen seen = seen_by(a, x, x.p0, x.p1);
   wait_all_loads();                              // (the rows and the first blocks: the compiler would wait for the rows in the loop, and so for the next blocks)
   for (; t < blocks; t += NW) {
     const bool more = t + NW < blocks;
@@ -247,11 +234,11 @@ __device__ __forceinline__ void attend_rows(const PagedArgs& a, X x, int hk, uin
     dma_reuse_fence();
     if (more) issue(at, kb, a.k_sB, a.k_row, k_lds, kvoff);
     if (!seen.whole(key0)) {
-      const int low = a.window && pos >= 0 ? pos - a.window : -1;          // keys up to it are seen as sinks only
+      const int low = low_of(a, x, pos), sinks = sinks_of(a, x);           // keys up to `low` are seen as sinks only
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
         const int key = key0 + acc_row(v, kh);
-        if ((key > pos) | ((key <= low) & (key >= a.sinks))) s[v] = -INFINITY;
+        if ((key > pos) | ((key <= low) & (key >= sinks))) s[v] = -INFINITY;
       }
     }
     // (the maximum is taken over the raw products - the scale is not negative - and the scale enters with the subtraction)
@@ -309,9 +296,6 @@ __device__ __forceinline__ void attend_rows(const PagedArgs& a, X x, int hk, uin
     dma_reuse_fence();
     if (more) issue(at, vb, a.v_sB, a.v_row, v_lds, vvoff);
   }
-
-  if constexpr (X::kSegments > 1)
-    if (++seg < x.segments) goto range;
 
   // ---- join the waves: all outputs to LDS, each wave finishes an equal part of the channels ----
   // (a wave without keys has m = kLowestLogit, l = 0 and zeros)
@@ -378,7 +362,7 @@ __device__ __forceinline__ void attend_rows(const PagedArgs& a, X x, int hk, uin
 // tile is worth 0.2 us of matrix instructions there, less than a trip to memory.
 template <int D> constexpr int kStages = D == 64 ? 3 : 2;
 template <int DT, int D, class X>
-__device__ __forceinline__ void attend_tiles(const PagedArgs& a, X x, int hk, uint8_t* mem) {
+__device__ __forceinline__ void attend_tiles(const PagedArgs& a, const X& x, int hk, uint8_t* mem) {
   using T = Tile<DT, D>;
   constexpr int KEYS = kTile;
   constexpr int TILE_B = KEYS * T::ROWB;
@@ -397,19 +381,13 @@ __device__ __forceinline__ void attend_tiles(const PagedArgs& a, X x, int hk, ui
   const uint32_t vs_lds = ks_lds + STAGES * TILE_B;
 
   const int wrows = min(max(x.rows - 32 * w, 0), 32);        // this wave's rows
-  u32x4 qf[T::NKC];
-  v16f oacc[CT];
-  float m, l;                                    // running maximum (log2 units), this half-wave's share of the sum
-  int seg = 0;
-[[maybe_unused]] range:
-  x.enter(a, seg);
   // the halves of this unit that the wave's rows see: all up to the last row's
-  const int wp0 = position(x, row_at(a, x, 32 * w).j), wp1 = wrows > 0 ? position(x, row_at(a, x, 32 * w + wrows - 1).j) : -1;
+  const int wp0 = position(x, row_at(a, x, 32 * w).j), wp1 = wrows > 0 ? position(x, row_at(a, x, 32 * w + wrows - 1).j) : INT_MIN;
   const int ntiles = x.t_hi - x.t_lo;
-  const Seen seen(a, wp0, wp1);
+  const Seen seen = seen_by(a, x, wp0, wp1);
   int nh = 0;
-  if (wp1 >= 0) {
-    const int t1 = wp1 / KEYS - x.first + x.sink_tiles - x.t_lo;          // the tile of the last row's own token
+  if (wp1 >= X::kFirst) {
+    const int t1 = tile_at(x, wp1) - x.t_lo;     // the tile of the last row's own token
     nh = t1 < 0 ? 0 : t1 >= ntiles ? 2 * ntiles : 2 * t1 + ((wp1 & 32) ? 2 : 1);
   }
 
@@ -423,7 +401,7 @@ __device__ __forceinline__ void attend_tiles(const PagedArgs& a, X x, int hk, ui
   int ids;
   auto pages = [&](int t) {
     const int key0 = tile_of(x, x.t_lo + t + lane) * KEYS + 16 * w;
-    ids = table_row(a, x)[min(key0 >> a.shift, table_cols(a, x) - 1)];
+    ids = *entry_of(a, x, key0);
   };
   const int turn = x.sink_tiles - x.t_lo;        // the tile behind the sinks'
   auto next_key = [&](int t, int key0, int off) { return t == turn ? x.first * KEYS + off : key0 + KEYS; };     // of tile t, key0 that of the one before
@@ -442,7 +420,7 @@ __device__ __forceinline__ void attend_tiles(const PagedArgs& a, X x, int hk, ui
     g.n = 16;
     if ((uint32_t)(g.key0 - all) >= all_span) g.n = keys_read(a, x, end, g.key0, g.id);
     if ((uint32_t)g.id >= (uint32_t)a.n_pages) g.n = 0;
-    const auto rs = keys_at(a, kb, a.k_sB, a.k_row, g.key0, g.id, g.n);
+    const auto rs = keys_at(a, x, kb, a.k_sB, a.k_row, g.key0, g.id, g.n);
     int v[NI];
     asm volatile("" : "+v"(krow), "+v"(kchunk));
 #pragma unroll
@@ -450,7 +428,7 @@ __device__ __forceinline__ void attend_tiles(const PagedArgs& a, X x, int hk, ui
     move_keys<NI>(ks_lds + place * TILE_B, rs, v);
   };
   auto v_issue = [&](int place, const Group& g) {
-    const auto rs = keys_at(a, vb, a.v_sB, a.v_row, g.key0, g.id, g.n);
+    const auto rs = keys_at(a, x, vb, a.v_sB, a.v_row, g.key0, g.id, g.n);
     int v[NI];
     asm volatile("" : "+v"(vplace));
 #pragma unroll
@@ -461,17 +439,15 @@ __device__ __forceinline__ void attend_tiles(const PagedArgs& a, X x, int hk, ui
 
   // this lane's row, straight into operand registers
   const int pos = r < wrows ? position(x, row_at(a, x, 32 * w + r).j) : INT_MIN;
-  if (seg == 0)
+  u32x4 qf[T::NKC];
 #pragma unroll
-    for (int kc = 0; kc < T::NKC; ++kc) qf[kc] = u32x4{0, 0, 0, 0};
-  if (seg == 0 && r < wrows) {
-    const Row me = row_at(a, x, 32 * w + r);
+  for (int kc = 0; kc < T::NKC; ++kc) qf[kc] = u32x4{0, 0, 0, 0};
+  if (r < wrows) {
+    const Row me = row_of(a, x, 32 * w + r);
     const uint8_t* qr = a.q + (hk * a.G + me.g) * a.q_sH + (int64_t)(x.qs + me.j) * a.q_sT + kh * 16;
 #pragma unroll
     for (int kc = 0; kc < T::NKC; ++kc) qf[kc] = *reinterpret_cast<const u32x4*>(qr + kc * 32);
   }
-  if constexpr (X::kSegments > 1)
-    if (seg) __syncthreads();                    // (the range before is done with LDS)
   Group g[AHEAD + 2];
 #pragma unroll
   for (int t = 0; t < AHEAD + 2; ++t) g[t] = group(t, t ? g[t - 1].key0 : tile_of(x, x.t_lo) * KEYS + 16 * w - KEYS);
@@ -515,12 +491,10 @@ __device__ __forceinline__ void attend_tiles(const PagedArgs& a, X x, int hk, ui
     f.x = l2.x; f.y = l2.y; f.z = h2.x; f.w = h2.y;
   };
 
-  if (seg == 0) {
+  v16f oacc[CT];
 #pragma unroll
-    for (int ct = 0; ct < CT; ++ct) oacc[ct] = v16f{};
-    m = kLowestLogit;
-    l = 0.f;
-  }
+  for (int ct = 0; ct < CT; ++ct) oacc[ct] = v16f{};
+  float m = kLowestLogit, l = 0.f;   // running maximum (log2 units), this half-wave's share of the sum
   KFrag kf;
   v16f s0, s1;
 
@@ -540,11 +514,11 @@ __device__ __forceinline__ void attend_tiles(const PagedArgs& a, X x, int hk, ui
     constexpr bool LAST = decltype(last_c)::value;
     u32x4 vf[2][CT];
     if (!seen_whole) {
-      const int low = a.window && pos >= 0 ? pos - a.window : -1;          // keys up to it are seen as sinks only
+      const int low = low_of(a, x, pos), sinks = sinks_of(a, x);           // keys up to `low` are seen as sinks only
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
         const int key = key0 + acc_row(v, kh);
-        if ((key > pos) | ((key <= low) & (key >= a.sinks))) sc[v] = -INFINITY;
+        if ((key > pos) | ((key <= low) & (key >= sinks))) sc[v] = -INFINITY;
       }
       tmax = half_max(sc);
     }
@@ -644,9 +618,6 @@ __device__ __forceinline__ void attend_tiles(const PagedArgs& a, X x, int hk, ui
   }
   for (; t < ntiles; ++t) top(t);                    // the other waves' tiles: their transfers and barriers
   wait_all_loads();                                  // (nothing is on its way to a workgroup's memory when it ends)
-
-  if constexpr (X::kSegments > 1)
-    if (++seg < x.segments) goto range;
 
   // ---- normalise and store: lane = row, accumulator v of tile ct = channel 32 ct + acc_row(v, kh) ----
   const float l_tot = l + __shfl_xor(l, 32);

@@ -27,43 +27,54 @@ struct SharedArgs : PagedArgs {
   int most_units, most_joins;                   // (units: partial results that there is room for)
 };
 
+// What a unit of the plan is, in words of its entry.
+enum Word { kFew, kGroup, kRequest, kPart, kRow0, kPast, kOwnKeys, kPrefixKeys, kToken, kHead, kRows, kLast, kFrom, kTo, kWords = 16 };
+typedef __attribute__((address_space(4))) const int* plan_ptr;
+
+// A unit's keys are one stream of tiles, those of the prefix in front: its keys have negative positions, -kTile * pre_tiles on, so that the last
+// of its tiles, which need not be full, ends in front of the request's own first key.  The places between, from `hole` to -1, are hidden.
 struct SharedUnit {
-  static constexpr int kSegments = 2;
-  int segments;                 // ranges of keys: the prefix, the request's own
+  static constexpr int kFirst = -1;
+  static constexpr int first = 0, sink_tiles = -(1 << 30);     // (tiles follow each other)
+  static constexpr uint32_t behind = 0;
   int qs, past, j0, g0, rows;   // the request's first row; tokens in front of its new ones; token and head of the block's first row, its rows
   int last;                     // rows of several requests: the block's last place in the list of tokens; -1: of one
-  const int* tokens;
   int part;                     // where its partial results go, -1: nothing to join
-  const int32_t* tables[2];
-  int columns[2], keys[2], from[2], to[2];
-  // the range in hand
-  const int32_t* table;
-  int cols, kv, t_lo, t_hi, p0, p1;
-  bool own;
-  static constexpr int first = 0, sink_tiles = 0;
-  static constexpr uint32_t behind = 0;
-  __device__ void enter(const PagedArgs& a, int s);
+  const int32_t *pre, *own;     // rows of the tables
+  int pre_tiles, hole, kv, t_lo, t_hi, p0, p1;
 };
-__device__ inline Row row_at(const PagedArgs& a, const SharedUnit& x, int r) {
-  Row me = row_at(a, x.j0, x.g0, r);
-  if (x.last >= 0) me.j = x.tokens[min(me.j, x.last)];
+__device__ inline Row row_at(const PagedArgs& a, const SharedUnit& x, int r) { return row_at(a, x.j0, x.g0, r); }
+__device__ inline Row row_of(const PagedArgs& a, const SharedUnit& x, int r) {
+  Row me = row_at(a, x, r);
+  if (x.last >= 0) me.j = static_cast<const SharedArgs&>(a).tokens[min(me.j, x.last)];
   return me;
 }
-__device__ inline int position(const SharedUnit& x, int j) { return x.own ? x.past + j : x.kv - 1; }
-__device__ inline void SharedUnit::enter(const PagedArgs& a, int s) {
-  const int i = segments == 2 ? s : from[0] < to[0] ? 0 : 1;
-  own = i == 1;
-  table = own ? tables[1] : tables[0];
-  cols = own ? columns[1] : columns[0];
-  kv = own ? keys[1] : keys[0];
-  t_lo = own ? from[1] : from[0];
-  t_hi = own ? to[1] : to[0];
-  p0 = own ? past + j0 : kv - 1;
-  p1 = own ? past + row_at(a, j0, g0, rows - 1).j : kv - 1;
+// (rows of several requests, and a row in front of its request's first token, see all of the prefix and nothing else)
+__device__ inline int position(const SharedUnit& x, int j) { return x.last >= 0 ? -1 : max(x.past + j, -1); }
+__device__ inline int tile_of(const SharedUnit& x, int t) { return t - x.pre_tiles; }
+__device__ inline int tile_at(const SharedUnit& x, int pos) { return (pos >> 6) + x.pre_tiles; }
+static_assert(kTile == 64, "tile_at");
+__device__ inline const int32_t* entry_of(const PagedArgs& args, const SharedUnit& x, int key0) {
+  const SharedArgs& a = static_cast<const SharedArgs&>(args);
+  const bool pre = key0 < 0;
+  const int block = (pre ? key0 + x.pre_tiles * kTile : key0) >> a.shift;
+  return pre ? x.pre + min(block, a.pre_cols - 1) : x.own + min(block, a.cols - 1);
 }
-__device__ inline int tile_of(const SharedUnit&, int t) { return t; }
-__device__ inline const int32_t* table_row(const PagedArgs&, const SharedUnit& x) { return x.table; }
-__device__ inline int table_cols(const PagedArgs&, const SharedUnit& x) { return x.cols; }
+__device__ inline int keys_read(const PagedArgs& a, const SharedUnit& x, int end, int key0, int id) {
+  return keys_read(a.n_pages, 0, 0, key0 < 0 ? min(end, x.hole) : end, key0, id);
+}
+__device__ inline __amdgpu_buffer_rsrc_t keys_at(const PagedArgs& a, const SharedUnit& x, const uint8_t* head, uint32_t sB, uint32_t row, int key0, int id, int n) {
+  return keys_at(a.shift, head, sB, row, key0 < 0 ? key0 + x.pre_tiles * kTile : key0, id, n);
+}
+__device__ inline Seen seen_by(const PagedArgs&, const SharedUnit& x, int p0, int) {
+  Seen s;
+  s.low = 0;
+  s.span = max(p0 - 30, 0);
+  s.sink = x.hole - 31;
+  return s;
+}
+__device__ inline int low_of(const PagedArgs&, const SharedUnit&, int) { return -1; }
+__device__ inline int sinks_of(const PagedArgs&, const SharedUnit& x) { return x.hole; }
 __device__ inline bool is_whole(const SharedUnit& x) { return x.part < 0; }
 __device__ inline int64_t part_of(const PagedArgs& a, const SharedUnit& x, int hk) { return part_row(a, hk, x.part); }
 
@@ -170,7 +181,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_shared_plan(SharedArgs a, int 
   };
   const auto put = [&](int u, int part, int4 w0, int4 w1, int4 w2, int4 w3) {
     if (u >= a.most_units) return;                         // (never of lengths that ascend)
-    if (part >= a.units) w0.w = w2.z = w3.x = w3.y = w3.z = w3.w = 0;
+    if (part >= a.units) w0.w = w2.z = w3.x = w3.y = 0;
     int4* d = a.plan + (int64_t)u * 4;
     d[0] = w0; d[1] = w1; d[2] = w2; d[3] = w3;
   };
@@ -226,11 +237,11 @@ __global__ __launch_bounds__(kPlanThreads) void k_shared_plan(SharedArgs a, int 
       const Blocks32 k = blocks_of(rows, many);
       const int rb = k.few ? 32 : many, i0 = b * rb, j0 = i0 / a.G, g0 = i0 - j0 * a.G, take = min(rb, rows - i0);
       const int past = kv - nq, p1 = past + (i0 + take - 1) / a.G;
-      const int pre = group >= 0 ? g_kv[group] : 0, pre_tiles = together ? 0 : (pre + kTile - 1) / kTile, tiles = pre_tiles + (p1 < 0 ? 0 : p1 / kTile + 1);
+      const int pre = group >= 0 && !together ? g_kv[group] : 0, tiles = (pre + kTile - 1) / kTile + (p1 < 0 ? 0 : p1 / kTile + 1);
       const int q = tiles / n, rem = tiles - q * n, lo = p * q + min(p, rem), hi = lo + q + (p < rem ? 1 : 0);
       const int part = s_part[e] >= 0 ? parts + s_part[e] + b0 * n + p : -1;
       put(units + u, part, make_int4(k.few, group < 0 ? 0 : group, r0 + e, part), make_int4(s_qs[e], past, kv, pre), make_int4(j0, g0, take, -1),
-          make_int4(min(lo, pre_tiles), min(hi, pre_tiles), max(lo, pre_tiles) - pre_tiles, max(hi, pre_tiles) - pre_tiles));
+          make_int4(lo, hi, 0, 0));
       const int join = joins + s_join[e] + b0;
       if (p == 0 && part >= 0 && join < a.most_joins) {
         int4 w = make_int4(g0, 0, 0, 0);
@@ -260,21 +271,21 @@ __global__ __launch_bounds__(256, DT == ZC_F32 && D == 128 ? 1 : 2) void k_share
   static_assert(kBytes >= RowsMemory<DT, D, 4>::kBytes, "blocks of few rows find room");
   __shared__ __align__(1024) uint8_t mem[kBytes];
   __shared__ float sum[4][2][64];
-  typedef __attribute__((address_space(4))) const int* scalar;
   const int u = unit_of_grid();
-  if (u >= ((scalar)(uintptr_t)a.counts)[0]) return;
-  const scalar d = (scalar)(uintptr_t)(a.plan + (int64_t)u * 4);
+  if (u >= ((plan_ptr)(uintptr_t)a.counts)[0]) return;
+  const plan_ptr d = (plan_ptr)(uintptr_t)(a.plan + (int64_t)u * (kWords / 4));
   SharedUnit x;
-  const int group = d[1], r = d[2];
-  x.part = d[3];
-  x.qs = d[4]; x.past = d[5];
-  x.j0 = d[8]; x.g0 = d[9]; x.rows = d[10]; x.last = d[11];
-  x.tokens = a.tokens;
-  x.tables[0] = a.pre_table + group * a.pre_row; x.columns[0] = a.pre_cols; x.keys[0] = d[7]; x.from[0] = d[12]; x.to[0] = d[13];
-  x.tables[1] = a.table + r * a.row; x.columns[1] = a.cols; x.keys[1] = d[6]; x.from[1] = d[14]; x.to[1] = d[15];
-  x.segments = x.from[0] < x.to[0] && x.from[1] < x.to[1] ? 2 : 1;
+  x.qs = d[kRow0]; x.past = d[kPast]; x.j0 = d[kToken]; x.g0 = d[kHead]; x.rows = d[kRows]; x.last = d[kLast]; x.part = d[kPart];
+  x.pre = a.pre_table + d[kGroup] * a.pre_row;
+  x.own = a.table + d[kRequest] * a.row;
+  x.kv = d[kOwnKeys];
+  x.pre_tiles = (d[kPrefixKeys] + kTile - 1) / kTile;
+  x.hole = d[kPrefixKeys] - x.pre_tiles * kTile;
+  x.t_lo = d[kFrom]; x.t_hi = d[kTo];
+  x.p0 = position(x, x.j0);
+  x.p1 = position(x, row_at(a, x, x.rows - 1).j);
   if constexpr (DT != ZC_F32) {
-    if (!d[0]) {
+    if (!d[kFew]) {
       attend_tiles<DT, D>(a, x, blockIdx.x, mem);
       return;
     }
