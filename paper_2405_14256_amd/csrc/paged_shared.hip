@@ -24,12 +24,13 @@ struct SharedArgs : PagedArgs {
   int4* plan;                                   // [unit][4]
   int4* joins;                                  // [block][2]
   int* tokens;                                  // the tokens that go through a prefix together, group after group
+  int least;                                    // tiles, below which a block is not split (fp32)
+  float worth;                                  // tiles that a shared prefix has to spare
   int most_units, most_joins;                   // (units: partial results that there is room for)
 };
 
 // What a unit of the plan is, in words of its entry.
 enum Word { kFew, kGroup, kRequest, kPart, kRow0, kPast, kOwnKeys, kPrefixKeys, kToken, kHead, kRows, kLast, kFrom, kTo, kWords = 16 };
-typedef __attribute__((address_space(4))) const int* plan_ptr;
 
 // A unit's keys are one stream of tiles, those of the prefix in front: its keys have negative positions, -kTile * pre_tiles on, so that the last
 // of its tiles, which need not be full, ends in front of the request's own first key.  The places between, from `hole` to -1, are hidden.
@@ -39,6 +40,7 @@ struct SharedUnit {
   static constexpr uint32_t behind = 0;
   int qs, past, j0, g0, rows;   // the request's first row; tokens in front of its new ones; token and head of the block's first row, its rows
   int last;                     // rows of several requests: the block's last place in the list of tokens; -1: of one
+  int token;                    // then: of this lane's row
   int part;                     // where its partial results go, -1: nothing to join
   const int32_t *pre, *own;     // rows of the tables
   int pre_tiles, hole, kv, t_lo, t_hi, p0, p1;
@@ -46,7 +48,7 @@ struct SharedUnit {
 __device__ inline Row row_at(const PagedArgs& a, const SharedUnit& x, int r) { return row_at(a, x.j0, x.g0, r); }
 __device__ inline Row row_of(const PagedArgs& a, const SharedUnit& x, int r) {
   Row me = row_at(a, x, r);
-  if (x.last >= 0) me.j = static_cast<const SharedArgs&>(a).tokens[min(me.j, x.last)];
+  if (x.last >= 0) me.j = x.token;
   return me;
 }
 // (rows of several requests, and a row in front of its request's first token, see all of the prefix and nothing else)
@@ -79,102 +81,119 @@ __device__ inline bool is_whole(const SharedUnit& x) { return x.part < 0; }
 __device__ inline int64_t part_of(const PagedArgs& a, const SharedUnit& x, int hk) { return part_row(a, hk, x.part); }
 
 // ---- the plan -------------------------------------------------------------------------------------
-// One workgroup, a thread a request or group at first, then a thread a unit.  Bound by its chain of lengths, rows and barriers.
-constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64;
-
-// What is planned for an entry, a request or a group.
-struct Blocks32 { int few, blocks; };
-__device__ inline Blocks32 blocks_of(int rows, int many) {
+// Entries of the plan are the requests: what their rows are, and that they go through their prefix together with others' if they are few.
+struct Entry { int qs, nq, kv, group, pre, few, blocks, tiles, together; };
+struct Cut { int few, blocks; };                           // blocks of 32 rows or of `many`
+__device__ inline Cut cut_of(int rows, int many) {
   const bool few = rows <= kFewRows || many == 32;
   return {few, few ? (rows + 31) / 32 : (rows + many - 1) / many};
 }
 
-__global__ __launch_bounds__(kPlanThreads) void k_shared_plan(SharedArgs a, int many) {
-  __shared__ int g_start[kGroups + 1], g_kv[kGroups], g_first[kGroups], g_end[kGroups], g_part[kGroups], g_parts[kGroups];
+constexpr int kListed = 130;                               // tokens that a block's rows are of, at most
+template <int THREADS>
+struct PlanMemory {
+  int g_start[kGroups + 1], g_kv[kGroups], g_first[kGroups], g_end[kGroups], g_part[kGroups], g_parts[kGroups];
   // of the entries in hand
-  __shared__ int s_unit[kPlanThreads], s_join[kPlanThreads], s_part[kPlanThreads], s_parts[kPlanThreads], s_blocks[kPlanThreads];
-  __shared__ int s_qs[kPlanThreads], s_nq[kPlanThreads], s_kv[kPlanThreads], s_group[kPlanThreads], s_place[kPlanThreads];
-  __shared__ int waves[4][kPlanWaves];
-  __shared__ unsigned long long s_work;
+  int unit[THREADS], join[THREADS], part[THREADS], parts[THREADS], blocks[THREADS], qs[THREADS], nq[THREADS], kv[THREADS], group[THREADS], place[THREADS];
+  int waves[3][THREADS / 64], four[4][THREADS / 64];
+  float sums[2][THREADS / 64];
+  int one[kWords], list[kListed];                          // of one unit: its entry, the tokens of its rows
+};
+
+// ALL: units, joins and the list of tokens go to memory.  Otherwise unit `wanted` stays in LDS (false: there is none), with the tokens of its rows, and
+// what it is joined with goes to memory.
+template <int THREADS, bool ALL>
+__device__ bool plan(const SharedArgs& a, int many, int wanted, PlanMemory<THREADS>& s) {
+  constexpr int NW = THREADS / 64;
   const int tid = threadIdx.x;
-  for (int e = tid; e <= a.P; e += kPlanThreads) {
-    g_start[e] = min(max(a.group_start[e], 0), a.R);
-    if (e < a.P) {
-      g_kv[e] = min(max(a.pre_len[e], 0), a.pre_cap);
-      g_first[e] = g_end[e] = 0;
-    }
-  }
-  if (tid == 0) s_work = 0;
-  struct Entry { int qs, nq, kv, group, pre, few, blocks, tiles, together; };
-  const auto entry = [&](int r) {                          // of request r (g_start and g_kv are there)
+  bool share = false;                                      // (set below)
+  struct Given { int from, to, kv; };
+  const auto given = [&](int r) { return r < a.R ? Given{a.q_start[r], a.q_start[r + 1], a.kv_len[r]} : Given{0, 0, 0}; };
+  const auto entry = [&](int r, const Given& in) {         // (g_start and g_kv are there)
     Entry x = {0, 0, 0, -1, 0, 0, 0, 0, 0};
     if (r >= a.R) return x;
-    const int s = a.q_start[r], e = a.q_start[r + 1], kv = a.kv_len[r];
-    x.qs = min(max(s, 0), a.T);
-    x.nq = max(min(e, a.T) - x.qs, 0);
-    x.kv = min(max(kv, 0), a.cap);
+    x.qs = min(max(in.from, 0), a.T);
+    x.nq = max(min(in.to, a.T) - x.qs, 0);
+    x.kv = min(max(in.kv, 0), a.cap);
     int lo = 0, hi = a.P + 1;                              // how many groups begin at or in front of it
     while (lo < hi) {
       const int mid = (lo + hi) / 2;
-      if (g_start[mid] <= r) lo = mid + 1;
+      if (s.g_start[mid] <= r) lo = mid + 1;
       else hi = mid;
     }
     if (lo > 0 && lo <= a.P) {
       x.group = lo - 1;
-      x.pre = g_kv[lo - 1];
+      x.pre = s.g_kv[lo - 1];
     }
     const int rows = x.nq * a.G;
-    const Blocks32 b = blocks_of(rows, many);
-    x.few = b.few;
-    x.blocks = b.blocks;
-    x.together = rows <= kFewRows && x.pre > 0;
+    const Cut c = cut_of(rows, many);
+    x.few = c.few;
+    x.blocks = c.blocks;
+    x.together = share && rows > 0 && rows <= kFewRows && x.pre > 0 && s.g_start[lo] - s.g_start[lo - 1] > 1;
     x.tiles = (x.kv + kTile - 1) / kTile + (x.together ? 0 : (x.pre + kTile - 1) / kTile);
     return x;
   };
+  const Given front = given(tid);
+  for (int e = tid; e <= a.P; e += THREADS) {
+    s.g_start[e] = min(max(a.group_start[e], 0), a.R);
+    if (e < a.P) {
+      s.g_kv[e] = min(max(a.pre_len[e], 0), a.pre_cap);
+      s.g_first[e] = s.g_end[e] = 0;
+    }
+  }
   __syncthreads();
+  // Whether it pays: tiles that need not be read again, of all heads.
+  float again = 0.f;
+  for (int g = tid & 63; g < a.P; g += 64) again += (float)max(s.g_start[g + 1] - s.g_start[g] - 1, 0) * (float)((s.g_kv[g] + kTile - 1) / kTile);
+  share = wave_sum(again) * (float)a.Hkv > a.worth;
 
   // ---- rows that go through a prefix together; all work
   int placed = 0;
-  unsigned long long work = 0;
-  for (int r0 = 0; r0 < a.R; r0 += kPlanThreads) {
+  float work = 0.f, n_blocks = 0.f;                        // tiles of all blocks
+  Entry held;                                              // (of the first entries)
+  for (int r0 = 0; r0 < a.R; r0 += THREADS) {
     const int r = r0 + tid;
-    const Entry x = entry(r);
+    const Entry x = entry(r, r0 ? given(r) : front);
+    if (r0 == 0) held = x;
     const int n = x.together ? x.nq : 0;
     int all;
-    const int upto = placed + block_inclusive_sum<kPlanWaves>(n, waves[(r0 / kPlanThreads) & 1], all), at = upto - n;
-    for (int j = 0; j < n; ++j)
-      if (at + j < a.T) a.tokens[at + j] = x.qs + j;
+    const int upto = placed + block_inclusive_sum<NW>(n, s.waves[(r0 / THREADS) & 1], all), at = upto - n;
+    if constexpr (ALL)
+      for (int j = 0; j < n; ++j)
+        if (at + j < a.T) a.tokens[at + j] = x.qs + j;
     if (x.group >= 0) {
-      if (r == g_start[x.group]) g_first[x.group] = at;
-      if (r == g_start[x.group + 1] - 1) g_end[x.group] = upto;
+      if (r == s.g_start[x.group]) s.g_first[x.group] = at;
+      if (r == s.g_start[x.group + 1] - 1) s.g_end[x.group] = upto;
     }
-    work += (unsigned long long)x.blocks * x.tiles;
+    work += (float)x.blocks * (float)x.tiles;
+    n_blocks += (float)x.blocks;
     placed += all;
   }
   __syncthreads();
-  Blocks32 gb = {0, 0};
-  int g_tiles = 0;
-  if (tid < a.P) {
-    gb = blocks_of((g_end[tid] - g_first[tid]) * a.G, many);
-    g_tiles = (g_kv[tid] + kTile - 1) / kTile;
-    work += (unsigned long long)gb.blocks * g_tiles;
+  for (int g = tid; g < a.P; g += THREADS) {
+    const int blocks = cut_of((s.g_end[g] - s.g_first[g]) * a.G, many).blocks;
+    work += (float)blocks * (float)((s.g_kv[g] + kTile - 1) / kTile);
+    n_blocks += (float)blocks;
   }
-  atomicAdd(&s_work, work);                                // (whole numbers: in any order)
+  work = wave_sum(work);
+  n_blocks = wave_sum(n_blocks);
+  if ((tid & 63) == 0) { s.sums[0][tid >> 6] = work; s.sums[1][tid >> 6] = n_blocks; }
   __syncthreads();
-  const unsigned long long each = (s_work + a.target - 1) / a.target;
-  const int per = each < 1 ? 1 : each > 0x3fffffff ? 0x3fffffff : (int)each;    // tiles of a part, at most
-  const auto parts_of = [&](int tiles, int few) {
-    const int most = max(per, few ? 2 : 4);
-    return tiles <= most ? 1 : (tiles + most - 1) / most;
-  };
-  int units = 0, joins = 0, parts = 0;
+  work = n_blocks = 0.f;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) { work += s.sums[0][w]; n_blocks += s.sums[1][w]; }
+  const int per = (int)fminf(fmaxf(ceilf(work / (float)a.target), 1.f), 1e9f);  // tiles of a part, at most
+  // (below which a part is not worth its way through memory, as for the paged attention)
+  n_blocks *= (float)a.Hkv;
+  const int least = many == 32 ? a.least : n_blocks >= 128.f ? 16 : n_blocks >= 64.f ? 10 : 6;
+  const auto parts_of = [&](int tiles) { return tiles <= max(per, least) ? 1 : (tiles + per - 1) / per; };
 
-  // The entry of this workgroup's that a unit belongs to.
+  // The entry in hand that a unit belongs to: the last that begins at or in front of it.
   const auto owner = [&](int u, int n) {
-    int lo = 0, hi = n;                                    // the last that begins at or in front of it
+    int lo = 0, hi = n;
     while (hi - lo > 1) {
       const int mid = (lo + hi) / 2;
-      if (s_unit[mid] <= u) lo = mid;
+      if (s.unit[mid] <= u) lo = mid;
       else hi = mid;
     }
     return lo;
@@ -182,98 +201,148 @@ __global__ __launch_bounds__(kPlanThreads) void k_shared_plan(SharedArgs a, int 
   const auto put = [&](int u, int part, int4 w0, int4 w1, int4 w2, int4 w3) {
     if (u >= a.most_units) return;                         // (never of lengths that ascend)
     if (part >= a.units) w0.w = w2.z = w3.x = w3.y = 0;
-    int4* d = a.plan + (int64_t)u * 4;
+    int4* d = ALL ? a.plan + (int64_t)u * (kWords / 4) : reinterpret_cast<int4*>(s.one);
     d[0] = w0; d[1] = w1; d[2] = w2; d[3] = w3;
+  };
+  // f(u, entry) for units u of `all` in hand, the first of which has number `first`; this thread's `count` entry has those from `begin` on.
+  const auto units_in_hand = [&](int first, int all, int n, int begin, int count, auto&& f) {
+    if constexpr (ALL) {
+      __syncthreads();
+      for (int u = tid; u < all; u += THREADS) f(u, owner(u, n));
+    } else if (wanted - first >= begin && wanted - first < begin + count) {
+      f(wanted - first, tid);
+    }
   };
 
   // ---- units of the prefixes
-  {
-    const int n = parts_of(g_tiles, gb.few), mine = gb.blocks * n;
+  int units = 0, joins = 0, parts = 0;
+  for (int g0 = 0; g0 < a.P; g0 += THREADS) {
+    const int g = g0 + tid, rows = g < a.P ? (s.g_end[g] - s.g_first[g]) * a.G : 0, tiles = g < a.P ? (s.g_kv[g] + kTile - 1) / kTile : 0;
+    const Cut c = cut_of(rows, many);
+    const int n = parts_of(tiles), mine = c.blocks * n;
     int all;
-    const int before = block_inclusive_sum<kPlanWaves>(mine, waves[2], all) - mine;
-    s_unit[tid] = before;
-    s_parts[tid] = n;
-    if (tid < a.P) {
-      g_part[tid] = before;
-      g_parts[tid] = n;
+    if (g0) __syncthreads();
+    const int before = block_inclusive_sum<NW>(mine, s.waves[2], all) - mine;
+    s.unit[tid] = before;
+    s.parts[tid] = n;
+    if (g < a.P) {
+      s.g_part[g] = units + before;
+      s.g_parts[g] = n;
     }
-    __syncthreads();
-    for (int u = tid; u < all; u += kPlanThreads) {
-      const int e = owner(u, a.P), rest = u - s_unit[e], b = rest / s_parts[e], p = rest - b * s_parts[e];
-      const int rows = (g_end[e] - g_first[e]) * a.G, tiles = (g_kv[e] + kTile - 1) / kTile;
-      const Blocks32 k = blocks_of(rows, many);
-      const int rb = k.few ? 32 : many, i0 = b * rb, j = i0 / a.G, q = tiles / s_parts[e], rem = tiles - q * s_parts[e];
+    units_in_hand(units, all, min(a.P - g0, THREADS), before, mine, [&](int u, int i) {
+      const int e = g0 + i, n = s.parts[i], rest = u - s.unit[i], b = rest / n, p = rest - b * n;
+      const int rows = (s.g_end[e] - s.g_first[e]) * a.G, tiles = (s.g_kv[e] + kTile - 1) / kTile;
+      const Cut k = cut_of(rows, many);
+      const int rb = k.few ? 32 : many, i0 = b * rb, j = i0 / a.G, q = tiles / n, rem = tiles - q * n;
       const int lo = p * q + min(p, rem), hi = lo + q + (p < rem ? 1 : 0);
-      put(u, u, make_int4(k.few, e, 0, u), make_int4(0, 0, 0, g_kv[e]), make_int4(g_first[e] + j, i0 - j * a.G, min(rb, rows - i0), g_end[e] - 1),
-          make_int4(lo, hi, 0, 0));
-    }
-    units = parts = all;
+      put(units + u, units + u, make_int4(k.few, e, 0, units + u), make_int4(0, 0, 0, s.g_kv[e]),
+          make_int4(s.g_first[e] + j, i0 - j * a.G, min(rb, rows - i0), s.g_end[e] - 1), make_int4(lo, hi, 0, 0));
+    });
+    units += all;
   }
+  parts = units;
 
   // ---- units of the requests, and what is joined
   placed = 0;
-  for (int r0 = 0; r0 < a.R; r0 += kPlanThreads) {
-    const Entry x = entry(r0 + tid);
-    const int n = parts_of(x.tiles, x.few), apart = x.together || n > 1;
-    int all_units, all_joins, all_parts, all_placed;
-    __syncthreads();                                       // (the entries before are done with)
-    const int u1 = block_inclusive_sum<kPlanWaves>(x.blocks * n, waves[0], all_units);
-    const int j1 = block_inclusive_sum<kPlanWaves>(apart ? x.blocks : 0, waves[1], all_joins);
-    const int p1 = block_inclusive_sum<kPlanWaves>(apart ? x.blocks * n : 0, waves[2], all_parts);
-    const int t = x.together ? x.nq : 0, t1 = block_inclusive_sum<kPlanWaves>(t, waves[3], all_placed);
-    s_unit[tid] = u1 - x.blocks * n;
-    s_join[tid] = j1 - (apart ? x.blocks : 0);
-    s_part[tid] = apart ? p1 - x.blocks * n : -1;
-    s_parts[tid] = n;
-    s_blocks[tid] = x.blocks;
-    s_qs[tid] = x.qs; s_nq[tid] = x.nq; s_kv[tid] = x.kv;
-    s_group[tid] = x.group;
-    s_place[tid] = x.together ? placed + t1 - t : -1;      // of its first token
-    __syncthreads();
-    for (int u = tid; u < all_units; u += kPlanThreads) {
-      const int e = owner(u, kPlanThreads), n = s_parts[e], rest = u - s_unit[e], b0 = rest / n, p = rest - b0 * n;
-      const int b = s_blocks[e] - 1 - b0;                  // (a chunk's last rows see the most keys: first)
-      const int nq = s_nq[e], kv = s_kv[e], rows = nq * a.G, group = s_group[e], together = s_place[e] >= 0;
-      const Blocks32 k = blocks_of(rows, many);
+  for (int r0 = 0; r0 < a.R; r0 += THREADS) {
+    const Entry x = r0 ? entry(r0 + tid, given(r0 + tid)) : held;
+    const int n = parts_of(x.tiles), apart = x.together || n > 1;
+    int all[4];                                            // units, joins, partial results, tokens that go together
+    if (ALL || r0) __syncthreads();                        // (the entries before are done with)
+    const int t = x.together ? x.nq : 0, mine = x.blocks * n;
+    int upto[4] = {mine, apart ? x.blocks : 0, apart ? mine : 0, t};
+    block_inclusive_sums<NW>(upto, s.four, all);
+    s.unit[tid] = upto[0] - mine;
+    s.join[tid] = upto[1] - (apart ? x.blocks : 0);
+    s.part[tid] = apart ? upto[2] - mine : -1;
+    s.parts[tid] = n;
+    s.blocks[tid] = x.blocks;
+    s.qs[tid] = x.qs; s.nq[tid] = x.nq; s.kv[tid] = x.kv;
+    s.group[tid] = x.group;
+    s.place[tid] = x.together ? placed + upto[3] - t : -1; // of its first token in the list
+    units_in_hand(units, all[0], THREADS, upto[0] - mine, mine, [&](int u, int e) {
+      const int n = s.parts[e], rest = u - s.unit[e], b0 = rest / n, p = rest - b0 * n;
+      const int b = s.blocks[e] - 1 - b0;                  // (a chunk's last rows see the most keys: first)
+      const int past = s.kv[e] - s.nq[e], rows = s.nq[e] * a.G, group = s.group[e], together = s.place[e] >= 0;
+      const Cut k = cut_of(rows, many);
       const int rb = k.few ? 32 : many, i0 = b * rb, j0 = i0 / a.G, g0 = i0 - j0 * a.G, take = min(rb, rows - i0);
-      const int past = kv - nq, p1 = past + (i0 + take - 1) / a.G;
-      const int pre = group >= 0 && !together ? g_kv[group] : 0, tiles = (pre + kTile - 1) / kTile + (p1 < 0 ? 0 : p1 / kTile + 1);
+      const int p1 = past + (i0 + take - 1) / a.G;
+      const int pre = group >= 0 && !together ? s.g_kv[group] : 0, tiles = (pre + kTile - 1) / kTile + (p1 < 0 ? 0 : p1 / kTile + 1);
       const int q = tiles / n, rem = tiles - q * n, lo = p * q + min(p, rem), hi = lo + q + (p < rem ? 1 : 0);
-      const int part = s_part[e] >= 0 ? parts + s_part[e] + b0 * n + p : -1;
-      put(units + u, part, make_int4(k.few, group < 0 ? 0 : group, r0 + e, part), make_int4(s_qs[e], past, kv, pre), make_int4(j0, g0, take, -1),
+      const int part = s.part[e] >= 0 ? parts + s.part[e] + b0 * n + p : -1;
+      put(units + u, part, make_int4(k.few, group < 0 ? 0 : group, r0 + e, part), make_int4(s.qs[e], past, s.kv[e], pre), make_int4(j0, g0, take, -1),
           make_int4(lo, hi, 0, 0));
-      const int join = joins + s_join[e] + b0;
+      const int join = joins + s.join[e] + b0;
       if (p == 0 && part >= 0 && join < a.most_joins) {
         int4 w = make_int4(g0, 0, 0, 0);
         if (together) {
-          const bool big = !blocks_of((g_end[group] - g_first[group]) * a.G, many).few;
-          w = make_int4(g0, g_part[group], g_parts[group] << 1 | (big ? 1 : 0), (s_place[e] - g_first[group]) * a.G + i0);
+          const bool big = !cut_of((s.g_end[group] - s.g_first[group]) * a.G, many).few;
+          w = make_int4(g0, s.g_part[group], s.g_parts[group] << 1 | (big ? 1 : 0), (s.place[e] - s.g_first[group]) * a.G + i0);
         }
-        a.joins[2 * join] = make_int4(part, n, take, s_qs[e] + j0);
+        a.joins[2 * join] = make_int4(part, n, take, s.qs[e] + j0);
         a.joins[2 * join + 1] = w;
       }
-    }
-    units += all_units;
-    joins += all_joins;
-    parts += all_parts;
-    placed += all_placed;
+    });
+    units += all[0];
+    joins += all[1];
+    parts += all[2];
+    placed += all[3];
   }
-  if (tid == 0) {
+  if (tid == 0 && (ALL || wanted == 0)) {
     a.counts[0] = min(units, a.most_units);
     a.counts[1] = min(joins, a.most_joins);
   }
+  if constexpr (ALL) return true;
+  if (wanted >= min(units, a.most_units)) return false;
+  __syncthreads();
+  const int last = s.one[kLast], j0 = s.one[kToken];
+  if (last < 0) return true;
+  // the tokens of the unit's rows, `last` and all in front of it that a block can have
+  placed = 0;
+  for (int r0 = 0; r0 < a.R; r0 += THREADS) {
+    const Entry x = r0 ? entry(r0 + tid, given(r0 + tid)) : held;
+    const int n = x.together ? x.nq : 0;
+    int all;
+    const int at = placed + block_inclusive_sum<NW>(n, s.waves[(r0 / THREADS) & 1], all) - n;
+    for (int j = max(j0 - at, 0); j < n && at + j <= last && at + j - j0 < kListed; ++j) s.list[at + j - j0] = x.qs + j;
+    placed += all;
+  }
+  __syncthreads();
+  return true;
+}
+
+// One workgroup, a thread an entry at first, then a thread a unit.
+constexpr int kPlanThreads = 1024;
+__global__ __launch_bounds__(kPlanThreads) void k_shared_plan(SharedArgs a, int many) {
+  __shared__ __align__(16) PlanMemory<kPlanThreads> s;
+  plan<kPlanThreads, true>(a, many, 0, s);
 }
 
 // ---- the units ------------------------------------------------------------------------------------
-template <int DT, int D>
+// PLANNED: by k_shared_plan.  Otherwise every workgroup finds its unit itself, which spares a launch.
+template <int DT, int D, bool PLANNED>
 __global__ __launch_bounds__(256, DT == ZC_F32 && D == 128 ? 1 : 2) void k_shared_attention(SharedArgs a) {
   constexpr int kBytes = DT == ZC_F32 ? RowsMemory<DT, D, 4>::kBytes : kStages<D> * 2 * kTile * Tile<DT, D>::ROWB;
   static_assert(kBytes >= RowsMemory<DT, D, 4>::kBytes, "blocks of few rows find room");
+  static_assert(kBytes >= (int)sizeof(PlanMemory<256>), "and the plan");
   __shared__ __align__(1024) uint8_t mem[kBytes];
   __shared__ float sum[4][2][64];
-  const int u = unit_of_grid();
-  if (u >= ((plan_ptr)(uintptr_t)a.counts)[0]) return;
-  const plan_ptr d = (plan_ptr)(uintptr_t)(a.plan + (int64_t)u * (kWords / 4));
+  constexpr int kMany = DT == ZC_F32 ? 32 : 128;
+  const int u = unit_of_grid(), hk = blockIdx.x;
+  int d[kWords];
+  int token = 0;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  if constexpr (PLANNED) {
+    typedef __attribute__((address_space(4))) const int* scalar;
+    if (u >= ((scalar)(uintptr_t)a.counts)[0]) return;
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) d[i] = ((scalar)(uintptr_t)(a.plan + (int64_t)u * (kWords / 4)))[i];
+  } else {
+    PlanMemory<256>& s = *reinterpret_cast<PlanMemory<256>*>(mem);
+    if (!plan<256, false>(a, kMany, u, s)) return;
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) d[i] = __builtin_amdgcn_readfirstlane(s.one[i]);
+  }
   SharedUnit x;
   x.qs = d[kRow0]; x.past = d[kPast]; x.j0 = d[kToken]; x.g0 = d[kHead]; x.rows = d[kRows]; x.last = d[kLast]; x.part = d[kPart];
   x.pre = a.pre_table + d[kGroup] * a.pre_row;
@@ -284,13 +353,20 @@ __global__ __launch_bounds__(256, DT == ZC_F32 && D == 128 ? 1 : 2) void k_share
   x.t_lo = d[kFrom]; x.t_hi = d[kTo];
   x.p0 = position(x, x.j0);
   x.p1 = position(x, row_at(a, x, x.rows - 1).j);
+  if (x.last >= 0) {
+    const int j = min(row_at(a, x, (d[kFew] ? 0 : 32 * w) + (lane & 31)).j, x.last);
+    if constexpr (PLANNED) token = a.tokens[j];
+    else token = reinterpret_cast<PlanMemory<256>*>(mem)->list[j - x.j0];
+  }
+  x.token = min(max(token, 0), a.T - 1);
+  if constexpr (!PLANNED) __syncthreads();                 // (the plan is done with LDS)
   if constexpr (DT != ZC_F32) {
     if (!d[kFew]) {
-      attend_tiles<DT, D>(a, x, blockIdx.x, mem);
+      attend_tiles<DT, D>(a, x, hk, mem);
       return;
     }
   }
-  attend_rows<DT, D, 4>(a, x, blockIdx.x, mem, sum);
+  attend_rows<DT, D, 4>(a, x, hk, mem, sum);
 }
 
 // ---- the join -------------------------------------------------------------------------------------
@@ -301,64 +377,66 @@ __global__ __launch_bounds__(256) void k_shared_join(SharedArgs a) {
   constexpr int TPR = D / 4, GROUPS = 256 / TPR;
   __shared__ __align__(16) float so[GROUPS][D];
   __shared__ float2 sml[GROUPS];
-  const int turn = (int)blockIdx.x / a.Hkv, hk = blockIdx.x - turn * a.Hkv, join = unit_of_grid();
-  if (join >= a.counts[1]) return;
-  const int4 w = a.joins[2 * join], v = a.joins[2 * join + 1];
-  const int first = w.x, own = w.y, rows = w.z, pre = v.z >> 1, shift = v.z & 1 ? 7 : 5, parts = own + pre;
-  if (first + own > a.units) return;
-  const int grp = threadIdx.x / TPR, c = threadIdx.x % TPR * 4;
-  for (int row0 = turn * GROUPS; row0 < rows; row0 += kSharedJoinGroups * GROUPS) {
-    const int n = min(rows - row0, GROUPS);
-    int ways = 1;                                          // groups to a row
-    while (2 * ways * n <= GROUPS && 2 * ways <= parts) ways *= 2;
-    const int way = grp & (ways - 1), row = row0 + grp / ways;
-    const bool mine = row < row0 + n;
-    const int i = v.w + row, pre0 = v.y + (i >> shift) * pre, pre_row = i & ((1 << shift) - 1);
-    float M = kLowestLogit, l = 0.f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (mine && (pre == 0 || pre0 + pre <= a.units)) {
-      constexpr int U = 4;                                 // parts requested at a time
-      for (int s0 = way; s0 < parts; s0 += U * ways) {
-        float2 ml[U];
-        float4 t[U];
+  const int turn = (int)blockIdx.x / a.Hkv, hk = blockIdx.x - turn * a.Hkv;
+  const int grp = threadIdx.x / TPR, c = threadIdx.x % TPR * 4, joins = a.counts[1];
+  for (int join = blockIdx.y; join < joins; join += gridDim.y) {
+    const int4 w = a.joins[2 * join], v = a.joins[2 * join + 1];
+    const int first = w.x, own = w.y, rows = w.z, pre = v.z >> 1, shift = v.z & 1 ? 7 : 5, parts = own + pre;
+    if (first + own > a.units) continue;
+    const int step = min((rows + kSharedJoinGroups - 1) / kSharedJoinGroups, GROUPS);        // rows at a time: few rows are spread over the workgroups too
+    for (int row0 = turn * step; row0 < rows; row0 += kSharedJoinGroups * step) {
+      const int n = min(rows - row0, step);
+      int ways = 1;                                          // groups to a row
+      while (2 * ways * n <= GROUPS && 2 * ways <= parts) ways *= 2;
+      const int way = grp & (ways - 1), row = row0 + grp / ways;
+      const bool mine = row < row0 + n;
+      const int i = v.w + row, pre0 = v.y + (i >> shift) * pre, pre_row = i & ((1 << shift) - 1);
+      float M = kLowestLogit, l = 0.f;
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (mine && (pre == 0 || pre0 + pre <= a.units)) {
+        constexpr int U = 4;                                 // parts requested at a time
+        for (int s0 = way; s0 < parts; s0 += U * ways) {
+          float2 ml[U];
+          float4 t[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const int s = s0 + u * ways < parts ? s0 + u * ways : s0;
-          const int64_t p = s < pre ? part_row(a, hk, pre0 + s) + pre_row : part_row(a, hk, first + s - pre) + row;
-          ml[u] = *reinterpret_cast<const float2*>(a.part_ml + p * 2);
-          t[u] = *reinterpret_cast<const float4*>(a.part_o + p * D + c);
-        }
-        float top = M;
+          for (int u = 0; u < U; ++u) {
+            const int s = s0 + u * ways < parts ? s0 + u * ways : s0;
+            const int64_t p = s < pre ? part_row(a, hk, pre0 + s) + pre_row : part_row(a, hk, first + s - pre) + row;
+            ml[u] = *reinterpret_cast<const float2*>(a.part_ml + p * 2);
+            t[u] = *reinterpret_cast<const float4*>(a.part_o + p * D + c);
+          }
+          float top = M;
 #pragma unroll
-        for (int u = 0; u < U; ++u) top = fmaxf(top, ml[u].x);
-        const float f0 = __builtin_amdgcn_exp2f(M - top);
-        M = top;
-        l *= f0; o.x *= f0; o.y *= f0; o.z *= f0; o.w *= f0;
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const float f = s0 + u * ways < parts ? __builtin_amdgcn_exp2f(ml[u].x - M) : 0.f;
-          l = fmaf(ml[u].y, f, l);
-          o.x = fmaf(t[u].x, f, o.x); o.y = fmaf(t[u].y, f, o.y); o.z = fmaf(t[u].z, f, o.z); o.w = fmaf(t[u].w, f, o.w);
-        }
-      }
-    }
-    if (ways > 1) {
-      if (c == 0) sml[grp] = make_float2(M, l);
-      *reinterpret_cast<float4*>(&so[grp][c]) = o;
-      __syncthreads();
-      if (mine && way == 0) {
-        for (int y = 1; y < ways; ++y) {
-          const float2 ml = sml[grp + y];
-          const float4 t = *reinterpret_cast<const float4*>(&so[grp + y][c]);
-          const float top = fmaxf(M, ml.x), f0 = __builtin_amdgcn_exp2f(M - top), f = __builtin_amdgcn_exp2f(ml.x - top);
+          for (int u = 0; u < U; ++u) top = fmaxf(top, ml[u].x);
+          const float f0 = __builtin_amdgcn_exp2f(M - top);
           M = top;
-          l = fmaf(ml.y, f, l * f0);
-          o.x = fmaf(t.x, f, o.x * f0); o.y = fmaf(t.y, f, o.y * f0); o.z = fmaf(t.z, f, o.z * f0); o.w = fmaf(t.w, f, o.w * f0);
+          l *= f0; o.x *= f0; o.y *= f0; o.z *= f0; o.w *= f0;
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            const float f = s0 + u * ways < parts ? __builtin_amdgcn_exp2f(ml[u].x - M) : 0.f;
+            l = fmaf(ml[u].y, f, l);
+            o.x = fmaf(t[u].x, f, o.x); o.y = fmaf(t[u].y, f, o.y); o.z = fmaf(t[u].z, f, o.z); o.w = fmaf(t[u].w, f, o.w);
+          }
         }
       }
-      __syncthreads();
+      if (ways > 1) {
+        if (c == 0) sml[grp] = make_float2(M, l);
+        *reinterpret_cast<float4*>(&so[grp][c]) = o;
+        __syncthreads();
+        if (mine && way == 0) {
+          for (int y = 1; y < ways; ++y) {
+            const float2 ml = sml[grp + y];
+            const float4 t = *reinterpret_cast<const float4*>(&so[grp + y][c]);
+            const float top = fmaxf(M, ml.x), f0 = __builtin_amdgcn_exp2f(M - top), f = __builtin_amdgcn_exp2f(ml.x - top);
+            M = top;
+            l = fmaf(ml.y, f, l * f0);
+            o.x = fmaf(t.x, f, o.x * f0); o.y = fmaf(t.y, f, o.y * f0); o.z = fmaf(t.z, f, o.z * f0); o.w = fmaf(t.w, f, o.w * f0);
+          }
+        }
+        __syncthreads();
+      }
+      if (mine && way == 0) store_row<DT>(a, w.w, v.x, hk, row, c, M, l, o);
     }
-    if (mine && way == 0) store_row<DT>(a, w.w, v.x, hk, row, c, M, l, o);
   }
 }
 
@@ -369,14 +447,17 @@ static Most most_of(int64_t P, int64_t R, int64_t T, int64_t G, int64_t Hkv, boo
   Most m;
   const int64_t with = R < T ? R : T, rows = T * G, many = fp32 ? 32 : 128, groups = P < with ? P : with;
   m.slot = fp32 || rows <= kFewRows ? 32 : 128;
-  m.target = ceil_div64(512, Hkv);
+  // What the chip holds at a time: more parts cost more on their way through memory than they even out.  us at 256, 384, 512, 768 and 1024 units: bf16, 32 heads over 8 of 128
+  // channels, 64 tokens after 8192 56.8, 56.7, 56.7, 63.5 and 68.4; fp16, 16 over 4 of 64, 20 tokens and 7 chunks after up to 4000 35.8, 32.7, 36.7, 41.0 and 42.9; 24 over 8 of 64, 90
+  // tokens of up to 3843 after up to 2314 115, 115, 110 and 105; fp32, 16 heads of 128, 74 tokens after up to 593 91.7, 97.2, 101 and 106.
+  m.target = ceil_div64(fp32 && D == 128 ? 256 : 512, Hkv);
   // (a request has one block that is not full; where blocks of 128 rows are the rule, one of 33 to 64 rows is two of 32)
   const int64_t two = rows / 33 < with ? rows / 33 : with, blocks = rows / many + with + two;
   const int64_t few = rows / 32 + with < 2 * with ? rows / 32 + with : 2 * with;
   const int64_t together = rows < kFewRows * with ? rows : kFewRows * with, pre = together / many + 2 * groups;
-  // a block is cut into at most tiles / (all work / target) + 1 parts; one of many rows leaves none if it is not cut
-  m.units = m.target + blocks + pre;
-  m.parts = 2 * m.target + few + pre;
+  // a block is cut into at most tiles / (all work / target) + 1 parts; one of many rows leaves none if it is not cut (2: sums of work are rounded)
+  m.units = m.target + blocks + pre + 2;
+  m.parts = 2 * m.target + few + pre + 2;
   m.joins = blocks;
   m.bytes = (int64_t)Hkv * m.parts * m.slot * (D + 2) * 4 + m.units * 64 + m.joins * 32 + align_up64(T * 4, 16) + 16;
   return m;
@@ -384,12 +465,24 @@ static Most most_of(int64_t P, int64_t R, int64_t T, int64_t G, int64_t Hkv, boo
 
 template <int DT, int D>
 static int launch_shared(SharedArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL(k_shared_plan, dim3(1), dim3(kPlanThreads), 0, st, a, DT == ZC_F32 ? 32 : 128);
-  ZC_LAUNCH_CHECK();
+  // A workgroup finds its unit in about 2 us, a plan takes a launch of 5 to 8.  us found and planned: bf16, 32 heads over 8 of 128 channels, 8 tokens after 1000 19.3 and 24.9 (one
+  // round of workgroups), 64 after 8192 56.2 and 58.8 (two); fp16, 40 heads, 42 tokens 47.0 and 39.3 (eight), 12 chunks after 4096 307 and 312 (five); fp32, 16 heads of
+  // 128, 21 requests 32.8 and 29.9 (five), 74 104.8 and 88.4 (ten); 16 over 4 of 64, 22 chunks 85.7 and 73.6 (five).
+  const int64_t places = DT == ZC_F32 && D == 128 ? 256 : DT != ZC_F32 && D == 64 ? 768 : 512;
+  const bool planned = a.most_units * a.Hkv > 4 * places;
+  const int64_t own_tiles = ceil_div64(a.cap, kTile), pre_tiles = ceil_div64(a.pre_cap, kTile);
+  const bool joined = own_tiles + pre_tiles > (DT == ZC_F32 ? a.least : 6) || (float)(a.R * pre_tiles * a.Hkv) > a.worth;     // (the plan's rules)
+  if (planned) {
+    hipLaunchKernelGGL(k_shared_plan, dim3(1), dim3(kPlanThreads), 0, st, a, DT == ZC_F32 ? 32 : 128);
+    ZC_LAUNCH_CHECK();
+  }
   const auto grid = [](int64_t x, int64_t n) { return dim3((unsigned)x, (unsigned)(n < 65535 ? n : 65535), (unsigned)ceil_div64(n, 65535)); };
-  hipLaunchKernelGGL((k_shared_attention<DT, D>), grid(a.Hkv, a.most_units), dim3(256), 0, st, a);
+  if (planned) hipLaunchKernelGGL((k_shared_attention<DT, D, true>), grid(a.Hkv, a.most_units), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((k_shared_attention<DT, D, false>), grid(a.Hkv, a.most_units), dim3(256), 0, st, a);
   ZC_LAUNCH_CHECK();
-  hipLaunchKernelGGL((k_shared_join<DT, D>), grid(a.Hkv * kSharedJoinGroups, a.most_joins), dim3(256), 0, st, a);
+  if (!joined) return ZC_OK;
+  const int64_t turns = ceil_div64(2048, a.Hkv * kSharedJoinGroups);
+  hipLaunchKernelGGL((k_shared_join<DT, D>), dim3((unsigned)(a.Hkv * kSharedJoinGroups), (unsigned)(turns < a.most_joins ? turns : a.most_joins)), dim3(256), 0, st, a);
   ZC_LAUNCH_CHECK();
   return ZC_OK;
 }
@@ -463,6 +556,11 @@ extern "C" int zc_paged_shared_attention(const zc_tensor4* q, const zc_tensor4* 
   a.todo = nullptr;
   a.pre_table = prefix_table; a.pre_len = prefix_len; a.group_start = group_start; a.pre_row = prefix_row_stride;
   a.pre_cols = (int)prefix_max_blocks; a.pre_cap = (int)room(prefix_max_blocks); a.P = (int)P;
+  a.least = q->D == 64 ? 4 : 2;
+  // Rows that go through their prefix together have parts to be joined, so as much has to be spared.  us together and each request by itself: 8 tokens after 1000
+  // (32 heads over 8 of 128 channels; 29 MB spared) 19.5 and 20.3, 22 after up to 1412 (8 heads of 64; 48 MB) 18.2 and 21.8, 16 chunks of up to 17 after 355 (8 of 64; 12 MB) 18.9 and
+  // 15.9, 64 after 8192 (2.1 GB) 55.6 and 189.
+  a.worth = 28e6f / (float)(2 * kTile * q->D * eb);
   a.most_units = (int)m.units; a.most_joins = (int)m.joins;
   uint8_t* at = (uint8_t*)ws;
   a.counts = (int*)at; at += 16;

@@ -151,6 +151,24 @@ __device__ inline int block_inclusive_sum(int v, int* waves, int& total) {
   return v + (w ? __builtin_amdgcn_readlane(upto, w - 1) : 0);
 }
 
+// The same of N values with one barrier.
+template <int NW, int N>
+__device__ inline void block_inclusive_sums(int (&v)[N], int (*waves)[NW], int (&total)[N]) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    v[i] = wave_inclusive_sum(v[i]);
+    if (lane == 63) waves[i][w] = v[i];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int upto = wave_inclusive_sum(lane < NW ? waves[i][lane] : 0);
+    total[i] = __builtin_amdgcn_readlane(upto, NW - 1);
+    v[i] += w ? __builtin_amdgcn_readlane(upto, w - 1) : 0;
+  }
+}
+
 }  // namespace zc
 
 // Host-side validation shared by the entry points (defined in api.hip).

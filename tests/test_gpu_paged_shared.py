@@ -218,3 +218,55 @@ def test_threads_that_share_a_stream_and_calls_on_two():
             t.join()
         for results, w in zip(out, want):
             assert all(torch.equal(x, w[0]) and torch.equal(y, w[1]) for x, y in results)
+
+
+# ---- prefixes long enough, and of requests enough, that their rows go through them together -------------------------
+@pytest.mark.parametrize("dtype,D,Hq,Hkv,page,by_head", [(BF, 128, 8, 2, 16, True), (HF, 64, 4, 4, 32, False), (FL, 64, 6, 2, 64, True), (FL, 128, 4, 1, 16, False),
+                                                         (BF, 64, 8, 1, 128, True), (HF, 128, 3, 3, 16, True)])
+def test_rows_that_go_together(dtype, D, Hq, Hkv, page, by_head):
+    kw = dict(page=page, by_head=by_head, pad=2)
+    run(plain.Shared([1] * 24, [1 + 13 * i for i in range(24)], [0, 24], [5000], Hq, Hkv, D, dtype, **kw))
+    # with chunks that go alone, requests that have no tokens, some in front of the groups and some behind
+    q = [1, 3, 0, 1, 200, 1, 2, 1, 1, 70, 1, 5, 1, 1, 0, 1, 1, 16, 1, 1, 1, 90, 1, 1]
+    run(plain.Shared(q, [n + 11 * i for i, n in enumerate(q)], [2, 9, 9, 21], [4700, 100, 4001], Hq, Hkv, D, dtype, **kw))
+
+
+@pytest.mark.parametrize("n", [1, 63, 64, 65, 127, 1000])
+@pytest.mark.parametrize("dtype", [HF, FL])
+def test_short_prefixes_beside_a_long_one(n, dtype):
+    run(plain.Shared([1] * 20, [3 + 7 * i for i in range(20)], [0, 6, 20], [n, 5000], 4, 2, 64, dtype, seed=n))
+
+
+@pytest.mark.parametrize("G,q_len", [(1, [1] * 31), (1, [1] * 33), (1, [64, 64] * 10), (1, [63, 1, 65, 2] * 6), (2, [1] * 64), (2, [1] * 65), (3, [21, 1, 22] * 8),
+                                     (5, [1] * 26), (5, [12, 13] * 10), (7, [1, 9, 2] * 7), (33, [1] * 20), (64, [1] * 20), (65, [1] * 20)])
+@pytest.mark.parametrize("dtype", [BF, FL])
+def test_blocks_of_rows_that_go_together(G, q_len, dtype):
+    run(plain.Shared(q_len, [n + 5 * i % 60 for i, n in enumerate(q_len)], [0, len(q_len)], [3500], 2 * G, 2, 64, dtype))
+
+
+def test_many_groups_that_go_together():
+    R = 300
+    run(plain.Shared([1] * R, [1 + i % 90 for i in range(R)], [0] + list(range(5, 291, 5)), [900 + 7 * g for g in range(58)], 4, 2, 64, BF))
+    R = 1100                                                                # (planned in front)
+    run(plain.Shared([1 if i % 9 else 3 for i in range(R)], [3 + i % 20 for i in range(R)], [3, 500, 1050], [700, 1300], 2, 1, 64, BF))
+    run(plain.Shared([1] * R, [3 + i % 20 for i in range(R)], [1] + list(range(76, 1077, 4)), [100 + g for g in range(251)], 4, 4, 64, HF))
+
+
+def test_a_planned_step_and_a_found_one_in_one_graph():
+    """Two steps of different kinds behind each other, replayed: their plans and partial results do not mix."""
+    steps = [plain.Shared([1] * 900, [3 + i % 50 for i in range(900)], [0, 900], [600], 4, 2, 64, BF, seed=5),
+             plain.Shared([1] * 24, [1 + 13 * i for i in range(24)], [0, 24], [5000], 8, 2, 128, BF, seed=6)]
+    want = [run(s) for s in steps]
+    now = [[torch.zeros_like(x) for x in w] for w in want]
+    g = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        for s, x in zip(steps, now):
+            zb.zc_paged_shared_attention(*s.args(), out=x[0], lse=x[1])
+    for _ in range(3):
+        for x in now[0] + now[1]:
+            x.fill_(7.0)
+        g.replay()
+        torch.cuda.synchronize()
+        for w, x in zip(want, now):
+            assert torch.equal(w[0], x[0]) and torch.equal(w[1], x[1])
