@@ -10,6 +10,8 @@
 // requests: every wave finds its unit from the lengths.
 #include <limits.h>
 
+#include <type_traits>
+
 #include "paged_args.hpp"
 #include "paged_keys.hpp"
 
@@ -26,6 +28,7 @@ struct ScoreArgs {
   float scale_log2, decay;
   const float* lse;                             // [Hq, T]
   float* scores;                                // [page][head][row]
+  int near_rows;                                // 16 rows of whole tokens lie within 4 GB
   float target;                                 // units a head's keys are split into, about
   uint32_t over_G;                              // ceil(2^32 / G)
 };
@@ -40,6 +43,9 @@ struct Span {
   uint32_t behind;              // 16 keys from key0 on are behind every window if key0 - sinks, without sign, is less than this
 };
 __device__ inline int tile_of(const Span& x, int t) { return t < x.sink_tiles ? t : x.first + t - x.sink_tiles; }
+
+// A copy that the compiler knows nothing of: what is computed from it is computed where it is used, not kept in registers across a loop.
+__device__ inline uint32_t opaque(uint32_t x) { asm volatile("" : "+v"(x)); return x; }
 
 // Unit u of a head; false: there are fewer.
 __device__ inline bool find_span(const ScoreArgs& a, int u, Span& x) {
@@ -66,7 +72,10 @@ __device__ inline bool find_span(const ScoreArgs& a, int u, Span& x) {
     const Part p = part(r0 + lane);
     all += (float)p.tiles * (float)p.passes;
   }
-  const float per = wave_sum(all) / a.target;                                  // work of a unit
+  // Work of a unit: as many units as the chip holds twice, where work is little as it holds once.  us at 512, 1024 and 2048 units: 64 tokens over 64 to 8192 (32 heads over 8 of 128
+  // channels, bf16) 74, 65 and 66, 16 over up to 1694 (8 heads of 64) 14.6, 17.2 and 23.3, 3 requests with 6 tokens over up to 3840 (12 of 64) 11.1, 14.7 and 14.7, 2048 tokens over
+  // 16384 295, 295 and 298.
+  const float share = wave_sum(all) / a.target, per = fmaxf(share, fminf(2.f * share, 5.f));
   int units = 0;
   for (int r0 = 0; r0 < a.R; r0 += 64) {
     const Part p = r0 ? part(r0 + lane) : head;
@@ -108,18 +117,24 @@ __device__ inline float* score_at(const ScoreArgs& a, const Span& x, int hk, int
   return (uint32_t)id < (uint32_t)a.n_pages ? a.scores + (((int64_t)id * a.Hkv + hk) << a.shift) + (key & ((1 << a.shift) - 1)) : nullptr;
 }
 
+// Accumulator v of a 32 x 32 product that was summed in N (of fp32, four: the roundings of one chain of D products are most of a logit's error).
+template <int N> __device__ inline float logit(const v16f (&p)[N], int v) {
+  if constexpr (N == 4) return (p[0][v] + p[1][v]) + (p[2][v] + p[3][v]);
+  else return p[0][v];
+}
+
 // ---- up to 32 rows: single tokens ------------------------------------------------------------------
-// Bound by memory.  A wave has a place for two K blocks in LDS: one is multiplied, the next is on its way.
-template <int DT, int D> struct FewMemory { static constexpr int kBlock = 32 * Tile<DT, D>::ROWB, kBytes = 4 * 2 * kBlock; };
+// Bound by memory.  A wave has a place for one K block in LDS; the next is requested when it has been multiplied.
+template <int DT, int D> struct FewMemory { static constexpr int kBlock = 32 * Tile<DT, D>::ROWB, kBytes = 4 * kBlock; };
 template <int DT, int D>
-__device__ __forceinline__ void score_rows(const ScoreArgs& a, const Span& x, int hk, uint8_t* mem, float* norms) {
+__device__ __forceinline__ void score_rows(const ScoreArgs& a, const Span& x, int hk, uint8_t* mem, float* norms, int* where) {
   using T = Tile<DT, D>;
   constexpr int BLK = FewMemory<DT, D>::kBlock, PG = 16 / T::RPI;
-  constexpr int SUMS = DT == ZC_F32 ? 4 : 1;     // accumulators of an fp32 logit: the roundings of one chain of D products are most of its error
-  const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, kh = lane >> 5;
+  constexpr int SUMS = DT == ZC_F32 ? 4 : 1;
+  const int tid = (int)opaque(threadIdx.x), lane = tid & 63, r = lane & 31, kh = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const uint8_t* kb = a.k + hk * a.k_sH;
-  const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)mem + w * 2 * BLK;
+  const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)mem + w * BLK;
   const int32_t* table = a.table + x.r * a.row;
 
   int voff[PG];
@@ -133,14 +148,14 @@ __device__ __forceinline__ void score_rows(const ScoreArgs& a, const Span& x, in
   // A block's keys are requested, and this lane's score so far.
   float* to = nullptr;
   float old = 0.f;
-  const auto issue = [&](int key0, int place) {
+  const auto issue = [&](int key0) {
     int id[2];
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
       const int k16 = key0 + 16 * g;
       id[g] = page_of(table, a.cols, a.shift, k16);
       const int n = keys_read(a.n_pages, a.sinks, x.behind, x.kv, k16, id[g]);
-      move_keys<PG>(lds + place * BLK + g * 16 * T::ROWB, keys_at(a.shift, kb, a.k_sB, a.k_row, k16, id[g], n), voff);
+      move_keys<PG>(lds + g * 16 * T::ROWB, keys_at(a.shift, kb, a.k_sB, a.k_row, k16, id[g], n), voff);
     }
     const int key = key0 + r, mine = r < 16 ? id[0] : id[1];
     to = nullptr;
@@ -151,7 +166,7 @@ __device__ __forceinline__ void score_rows(const ScoreArgs& a, const Span& x, in
     }
   };
   int b = w, key0 = key_of(b);
-  if (b < blocks) issue(key0, 0);
+  if (b < blocks) issue(key0);
 
   // the rows, straight into operand registers; their normalisers
   const int rows = x.nq * a.G;
@@ -165,21 +180,16 @@ __device__ __forceinline__ void score_rows(const ScoreArgs& a, const Span& x, in
     for (int kc = 0; kc < T::NKC; ++kc) qf[kc] = *reinterpret_cast<const u32x4*>(qr + kc * 32);
   }
   __syncthreads();                               // (the unit before is done with the normalisers)
-  if (tid < 32) norms[tid] = tid < rows ? norm_of(a.lse[(int64_t)(hk * a.G + me.y) * a.T + x.qs + me.x]) : INFINITY;
-  __syncthreads();
-  float norm[16];
-  int pos[16];
-#pragma unroll
-  for (int v = 0; v < 16; ++v) {
-    norm[v] = norms[acc_row(v, kh)];
-    pos[v] = x.kv - x.nq + row_of(a, 0, acc_row(v, kh)).x;
+  if (tid < 32) {
+    norms[tid] = tid < rows ? norm_of(a.lse[(int64_t)(hk * a.G + me.y) * a.T + x.qs + me.x]) : INFINITY;
+    where[tid] = x.kv - x.nq + me.x;
   }
+  __syncthreads();
   typedef __attribute__((address_space(3))) const uint8_t* lds_ptr;
   const uint32_t kaddr = lds + T::slot(r, kh);
   const int p0 = x.kv - x.nq, p1 = x.kv - 1;
-  int place = 0;
   wait_all_loads();
-  for (; b < blocks; b += 4, place ^= 1) {
+  for (; b < blocks; b += 4) {
     const int key = key0 + r, next = b + 4 < blocks ? key_of(b + 4) : 0;
     const int seen_from = p1 - a.window;                                       // keys above it are in every row's window
     const bool whole = key0 + 31 <= p0 && (!a.window || key0 > seen_from || key0 + 31 < a.sinks);
@@ -188,24 +198,28 @@ __device__ __forceinline__ void score_rows(const ScoreArgs& a, const Span& x, in
     wait_all_loads();
     float* const put = to;
     const float before = old;
-    if (b + 4 < blocks) issue(next, place ^ 1);
     float sum = 0.f;
+    v16f acc[SUMS] = {};
     if (any) {
-      v16f acc[SUMS] = {};
 #pragma unroll
       for (int kc = 0; kc < T::NKC; ++kc) {
-        const u32x4 kf = *(__attribute__((address_space(3))) const u32x4*)((lds_ptr)(uintptr_t)(kaddr ^ (32 * kc)) + place * BLK);
+        const u32x4 kf = *(__attribute__((address_space(3))) const u32x4*)(lds_ptr)(uintptr_t)(kaddr ^ (32 * kc));
         mma_chunk<DT>(acc[kc % SUMS], qf[kc], kf);
       }
+    }
+    dma_reuse_fence();
+    if (b + 4 < blocks) issue(next);
+    if (any) {
 #pragma unroll
       for (int v4 = 0; v4 < 4; ++v4) {
         if (8 * v4 >= rows) break;
+        const float4 nv = *reinterpret_cast<const float4*>(&norms[8 * v4 + 4 * kh]);
+        const int4 pv = *reinterpret_cast<const int4*>(&where[8 * v4 + 4 * kh]);
 #pragma unroll
-        for (int v = 4 * v4; v < 4 * v4 + 4; ++v) {
-          float s = acc[0][v];
-          if constexpr (SUMS == 4) s = (acc[0][v] + acc[1][v]) + (acc[2][v] + acc[3][v]);
-          const float e = __builtin_amdgcn_exp2f(fmaf(s, a.scale_log2, -norm[v]));
-          const bool sees = whole || ((key <= pos[v]) & (!a.window || key > pos[v] - a.window || key < a.sinks));
+        for (int u = 0; u < 4; ++u) {
+          const float e = __builtin_amdgcn_exp2f(fmaf(logit<SUMS>(acc, 4 * v4 + u), a.scale_log2, -(&nv.x)[u]));
+          const int p = (&pv.x)[u];
+          const bool sees = whole || ((key <= p) & (!a.window || key > p - a.window || key < a.sinks));
           sum += sees ? e : 0.f;
         }
       }
@@ -217,21 +231,23 @@ __device__ __forceinline__ void score_rows(const ScoreArgs& a, const Span& x, in
 }
 
 // ---- more rows: chunks -----------------------------------------------------------------------------
-// The waves take 64 of a tile's keys and 32 of 64 rows each: K operands stay in registers, rows stream through LDS.
-template <int DT, int D> struct ManyMemory { static constexpr int kTileB = 64 * Tile<DT, D>::ROWB, kBytes = 2 * kTileB; };
+// The waves take 64 of a tile's keys and 32 of every 64 rows each: K operands stay in registers, rows stream through LDS.
+template <int DT, int D> struct ManyMemory { static constexpr int kRows = DT == ZC_F32 ? 64 : 128, kTileB = kRows * Tile<DT, D>::ROWB, kBytes = 2 * kTileB; };
+constexpr int kMostRows = 128;
 template <int DT, int D>
-__device__ __forceinline__ void score_tiles(const ScoreArgs& a, const Span& x, int hk, uint8_t* mem, float (*norms)[64], int (*where)[64], float (*sums)[kScoreTile]) {
+__device__ __forceinline__ void score_tiles(const ScoreArgs& a, const Span& x, int hk, uint8_t* mem, float (*norms)[kMostRows], int (*where)[kMostRows], float (*sums)[kScoreTile]) {
   using T = Tile<DT, D>;
-  constexpr int TILE_B = ManyMemory<DT, D>::kTileB, NI = 64 / T::RPI / 4, PG = 16 / T::RPI;
+  constexpr int QT = ManyMemory<DT, D>::kRows, TILE_B = ManyMemory<DT, D>::kTileB, NI = QT / T::RPI / 4, PG = 16 / T::RPI;
+  static_assert(2 * QT >= kScoreTile, "K passes through both row buffers");
   constexpr int SUMS = DT == ZC_F32 ? 4 : 1;
-  const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, kh = lane >> 5;
+  const int tid = (int)opaque(threadIdx.x), lane = tid & 63, r = lane & 31, kh = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6), rw = w >> 1, kw = w & 1;       // rows 32 rw on of 64, keys 64 kw on of 128
   const uint8_t* kb = a.k + hk * a.k_sH;
   const uint8_t* qb = a.q + (int64_t)hk * a.G * a.q_sH + (int64_t)x.qs * a.q_sT;
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)mem;
   const int32_t* table = a.table + x.r * a.row;
   const int past = x.kv - x.nq;                  // position of the first row's token
-  const int64_t rows = (int64_t)x.nq * a.G;
+  const uint32_t rows = (uint32_t)x.nq * a.G;
   typedef __attribute__((address_space(3))) const uint8_t* lds_ptr;
   using lds_u32x4 = __attribute__((address_space(3))) const u32x4;
 
@@ -239,10 +255,11 @@ __device__ __forceinline__ void score_tiles(const ScoreArgs& a, const Span& x, i
     const int key0 = tile_of(x, t) * kScoreTile;
     // ---- K to registers, by way of both row buffers
     int voff[PG];
+    const int kl = (int)opaque(lane);
 #pragma unroll
     for (int j = 0; j < PG; ++j) {
-      const int row = j * T::RPI + lane / T::CPR;
-      voff[j] = (int)(row * a.k_row) + (((lane % T::CPR) ^ T::swz(row)) << 4);
+      const int row = j * T::RPI + kl / T::CPR;
+      voff[j] = (int)(row * a.k_row) + (((kl % T::CPR) ^ T::swz(row)) << 4);
     }
     __syncthreads();                             // (the tile before is done with LDS)
 #pragma unroll
@@ -270,71 +287,179 @@ __device__ __forceinline__ void score_tiles(const ScoreArgs& a, const Span& x, i
     const int key1 = min(key0 + kScoreTile, x.kv) - 1;
     int j_first = max(key0 - past, 0), j_end = x.nq;
     if (a.window && key0 >= a.sinks) j_end = (int)min((int64_t)x.nq, (int64_t)key1 + a.window - past);
-    const int64_t i_first = (int64_t)j_first * a.G / 64 * 64, i_end = (int64_t)max(j_end, 0) * a.G;
-    int j0 = (int)(i_first / a.G), g0 = (int)(i_first - (int64_t)j0 * a.G);    // token and head of the tile's first row
-    const auto advance = [&](int& j, int& g) { const int2 n = row_of(a, j, g + 64); j = n.x; g = n.y; };
+    const uint32_t i_first = (uint32_t)j_first * a.G / QT * QT, i_end = (uint32_t)max(j_end, 0) * a.G;
+    int j0 = (int)(i_first / (uint32_t)a.G), g0 = (int)(i_first - (uint32_t)j0 * a.G);     // token and head of the tile's first row
+    // Rows to LDS, and this thread's normaliser to a register.  Where 16 rows are whole tokens all tiles but one that is not full lie alike: a
+    // base that advances, and one offset a lane.
+    constexpr bool SAME = 4 * T::RPI % 16 == 0;  // (the swizzle repeats from one of a wave's transfers to the next)
+    const bool even = SAME && 16 % a.G == 0 && a.near_rows;
+    uint32_t off = 0;
+    if (even) {
+      const int row = w * T::RPI + lane / T::CPR;
+      const int2 me = row_of(a, 0, row);
+      off = (uint32_t)(me.y * a.q_sH + me.x * a.q_sT) + (((lane % T::CPR) ^ T::swz(row)) << 4);
+    }
+    const int hop = 4 * T::RPI / a.G, tokens = QT / a.G;                       // of a transfer to the next, of a tile
+    const uint8_t* base = qb + (int64_t)j0 * a.q_sT;
+    const int64_t q_hop = hop * a.q_sT, q_step = tokens * a.q_sT - NI * q_hop;
+    const int2 at0 = row_of(a, j0, g0 + (tid < QT ? tid : 0));
+    const float* norm_from = a.lse + (int64_t)(hk * a.G + at0.y) * a.T + x.qs + at0.x;
     float norm;
-    int pos;
-    const auto issue = [&](int64_t i0, int j, int g, int buf) {
-      const int left = (int)min((int64_t)64, rows - i0);
+    int pos = past + at0.x - tokens;
+    const auto issue = [&](uint32_t i0, int j, int g, int buf) {
+      const uint32_t left = rows - i0;
+      if (even && left >= QT) {
 #pragma unroll
-      for (int jj = 0; jj < NI; ++jj) {
-        const int row = (w + 4 * jj) * T::RPI + lane / T::CPR;
-        const int2 me = row_of(a, j, g + min(row, left - 1));
-        gdma16(lds + buf * TILE_B + (w + 4 * jj) * 1024, qb + (int64_t)me.y * a.q_sH + (int64_t)me.x * a.q_sT + (((lane % T::CPR) ^ T::swz(row)) << 4));
+        for (int jj = 0; jj < NI; ++jj, base += q_hop) gdma16(lds + buf * TILE_B + (w + 4 * jj) * 1024, base, off);
+        base += q_step;
+        pos += tokens;
+        if (tid < QT) norm = *norm_from;
+        norm_from += tokens;
+        return;
       }
-      if (tid < 64) {
-        const int2 me = row_of(a, j, g + min(tid, left - 1));
-        norm = tid < left ? norm_of(a.lse[(int64_t)(hk * a.G + me.y) * a.T + x.qs + me.x]) : INFINITY;
+      const int ql = (int)opaque(lane), qt = (int)opaque(tid);
+#pragma unroll 1
+      for (int jj = 0; jj < NI; ++jj) {
+        const int row = (w + 4 * jj) * T::RPI + ql / T::CPR;
+        const int2 me = row_of(a, j, g + min(row, (int)min(left, (uint32_t)QT) - 1));
+        gdma16(lds + buf * TILE_B + (w + 4 * jj) * 1024, qb + (int64_t)me.y * a.q_sH + (int64_t)me.x * a.q_sT + (((ql % T::CPR) ^ T::swz(row)) << 4));
+      }
+      if (qt < QT) {
+        const bool there = (uint32_t)qt < left;
+        const int2 me = row_of(a, j, g + (there ? qt : 0));
+        norm = there ? a.lse[(int64_t)(hk * a.G + me.y) * a.T + x.qs + me.x] : -INFINITY;
         pos = past + me.x;
       }
     };
     float sum[2] = {0.f, 0.f};
+    v16f acc[2][SUMS];
+    // Weights of 32 rows (norms and positions: `rows_of`) and the keys n, which not all rows see.
+    const auto masked = [&](int n, const float* norm_of_row, const int* pos_of_row) {
+      const int key = key0 + 64 * kw + 32 * n + r;
+#pragma unroll
+      for (int v4 = 0; v4 < 4; ++v4) {
+        const float4 nv = *reinterpret_cast<const float4*>(norm_of_row + 8 * v4);
+        const int4 pv = *reinterpret_cast<const int4*>(pos_of_row + 8 * v4);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int p = (&pv.x)[u];
+          const float e = __builtin_amdgcn_exp2f(fmaf(logit<SUMS>(acc[n], 4 * v4 + u), a.scale_log2, -(&nv.x)[u]));
+          sum[n] += ((key <= p) & (!a.window || key > p - a.window || key < a.sinks)) ? e : 0.f;
+          __builtin_amdgcn_sched_barrier(0);     // (or the operands of all 16 are brought in front, into registers there are not)
+        }
+      }
+    };
+    // Products of the keys n with 32 rows, and meanwhile, of 16-bit types, the weights of the products before, of keys m, if all rows see them.
+    const auto step = [&](auto weigh, int n, uint32_t row, int m, const float* norm_of_row) {
+      constexpr bool WEIGH = decltype(weigh)::value;
+      row = opaque(row);
+#pragma unroll
+      for (int i = 0; i < SUMS; ++i) acc[n][i] = v16f{};
+      u32x4 q[2];
+      q[0] = *reinterpret_cast<lds_u32x4*>((lds_ptr)(uintptr_t)row);
+      q[1] = *reinterpret_cast<lds_u32x4*>((lds_ptr)(uintptr_t)(row ^ 32));
+      float4 nv;
+      constexpr int EACH = 16 / T::NKC;          // weights of a step
+#pragma unroll
+      for (int kc = 0; kc < T::NKC; ++kc) {
+        if constexpr (WEIGH)
+          if (kc * EACH % 4 == 0) nv = *reinterpret_cast<const float4*>(norm_of_row + 2 * kc * EACH);
+        mma_chunk<DT>(acc[n][kc % SUMS], q[kc & 1], kf[n][kc]);
+        if (kc + 2 < T::NKC) q[kc & 1] = *reinterpret_cast<lds_u32x4*>((lds_ptr)(uintptr_t)(row ^ ((kc + 2) << 5)));
+        if constexpr (WEIGH)
+#pragma unroll
+          for (int v = kc * EACH; v < (kc + 1) * EACH; ++v)
+            sum[m] += __builtin_amdgcn_exp2f(fmaf(logit<SUMS>(acc[m], v), a.scale_log2, -(&nv.x)[v & 3]));
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    // The same of 16-bit types with the rows' operands `q` in registers, and their normalisers `nv` of the weights: what a step has used is replaced by
+    // what the step after the next (q) or the next (nv) needs, so that no step waits for LDS.
+    u32x4 q[DT == ZC_F32 ? 1 : T::NKC];
+    float4 nv[4];
+    const auto flow = [&](auto weigh, auto keys, auto refill, uint32_t next_row, const float* next_norm) {
+      constexpr bool WEIGH = decltype(weigh)::value, REFILL = decltype(refill)::value;
+      constexpr int n = decltype(keys)::value;       // (keys 0: the rows' normalisers come, keys 1: the next rows)
+      constexpr int EACH = 16 / T::NKC;
+      acc[n][0] = v16f{};
+      if constexpr (REFILL) next_row = opaque(next_row);
+#pragma unroll
+      for (int kc = 0; kc < T::NKC; ++kc) {
+        mma_chunk<DT>(acc[n][0], q[kc], kf[n][kc]);
+        if constexpr (WEIGH)
+#pragma unroll
+          for (int v = kc * EACH; v < (kc + 1) * EACH; ++v)
+            sum[n ^ 1] += __builtin_amdgcn_exp2f(fmaf(acc[n ^ 1][0][v], a.scale_log2, -(&nv[v >> 2].x)[v & 3]));
+        if constexpr (REFILL) q[kc] = *reinterpret_cast<lds_u32x4*>((lds_ptr)(uintptr_t)(next_row ^ (kc << 5)));
+        if (n == 0 && (kc + 1) * EACH % 4 == 0) nv[(kc + 1) * EACH / 4 - 1] = *reinterpret_cast<const float4*>(next_norm + 2 * ((kc + 1) * EACH - 4));
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    const auto weigh_only = [&](int m, const float* norm_of_row) {
+#pragma unroll
+      for (int v4 = 0; v4 < 4; ++v4) {
+        const float4 nv = *reinterpret_cast<const float4*>(norm_of_row + 8 * v4);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) sum[m] += __builtin_amdgcn_exp2f(fmaf(logit<SUMS>(acc[m], 4 * v4 + u), a.scale_log2, -(&nv.x)[u]));
+      }
+    };
     __syncthreads();                             // (K is in registers)
     if (i_first < i_end) issue(i_first, j0, g0, 0);
     int buf = 0;
-    for (int64_t i0 = i_first; i0 < i_end; i0 += 64, buf ^= 1) {
-      int jn = j0, gn = g0;
-      advance(jn, gn);
+    const int mine = 32 * rw + 4 * kh;           // of the tile's rows, the first that this lane's accumulators hold
+    bool pending = false;                        // weights of keys 1 of the tile before, which all its rows see
+    for (uint32_t i0 = i_first; i0 < i_end; i0 += QT, buf ^= 1) {
+      const int2 next = row_of(a, j0, g0 + QT);
       wait_vmem<0>();
       wait_all_loads();
-      if (tid < 64) { norms[buf][tid] = norm; where[buf][tid] = pos; }
+      if (tid < QT) { norms[buf][tid] = norm_of(norm); where[buf][tid] = pos; }
       __syncthreads();                           // rows and normalisers are there, and nobody still reads the other buffer
-      if (i0 + 64 < i_end) issue(i0 + 64, jn, gn, buf ^ 1);
+      if (i0 + QT < i_end) issue(i0 + QT, next.x, next.y, buf ^ 1);
       const uint32_t row = lds + buf * TILE_B + 32 * rw * T::ROWB + T::slot(r, kh);
-      const int pa = past + j0, pb = past + row_of(a, j0, g0 + 63).x;          // positions of the tile's first and last row
+      const int pa = past + j0, pb = past + row_of(a, j0, g0 + QT - 1).x;          // positions of the tile's first and last row
       const bool whole = key0 + kScoreTile - 1 <= pa && (!a.window || key0 > pb - a.window || key0 + kScoreTile - 1 < a.sinks);
+      if constexpr (DT == ZC_F32) {
+        if (pending) step(std::true_type{}, 0, row, 1, &norms[buf ^ 1][mine]);
+        else step(std::false_type{}, 0, row, 1, nullptr);
+        if (whole) step(std::true_type{}, 1, row, 0, &norms[buf][mine]);
+        else step(std::false_type{}, 1, row, 0, nullptr);
+      } else {
+        const uint32_t first = opaque(row);
 #pragma unroll
-      for (int n = 0; n < 2; ++n) {
-        v16f acc[SUMS] = {};
+        for (int kc = 0; kc < T::NKC; ++kc) q[kc] = *reinterpret_cast<lds_u32x4*>((lds_ptr)(uintptr_t)(first ^ (kc << 5)));
 #pragma unroll
-        for (int kc = 0; kc < T::NKC; ++kc) {
-          const u32x4 qf = *reinterpret_cast<lds_u32x4*>((lds_ptr)(uintptr_t)(row ^ (32 * kc)));
-          mma_chunk<DT>(acc[kc % SUMS], qf, kf[n][kc]);
-        }
-        const int key = key0 + 64 * kw + 32 * n + r;
-#pragma unroll
-        for (int v4 = 0; v4 < 4; ++v4) {
-          const float4 nv = *reinterpret_cast<const float4*>(&norms[buf][32 * rw + 8 * v4 + 4 * kh]);
-          const int4 pv = *reinterpret_cast<const int4*>(&where[buf][32 * rw + 8 * v4 + 4 * kh]);
-#pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            const int v = 4 * v4 + u;
-            float s = acc[0][v];
-            if constexpr (SUMS == 4) s = (acc[0][v] + acc[1][v]) + (acc[2][v] + acc[3][v]);
-            const float e = __builtin_amdgcn_exp2f(fmaf(s, a.scale_log2, -(&nv.x)[u]));
-            if (whole) {
-              sum[n] += e;
-            } else {
-              const int p = (&pv.x)[u];
-              sum[n] += ((key <= p) & (!a.window || key > p - a.window || key < a.sinks)) ? e : 0.f;
-            }
+        for (int h = 0; h < QT / 64; ++h) {
+          using K0 = std::integral_constant<int, 0>;
+          using K1 = std::integral_constant<int, 1>;
+          const float* const of_these = &norms[buf][mine + 64 * h];
+          const uint32_t behind = row + 64 * (h + 1) * T::ROWB;
+          if (pending) flow(std::true_type{}, K0{}, std::false_type{}, 0, of_these);
+          else flow(std::false_type{}, K0{}, std::false_type{}, 0, of_these);
+          if (h + 1 < QT / 64) {
+            if (whole) flow(std::true_type{}, K1{}, std::true_type{}, behind, nullptr);
+            else flow(std::false_type{}, K1{}, std::true_type{}, behind, nullptr);
+          } else {
+            if (whole) flow(std::true_type{}, K1{}, std::false_type{}, 0, nullptr);
+            else flow(std::false_type{}, K1{}, std::false_type{}, 0, nullptr);
+          }
+          pending = whole;
+          if (!whole) {
+            masked(0, &norms[buf][mine + 64 * h], &where[buf][mine + 64 * h]);
+            masked(1, &norms[buf][mine + 64 * h], &where[buf][mine + 64 * h]);
           }
         }
       }
-      j0 = jn;
-      g0 = gn;
+      if constexpr (DT == ZC_F32) {
+        pending = whole;
+        if (!whole) {
+          masked(0, &norms[buf][mine], &where[buf][mine]);
+          masked(1, &norms[buf][mine], &where[buf][mine]);
+        }
+      }
+      j0 = next.x;
+      g0 = next.y;
     }
+    if (pending) weigh_only(1, &norms[buf ^ 1][mine + QT - 64]);
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
       sum[n] += __shfl_xor(sum[n], 32);
@@ -346,15 +471,15 @@ __device__ __forceinline__ void score_tiles(const ScoreArgs& a, const Span& x, i
 }
 
 template <int DT, int D>
-__global__ __launch_bounds__(256, DT == ZC_F32 && D == 128 ? 1 : 2) void k_paged_scores(ScoreArgs a) {
+__global__ __launch_bounds__(256, DT != ZC_F32 ? 2 : D == 64 ? 2 : 1) void k_paged_scores(ScoreArgs a) {
   constexpr int kFew = FewMemory<DT, D>::kBytes, kMany = ManyMemory<DT, D>::kBytes;
   __shared__ __align__(1024) uint8_t mem[kFew > kMany ? kFew : kMany];
-  __shared__ __align__(16) float norms[2][64];
-  __shared__ __align__(16) int where[2][64];
+  __shared__ __align__(16) float norms[2][kMostRows];
+  __shared__ __align__(16) int where[2][kMostRows];
   __shared__ float sums[2][kScoreTile];
   Span x;
   for (int u = blockIdx.y; find_span(a, u, x); u += gridDim.y) {
-    if ((int64_t)x.nq * a.G <= 32) score_rows<DT, D>(a, x, blockIdx.x, mem, norms[0]);
+    if ((int64_t)x.nq * a.G <= 32) score_rows<DT, D>(a, x, blockIdx.x, mem, norms[0], where[0]);
     else score_tiles<DT, D>(a, x, blockIdx.x, mem, norms, where, sums);
   }
 }
@@ -407,7 +532,10 @@ extern "C" int zc_paged_scores(const zc_tensor4* q, const zc_tensor4* k_pages, c
   a.over_G = G == 1 ? 0 : (uint32_t)(((1ull << 32) + G - 1) / G);
   const int64_t target = ceil_div64(1024, Hkv), tiles = ceil_div64(room, kScoreTile), with = R < T ? R : T;
   a.target = (float)target;
-  const int64_t most = tiles > 65535 / with ? 65535 : tiles * with, units = target + with < most ? target + with : most;
+  a.near_rows = q->sH >= 0 && q->sL >= 0 && G * a.q_sH + 16 * a.q_sT < 0xffffff00ll;
+  // (a workgroup takes more units where there are; those that find none cost their places: where a table's room allows few tiles, as many as the chip holds)
+  const int64_t all = tiles > 65535 / with ? 65535 : tiles * with, at_once = T * G <= 32 * R && all * Hkv <= 2560 ? ceil_div64(512, Hkv) : target;
+  const int64_t units = at_once + with < all ? at_once + with : all;
   hipStream_t st = (hipStream_t)stream;
 #define ZC_PS(DT) (q->D == 128 ? launch_scores<DT, 128>(a, (int)units, st) : launch_scores<DT, 64>(a, (int)units, st))
   if (q->dtype == ZC_F32) rc = ZC_PS(ZC_F32);
