@@ -465,9 +465,9 @@ int zc_paged_scores(const zc_tensor4* q, const zc_tensor4* k_pages, const int32_
  * A request's pages must be its own: not another's, not twice in its row.  A token whose entry is no page has a score of 0 and zeros for
  * its rows, a place without a page takes nothing, and among the pages that are left such an entry is written like any other: evict with the lengths
  * that zc_paged_tables found pages for.  kv_len outside [0, max_blocks * page] is taken for the nearest.
- * Deterministic.  R may be 0; R and 3 Hkv <= 65535.  Workspace: zc_paged_evict_workspace() bytes, 16-byte aligned, with any contents (0 without
- * `together`, else 4 for every place of every row of the table); calls that share one must not run concurrently. */
-size_t zc_paged_evict_workspace(int64_t R, int64_t max_blocks, int64_t page, int32_t together);
+ * Deterministic.  R may be 0; R and 3 Hkv <= 65535.  Workspace: zc_paged_evict_workspace() bytes, 16-byte aligned, with any contents (4 for every
+ * list, with `together` 4 for every place of every row of the table too); calls that share one must not run concurrently. */
+size_t zc_paged_evict_workspace(int64_t R, int64_t Hkv, int64_t max_blocks, int64_t page, int32_t together);
 int zc_paged_evict(const zc_tensor4* k_pages, const zc_tensor4* v_pages, float* scores, const int32_t* block_table, int64_t row_stride,
                    int64_t max_blocks, const int32_t* kv_len, const int32_t* keep, int64_t R, int64_t most, int32_t sinks, int32_t recent,
                    int32_t together, int32_t* new_len, int32_t* kept, int32_t* free_pages, int64_t n_list, const int32_t* n_free,

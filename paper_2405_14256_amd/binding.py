@@ -125,7 +125,7 @@ def load() -> C.CDLL:
     lib.zc_paged_scores.restype = C.c_int
     lib.zc_paged_scores.argtypes = [T4, T4, P, I64, I64, P, P, I64, I32, I32, F, P, F, P, P]
     lib.zc_paged_evict_workspace.restype = SZ
-    lib.zc_paged_evict_workspace.argtypes = [I64, I64, I64, I32]
+    lib.zc_paged_evict_workspace.argtypes = [I64, I64, I64, I64, I32]
     lib.zc_paged_evict.restype = C.c_int
     lib.zc_paged_evict.argtypes = [T4, T4, P, P, I64, I64, P, P, I64, I64, I32, I32, I32, P, P, P, I64, P, P, P, SZ, P]
     lib.zc_arena_bytes.restype = SZ

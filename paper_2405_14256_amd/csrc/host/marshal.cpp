@@ -626,7 +626,7 @@ PyObject* paged_evict(PyObject*, Args a, Py_ssize_t n) {
     const auto* n_free = ints(a[13], "n_free", 1);
     auto* n_freed = ints(a[14], "n_freed", 1);
     const hipStream_t st = current_stream();
-    const size_t need = ZC_FN(kPagedEvictWs, zc_paged_evict_workspace)(t.R, t.cols, kp.L, together);
+    const size_t need = ZC_FN(kPagedEvictWs, zc_paged_evict_workspace)(t.R, kp.H, t.cols, kp.L, together);
     const Scratch ws = paged_scratch(need, tensor_of(a[0]), kScratchEvict, st);
     void* wp = ws.ptr;
     const size_t wn = ws.bytes;

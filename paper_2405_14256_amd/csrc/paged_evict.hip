@@ -6,6 +6,8 @@
 // list[i] >= i.  So a workgroup that takes some channels of a (request, head) for itself may go through the list from its start, reading
 // as far ahead as it likes, and needs no copy and no other workgroup: the place i that it fills was read by then, as the
 // token there, if it stays, is the i-th of the list or one before.
+#include <limits.h>
+
 #include "lds_dma.hpp"
 #include "paged_args.hpp"
 
@@ -24,6 +26,7 @@ struct EvictArgs {
   const int32_t* n_free;
   int64_t n_list;
   const float* sums;                                     // [R, cap], of all heads (null: every head by its own scores)
+  int* moved;                                            // [R, heads], the first of a list that lies elsewhere than it will
   int rowb, slice, lanes;                                // bytes of a row, of a workgroup's part of it; 16-byte pieces of that, as a shift
 };
 
@@ -111,7 +114,7 @@ __global__ __launch_bounds__(THREADS) void k_evict_pick(EvictArgs a) {
   constexpr int NW = THREADS / 64, CHUNK = THREADS * kEach, PER = kBins / THREADS;
   __shared__ __align__(16) int bins[3][kBins];
   __shared__ int waves[5][NW];
-  __shared__ int s_digit[3], s_above[3], s_count[3];
+  __shared__ int s_digit[3], s_above[3], s_count[3], s_moved;
   const int r = blockIdx.y, h = blockIdx.x, tid = threadIdx.x;
   int id[HELD];
 #pragma unroll
@@ -131,7 +134,11 @@ __global__ __launch_bounds__(THREADS) void k_evict_pick(EvictArgs a) {
   const int chunks = (int)(((int64_t)hi + CHUNK - 1) / CHUNK);
   for (int i = tid; i < sinks; i += THREADS) list[i] = i;
   for (int i = tid; i < recent; i += THREADS) list[stay - recent + i] = kv - recent + i;
-  if (need == 0) return;
+  if (need == 0) {
+    if (tid == 0) a.moved[r * a.heads + h] = sinks;
+    return;
+  }
+  if (tid == 0) s_moved = stay - recent;
   Images held[HELD];
 #pragma unroll
   for (int c = 0; c < HELD; ++c) held[c] = images(a, r, h, c * CHUNK + tid * kEach, hi, id[c]);
@@ -197,6 +204,7 @@ __global__ __launch_bounds__(THREADS) void k_evict_pick(EvictArgs a) {
   }
 
   int placed = sinks, equal = 0;                           // of the chunks before
+  int moved = INT_MAX;                                     // the first of this wave's that moves
   sweep([&](int i0, const Images& m) {
     int over = 0, same = 0;
 #pragma unroll
@@ -207,16 +215,24 @@ __global__ __launch_bounds__(THREADS) void k_evict_pick(EvictArgs a) {
     int all_same, all_mine;
     int left = max(ties - equal - (block_inclusive_sum<NW>(same, waves[3], all_same) - same), 0);      // equals that stay from this thread's first on
     const int mine = over + min(left, same);
-    int at = placed + block_inclusive_sum<NW>(mine, waves[4], all_mine) - mine;
+    int at = placed + block_inclusive_sum<NW>(mine, waves[4], all_mine) - mine, first = INT_MAX;
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
       const bool tie = candidate(i0 + e) && m.x[e] == least && left > 0;
       left -= tie;
-      if (tie || (candidate(i0 + e) && m.x[e] > least)) list[at++] = i0 + e;
+      if (tie || (candidate(i0 + e) && m.x[e] > least)) {
+        if (at != i0 + e) first = min(first, at);
+        list[at++] = i0 + e;
+      }
     }
     equal += all_same;
     placed += all_mine;
+    const uint64_t any = __builtin_amdgcn_ballot_w64(first != INT_MAX);          // (places ascend with the lanes, and with the chunks)
+    if (any && moved == INT_MAX) moved = __builtin_amdgcn_readlane(first, __builtin_ctzll(any));
   });
+  if ((tid & 63) == 0 && moved != INT_MAX) atomicMin(&s_moved, moved);
+  __syncthreads();
+  if (tid == 0) a.moved[r * a.heads + h] = s_moved;
 }
 
 // ---- the rows -------------------------------------------------------------------------------------
@@ -260,13 +276,14 @@ __global__ __launch_bounds__(kMoveThreads, 4) void k_evict_move(EvictArgs a) {
       if (next[u] != i) x[u] = {slot_at(a, r, next[u]), slot_at(a, r, i)};
     }
   };
-  const int step = per * kMove;
-  entries(0);
-  find(0, m);
-  entries(step);
+  const int step = per * kMove, begin = a.moved[r * a.heads + (a.heads > 1 ? h : 0)];       // (what is in front of it stays where it is)
+  if (begin >= stay) return;
+  entries(begin);
+  find(begin, m);
+  entries(begin + step);
   if (what == 2) {
     const auto at = [&](int slot) { return a.scores + (((int64_t)(slot >> a.shift) * a.Hkv + h) << a.shift) + (slot & inside); };
-    for (int i0 = 0; i0 < stay; i0 += step) {
+    for (int i0 = begin; i0 < stay; i0 += step) {
       float x[kMove];
       find(i0 + step, ahead);
 #pragma unroll
@@ -285,7 +302,7 @@ __global__ __launch_bounds__(kMoveThreads, 4) void k_evict_move(EvictArgs a) {
   uint8_t* pool = a.pool[what] + blockIdx.x * a.slice + (threadIdx.x & ((1 << lanes) - 1)) * 16 + h * a.sH[what];
   const int64_t sB = a.sB[what], sL = a.sL[what];
   const auto at = [&](int slot) { return reinterpret_cast<piece16*>(pool + (slot >> a.shift) * sB + (slot & inside) * sL); };
-  for (int i0 = 0; i0 < stay; i0 += step) {
+  for (int i0 = begin; i0 < stay; i0 += step) {
     piece16 x[kMove];
     find(i0 + step, ahead);
 #pragma unroll
@@ -310,9 +327,9 @@ using namespace zc;
 
 __global__ void k_evict_none(int32_t* n_freed) { *n_freed = 0; }
 
-extern "C" size_t zc_paged_evict_workspace(int64_t R, int64_t max_blocks, int64_t page, int32_t together) {
-  if (!together || R <= 0 || max_blocks <= 0 || page <= 0 || R > 65535 || max_blocks > 0x7fff0000 / page) return 0;
-  return (size_t)(R * max_blocks * page) * sizeof(float);
+extern "C" size_t zc_paged_evict_workspace(int64_t R, int64_t Hkv, int64_t max_blocks, int64_t page, int32_t together) {
+  if (R <= 0 || Hkv <= 0 || max_blocks < 0 || page <= 0 || R > 65535 || Hkv > 65535 || max_blocks > 0x7fff0000 / page) return 0;
+  return (size_t)align_up64(R * (together ? 1 : Hkv) * 4, 16) + (together ? (size_t)(R * max_blocks * page) * sizeof(float) : 0);
 }
 
 extern "C" int zc_paged_evict(const zc_tensor4* k_pages, const zc_tensor4* v_pages, float* scores, const int32_t* block_table, int64_t row_stride,
@@ -340,8 +357,8 @@ extern "C" int zc_paged_evict(const zc_tensor4* k_pages, const zc_tensor4* v_pag
   if (R > 65535 || 3 * H > 65535 || most > 0x7fffffff || max_blocks > 0x7fff0000 / page || n_list > 0x7fffffff) return ZC_ERR_UNSUPPORTED;
   for (const int32_t* p : {kv_len, keep})                // (lengths are read until the last launch)
     if (new_len < p + R && p < new_len + R) return ZC_ERR_INVALID_ARG;
-  const size_t need = zc_paged_evict_workspace(R, max_blocks, page, together);
-  if (need && (!ws || ws_bytes < need || (reinterpret_cast<uintptr_t>(ws) & 15))) return ZC_ERR_WORKSPACE;
+  const size_t need = zc_paged_evict_workspace(R, H, max_blocks, page, together);
+  if ((!ws || ws_bytes < need || (reinterpret_cast<uintptr_t>(ws) & 15))) return ZC_ERR_WORKSPACE;
 
   const int64_t eb = elem_bytes(k_pages->dtype);
   EvictArgs a;
@@ -357,10 +374,12 @@ extern "C" int zc_paged_evict(const zc_tensor4* k_pages, const zc_tensor4* v_pag
   a.most = most; a.sinks = sinks; a.recent = recent;
   a.new_len = new_len; a.kept = kept; a.free_pages = free_pages; a.n_freed = n_freed; a.n_free = n_free; a.n_list = n_list;
   a.sums = nullptr;
-  if (need) {
-    hipLaunchKernelGGL(k_evict_sums, dim3((unsigned)ceil_div64(a.cap, 256), (unsigned)R), dim3(64), 0, st, a, (float*)ws);
+  a.moved = (int*)ws;
+  if (together && a.cap) {
+    float* sums = (float*)((uint8_t*)ws + align_up64(R * 4, 16));
+    hipLaunchKernelGGL(k_evict_sums, dim3((unsigned)ceil_div64(a.cap, 256), (unsigned)R), dim3(64), 0, st, a, sums);
     ZC_LAUNCH_CHECK();
-    a.sums = (const float*)ws;
+    a.sums = sums;
   }
   const dim3 lists((unsigned)a.heads + 1, (unsigned)R);
   if (a.cap <= 512 * kEach) hipLaunchKernelGGL((k_evict_pick<512, 1>), lists, dim3(512), 0, st, a);

@@ -18,7 +18,7 @@ def test_refuses_bad_arguments_before_launch():
     lib = zb.load()
 
     def call(kp=None, vp=None, scores=0x20000, table=0x30000, row=8, cols=8, kv=0x40000, keep=0x50000, R=4, most=20, sinks=0, recent=0, together=0,
-             new=0x60000, kept=0x70000, free=0x80000, n_list=9, n_free=0x90000, n_freed=0xa0000, ws=None, wn=0):
+             new=0x60000, kept=0x70000, free=0x80000, n_list=9, n_free=0x90000, n_freed=0xa0000, ws=0xb0000, wn=1 << 30):
         kp, vp = kp or _pool(), vp or _pool()
         return lib.zc_paged_evict(C.byref(kp), C.byref(vp), scores, table, row, cols, kv, keep, R, most, sinks, recent, together, new, kept, free, n_list,
                                   n_free, n_freed, ws, wn, None)
@@ -31,12 +31,14 @@ def test_refuses_bad_arguments_before_launch():
     for kw in (dict(R=65536), dict(most=1 << 31), dict(cols=1 << 28, row=1 << 28), dict(n_list=1 << 31), dict(kp=_pool(L=24), vp=_pool(L=24)),
                dict(kp=_pool(H=21846), vp=_pool(H=21846)), dict(kp=_pool(D=96), vp=_pool(D=96))):
         assert call(**kw) == UNS, kw
-    need = lib.zc_paged_evict_workspace(4, 8, 16, 1)
-    assert need == 4 * 8 * 16 * 4 and lib.zc_paged_evict_workspace(4, 8, 16, 0) == 0 and lib.zc_paged_evict_workspace(0, 8, 16, 1) == 0
-    for kw in (dict(), dict(ws=0xb0000, wn=need - 1), dict(ws=0xb0008, wn=need)):
-        assert call(together=1, **kw) == WSP, kw
+    size = lib.zc_paged_evict_workspace
+    assert size(4, 8, 8, 16, 1) == 4 * 8 * 16 * 4 + 16 and size(4, 8, 8, 16, 0) == 4 * 8 * 4 and size(0, 8, 8, 16, 1) == 0
+    for together in (0, 1):
+        need = size(4, 8, 8, 16, together)
+        for kw in (dict(ws=None), dict(wn=need - 1), dict(ws=0xb0008)):
+            assert call(together=together, **kw) == WSP, kw
     # nothing to do is no error
-    assert call(R=0, kv=None, keep=None, new=None, kept=None, table=None, free=None, n_free=None, n_freed=None) == 0
+    assert call(R=0, kv=None, keep=None, new=None, kept=None, table=None, free=None, n_free=None, n_freed=None, ws=None, wn=0) == 0
 
 
 def test_binding_refuses_tensors_that_are_not_what_a_call_needs():
