@@ -64,22 +64,21 @@ __global__ __launch_bounds__(64) void k_evict_sums(EvictArgs a, float* sums) {
 // from histograms in LDS, until every score with the digits so far stays; then every thread counts what it has above and at that score, and
 // a scan of the counts gives the places.  A thread has consecutive tokens, so the list comes out in order and of equal scores the
 // first ones stay.
-constexpr int kEach = 8, kBins = 2048;
+constexpr int kEach = 4, kBins = 2048;
 
-// A thread's scores of eight tokens from i0 on, as order-preserving images.  id: the page of i0.
+// A thread's scores of four tokens from i0 on, as order-preserving images.  id: the page of i0.
 struct Images { uint32_t x[kEach]; };
 __device__ inline Images images(const EvictArgs& a, int r, int h, int i0, int hi, int id) {
-  float4 v[2] = {};
+  float4 v = {};
   const bool page = (uint32_t)id < (uint32_t)a.n_pages;
   if (i0 < hi && (a.sums || page)) {
     const float* s = a.sums ? a.sums + (int64_t)r * a.cap + i0       // (cap: whole pages)
                             : a.scores + (((int64_t)id * a.Hkv + h) << a.shift) + (i0 & ((1 << a.shift) - 1));
-    v[0] = reinterpret_cast<const float4*>(s)[0];
-    v[1] = reinterpret_cast<const float4*>(s)[1];
+    v = *reinterpret_cast<const float4*>(s);
   }
   Images m;
 #pragma unroll
-  for (int e = 0; e < kEach; ++e) m.x[e] = float_key((&v[e >> 2].x)[e & 3] + 0.f);      // (-0 ties with 0)
+  for (int e = 0; e < kEach; ++e) m.x[e] = float_key((&v.x)[e] + 0.f);      // (-0 ties with 0)
   return m;
 }
 __device__ inline int page_of(const EvictArgs& a, int r, int i) { return a.cols ? a.table[r * a.row + min(i >> a.shift, a.cols - 1)] : -1; }
@@ -155,9 +154,7 @@ __global__ __launch_bounds__(THREADS) void k_evict_pick(EvictArgs a) {
   };
   const auto candidate = [&](int i) { return i >= lo && i < hi; };
 
-#pragma unroll
-  for (int p = 0; p < 3; ++p)
-    for (int b = tid; b < kBins; b += THREADS) bins[p][b] = 0;
+  for (int b = tid; b < 3 * kBins / 4; b += THREADS) reinterpret_cast<int4*>(bins)[b] = make_int4(0, 0, 0, 0);
   __syncthreads();
   // What is above `least` stays, and the first `ties` of its equals.
   uint32_t prefix = 0, least = 0;
@@ -384,7 +381,8 @@ extern "C" int zc_paged_evict(const zc_tensor4* k_pages, const zc_tensor4* v_pag
   const dim3 lists((unsigned)a.heads + 1, (unsigned)R);
   if (a.cap <= 512 * kEach) hipLaunchKernelGGL((k_evict_pick<512, 1>), lists, dim3(512), 0, st, a);
   else if (a.cap <= 1024 * kEach) hipLaunchKernelGGL((k_evict_pick<1024, 1>), lists, dim3(1024), 0, st, a);
-  else hipLaunchKernelGGL((k_evict_pick<1024, 2>), lists, dim3(1024), 0, st, a);
+  else if (a.cap <= 2 * 1024 * kEach) hipLaunchKernelGGL((k_evict_pick<1024, 2>), lists, dim3(1024), 0, st, a);
+  else hipLaunchKernelGGL((k_evict_pick<1024, 4>), lists, dim3(1024), 0, st, a);
   ZC_LAUNCH_CHECK();
   a.rowb = (int)(k_pages->D * eb);
   const int64_t chains = R * H * 2;
