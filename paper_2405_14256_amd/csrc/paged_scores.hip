@@ -126,7 +126,7 @@ template <int N> __device__ inline float logit(const v16f (&p)[N], int v) {
 // ---- up to 32 rows: single tokens ------------------------------------------------------------------
 // Bound by memory.  A wave has a place for one K block in LDS; the next is requested when it has been multiplied.
 template <int DT, int D> struct FewMemory { static constexpr int kBlock = 32 * Tile<DT, D>::ROWB, kBytes = 4 * kBlock; };
-template <int DT, int D>
+template <int DT, int D, int SETS>
 __device__ __forceinline__ void score_rows(const ScoreArgs& a, const Span& x, int hk, uint8_t* mem, float* norms, int* where) {
   using T = Tile<DT, D>;
   constexpr int BLK = FewMemory<DT, D>::kBlock, PG = 16 / T::RPI;
@@ -170,17 +170,21 @@ __device__ __forceinline__ void score_rows(const ScoreArgs& a, const Span& x, in
 
   // the rows, straight into operand registers; their normalisers
   const int rows = x.nq * a.G;
-  const int2 me = row_of(a, 0, r);
-  u32x4 qf[T::NKC];
+  u32x4 qf[SETS][T::NKC];
 #pragma unroll
-  for (int kc = 0; kc < T::NKC; ++kc) qf[kc] = u32x4{0, 0, 0, 0};
-  if (r < rows) {
-    const uint8_t* qr = a.q + (int64_t)(hk * a.G + me.y) * a.q_sH + (int64_t)(x.qs + me.x) * a.q_sT + kh * 16;
+  for (int s = 0; s < SETS; ++s) {
 #pragma unroll
-    for (int kc = 0; kc < T::NKC; ++kc) qf[kc] = *reinterpret_cast<const u32x4*>(qr + kc * 32);
+    for (int kc = 0; kc < T::NKC; ++kc) qf[s][kc] = u32x4{0, 0, 0, 0};
+    if (32 * s + r < rows) {
+      const int2 me = row_of(a, 0, 32 * s + r);
+      const uint8_t* qr = a.q + (int64_t)(hk * a.G + me.y) * a.q_sH + (int64_t)(x.qs + me.x) * a.q_sT + kh * 16;
+#pragma unroll
+      for (int kc = 0; kc < T::NKC; ++kc) qf[s][kc] = *reinterpret_cast<const u32x4*>(qr + kc * 32);
+    }
   }
   __syncthreads();                               // (the unit before is done with the normalisers)
-  if (tid < 32) {
+  if (tid < 32 * SETS) {
+    const int2 me = row_of(a, 0, tid);
     norms[tid] = tid < rows ? norm_of(a.lse[(int64_t)(hk * a.G + me.y) * a.T + x.qs + me.x]) : INFINITY;
     where[tid] = x.kv - x.nq + me.x;
   }
@@ -199,25 +203,26 @@ __device__ __forceinline__ void score_rows(const ScoreArgs& a, const Span& x, in
     float* const put = to;
     const float before = old;
     float sum = 0.f;
-    v16f acc[SUMS] = {};
+    v16f acc[SETS][SUMS] = {};
     if (any) {
 #pragma unroll
       for (int kc = 0; kc < T::NKC; ++kc) {
         const u32x4 kf = *(__attribute__((address_space(3))) const u32x4*)(lds_ptr)(uintptr_t)(kaddr ^ (32 * kc));
-        mma_chunk<DT>(acc[kc % SUMS], qf[kc], kf);
+#pragma unroll
+        for (int s = 0; s < SETS; ++s) mma_chunk<DT>(acc[s][kc % SUMS], qf[s][kc], kf);
       }
     }
     dma_reuse_fence();
     if (b + 4 < blocks) issue(next);
     if (any) {
 #pragma unroll
-      for (int v4 = 0; v4 < 4; ++v4) {
+      for (int v4 = 0; v4 < 4 * SETS; ++v4) {
         if (8 * v4 >= rows) break;
         const float4 nv = *reinterpret_cast<const float4*>(&norms[8 * v4 + 4 * kh]);
         const int4 pv = *reinterpret_cast<const int4*>(&where[8 * v4 + 4 * kh]);
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-          const float e = __builtin_amdgcn_exp2f(fmaf(logit<SUMS>(acc, 4 * v4 + u), a.scale_log2, -(&nv.x)[u]));
+          const float e = __builtin_amdgcn_exp2f(fmaf(logit<SUMS>(acc[v4 >> 2], 4 * (v4 & 3) + u), a.scale_log2, -(&nv.x)[u]));
           const int p = (&pv.x)[u];
           const bool sees = whole || ((key <= p) & (!a.window || key > p - a.window || key < a.sinks));
           sum += sees ? e : 0.f;
@@ -479,7 +484,9 @@ __global__ __launch_bounds__(256, DT != ZC_F32 ? 2 : D == 64 ? 2 : 1) void k_pag
   __shared__ float sums[2][kScoreTile];
   Span x;
   for (int u = blockIdx.y; find_span(a, u, x); u += gridDim.y) {
-    if ((int64_t)x.nq * a.G <= 32) score_rows<DT, D>(a, x, blockIdx.x, mem, norms[0], where[0]);
+    const int64_t rows = (int64_t)x.nq * a.G;
+    if (rows <= 32) score_rows<DT, D, 1>(a, x, blockIdx.x, mem, norms[0], where[0]);
+    else if (rows <= 64) score_rows<DT, D, 2>(a, x, blockIdx.x, mem, norms[0], where[0]);
     else score_tiles<DT, D>(a, x, blockIdx.x, mem, norms, where, sums);
   }
 }
