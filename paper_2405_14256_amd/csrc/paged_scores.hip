@@ -33,13 +33,17 @@ struct ScoreArgs {
   uint32_t over_G;                              // ceil(2^32 / G)
 };
 
-// A request's keys go in tiles of 128: of up to 32 rows a wave takes every fourth 32 keys, of more the four waves share a tile.
+// A request's keys go in tiles of 128, or 64 where those are few: of up to 64 rows a wave takes every fourth 32 keys, of more the four waves share a tile.
 constexpr int kScoreTile = 128;
+// Tiles of chunks and heads below which they are halved: more workgroups, which all take every row.  us of 128 and 64 keys a tile (32 heads over 8 of 128 channels, bf16): a prompt of
+// 2048 103 and 78, four of 500 42 and 30, 500 tokens over 4096 53 and 37, over 8192 (512 tiles) 56 and 69; fp32, 500 over 4096 189 and 119.
+constexpr float kFewTiles = 384.f;
 
 struct Span {
   int r, qs, nq, kv;            // request, its first row, new tokens, tokens
   int first, sink_tiles;        // tile t is t of the first sink_tiles, then first + t - sink_tiles
   int t_lo, t_hi;               // tiles of this unit
+  int shift;                    // of a tile's keys: 7 or 6
   uint32_t behind;              // 16 keys from key0 on are behind every window if key0 - sinks, without sign, is less than this
 };
 __device__ inline int tile_of(const Span& x, int t) { return t < x.sink_tiles ? t : x.first + t - x.sink_tiles; }
@@ -51,6 +55,7 @@ __device__ inline uint32_t opaque(uint32_t x) { asm volatile("" : "+v"(x)); retu
 __device__ inline bool find_span(const ScoreArgs& a, int u, Span& x) {
   const int lane = threadIdx.x & 63;
   struct Part { int qs, nq, kv, first, sink_tiles, tiles, passes; };           // passes: of 64 rows over a tile
+  int shift = 7;
   const auto part = [&](int r) {
     Part p = {0, 0, 0, 0, 0, 0, 1};
     if (r >= a.R) return p;
@@ -60,22 +65,31 @@ __device__ inline bool find_span(const ScoreArgs& a, int u, Span& x) {
     p.kv = min(max(kv, 0), a.cap);
     // (weights that fade change every token's score, seen or not)
     const int p0 = max(p.kv - p.nq, 0), low = a.window && a.decay == 1.f ? max(0, p0 - a.window + 1) : 0;
-    p.first = low / kScoreTile;
-    p.sink_tiles = min((min(a.sinks, low) + kScoreTile - 1) / kScoreTile, p.first);
-    if (p.nq) p.tiles = p.sink_tiles + (p.kv + kScoreTile - 1) / kScoreTile - p.first;
+    const int up = (1 << shift) - 1;
+    p.first = low >> shift;
+    p.sink_tiles = min((min(a.sinks, low) + up) >> shift, p.first);
+    if (p.nq) p.tiles = p.sink_tiles + ((p.kv + up) >> shift) - p.first;
     p.passes = (int)(((int64_t)p.nq * a.G + 63) / 64);
     return p;
   };
-  const Part head = part(lane);
-  float all = (float)head.tiles * (float)head.passes;
+  Part head = part(lane);
+  float all = (float)head.tiles * (float)head.passes, chunks = head.passes > 1 ? (float)head.tiles : 0.f;
   for (int r0 = 64; r0 < a.R; r0 += 64) {
     const Part p = part(r0 + lane);
     all += (float)p.tiles * (float)p.passes;
+    chunks += p.passes > 1 ? (float)p.tiles : 0.f;
+  }
+  all = wave_sum(all);
+  chunks = wave_sum(chunks);
+  if (__builtin_amdgcn_readfirstlane(chunks > 0.f && chunks * (float)a.Hkv < kFewTiles)) {
+    shift = 6;
+    head = part(lane);
+    all *= 2.f;
   }
   // Work of a unit: as many units as the chip holds twice, where work is little as it holds once.  us at 512, 1024 and 2048 units: 64 tokens over 64 to 8192 (32 heads over 8 of 128
   // channels, bf16) 74, 65 and 66, 16 over up to 1694 (8 heads of 64) 14.6, 17.2 and 23.3, 3 requests with 6 tokens over up to 3840 (12 of 64) 11.1, 14.7 and 14.7, 2048 tokens over
   // 16384 295, 295 and 298.
-  const float share = wave_sum(all) / a.target, per = fmaxf(share, fminf(2.f * share, 5.f));
+  const float share = all / a.target, per = fmaxf(share, fminf(2.f * share, 5.f));
   int units = 0;
   for (int r0 = 0; r0 < a.R; r0 += 64) {
     const Part p = r0 ? part(r0 + lane) : head;
@@ -93,6 +107,7 @@ __device__ inline bool find_span(const ScoreArgs& a, int u, Span& x) {
       const int q = (int)((uint32_t)tiles / (uint32_t)n), rem = tiles - q * n;
       x.t_lo = b * q + min(b, rem);
       x.t_hi = x.t_lo + q + (b < rem ? 1 : 0);
+      x.shift = shift;
       const int far = max(x.kv - x.nq, 0) - a.window - 14;
       x.behind = a.window && far > a.sinks ? far - a.sinks : 0;
       return true;
@@ -123,8 +138,10 @@ template <int N> __device__ inline float logit(const v16f (&p)[N], int v) {
   else return p[0][v];
 }
 
-// ---- up to 32 rows: single tokens ------------------------------------------------------------------
-// Bound by memory.  A wave has a place for one K block in LDS; the next is requested when it has been multiplied.
+// ---- up to 64 rows: single tokens ------------------------------------------------------------------
+// Bound by memory.  A wave has a place for one K block in LDS; the next is requested when it has been multiplied, and the rows' operands stay in registers.  64 tokens over 64 to 8192
+// (8 KV heads of 128 channels, bf16, 277 MB): 64 us, 4.4 TB/s.  33 to 64 rows as two sets over one block, against the way of chunks (16 tokens of each of 16 requests over 4096): 49 and
+// 66 us, 9 tokens 43 and 66.
 template <int DT, int D> struct FewMemory { static constexpr int kBlock = 32 * Tile<DT, D>::ROWB, kBytes = 4 * kBlock; };
 template <int DT, int D, int SETS>
 __device__ __forceinline__ void score_rows(const ScoreArgs& a, const Span& x, int hk, uint8_t* mem, float* norms, int* where) {
@@ -143,8 +160,8 @@ __device__ __forceinline__ void score_rows(const ScoreArgs& a, const Span& x, in
     const int row = j * T::RPI + lane / T::CPR;
     voff[j] = (int)(row * a.k_row) + (((lane % T::CPR) ^ T::swz(row)) << 4);
   }
-  const int blocks = 4 * (x.t_hi - x.t_lo);
-  const auto key_of = [&](int b) { return tile_of(x, x.t_lo + (b >> 2)) * kScoreTile + 32 * (b & 3); };
+  const int up = x.shift - 5, blocks = (x.t_hi - x.t_lo) << up;
+  const auto key_of = [&](int b) { return (tile_of(x, x.t_lo + (b >> up)) << x.shift) + 32 * (b & ((1 << up) - 1)); };
   // A block's keys are requested, and this lane's score so far.
   float* to = nullptr;
   float old = 0.f;
@@ -236,17 +253,19 @@ __device__ __forceinline__ void score_rows(const ScoreArgs& a, const Span& x, in
 }
 
 // ---- more rows: chunks -----------------------------------------------------------------------------
-// The waves take 64 of a tile's keys and 32 of every 64 rows each: K operands stay in registers, rows stream through LDS.
+// The waves take half of a tile's keys and 32 of every 64 rows each: K operands stay in registers, rows stream through LDS, 128 (fp32 64) at a time, one tile ahead.  Bound by the matrix
+// pipe and the exponentials beside it, which are issued between the products of the next 32 keys (16-bit types) or of the other half: 2048 tokens over 16384 (32 heads over 8 of 128
+// channels, bf16) 294 us, 870 TFLOP/s of logits that are seen.  256 VGPRs allow two workgroups a CU; three spill.
 template <int DT, int D> struct ManyMemory { static constexpr int kRows = DT == ZC_F32 ? 64 : 128, kTileB = kRows * Tile<DT, D>::ROWB, kBytes = 2 * kTileB; };
 constexpr int kMostRows = 128;
-template <int DT, int D>
+template <int DT, int D, int KEYS>
 __device__ __forceinline__ void score_tiles(const ScoreArgs& a, const Span& x, int hk, uint8_t* mem, float (*norms)[kMostRows], int (*where)[kMostRows], float (*sums)[kScoreTile]) {
   using T = Tile<DT, D>;
   constexpr int QT = ManyMemory<DT, D>::kRows, TILE_B = ManyMemory<DT, D>::kTileB, NI = QT / T::RPI / 4, PG = 16 / T::RPI;
   static_assert(2 * QT >= kScoreTile, "K passes through both row buffers");
-  constexpr int SUMS = DT == ZC_F32 ? 4 : 1;
+  constexpr int SUMS = DT == ZC_F32 ? 4 : 1, TILE = 64 * KEYS;
   const int tid = (int)opaque(threadIdx.x), lane = tid & 63, r = lane & 31, kh = lane >> 5;
-  const int w = __builtin_amdgcn_readfirstlane(tid >> 6), rw = w >> 1, kw = w & 1;       // rows 32 rw on of 64, keys 64 kw on of 128
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6), rw = w >> 1, kw = w & 1;       // rows 32 rw on of 64, keys 32 KEYS kw on of the tile's
   const uint8_t* kb = a.k + hk * a.k_sH;
   const uint8_t* qb = a.q + (int64_t)hk * a.G * a.q_sH + (int64_t)x.qs * a.q_sT;
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)mem;
@@ -257,7 +276,7 @@ __device__ __forceinline__ void score_tiles(const ScoreArgs& a, const Span& x, i
   using lds_u32x4 = __attribute__((address_space(3))) const u32x4;
 
   for (int t = x.t_lo; t < x.t_hi; ++t) {
-    const int key0 = tile_of(x, t) * kScoreTile;
+    const int key0 = tile_of(x, t) * TILE;
     // ---- K to registers, by way of both row buffers
     int voff[PG];
     const int kl = (int)opaque(lane);
@@ -268,28 +287,28 @@ __device__ __forceinline__ void score_tiles(const ScoreArgs& a, const Span& x, i
     }
     __syncthreads();                             // (the tile before is done with LDS)
 #pragma unroll
-    for (int g = 0; g < 2; ++g) {
-      const int k16 = key0 + 32 * w + 16 * g, id = page_of(table, a.cols, a.shift, k16);
-      move_keys<PG>(lds + (32 * w + 16 * g) * T::ROWB, keys_at(a.shift, kb, a.k_sB, a.k_row, k16, id, keys_read(a.n_pages, a.sinks, x.behind, x.kv, k16, id)), voff);
+    for (int g = 0; g < KEYS; ++g) {
+      const int at = 16 * KEYS * w + 16 * g, k16 = key0 + at, id = page_of(table, a.cols, a.shift, k16);
+      move_keys<PG>(lds + at * T::ROWB, keys_at(a.shift, kb, a.k_sB, a.k_row, k16, id, keys_read(a.n_pages, a.sinks, x.behind, x.kv, k16, id)), voff);
     }
     float* to = nullptr;
     float old = 0.f;
-    if (tid < kScoreTile && key0 + tid < x.kv) {
+    if (tid < TILE && key0 + tid < x.kv) {
       to = score_at(a, x, hk, key0 + tid);
       if (to && key0 + tid < past && a.decay != 0.f) old = *to;
     }
     wait_vmem<0>();
     wait_all_loads();
     __syncthreads();
-    u32x4 kf[2][T::NKC];
+    u32x4 kf[KEYS][T::NKC];
 #pragma unroll
-    for (int n = 0; n < 2; ++n)
+    for (int n = 0; n < KEYS; ++n)
 #pragma unroll
       for (int kc = 0; kc < T::NKC; ++kc)
-        kf[n][kc] = *reinterpret_cast<lds_u32x4*>((lds_ptr)(uintptr_t)((lds + T::slot(r, kh)) ^ (32 * kc)) + (64 * kw + 32 * n) * T::ROWB);
+        kf[n][kc] = *reinterpret_cast<lds_u32x4*>((lds_ptr)(uintptr_t)((lds + T::slot(r, kh)) ^ (32 * kc)) + (32 * KEYS * kw + 32 * n) * T::ROWB);
 
     // ---- rows that see some of these keys: up to the last row, or the last whose window reaches them
-    const int key1 = min(key0 + kScoreTile, x.kv) - 1;
+    const int key1 = min(key0 + TILE, x.kv) - 1;
     int j_first = max(key0 - past, 0), j_end = x.nq;
     if (a.window && key0 >= a.sinks) j_end = (int)min((int64_t)x.nq, (int64_t)key1 + a.window - past);
     const uint32_t i_first = (uint32_t)j_first * a.G / QT * QT, i_end = (uint32_t)max(j_end, 0) * a.G;
@@ -336,11 +355,12 @@ __device__ __forceinline__ void score_tiles(const ScoreArgs& a, const Span& x, i
         pos = past + me.x;
       }
     };
+    // Two products are under way, of both halves of a wave's 64 keys with the same 32 rows or of its 32 keys with one 32 rows after the other.
     float sum[2] = {0.f, 0.f};
     v16f acc[2][SUMS];
-    // Weights of 32 rows (norms and positions: `rows_of`) and the keys n, which not all rows see.
+    // Weights of product n's 32 rows and its keys, which not all rows see.
     const auto masked = [&](int n, const float* norm_of_row, const int* pos_of_row) {
-      const int key = key0 + 64 * kw + 32 * n + r;
+      const int key = key0 + 32 * KEYS * kw + (KEYS == 2 ? 32 * n : 0) + r;
 #pragma unroll
       for (int v4 = 0; v4 < 4; ++v4) {
         const float4 nv = *reinterpret_cast<const float4*>(norm_of_row + 8 * v4);
@@ -378,25 +398,26 @@ __device__ __forceinline__ void score_tiles(const ScoreArgs& a, const Span& x, i
         __builtin_amdgcn_sched_barrier(0);
       }
     };
-    // The same of 16-bit types with the rows' operands `q` in registers, and their normalisers `nv` of the weights: what a step has used is replaced by
+    // As above of 16-bit types with the rows' operands `q` in registers, and their normalisers `nv` of the weights: what a step has used is replaced by
     // what the step after the next (q) or the next (nv) needs, so that no step waits for LDS.
     u32x4 q[DT == ZC_F32 ? 1 : T::NKC];
     float4 nv[4];
     const auto flow = [&](auto weigh, auto keys, auto refill, uint32_t next_row, const float* next_norm) {
       constexpr bool WEIGH = decltype(weigh)::value, REFILL = decltype(refill)::value;
-      constexpr int n = decltype(keys)::value;       // (keys 0: the rows' normalisers come, keys 1: the next rows)
+      constexpr int n = decltype(keys)::value;
+      constexpr bool NORMS = n == 0 || KEYS == 1;    // (the first of these rows' products: their normalisers come)
       constexpr int EACH = 16 / T::NKC;
       acc[n][0] = v16f{};
       if constexpr (REFILL) next_row = opaque(next_row);
 #pragma unroll
       for (int kc = 0; kc < T::NKC; ++kc) {
-        mma_chunk<DT>(acc[n][0], q[kc], kf[n][kc]);
+        mma_chunk<DT>(acc[n][0], q[kc], kf[KEYS == 2 ? n : 0][kc]);
         if constexpr (WEIGH)
 #pragma unroll
           for (int v = kc * EACH; v < (kc + 1) * EACH; ++v)
             sum[n ^ 1] += __builtin_amdgcn_exp2f(fmaf(acc[n ^ 1][0][v], a.scale_log2, -(&nv[v >> 2].x)[v & 3]));
         if constexpr (REFILL) q[kc] = *reinterpret_cast<lds_u32x4*>((lds_ptr)(uintptr_t)(next_row ^ (kc << 5)));
-        if (n == 0 && (kc + 1) * EACH % 4 == 0) nv[(kc + 1) * EACH / 4 - 1] = *reinterpret_cast<const float4*>(next_norm + 2 * ((kc + 1) * EACH - 4));
+        if (NORMS && (kc + 1) * EACH % 4 == 0) nv[(kc + 1) * EACH / 4 - 1] = *reinterpret_cast<const float4*>(next_norm + 2 * ((kc + 1) * EACH - 4));
         __builtin_amdgcn_sched_barrier(0);
       }
     };
@@ -422,8 +443,12 @@ __device__ __forceinline__ void score_tiles(const ScoreArgs& a, const Span& x, i
       if (i0 + QT < i_end) issue(i0 + QT, next.x, next.y, buf ^ 1);
       const uint32_t row = lds + buf * TILE_B + 32 * rw * T::ROWB + T::slot(r, kh);
       const int pa = past + j0, pb = past + row_of(a, j0, g0 + QT - 1).x;          // positions of the tile's first and last row
-      const bool whole = key0 + kScoreTile - 1 <= pa && (!a.window || key0 > pb - a.window || key0 + kScoreTile - 1 < a.sinks);
-      if constexpr (DT == ZC_F32) {
+      const bool whole = key0 + TILE - 1 <= pa && (!a.window || key0 > pb - a.window || key0 + TILE - 1 < a.sinks);
+      if constexpr (DT == ZC_F32 && KEYS == 1) {     // (the weights are little beside the products)
+        step(std::false_type{}, 0, row, 1, nullptr);
+        if (whole) weigh_only(0, &norms[buf][mine]);
+        else masked(0, &norms[buf][mine], &where[buf][mine]);
+      } else if constexpr (DT == ZC_F32) {
         if (pending) step(std::true_type{}, 0, row, 1, &norms[buf ^ 1][mine]);
         else step(std::false_type{}, 0, row, 1, nullptr);
         if (whole) step(std::true_type{}, 1, row, 0, &norms[buf][mine]);
@@ -432,12 +457,21 @@ __device__ __forceinline__ void score_tiles(const ScoreArgs& a, const Span& x, i
         const uint32_t first = opaque(row);
 #pragma unroll
         for (int kc = 0; kc < T::NKC; ++kc) q[kc] = *reinterpret_cast<lds_u32x4*>((lds_ptr)(uintptr_t)(first ^ (kc << 5)));
-#pragma unroll
-        for (int h = 0; h < QT / 64; ++h) {
+        const auto half = [&](auto of) {
+          constexpr int h = decltype(of)::value;
           using K0 = std::integral_constant<int, 0>;
           using K1 = std::integral_constant<int, 1>;
           const float* const of_these = &norms[buf][mine + 64 * h];
           const uint32_t behind = row + 64 * (h + 1) * T::ROWB;
+          if constexpr (KEYS == 1) {
+            using KH = std::integral_constant<int, h & 1>;
+            using MORE = std::bool_constant<h + 1 < QT / 64>;
+            if (pending) flow(std::true_type{}, KH{}, MORE{}, behind, of_these);
+            else flow(std::false_type{}, KH{}, MORE{}, behind, of_these);
+            pending = whole;
+            if (!whole) masked(h & 1, of_these, &where[buf][mine + 64 * h]);
+            return;
+          }
           if (pending) flow(std::true_type{}, K0{}, std::false_type{}, 0, of_these);
           else flow(std::false_type{}, K0{}, std::false_type{}, 0, of_these);
           if (h + 1 < QT / 64) {
@@ -452,9 +486,12 @@ __device__ __forceinline__ void score_tiles(const ScoreArgs& a, const Span& x, i
             masked(0, &norms[buf][mine + 64 * h], &where[buf][mine + 64 * h]);
             masked(1, &norms[buf][mine + 64 * h], &where[buf][mine + 64 * h]);
           }
-        }
+        };
+        half(std::integral_constant<int, 0>{});
+        half(std::integral_constant<int, 1>{});
+        static_assert(QT == 128, "two halves");
       }
-      if constexpr (DT == ZC_F32) {
+      if constexpr (DT == ZC_F32 && KEYS == 2) {
         pending = whole;
         if (!whole) {
           masked(0, &norms[buf][mine], &where[buf][mine]);
@@ -466,9 +503,10 @@ __device__ __forceinline__ void score_tiles(const ScoreArgs& a, const Span& x, i
     }
     if (pending) weigh_only(1, &norms[buf ^ 1][mine + QT - 64]);
 #pragma unroll
-    for (int n = 0; n < 2; ++n) {
-      sum[n] += __shfl_xor(sum[n], 32);
-      if (kh == 0) sums[rw][64 * kw + 32 * n + r] = sum[n];
+    for (int n = 0; n < KEYS; ++n) {
+      float all = KEYS == 2 ? sum[n] : sum[0] + sum[1];
+      all += __shfl_xor(all, 32);
+      if (kh == 0) sums[rw][32 * KEYS * kw + 32 * n + r] = all;
     }
     __syncthreads();
     if (to) *to = fmaf(old, a.decay, sums[0][tid] + sums[1][tid]);
@@ -487,7 +525,8 @@ __global__ __launch_bounds__(256, DT != ZC_F32 ? 2 : D == 64 ? 2 : 1) void k_pag
     const int64_t rows = (int64_t)x.nq * a.G;
     if (rows <= 32) score_rows<DT, D, 1>(a, x, blockIdx.x, mem, norms[0], where[0]);
     else if (rows <= 64) score_rows<DT, D, 2>(a, x, blockIdx.x, mem, norms[0], where[0]);
-    else score_tiles<DT, D>(a, x, blockIdx.x, mem, norms, where, sums);
+    else if (x.shift == 7) score_tiles<DT, D, 2>(a, x, blockIdx.x, mem, norms, where, sums);
+    else score_tiles<DT, D, 1>(a, x, blockIdx.x, mem, norms, where, sums);
   }
 }
 
@@ -537,7 +576,7 @@ extern "C" int zc_paged_scores(const zc_tensor4* q, const zc_tensor4* k_pages, c
   a.lse = lse;
   a.scores = scores;
   a.over_G = G == 1 ? 0 : (uint32_t)(((1ull << 32) + G - 1) / G);
-  const int64_t target = ceil_div64(1024, Hkv), tiles = ceil_div64(room, kScoreTile), with = R < T ? R : T;
+  const int64_t target = ceil_div64(1024, Hkv), tiles = ceil_div64(room, T * G > 64 * R ? kScoreTile / 2 : kScoreTile), with = R < T ? R : T;
   a.target = (float)target;
   a.near_rows = q->sH >= 0 && q->sL >= 0 && G * a.q_sH + 16 * a.q_sT < 0xffffff00ll;
   // (a workgroup takes more units where there are; those that find none cost their places: where a table's room allows few tiles, as many as the chip holds)

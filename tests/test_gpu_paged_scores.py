@@ -71,6 +71,13 @@ def test_single_tokens_and_chunks(dtype, D, Hq, Hkv, page, by_head, window, sink
     Step([1, 70, 0, 1, 5, 300, 33], [900, 500, 40, 1, 5, 300, 700], Hq, Hkv, D, dtype, page, by_head, pad=5, window=window, sinks=sinks, decay=decay).run()
 
 
+@pytest.mark.parametrize("dtype,D,Hq,page", [(BF, 128, 16, 16), (HF, 64, 24, 64), (FL, 64, 16, 32), (FL, 128, 24, 16)])
+@pytest.mark.parametrize("window,sinks,decay", [(0, 0, 1.0), (300, 150, 0.5), (1800, 70, 1.0)])
+def test_chunks_over_many_keys(dtype, D, Hq, page, window, sinks, decay):
+    """As many keys as it takes for their tiles to be the larger of the two."""
+    Step([40, 70, 0, 1, 300, 129, 30], [3000, 2500, 40, 500, 1500, 700, 900], Hq, 8, D, dtype, page, pad=5, window=window, sinks=sinks, decay=decay).run()
+
+
 @pytest.mark.parametrize("dtype", [BF, FL])
 @pytest.mark.parametrize("rows", [1, 7, 8, 9, 31, 32, 33, 63, 64, 65, 127, 128, 129])
 def test_numbers_of_rows(dtype, rows):
