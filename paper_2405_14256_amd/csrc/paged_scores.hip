@@ -36,8 +36,9 @@ struct ScoreArgs {
 // A request's keys go in tiles of 128, or 64 where those are few: of up to 64 rows a wave takes every fourth 32 keys, of more the four waves share a tile.
 constexpr int kScoreTile = 128;
 // Tiles of chunks and heads below which they are halved: more workgroups, which all take every row.  us of 128 and 64 keys a tile (32 heads over 8 of 128 channels, bf16): a prompt of
-// 2048 103 and 78, four of 500 42 and 30, 500 tokens over 4096 53 and 37, over 8192 (512 tiles) 56 and 69; fp32, 500 over 4096 189 and 119.
-constexpr float kFewTiles = 384.f;
+// 2048 103 and 78, four of 500 42 and 30, 500 tokens over 4096 (256 tiles)
+// 44 and 37, 300 over 6000 (376) 41 and 44, 500 over 8192 (512) 56 and 69; fp32, 500 over 4096 (16 heads over 4) 190 and 119.
+constexpr float kFewTiles = 320.f;
 
 struct Span {
   int r, qs, nq, kv;            // request, its first row, new tokens, tokens
