@@ -191,20 +191,16 @@ __device__ __forceinline__ void score_rows(const ScoreArgs& a, const Span& x, in
   u32x4 qf[SETS][T::NKC];
 #pragma unroll
   for (int s = 0; s < SETS; ++s) {
+    const int2 me = row_of(a, 0, min(32 * s + r, rows - 1));       // (places behind the last row: that row once more, of no weight; zeros would make NaN of infinite keys)
+    const uint8_t* qr = a.q + (int64_t)(hk * a.G + me.y) * a.q_sH + (int64_t)(x.qs + me.x) * a.q_sT + kh * 16;
 #pragma unroll
-    for (int kc = 0; kc < T::NKC; ++kc) qf[s][kc] = u32x4{0, 0, 0, 0};
-    if (32 * s + r < rows) {
-      const int2 me = row_of(a, 0, 32 * s + r);
-      const uint8_t* qr = a.q + (int64_t)(hk * a.G + me.y) * a.q_sH + (int64_t)(x.qs + me.x) * a.q_sT + kh * 16;
-#pragma unroll
-      for (int kc = 0; kc < T::NKC; ++kc) qf[s][kc] = *reinterpret_cast<const u32x4*>(qr + kc * 32);
-    }
+    for (int kc = 0; kc < T::NKC; ++kc) qf[s][kc] = *reinterpret_cast<const u32x4*>(qr + kc * 32);
   }
   __syncthreads();                               // (the unit before is done with the normalisers)
   if (tid < 32 * SETS) {
     const int2 me = row_of(a, 0, tid);
     norms[tid] = tid < rows ? norm_of(a.lse[(int64_t)(hk * a.G + me.y) * a.T + x.qs + me.x]) : INFINITY;
-    where[tid] = x.kv - x.nq + me.x;
+    where[tid] = tid < rows ? x.kv - x.nq + me.x : -1;
   }
   __syncthreads();
   typedef __attribute__((address_space(3))) const uint8_t* lds_ptr;
@@ -353,7 +349,7 @@ __device__ __forceinline__ void score_tiles(const ScoreArgs& a, const Span& x, i
         const bool there = (uint32_t)qt < left;
         const int2 me = row_of(a, j, g + (there ? qt : 0));
         norm = there ? a.lse[(int64_t)(hk * a.G + me.y) * a.T + x.qs + me.x] : -INFINITY;
-        pos = past + me.x;
+        pos = there ? past + me.x : -1;
       }
     };
     // Two products are under way, of both halves of a wave's 64 keys with the same 32 rows or of its 32 keys with one 32 rows after the other.

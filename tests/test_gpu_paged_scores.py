@@ -131,6 +131,23 @@ def test_a_scale_of_the_callers():
     Step([1, 40], [200, 300], 4, 2, 64, FL, sm_scale=0.3).run()
 
 
+@pytest.mark.parametrize("dtype,nq", [(BF, 1), (HF, 3), (BF, 9), (FL, 3), (FL, 19), (HF, 60), (BF, 100), (FL, 100)])
+def test_keys_of_no_weight(dtype, nq):
+    """Logits of -inf, of keys that rows see and that they do not: places behind a block's last row add nothing to them."""
+    s = Step([nq], [700], 6, 2, 64, dtype, window=300, sinks=4)
+    p = s.p
+    p.q[:, :, 0] = p.q[:, :, 0].abs() + 0.5
+    page, row = s.places(0)
+    for i in (0, 131, 402, 520, 690, 699):
+        p.k[0][:, i, 0] = -math.inf
+        p.kp[page[i], :, row[i], 0] = -math.inf
+    s.lse = plain.normalisers(p, 300, 4)
+    s.run()
+    got = s.scores.clone()
+    s.call(got)
+    assert s.at(got, 0)[0].isfinite().all()
+
+
 def test_missing_pages_have_no_scores():
     s = Step([1, 50], [300, 200], 4, 2, 64, BF)
     want = s.scores.clone()
