@@ -460,7 +460,7 @@ int zc_paged_scores(const zc_tensor4* q, const zc_tensor4* k_pages, const int32_
  * with `together`) the places that the tokens had, ascending; entries behind them are left as they were.
  * Pages that a request then does not need, entries ceil(new_len / page) to ceil(kv_len / page) - 1 of its row, are written to free_pages
  * (device int32 [n_list]) from *n_free on (device int32), request after request, what passes the list's end left out; *n_freed
- * (device int32, may be NULL) is their number.  As in zc_paged_tables *n_free is not changed: add *n_freed to it, in the order of the stream.  block_table is
+ * (device int32, may be NULL, not n_free itself) is their number.  As in zc_paged_tables *n_free is not changed: add *n_freed to it, in the order of the stream.  block_table is
  * not changed.  free_pages may be NULL.
  * A request's pages must be its own: not another's, not twice in its row.  A token whose entry is no page has a score of 0 and zeros for
  * its rows, a place without a page takes nothing, and among the pages that are left such an entry is written like any other: evict with the lengths

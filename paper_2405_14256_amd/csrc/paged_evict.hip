@@ -341,6 +341,7 @@ extern "C" int zc_paged_evict(const zc_tensor4* k_pages, const zc_tensor4* v_pag
                         (const void*)free_pages, (const void*)n_free, (const void*)n_freed})
     if (reinterpret_cast<uintptr_t>(p) & 3) return ZC_ERR_INVALID_ARG;
   if (!scores || (reinterpret_cast<uintptr_t>(scores) & 15) || (free_pages && !n_free)) return ZC_ERR_INVALID_ARG;
+  if (n_freed && n_freed == n_free) return ZC_ERR_INVALID_ARG;       // (one workgroup writes it while others read it)
   hipStream_t st = (hipStream_t)stream;
   if (R == 0) {
     if (n_freed) {

@@ -24,7 +24,7 @@ def test_refuses_bad_arguments_before_launch():
                                   n_free, n_freed, ws, wn, None)
     for kw in (dict(scores=None), dict(scores=0x20008), dict(table=None), dict(row=7), dict(cols=-1), dict(kv=None), dict(keep=None), dict(R=-1), dict(most=-1),
                dict(sinks=-1), dict(recent=-1), dict(new=None), dict(kept=None), dict(n_list=-1), dict(n_free=None), dict(kv=0x40002), dict(keep=0x50001),
-               dict(new=0x60002), dict(kept=0x70002), dict(free=0x80002), dict(n_free=0x90001), dict(n_freed=0xa0001), dict(table=0x30002),
+               dict(new=0x60002), dict(kept=0x70002), dict(free=0x80002), dict(n_free=0x90001), dict(n_freed=0xa0001), dict(n_freed=0x90000), dict(table=0x30002),
                dict(new=0x40000), dict(new=0x50000), dict(new=0x4000c), dict(kv=0x5fff4), dict(vp=_pool(B=9)), dict(vp=_pool(dtype=zb.ZC_F16)),
                dict(vp=_pool(L=32)), dict(kp=_pool(ptr=None)), dict(kp=_pool(ptr=0x10008)), dict(kp=_pool(sH=0)), dict(vp=_pool(sH=8 * 128))):
         assert call(**kw) == INV, kw
