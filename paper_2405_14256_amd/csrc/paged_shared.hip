@@ -133,6 +133,8 @@ __device__ bool plan(const SharedArgs& a, int many, int wanted, PlanMemory<THREA
     x.tiles = (x.kv + kTile - 1) / kTile + (x.together ? 0 : (x.pre + kTile - 1) / kTile);
     return x;
   };
+  // Rows of a group that go through its prefix together (of starts that do not ascend they could be more than there are).
+  const auto rows_of = [&](int g) { return min(max(s.g_end[g] - s.g_first[g], 0), a.T) * a.G; };
   const Given front = given(tid);
   for (int e = tid; e <= a.P; e += THREADS) {
     s.g_start[e] = min(max(a.group_start[e], 0), a.R);
@@ -171,7 +173,7 @@ __device__ bool plan(const SharedArgs& a, int many, int wanted, PlanMemory<THREA
   }
   __syncthreads();
   for (int g = tid; g < a.P; g += THREADS) {
-    const int blocks = cut_of((s.g_end[g] - s.g_first[g]) * a.G, many).blocks;
+    const int blocks = cut_of(rows_of(g), many).blocks;
     work += (float)blocks * (float)((s.g_kv[g] + kTile - 1) / kTile);
     n_blocks += (float)blocks;
   }
@@ -217,7 +219,7 @@ __device__ bool plan(const SharedArgs& a, int many, int wanted, PlanMemory<THREA
   // ---- units of the prefixes
   int units = 0, joins = 0, parts = 0;
   for (int g0 = 0; g0 < a.P; g0 += THREADS) {
-    const int g = g0 + tid, rows = g < a.P ? (s.g_end[g] - s.g_first[g]) * a.G : 0, tiles = g < a.P ? (s.g_kv[g] + kTile - 1) / kTile : 0;
+    const int g = g0 + tid, rows = g < a.P ? rows_of(g) : 0, tiles = g < a.P ? (s.g_kv[g] + kTile - 1) / kTile : 0;
     const Cut c = cut_of(rows, many);
     const int n = parts_of(tiles), mine = c.blocks * n;
     int all;
@@ -231,7 +233,7 @@ __device__ bool plan(const SharedArgs& a, int many, int wanted, PlanMemory<THREA
     }
     units_in_hand(units, all, min(a.P - g0, THREADS), before, mine, [&](int u, int i) {
       const int e = g0 + i, n = s.parts[i], rest = u - s.unit[i], b = rest / n, p = rest - b * n;
-      const int rows = (s.g_end[e] - s.g_first[e]) * a.G, tiles = (s.g_kv[e] + kTile - 1) / kTile;
+      const int rows = rows_of(e), tiles = (s.g_kv[e] + kTile - 1) / kTile;
       const Cut k = cut_of(rows, many);
       const int rb = k.few ? 32 : many, i0 = b * rb, j = i0 / a.G, q = tiles / n, rem = tiles - q * n;
       const int lo = p * q + min(p, rem), hi = lo + q + (p < rem ? 1 : 0);
@@ -276,7 +278,7 @@ __device__ bool plan(const SharedArgs& a, int many, int wanted, PlanMemory<THREA
       if (p == 0 && part >= 0 && join < a.most_joins) {
         int4 w = make_int4(g0, 0, 0, 0);
         if (together) {
-          const bool big = !cut_of((s.g_end[group] - s.g_first[group]) * a.G, many).few;
+          const bool big = !cut_of(rows_of(group), many).few;
           w = make_int4(g0, s.g_part[group], s.g_parts[group] << 1 | (big ? 1 : 0), (s.place[e] - s.g_first[group]) * a.G + i0);
         }
         a.joins[2 * join] = make_int4(part, n, take, s.qs[e] + j0);
@@ -355,8 +357,8 @@ __global__ __launch_bounds__(256, DT == ZC_F32 && D == 128 ? 1 : 2) void k_share
   x.p1 = position(x, row_at(a, x, x.rows - 1).j);
   if (x.last >= 0) {
     const int j = min(row_at(a, x, (d[kFew] ? 0 : 32 * w) + (lane & 31)).j, x.last);
-    if constexpr (PLANNED) token = a.tokens[j];
-    else token = reinterpret_cast<PlanMemory<256>*>(mem)->list[j - x.j0];
+    if constexpr (PLANNED) token = a.tokens[min(j, a.T - 1)];
+    else token = reinterpret_cast<PlanMemory<256>*>(mem)->list[min(max(j - x.j0, 0), kListed - 1)];
   }
   x.token = min(max(token, 0), a.T - 1);
   if constexpr (!PLANNED) __syncthreads();                 // (the plan is done with LDS)
@@ -382,7 +384,7 @@ __global__ __launch_bounds__(256) void k_shared_join(SharedArgs a) {
   for (int join = blockIdx.y; join < joins; join += gridDim.y) {
     const int4 w = a.joins[2 * join], v = a.joins[2 * join + 1];
     const int first = w.x, own = w.y, rows = w.z, pre = v.z >> 1, shift = v.z & 1 ? 7 : 5, parts = own + pre;
-    if (first + own > a.units) continue;
+    if (first + own > a.units || pre > a.units) continue;
     const int step = min((rows + kSharedJoinGroups - 1) / kSharedJoinGroups, GROUPS);        // rows at a time: few rows are spread over the workgroups too
     for (int row0 = turn * step; row0 < rows; row0 += kSharedJoinGroups * step) {
       const int n = min(rows - row0, step);
@@ -393,7 +395,7 @@ __global__ __launch_bounds__(256) void k_shared_join(SharedArgs a) {
       const int i = v.w + row, pre0 = v.y + (i >> shift) * pre, pre_row = i & ((1 << shift) - 1);
       float M = kLowestLogit, l = 0.f;
       float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (mine && (pre == 0 || pre0 + pre <= a.units)) {
+      if (mine && (pre == 0 || (uint32_t)pre0 <= (uint32_t)(a.units - pre))) {
         constexpr int U = 4;                                 // parts requested at a time
         for (int s0 = way; s0 < parts; s0 += U * ways) {
           float2 ml[U];
