@@ -243,10 +243,11 @@ __device__ inline int slot_at(const EvictArgs& a, int r, int i) {
 
 // A workgroup takes `slice` bytes of every row of a (request, head, tensor), a row's by consecutive threads, kMove rows a thread at a time:
 // all of them are read before the first is stored.  Where the next ones lie is looked up meanwhile.
-constexpr int kMove = 4, kMoveThreads = 1024;
+constexpr int kMove = 4;
 struct Move { int src, dst; };                           // slots (src < 0: zeros, dst < 0: nothing to do)
 
-__global__ __launch_bounds__(kMoveThreads, 4) void k_evict_move(EvictArgs a) {
+template <int THREADS>
+__global__ __launch_bounds__(THREADS, 4) void k_evict_move(EvictArgs a) {
   const int r = blockIdx.z;
   const int kv = tokens_of(a, r), stay = stay_of(a, r, kv);
   if (stay == kv) return;
@@ -254,7 +255,7 @@ __global__ __launch_bounds__(kMoveThreads, 4) void k_evict_move(EvictArgs a) {
   if (what == 2 && blockIdx.x) return;
   const int32_t* list = a.kept + ((int64_t)r * a.heads + (a.heads > 1 ? h : 0)) * a.most;
   const int inside = (1 << a.shift) - 1, lanes = what == 2 ? 0 : a.lanes;
-  const int per = kMoveThreads >> lanes, first = threadIdx.x >> lanes;         // rows of a transfer
+  const int per = THREADS >> lanes, first = threadIdx.x >> lanes;         // rows of a transfer
   // Three steps of the way are under way at a time: the list's entries, their pages, the rows.
   int next[kMove];
   Move m[kMove], ahead[kMove];
@@ -380,7 +381,10 @@ extern "C" int zc_paged_evict(const zc_tensor4* k_pages, const zc_tensor4* v_pag
     a.sums = sums;
   }
   const dim3 lists((unsigned)a.heads + 1, (unsigned)R);
-  if (a.cap <= 512 * kEach) hipLaunchKernelGGL((k_evict_pick<512, 1>), lists, dim3(512), 0, st, a);
+  // Threads for four tokens each; short lists in workgroups of 256, of which a CU holds more.  us of 512 and 256 threads (and 1024 and 256 below): 37 requests of 20 tokens, 40 heads
+  // of 128 channels, 39 and 21; 128 of up to 250, 8 heads, 33 and 24; one of up to 900 14.2 and 14.5.
+  if (a.cap <= 256 * kEach) hipLaunchKernelGGL((k_evict_pick<256, 1>), lists, dim3(256), 0, st, a);
+  else if (a.cap <= 512 * kEach) hipLaunchKernelGGL((k_evict_pick<512, 1>), lists, dim3(512), 0, st, a);
   else if (a.cap <= 1024 * kEach) hipLaunchKernelGGL((k_evict_pick<1024, 1>), lists, dim3(1024), 0, st, a);
   else if (a.cap <= 2 * 1024 * kEach) hipLaunchKernelGGL((k_evict_pick<1024, 2>), lists, dim3(1024), 0, st, a);
   else hipLaunchKernelGGL((k_evict_pick<1024, 4>), lists, dim3(1024), 0, st, a);
@@ -391,9 +395,12 @@ extern "C" int zc_paged_evict(const zc_tensor4* k_pages, const zc_tensor4* v_pag
   // a row: one request of 4096, 1638 stay 39.0, 26.0, 22.8 and 21.9; 4 of up to 400, 256 stay 15.7, 15.7, 17.8 and 20.2; 15 of up to 8192, 2048 stay
   // 79 whole, 81 of 128.
   a.slice = a.rowb;
-  while (a.slice > 64 && chains * (a.rowb / a.slice) < 256 && most > kMove * kMoveThreads * 16 / a.slice) a.slice /= 2;
+  while (a.slice > 64 && chains * (a.rowb / a.slice) < 256 && most > kMove * 1024 * 16 / a.slice) a.slice /= 2;
   a.lanes = __builtin_ctz(a.slice / 16);
-  hipLaunchKernelGGL(k_evict_move, dim3((unsigned)(a.rowb / a.slice), (unsigned)(3 * H), (unsigned)R), dim3(kMoveThreads), 0, st, a);
+  // (one step is all that short lists take: a workgroup of a quarter of the threads does.  64 of up to 900 tokens, 64 stay 26.2 and 20.5, 16 of up to 250 15.0 and 15.2)
+  const dim3 grid((unsigned)(a.rowb / a.slice), (unsigned)(3 * H), (unsigned)R);
+  if (most <= kMove * 256 * 16 / a.slice) hipLaunchKernelGGL(k_evict_move<256>, grid, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(k_evict_move<1024>, grid, dim3(1024), 0, st, a);
   ZC_LAUNCH_CHECK();
   return ZC_OK;
 }

@@ -85,6 +85,17 @@ def test_long_requests(kv, keep, scores, together):
     Cache([kv, 40], 1 if not together else 2, 64, BF, page=64, scores=scores).check([keep, 40], sinks=4, recent=keep // 3, together=together)
 
 
+@pytest.mark.parametrize("kv", [1, 15, 1023, 1024, 1025, 2047, 2048, 2049, 4097])
+@pytest.mark.parametrize("keep", [1, 63, 64, 65, 256, 257])
+def test_sizes_of_workgroups(kv, keep):
+    Cache([kv, max(kv - 7, 0), min(kv, 70)], 2, 128 if keep < 200 else 64, BF).check([keep, keep - 1, 33], sinks=2, recent=3, together=kv % 2 == 0)
+
+
+def test_many_short_requests():
+    n = [(37 * i) % 150 for i in range(300)]
+    Cache(n, 3, 64, HF, page=32).check([k // 2 for k in n], recent=4)
+
+
 def test_lists_that_pages_do_not_fit():
     c = Cache([300, 200, 100], 1, 64, BF)
     for n_free, n_list in ((0, 10), (5, 6), (5, 5), (40, 10), (-4, 20)):
