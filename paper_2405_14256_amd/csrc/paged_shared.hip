@@ -26,6 +26,7 @@ struct SharedArgs : PagedArgs {
   int* tokens;                                  // the tokens that go through a prefix together, group after group
   int least;                                    // tiles, below which a block is not split (fp32)
   float worth;                                  // tiles that a shared prefix has to spare
+  int places;                                   // of a head's units at a time
   int most_units, most_joins;                   // (units: partial results that there is room for)
 };
 
@@ -184,7 +185,12 @@ __device__ bool plan(const SharedArgs& a, int many, int wanted, PlanMemory<THREA
   work = n_blocks = 0.f;
 #pragma unroll
   for (int w = 0; w < NW; ++w) { work += s.sums[0][w]; n_blocks += s.sums[1][w]; }
-  const int per = (int)fminf(fmaxf(ceilf(work / (float)a.target), 1.f), 1e9f);  // tiles of a part, at most
+  float share_of_work = fmaxf(ceilf(work / (float)a.target), 1.f);               // tiles of a part, at most
+  // Blocks of about one length in a few more parts than the chip has places for: some wait for a whole round of them.  Longer parts that fit, then.  us: 12 chunks of 17 and 31 tokens
+  // after 4096 (32 heads over 8 of 128 channels, bf16; 72 parts a head in 64 places, then 60) 64.7 and 51.8, 74.5 and 61.5.
+  const float length = work / fmaxf(n_blocks, 1.f), cuts = ceilf(length / share_of_work);
+  if (cuts >= 3.f && cuts * n_blocks > (float)a.places) share_of_work = fmaxf(share_of_work, ceilf(1.04f * length / (cuts - 1.f)));
+  const int per = (int)fminf(share_of_work, 1e9f);
   // (below which a part is not worth its way through memory, as for the paged attention)
   n_blocks *= (float)a.Hkv;
   const int least = many == 32 ? a.least : n_blocks >= 128.f ? 16 : n_blocks >= 64.f ? 10 : 6;
@@ -471,6 +477,7 @@ static int launch_shared(SharedArgs& a, hipStream_t st) {
   // round of workgroups), 64 after 8192 56.2 and 58.8 (two); fp16, 40 heads, 42 tokens 47.0 and 39.3 (eight), 12 chunks after 4096 307 and 312 (five); fp32, 16 heads of
   // 128, 21 requests 32.8 and 29.9 (five), 74 104.8 and 88.4 (ten); 16 over 4 of 64, 22 chunks 85.7 and 73.6 (five).
   const int64_t places = DT == ZC_F32 && D == 128 ? 256 : DT != ZC_F32 && D == 64 ? 768 : 512;
+  a.places = (int)(places / a.Hkv);
   const bool planned = a.most_units * a.Hkv > 4 * places;
   const int64_t own_tiles = ceil_div64(a.cap, kTile), pre_tiles = ceil_div64(a.pre_cap, kTile);
   const bool joined = own_tiles + pre_tiles > (DT == ZC_F32 ? a.least : 6) || (float)(a.R * pre_tiles * a.Hkv) > a.worth;     // (the plan's rules)
