@@ -244,6 +244,12 @@ def test_blocks_of_rows_that_go_together(G, q_len, dtype):
     run(plain.Shared(q_len, [n + 5 * i % 60 for i, n in enumerate(q_len)], [0, len(q_len)], [3500], 2 * G, 2, 64, dtype))
 
 
+@pytest.mark.parametrize("dtype,D", [(BF, 128), (HF, 64), (FL, 64), (FL, 128)])
+@pytest.mark.parametrize("R", [12, 13])
+def test_blocks_of_one_length(dtype, D, R):
+    run(plain.Shared([66] * R, [70 + i for i in range(R)], [0, R], [4096], 8, 8, D, dtype))
+
+
 def test_many_groups_that_go_together():
     R = 300
     run(plain.Shared([1] * R, [1 + i % 90 for i in range(R)], [0] + list(range(5, 291, 5)), [900 + 7 * g for g in range(58)], 4, 2, 64, BF))
