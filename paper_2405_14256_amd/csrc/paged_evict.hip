@@ -146,9 +146,15 @@ __global__ __launch_bounds__(THREADS) void k_evict_pick(EvictArgs a) {
 #pragma unroll
     for (int c = 0; c < HELD; ++c)
       if (c < chunks) f(c * CHUNK + tid * kEach, held[c]);
-    for (int c = HELD; c < chunks; ++c) {
-      const int i0 = c * CHUNK + tid * kEach;
-      const Images m = images(a, r, h, i0, hi, page_of(a, r, i0));
+    if (chunks <= HELD) return;
+    // (one chunk's scores and the next one's pages are on their way meanwhile)
+    int i0 = HELD * CHUNK + tid * kEach;
+    Images next = images(a, r, h, i0, hi, page_of(a, r, i0));
+    int ahead = page_of(a, r, i0 + CHUNK);
+    for (int c = HELD; c < chunks; ++c, i0 += CHUNK) {
+      const Images m = next;
+      next = images(a, r, h, i0 + CHUNK, hi, ahead);
+      ahead = page_of(a, r, i0 + 2 * CHUNK);
       f(i0, m);
     }
   };
@@ -251,8 +257,8 @@ __global__ __launch_bounds__(THREADS, 4) void k_evict_move(EvictArgs a) {
   const int r = blockIdx.z;
   const int kv = tokens_of(a, r), stay = stay_of(a, r, kv);
   if (stay == kv) return;
-  const int what = blockIdx.y / a.Hkv, h = blockIdx.y - what * a.Hkv;          // keys, values, scores of every head
-  if (what == 2 && blockIdx.x) return;
+  const int what = blockIdx.x / a.Hkv, h = blockIdx.x - what * a.Hkv;          // keys, values, scores of every head
+  if (what == 2 && blockIdx.y) return;
   const int32_t* list = a.kept + ((int64_t)r * a.heads + (a.heads > 1 ? h : 0)) * a.most;
   const int inside = (1 << a.shift) - 1, lanes = what == 2 ? 0 : a.lanes;
   const int per = THREADS >> lanes, first = threadIdx.x >> lanes;         // rows of a transfer
@@ -297,7 +303,7 @@ __global__ __launch_bounds__(THREADS, 4) void k_evict_move(EvictArgs a) {
     }
     return;
   }
-  uint8_t* pool = a.pool[what] + blockIdx.x * a.slice + (threadIdx.x & ((1 << lanes) - 1)) * 16 + h * a.sH[what];
+  uint8_t* pool = a.pool[what] + blockIdx.y * a.slice + (threadIdx.x & ((1 << lanes) - 1)) * 16 + h * a.sH[what];
   const int64_t sB = a.sB[what], sL = a.sL[what];
   const auto at = [&](int slot) { return reinterpret_cast<piece16*>(pool + (slot >> a.shift) * sB + (slot & inside) * sL); };
   for (int i0 = begin; i0 < stay; i0 += step) {
@@ -387,18 +393,20 @@ extern "C" int zc_paged_evict(const zc_tensor4* k_pages, const zc_tensor4* v_pag
   else if (a.cap <= 512 * kEach) hipLaunchKernelGGL((k_evict_pick<512, 1>), lists, dim3(512), 0, st, a);
   else if (a.cap <= 1024 * kEach) hipLaunchKernelGGL((k_evict_pick<1024, 1>), lists, dim3(1024), 0, st, a);
   else if (a.cap <= 2 * 1024 * kEach) hipLaunchKernelGGL((k_evict_pick<1024, 2>), lists, dim3(1024), 0, st, a);
-  else hipLaunchKernelGGL((k_evict_pick<1024, 4>), lists, dim3(1024), 0, st, a);
+  else if (a.cap <= 4 * 1024 * kEach) hipLaunchKernelGGL((k_evict_pick<1024, 4>), lists, dim3(1024), 0, st, a);
+  else hipLaunchKernelGGL((k_evict_pick<1024, 8>), lists, dim3(1024), 0, st, a);
   ZC_LAUNCH_CHECK();
   a.rowb = (int)(k_pages->D * eb);
   const int64_t chains = R * H * 2;
-  // Rows are cut where that fills the chip and saves steps of the way through the list.  us of whole rows, of 128, 64 and 32 bytes, 8 heads, 256 bytes
-  // a row: one request of 4096, 1638 stay 39.0, 26.0, 22.8 and 21.9; 4 of up to 400, 256 stay 15.7, 15.7, 17.8 and 20.2; 15 of up to 8192, 2048 stay
-  // 79 whole, 81 of 128.
+  // Rows are cut where that fills the chip and saves steps of the way through the list.  us of whole rows, of 128, 64 and 16 bytes, 8 heads, 256 bytes
+  // a row: one request of 4096, 1638 stay 39.0, 26.0, 20.2 and 18.6; of 131072, 32768 stay (64 and 16) 286 and 286; 4 of up to 400, 256 stay 15.7 and 15.7 (20.2 of 32);
+  // 15 of up to 8192, 2048 stay 79 whole, 81 of 128.
   a.slice = a.rowb;
-  while (a.slice > 64 && chains * (a.rowb / a.slice) < 256 && most > kMove * 1024 * 16 / a.slice) a.slice /= 2;
+  while (a.slice > 16 && chains * (a.rowb / a.slice) < 256 && most > kMove * 1024 * 16 / a.slice) a.slice /= 2;
   a.lanes = __builtin_ctz(a.slice / 16);
   // (one step is all that short lists take: a workgroup of a quarter of the threads does.  64 of up to 900 tokens, 64 stay 26.2 and 20.5, 16 of up to 250 15.0 and 15.2)
-  const dim3 grid((unsigned)(a.rowb / a.slice), (unsigned)(3 * H), (unsigned)R);
+  // (parts of a row beside each other in one L2: with the parts of a head as the fastest index the request of 131072 takes 299 us of 32 bytes, 388 of 16)
+  const dim3 grid((unsigned)(3 * H), (unsigned)(a.rowb / a.slice), (unsigned)R);
   if (most <= kMove * 256 * 16 / a.slice) hipLaunchKernelGGL(k_evict_move<256>, grid, dim3(256), 0, st, a);
   else hipLaunchKernelGGL(k_evict_move<1024>, grid, dim3(1024), 0, st, a);
   ZC_LAUNCH_CHECK();

@@ -79,7 +79,7 @@ def test_budgets(keep, most):
     Cache([100, 100, 100], 2, 64, BF).check(keep, most=most, recent=7)
 
 
-@pytest.mark.parametrize("kv,keep,scores", [(8192, 8191, "random"), (8193, 4000, "random"), (20000, 9000, "ties"), (24577, 1, "random"), (17000, 16384, "equal")])
+@pytest.mark.parametrize("kv,keep,scores", [(8192, 8191, "random"), (8193, 4000, "random"), (20000, 9000, "ties"), (24577, 1, "random"), (17000, 16384, "equal"), (32769, 9000, "ties"), (75000, 30000, "random")])
 @pytest.mark.parametrize("together", [False, True])
 def test_long_requests(kv, keep, scores, together):
     Cache([kv, 40], 1 if not together else 2, 64, BF, page=64, scores=scores).check([keep, 40], sinks=4, recent=keep // 3, together=together)
