@@ -36,9 +36,9 @@ struct ScoreArgs {
 // A request's keys go in tiles of 128, or 64 where those are few: of up to 64 rows a wave takes every fourth 32 keys, of more the four waves share a tile.
 constexpr int kScoreTile = 128;
 // Tiles of chunks and heads below which they are halved: more workgroups, which all take every row.  us of 128 and 64 keys a tile (32 heads over 8 of 128 channels, bf16): a prompt of
-// 2048 103 and 78, four of 500 42 and 30, 500 tokens over 4096 (256 tiles)
-// 44 and 37, 300 over 6000 (376) 41 and 44, 500 over 8192 (512) 56 and 69; fp32, 500 over 4096 (16 heads over 4) 190 and 119.
-constexpr float kFewTiles = 320.f;
+// 2048 103 and 80, four of 500 42 and 31, 500 tokens over 4096 (256 tiles) 44 and 37, 1000 that see 4096 each (328) 98 and 87, 300 over 6000 (376) 44 and 46, 500 over 8192 (512) 53
+// and 69; fp32, 500 over 4096 (16 heads over 4) 190 and 115.
+constexpr float kFewTiles = 340.f;
 
 struct Span {
   int r, qs, nq, kv;            // request, its first row, new tokens, tokens
@@ -55,29 +55,31 @@ __device__ inline uint32_t opaque(uint32_t x) { asm volatile("" : "+v"(x)); retu
 // Unit u of a head; false: there are fewer.
 __device__ inline bool find_span(const ScoreArgs& a, int u, Span& x) {
   const int lane = threadIdx.x & 63;
-  struct Part { int qs, nq, kv, first, sink_tiles, tiles, passes; };           // passes: of 64 rows over a tile
+  struct Part { int qs, nq, kv, first, sink_tiles, tiles, passes; float work; };         // passes: of 64 rows over a tile; work: of all tiles
   int shift = 7;
   const auto part = [&](int r) {
-    Part p = {0, 0, 0, 0, 0, 0, 1};
+    Part p = {0, 0, 0, 0, 0, 0, 1, 0.f};
     if (r >= a.R) return p;
     const int s = a.q_start[r], e = a.q_start[r + 1], kv = a.kv_len[r];
     p.qs = min(max(s, 0), a.T);
     p.nq = max(min(e, a.T) - p.qs, 0);
     p.kv = min(max(kv, 0), a.cap);
     // (weights that fade change every token's score, seen or not)
-    const int p0 = max(p.kv - p.nq, 0), low = a.window && a.decay == 1.f ? max(0, p0 - a.window + 1) : 0;
+    const int p0 = max(p.kv - p.nq, 0), reached = a.window ? max(0, p0 - a.window + 1) : 0, low = a.decay == 1.f ? reached : 0;
     const int up = (1 << shift) - 1;
     p.first = low >> shift;
     p.sink_tiles = min((min(a.sinks, low) + up) >> shift, p.first);
     if (p.nq) p.tiles = p.sink_tiles + ((p.kv + up) >> shift) - p.first;
     p.passes = (int)(((int64_t)p.nq * a.G + 63) / 64);
+    const int fade = min((reached >> shift) - p.first, p.tiles);     // tiles that no window reaches
+    p.work = (float)(p.tiles - fade) * (float)p.passes + (float)fade;
     return p;
   };
   Part head = part(lane);
-  float all = (float)head.tiles * (float)head.passes, chunks = head.passes > 1 ? (float)head.tiles : 0.f;
+  float all = head.work, chunks = head.passes > 1 ? (float)head.tiles : 0.f;
   for (int r0 = 64; r0 < a.R; r0 += 64) {
     const Part p = part(r0 + lane);
-    all += (float)p.tiles * (float)p.passes;
+    all += p.work;
     chunks += p.passes > 1 ? (float)p.tiles : 0.f;
   }
   all = wave_sum(all);
@@ -123,6 +125,9 @@ __device__ inline int2 row_of(const ScoreArgs& a, int j0, int v) {
   const int j = a.G == 1 ? v : (int)__umulhi((uint32_t)v, a.over_G);           // (exact while v G < 2^32)
   return make_int2(j0 + j, v - j * a.G);
 }
+
+// How far from a key a row may stand that sees it, at its position or behind it.
+__device__ inline uint32_t reach_of(const ScoreArgs& a, int key) { return !a.window || key < a.sinks ? 0x80000000u : (uint32_t)a.window; }
 
 // A row's normaliser in log2 units; of one that sees nothing (-inf) so that its weights are 0.
 __device__ inline float norm_of(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }
@@ -210,6 +215,7 @@ __device__ __forceinline__ void score_rows(const ScoreArgs& a, const Span& x, in
   for (; b < blocks; b += 4) {
     const int key = key0 + r, next = b + 4 < blocks ? key_of(b + 4) : 0;
     const int seen_from = p1 - a.window;                                       // keys above it are in every row's window
+    const uint32_t reach = reach_of(a, key);
     const bool whole = key0 + 31 <= p0 && (!a.window || key0 > seen_from || key0 + 31 < a.sinks);
     const bool any = (uint32_t)(key0 - a.sinks) >= x.behind || (uint32_t)(key0 + 16 - a.sinks) >= x.behind;      // of the block's keys a row may see some
     wait_vmem<0>();
@@ -237,9 +243,7 @@ __device__ __forceinline__ void score_rows(const ScoreArgs& a, const Span& x, in
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
           const float e = __builtin_amdgcn_exp2f(fmaf(logit<SUMS>(acc[v4 >> 2], 4 * (v4 & 3) + u), a.scale_log2, -(&nv.x)[u]));
-          const int p = (&pv.x)[u];
-          const bool sees = whole || ((key <= p) & (!a.window || key > p - a.window || key < a.sinks));
-          sum += sees ? e : 0.f;
+          sum += whole || (uint32_t)((&pv.x)[u] - key) < reach ? e : 0.f;
         }
       }
       sum += __shfl_xor(sum, 32);
@@ -358,17 +362,18 @@ __device__ __forceinline__ void score_tiles(const ScoreArgs& a, const Span& x, i
     // Weights of product n's 32 rows and its keys, which not all rows see.
     const auto masked = [&](int n, const float* norm_of_row, const int* pos_of_row) {
       const int key = key0 + 32 * KEYS * kw + (KEYS == 2 ? 32 * n : 0) + r;
+      const uint32_t reach = reach_of(a, key);
 #pragma unroll
       for (int v4 = 0; v4 < 4; ++v4) {
         const float4 nv = *reinterpret_cast<const float4*>(norm_of_row + 8 * v4);
         const int4 pv = *reinterpret_cast<const int4*>(pos_of_row + 8 * v4);
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-          const int p = (&pv.x)[u];
           const float e = __builtin_amdgcn_exp2f(fmaf(logit<SUMS>(acc[n], 4 * v4 + u), a.scale_log2, -(&nv.x)[u]));
-          sum[n] += ((key <= p) & (!a.window || key > p - a.window || key < a.sinks)) ? e : 0.f;
-          __builtin_amdgcn_sched_barrier(0);     // (or the operands of all 16 are brought in front, into registers there are not)
+          sum[n] += (uint32_t)((&pv.x)[u] - key) < reach ? e : 0.f;
+          if (DT == ZC_F32) __builtin_amdgcn_sched_barrier(0);
         }
+        __builtin_amdgcn_sched_barrier(0);       // (or the operands of all 16 are brought in front, into registers there are not)
       }
     };
     // Products of the keys n with 32 rows, and meanwhile, of 16-bit types, the weights of the products before, of keys m, if all rows see them.
