@@ -26,6 +26,7 @@ struct SharedArgs : PagedArgs {
   int* tokens;                                  // the tokens that go through a prefix together, group after group
   int least;                                    // tiles, below which a block is not split (fp32)
   float worth;                                  // tiles that a shared prefix has to spare
+  int far;                                      // tiles, above which a prefix is read once for 33 to 64 rows
   int places;                                   // of a head's units at a time
   int most_units, most_joins;                   // (units: partial results that there is room for)
 };
@@ -85,8 +86,8 @@ __device__ inline int64_t part_of(const PagedArgs& a, const SharedUnit& x, int h
 // Entries of the plan are the requests: what their rows are, and that they go through their prefix together with others' if they are few.
 struct Entry { int qs, nq, kv, group, pre, few, blocks, tiles, together; };
 struct Cut { int few, blocks; };                           // blocks of 32 rows or of `many`
-__device__ inline Cut cut_of(int rows, int many) {
-  const bool few = rows <= kFewRows || many == 32;
+__device__ inline Cut cut_of(int rows, int many, int few_rows = kFewRows) {
+  const bool few = rows <= few_rows || many == 32;
   return {few, few ? (rows + 31) / 32 : (rows + many - 1) / many};
 }
 
@@ -136,6 +137,7 @@ __device__ bool plan(const SharedArgs& a, int many, int wanted, PlanMemory<THREA
   };
   // Rows of a group that go through its prefix together (of starts that do not ascend they could be more than there are).
   const auto rows_of = [&](int g) { return min(max(s.g_end[g] - s.g_first[g], 0), a.T) * a.G; };
+  const auto cut_together = [&](int g) { return cut_of(rows_of(g), many, (s.g_kv[g] + kTile - 1) / kTile > a.far ? 32 : kFewRows); };
   const Given front = given(tid);
   for (int e = tid; e <= a.P; e += THREADS) {
     s.g_start[e] = min(max(a.group_start[e], 0), a.R);
@@ -174,7 +176,7 @@ __device__ bool plan(const SharedArgs& a, int many, int wanted, PlanMemory<THREA
   }
   __syncthreads();
   for (int g = tid; g < a.P; g += THREADS) {
-    const int blocks = cut_of(rows_of(g), many).blocks;
+    const int blocks = cut_together(g).blocks;
     work += (float)blocks * (float)((s.g_kv[g] + kTile - 1) / kTile);
     n_blocks += (float)blocks;
   }
@@ -226,7 +228,7 @@ __device__ bool plan(const SharedArgs& a, int many, int wanted, PlanMemory<THREA
   int units = 0, joins = 0, parts = 0;
   for (int g0 = 0; g0 < a.P; g0 += THREADS) {
     const int g = g0 + tid, rows = g < a.P ? rows_of(g) : 0, tiles = g < a.P ? (s.g_kv[g] + kTile - 1) / kTile : 0;
-    const Cut c = cut_of(rows, many);
+    const Cut c = g < a.P ? cut_together(g) : Cut{1, 0};
     const int n = parts_of(tiles), mine = c.blocks * n;
     int all;
     if (g0) __syncthreads();
@@ -240,7 +242,7 @@ __device__ bool plan(const SharedArgs& a, int many, int wanted, PlanMemory<THREA
     units_in_hand(units, all, min(a.P - g0, THREADS), before, mine, [&](int u, int i) {
       const int e = g0 + i, n = s.parts[i], rest = u - s.unit[i], b = rest / n, p = rest - b * n;
       const int rows = rows_of(e), tiles = (s.g_kv[e] + kTile - 1) / kTile;
-      const Cut k = cut_of(rows, many);
+      const Cut k = cut_together(e);
       const int rb = k.few ? 32 : many, i0 = b * rb, j = i0 / a.G, q = tiles / n, rem = tiles - q * n;
       const int lo = p * q + min(p, rem), hi = lo + q + (p < rem ? 1 : 0);
       put(units + u, units + u, make_int4(k.few, e, 0, units + u), make_int4(0, 0, 0, s.g_kv[e]),
@@ -284,7 +286,7 @@ __device__ bool plan(const SharedArgs& a, int many, int wanted, PlanMemory<THREA
       if (p == 0 && part >= 0 && join < a.most_joins) {
         int4 w = make_int4(g0, 0, 0, 0);
         if (together) {
-          const bool big = !cut_of(rows_of(group), many).few;
+          const bool big = !cut_together(group).few;
           w = make_int4(g0, s.g_part[group], s.g_parts[group] << 1 | (big ? 1 : 0), (s.place[e] - s.g_first[group]) * a.G + i0);
         }
         a.joins[2 * join] = make_int4(part, n, take, s.qs[e] + j0);
@@ -454,7 +456,7 @@ struct Most { int64_t target, units, parts, joins, slot, bytes; };
 static Most most_of(int64_t P, int64_t R, int64_t T, int64_t G, int64_t Hkv, bool fp32, int64_t D) {
   Most m;
   const int64_t with = R < T ? R : T, rows = T * G, many = fp32 ? 32 : 128, groups = P < with ? P : with;
-  m.slot = fp32 || rows <= kFewRows ? 32 : 128;
+  m.slot = fp32 || rows <= 32 ? 32 : 128;
   // What the chip holds at a time: more parts cost more on their way through memory than they even out.  us at 256, 384, 512, 768 and 1024 units: bf16, 32 heads over 8 of 128
   // channels, 64 tokens after 8192 56.8, 56.7, 56.7, 63.5 and 68.4; fp16, 16 over 4 of 64, 20 tokens and 7 chunks after up to 4000 35.8, 32.7, 36.7, 41.0 and 42.9; 24 over 8 of 64, 90
   // tokens of up to 3843 after up to 2314 115, 115, 110 and 105; fp32, 16 heads of 128, 74 tokens after up to 593 91.7, 97.2, 101 and 106.
@@ -570,6 +572,9 @@ extern "C" int zc_paged_shared_attention(const zc_tensor4* q, const zc_tensor4* 
   // (32 heads over 8 of 128 channels; 29 MB spared) 19.5 and 20.3, 22 after up to 1412 (8 heads of 64; 48 MB) 18.2 and 21.8, 16 chunks of up to 17 after 355 (8 of 64; 12 MB) 18.9 and
   // 15.9, 64 after 8192 (2.1 GB) 55.6 and 189.
   a.worth = 28e6f / (float)(2 * kTile * q->D * eb);
+  // Two blocks of 32 rows read a prefix twice, the second time from the caches as long as these hold it (256 MB); one of 128 is half empty.  us of two and of one, 16 tokens (32 heads
+  // over 8 of 128 channels, bf16) after 1000 26 and 38, 16384 (67 MB) 36 and 40, 131072 (537 MB) 166 and 120.
+  a.far = (int)(128e6f / (float)(2 * kTile * q->D * eb * Hkv));
   a.most_units = (int)m.units; a.most_joins = (int)m.joins;
   uint8_t* at = (uint8_t*)ws;
   a.counts = (int*)at; at += 16;

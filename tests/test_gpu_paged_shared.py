@@ -250,6 +250,13 @@ def test_blocks_of_one_length(dtype, D, R):
     run(plain.Shared([66] * R, [70 + i for i in range(R)], [0, R], [4096], 8, 8, D, dtype))
 
 
+@pytest.mark.parametrize("rows,dtype", [(32, BF), (33, BF), (64, BF), (40, FL)])
+def test_prefixes_that_caches_do_not_hold(rows, dtype):
+    """More than 128 MB of keys and values for up to 64 rows, beside a short prefix."""
+    n = 33000 if dtype == BF else 17000
+    run(plain.Shared([1] * (rows + 10), [2 + 5 * i for i in range(rows + 10)], [0, rows, rows + 9], [n, 700], 16, 16, 64, dtype, page=128))
+
+
 def test_many_groups_that_go_together():
     R = 300
     run(plain.Shared([1] * R, [1 + i % 90 for i in range(R)], [0] + list(range(5, 291, 5)), [900 + 7 * g for g in range(58)], 4, 2, 64, BF))
