@@ -6,8 +6,12 @@
 //   m = max(m_p, m_o),  l = l_p e^(m_p - m) + l_o e^(m_o - m),  o = (o_p e^(m_p - m) + o_o e^(m_o - m)) / l
 // A request with more than 64 rows fills blocks of its own: these take the prefix and then its own keys without a join.
 //
-// Lengths and groups are known to the GPU only.  One workgroup plans the step (k_shared_plan): what every unit of work is - a block of rows,
-// a range of tiles of the prefix, one of the request's own - how far long ranges are split, and what is to be joined.
+// Lengths and groups are known to the GPU only.  What every unit of work is - a block of rows, a range of tiles of the prefix, one of the
+// request's own - how far long ranges are split, and what is to be joined follows from sums over requests and groups, which every workgroup computes for itself, or where
+// there are many one workgroup in front (k_shared_plan).
+//
+// Bound by memory where rows are few: 64 tokens with 64 to 1024 of their own after 8192 (32 heads over 8 of 128 channels, bf16, 135 MB) 46 us and the join 7 with cold caches, 3.0 TB/s; one
+// after 131072 106 us, 5.1 TB/s; by the matrix cores where they are many: 4 chunks of 512 after 32768 1145 us, 970 TFLOP/s.
 #include "paged_attention_kernel.hpp"
 
 namespace zc {
