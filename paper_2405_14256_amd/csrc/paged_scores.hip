@@ -103,7 +103,9 @@ __device__ inline bool find_span(const ScoreArgs& a, int u, Span& x) {
     if (here) {
       const int l = __builtin_ctzll(here);
       const auto of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
-      const int n = of(parts), b = u - (units + of(cu) - n), tiles = of(p.tiles);
+      const int n = of(parts), tiles = of(p.tiles), half = (int)(0.25f * a.target);
+      int b = u - (units + of(cu) - n);
+      if (n > half && n <= 2 * half && b >= half) b = n - 1 - (b - half);
       x.r = r0 + l;
       x.qs = of(p.qs); x.nq = of(p.nq); x.kv = of(p.kv);
       x.first = of(p.first); x.sink_tiles = of(p.sink_tiles);
