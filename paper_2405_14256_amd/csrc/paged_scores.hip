@@ -413,17 +413,32 @@ __device__ __forceinline__ void score_tiles(const ScoreArgs& a, const Span& x, i
       constexpr int EACH = 16 / T::NKC;
       acc[n][0] = v16f{};
       if constexpr (REFILL) next_row = opaque(next_row);
+      float x[EACH], e[EACH];
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) e[i] = 0.f;
 #pragma unroll
       for (int kc = 0; kc < T::NKC; ++kc) {
         mma_chunk<DT>(acc[n][0], q[kc], kf[KEYS == 2 ? n : 0][kc]);
-        if constexpr (WEIGH)
+        if constexpr (WEIGH) {                       // (a weight's three instructions wait for each other: each goes with another step's)
+          if (kc > 1)
 #pragma unroll
-          for (int v = kc * EACH; v < (kc + 1) * EACH; ++v)
-            sum[n ^ 1] += __builtin_amdgcn_exp2f(fmaf(acc[n ^ 1][0][v], a.scale_log2, -(&nv[v >> 2].x)[v & 3]));
+            for (int i = 0; i < EACH; ++i) sum[n ^ 1] += e[i];
+          if (kc > 0)
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) e[i] = __builtin_amdgcn_exp2f(x[i]);
+#pragma unroll
+          for (int i = 0; i < EACH; ++i) {
+            const int v = kc * EACH + i;
+            x[i] = fmaf(acc[n ^ 1][0][v], a.scale_log2, -(&nv[v >> 2].x)[v & 3]);
+          }
+        }
         if constexpr (REFILL) q[kc] = *reinterpret_cast<lds_u32x4*>((lds_ptr)(uintptr_t)(next_row ^ (kc << 5)));
         if (NORMS && (kc + 1) * EACH % 4 == 0) nv[(kc + 1) * EACH / 4 - 1] = *reinterpret_cast<const float4*>(next_norm + 2 * ((kc + 1) * EACH - 4));
         __builtin_amdgcn_sched_barrier(0);
       }
+      if constexpr (WEIGH)
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) sum[n ^ 1] += e[i] + __builtin_amdgcn_exp2f(x[i]);
     };
     const auto weigh_only = [&](int m, const float* norm_of_row) {
 #pragma unroll
