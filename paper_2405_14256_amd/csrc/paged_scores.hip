@@ -36,7 +36,7 @@ struct ScoreArgs {
 // A request's keys go in tiles of 128, or 64 where those are few: of up to 64 rows a wave takes every fourth 32 keys, of more the four waves share a tile.
 constexpr int kScoreTile = 128;
 // Tiles of chunks and heads below which they are halved: more workgroups, which all take every row.  us of 128 and 64 keys a tile (32 heads over 8 of 128 channels, bf16): a prompt of
-// 2048 103 and 80, four of 500 42 and 31, 500 tokens over 4096 (256 tiles) 44 and 37, 1000 that see 4096 each (328) 98 and 87, 300 over 6000 (376) 44 and 46, 500 over 8192 (512) 53
+// 2048 103 and 72, four of 500 42 and 28, 500 tokens over 4096 (256 tiles) 44 and 35, 1000 that see 4096 each (328) 98 and 77, 300 over 6000 (376) 37 and 46, 500 over 8192 (512) 53
 // and 69; fp32, 500 over 4096 (16 heads over 4) 190 and 115.
 constexpr float kFewTiles = 340.f;
 
@@ -105,7 +105,9 @@ __device__ inline bool find_span(const ScoreArgs& a, int u, Span& x) {
       const auto of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
       const int n = of(parts), tiles = of(p.tiles), half = (int)(0.25f * a.target);
       int b = u - (units + of(cu) - n);
-      if (n > half && n <= 2 * half && b >= half) b = n - 1 - (b - half);
+      // (a chunk's first keys are seen by most rows: where all units run at once, the second on a CU is one of the last; a window evens that out by itself.  us of units in order and
+      // so, bf16, 32 heads over 8 of 128 channels: a prompt of 4096 161 and 154, 2048 over 32768 that see 4096 each 114 and 139)
+      if (!a.window && n > half && n <= 2 * half && b >= half) b = n - 1 - (b - half);
       x.r = r0 + l;
       x.qs = of(p.qs); x.nq = of(p.nq); x.kv = of(p.kv);
       x.first = of(p.first); x.sink_tiles = of(p.sink_tiles);
@@ -253,6 +255,14 @@ __device__ __forceinline__ void score_rows(const ScoreArgs& a, const Span& x, in
     if (put) *put = fmaf(before, a.decay, sum);
     key0 = next;
   }
+}
+
+// f with two conditions as types.
+template <typename F> __device__ __forceinline__ void with(bool x, bool y, const F& f) {
+  if (x && y) f(std::true_type{}, std::true_type{});
+  else if (x) f(std::true_type{}, std::false_type{});
+  else if (y) f(std::false_type{}, std::true_type{});
+  else f(std::false_type{}, std::false_type{});
 }
 
 // ---- more rows: chunks -----------------------------------------------------------------------------
@@ -406,8 +416,11 @@ __device__ __forceinline__ void score_tiles(const ScoreArgs& a, const Span& x, i
     // what the step after the next (q) or the next (nv) needs, so that no step waits for LDS.
     u32x4 q[DT == ZC_F32 ? 1 : T::NKC];
     float4 nv[4];
-    const auto flow = [&](auto weigh, auto keys, auto refill, uint32_t next_row, const float* next_norm) {
-      constexpr bool WEIGH = decltype(weigh)::value, REFILL = decltype(refill)::value;
+    // FETCH: the next tile's transfers, one a step: all at once a wave waits until the last has been taken.  That is where one workgroup has a CU for itself (a prompt of 2048 77 -> 71 us;
+    // two hide it from each other, 2048 tokens over 16384 305 and 305).
+    const auto flow = [&](auto weigh, auto fetch, auto keys, auto refill, uint32_t next_row, const float* next_norm, uint32_t to_lds, const uint8_t* from) {
+      constexpr bool WEIGH = decltype(weigh)::value, FETCH = decltype(fetch)::value, REFILL = decltype(refill)::value;
+      static_assert(DT == ZC_F32 || NI == T::NKC, "a transfer a step");
       constexpr int n = decltype(keys)::value;
       constexpr bool NORMS = n == 0 || KEYS == 1;    // (the first of these rows' products: their normalisers come)
       constexpr int EACH = 16 / T::NKC;
@@ -432,6 +445,7 @@ __device__ __forceinline__ void score_tiles(const ScoreArgs& a, const Span& x, i
             x[i] = fmaf(acc[n ^ 1][0][v], a.scale_log2, -(&nv[v >> 2].x)[v & 3]);
           }
         }
+        if constexpr (FETCH) gdma16(to_lds + kc * 4096, from + kc * q_hop, off);
         if constexpr (REFILL) q[kc] = *reinterpret_cast<lds_u32x4*>((lds_ptr)(uintptr_t)(next_row ^ (kc << 5)));
         if (NORMS && (kc + 1) * EACH % 4 == 0) nv[(kc + 1) * EACH / 4 - 1] = *reinterpret_cast<const float4*>(next_norm + 2 * ((kc + 1) * EACH - 4));
         __builtin_amdgcn_sched_barrier(0);
@@ -459,7 +473,17 @@ __device__ __forceinline__ void score_tiles(const ScoreArgs& a, const Span& x, i
       wait_all_loads();
       if (tid < QT) { norms[buf][tid] = norm_of(norm); where[buf][tid] = pos; }
       __syncthreads();                           // rows and normalisers are there, and nobody still reads the other buffer
-      if (i0 + QT < i_end) issue(i0 + QT, next.x, next.y, buf ^ 1);
+      const bool fetch = DT != ZC_F32 && KEYS == 1 && even && i0 + QT < i_end && rows - (i0 + QT) >= QT;      // by the products below
+      const uint32_t to_lds = lds + (buf ^ 1) * TILE_B + w * 1024;
+      const uint8_t* const from = base;
+      if (fetch) {
+        base += NI * q_hop + q_step;
+        pos += tokens;
+        if (tid < QT) norm = *norm_from;
+        norm_from += tokens;
+      } else if (i0 + QT < i_end) {
+        issue(i0 + QT, next.x, next.y, buf ^ 1);
+      }
       const uint32_t row = lds + buf * TILE_B + 32 * rw * T::ROWB + T::slot(r, kh);
       const int pa = past + j0, pb = past + row_of(a, j0, g0 + QT - 1).x;          // positions of the tile's first and last row
       const bool whole = key0 + TILE - 1 <= pa && (!a.window || key0 > pb - a.window || key0 + TILE - 1 < a.sinks);
@@ -485,21 +509,13 @@ __device__ __forceinline__ void score_tiles(const ScoreArgs& a, const Span& x, i
           if constexpr (KEYS == 1) {
             using KH = std::integral_constant<int, h & 1>;
             using MORE = std::bool_constant<h + 1 < QT / 64>;
-            if (pending) flow(std::true_type{}, KH{}, MORE{}, behind, of_these);
-            else flow(std::false_type{}, KH{}, MORE{}, behind, of_these);
+            with(pending, h == 0 && fetch, [&](auto weigh, auto get) { flow(weigh, get, KH{}, MORE{}, behind, of_these, to_lds, from); });
             pending = whole;
             if (!whole) masked(h & 1, of_these, &where[buf][mine + 64 * h]);
             return;
           }
-          if (pending) flow(std::true_type{}, K0{}, std::false_type{}, 0, of_these);
-          else flow(std::false_type{}, K0{}, std::false_type{}, 0, of_these);
-          if (h + 1 < QT / 64) {
-            if (whole) flow(std::true_type{}, K1{}, std::true_type{}, behind, nullptr);
-            else flow(std::false_type{}, K1{}, std::true_type{}, behind, nullptr);
-          } else {
-            if (whole) flow(std::true_type{}, K1{}, std::false_type{}, 0, nullptr);
-            else flow(std::false_type{}, K1{}, std::false_type{}, 0, nullptr);
-          }
+          with(pending, h == 0 && fetch, [&](auto weigh, auto get) { flow(weigh, get, K0{}, std::false_type{}, 0, of_these, to_lds, from); });
+          with(whole, false, [&](auto weigh, auto) { flow(weigh, std::false_type{}, K1{}, std::bool_constant<h + 1 < QT / 64>{}, behind, nullptr, 0, nullptr); });
           pending = whole;
           if (!whole) {
             masked(0, &norms[buf][mine + 64 * h], &where[buf][mine + 64 * h]);
