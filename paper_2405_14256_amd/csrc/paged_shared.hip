@@ -101,7 +101,7 @@ struct PlanMemory {
   int g_start[kGroups + 1], g_kv[kGroups], g_first[kGroups], g_end[kGroups], g_part[kGroups], g_parts[kGroups];
   // of the entries in hand
   int unit[THREADS], join[THREADS], part[THREADS], parts[THREADS], blocks[THREADS], qs[THREADS], nq[THREADS], kv[THREADS], group[THREADS], place[THREADS];
-  int waves[3][THREADS / 64], four[4][THREADS / 64];
+  int waves[3][THREADS / 64], five[5][THREADS / 64];
   float sums[2][THREADS / 64];
   int one[kWords], list[kListed];                          // of one unit: its entry, the tokens of its rows
 };
@@ -261,12 +261,17 @@ __device__ bool plan(const SharedArgs& a, int many, int wanted, PlanMemory<THREA
   for (int r0 = 0; r0 < a.R; r0 += THREADS) {
     const Entry x = r0 ? entry(r0 + tid, given(r0 + tid)) : held;
     const int n = parts_of(x.tiles), apart = x.together || n > 1;
-    int all[4];                                            // units, joins, partial results, tokens that go together
+    int all[5];                                            // units, joins, partial results, tokens that go together, units of long requests
     if (ALL || r0) __syncthreads();                        // (the entries before are done with)
     const int t = x.together ? x.nq : 0, mine = x.blocks * n;
-    int upto[4] = {mine, apart ? x.blocks : 0, apart ? mine : 0, t};
-    block_inclusive_sums<NW>(upto, s.four, all);
-    s.unit[tid] = upto[0] - mine;
+    // Units that do not run all at once: requests longer than the mean of the blocks first (of those in hand), or one of them begins last.  us in order and so (32 heads over 8 of 128
+    // channels, bf16): 100 tokens of 64 to 1000 after 4096 65.1 and 58.2, 64 after 8192 56.7 and 53.6; 40 of 500 to 1500 after 8192 (16 heads of 64, fp16) 52.6 and 54.9.  Where they do, it
+    // costs: 32 of up to 2000 after 4096 39.0 and 40.9.
+    const bool late = !ALL && (float)x.tiles <= length;
+    int upto[5] = {mine, apart ? x.blocks : 0, apart ? mine : 0, t, late ? 0 : mine};
+    block_inclusive_sums<NW>(upto, s.five, all);
+    const int begin = ALL || units + all[0] <= a.places ? upto[0] - mine : late ? all[4] + upto[0] - upto[4] - mine : upto[4] - mine;
+    s.unit[tid] = begin;
     s.join[tid] = upto[1] - (apart ? x.blocks : 0);
     s.part[tid] = apart ? upto[2] - mine : -1;
     s.parts[tid] = n;
@@ -274,7 +279,7 @@ __device__ bool plan(const SharedArgs& a, int many, int wanted, PlanMemory<THREA
     s.qs[tid] = x.qs; s.nq[tid] = x.nq; s.kv[tid] = x.kv;
     s.group[tid] = x.group;
     s.place[tid] = x.together ? placed + upto[3] - t : -1; // of its first token in the list
-    units_in_hand(units, all[0], THREADS, upto[0] - mine, mine, [&](int u, int e) {
+    units_in_hand(units, all[0], THREADS, begin, mine, [&](int u, int e) {
       const int n = s.parts[e], rest = u - s.unit[e], b0 = rest / n, p = rest - b0 * n;
       const int b = s.blocks[e] - 1 - b0;                  // (a chunk's last rows see the most keys: first)
       const int past = s.kv[e] - s.nq[e], rows = s.nq[e] * a.G, group = s.group[e], together = s.place[e] >= 0;
