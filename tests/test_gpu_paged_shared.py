@@ -257,6 +257,13 @@ def test_prefixes_that_caches_do_not_hold(rows, dtype):
     run(plain.Shared([1] * (rows + 10), [2 + 5 * i for i in range(rows + 10)], [0, rows, rows + 9], [n, 700], 16, 16, 64, dtype, page=128))
 
 
+@pytest.mark.parametrize("R,Hq,Hkv,D,dtype", [(100, 8, 8, 64, BF), (100, 8, 8, 64, FL), (300, 8, 4, 128, HF), (270, 4, 4, 64, BF)])
+def test_long_requests_go_first(R, Hq, Hkv, D, dtype):
+    """More units than run at a time, of requests of unlike lengths, some without tokens."""
+    n = [1 + (97 * i) % 600 for i in range(R)]
+    run(plain.Shared([0 if i % 11 == 5 else 1 + (i % 13 == 0) for i in range(R)], n, [1, R - 2], [1000], Hq, Hkv, D, dtype))
+
+
 def test_many_groups_that_go_together():
     R = 300
     run(plain.Shared([1] * R, [1 + i % 90 for i in range(R)], [0] + list(range(5, 291, 5)), [900 + 7 * g for g in range(58)], 4, 2, 64, BF))
