@@ -83,8 +83,7 @@ __device__ inline bool find_span(const ScoreArgs& a, int u, Span& x) {
     chunks += p.passes > 1 ? (float)p.tiles : 0.f;
   }
   all = wave_sum(all);
-  chunks = wave_sum(chunks);
-  if (__builtin_amdgcn_readfirstlane(chunks > 0.f && chunks * (float)a.Hkv < kFewTiles)) {
+  if (__builtin_amdgcn_ballot_w64(chunks > 0.f) && __builtin_amdgcn_readfirstlane(wave_sum(chunks) * (float)a.Hkv < kFewTiles)) {
     shift = 6;
     head = part(lane);
     all *= 2.f;
