@@ -10,7 +10,7 @@
 // request's own - how far long ranges are split, and what is to be joined follows from sums over requests and groups, which every workgroup computes for itself, or where
 // there are many one workgroup in front (k_shared_plan).
 //
-// Bound by memory where rows are few: 64 tokens with 64 to 1024 of their own after 8192 (32 heads over 8 of 128 channels, bf16, 135 MB) 46 us and the join 7 with cold caches, 3.0 TB/s; one
+// Bound by memory where rows are few: 64 tokens with 64 to 1024 of their own after 8192 (32 heads over 8 of 128 channels, bf16, 135 MB) 43 us and the join 7 with cold caches, 3.1 TB/s; one
 // after 131072 106 us, 5.1 TB/s; by the matrix cores where they are many: 4 chunks of 512 after 32768 1145 us, 970 TFLOP/s.
 #include "paged_attention_kernel.hpp"
 
