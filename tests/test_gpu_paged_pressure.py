@@ -7,7 +7,7 @@ import pytest
 import torch
 
 from paper_2405_14256_amd import binding as zb
-from tests import evict_plain
+from tests import evict_plain, shared_plain
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -162,3 +162,37 @@ def test_many_answers_to_a_long_prompt_under_pressure():
         s.step([1 + (r + turn) % 3 for r in range(40)] if turn else [1 + r % 30 for r in range(40)], decay=1.0)
         s.evict([16] * 40, sinks=0, recent=4, together=False)
         s.check_pages()
+
+
+@pytest.mark.parametrize("dtype,by_head", [(BF, True), (FL, False)])
+def test_offsets_past_32_bits(dtype, by_head):
+    """Pools of more than 4 GB each: with the pages at their ends every operator gives what it gives with few pages."""
+    s = shared_plain.Shared([1, 90, 1], [700, 333, 64], [0, 3], [500], 8, 4, 128, dtype, seed=3, page=64)
+    p = s.p
+    n, N = p.kp.shape[0], (5 << 30) // (4 * 64 * 128 * dtype.itemsize)
+    g = torch.Generator(device=DEV).manual_seed(1)
+    weights = torch.rand(n, 4, 64, generator=g, device=DEV)
+    keep = torch.tensor([100, 333, 20], dtype=torch.int32, device=DEV)
+    shape = (N, 4, 64, 128) if by_head else (N, 64, 4, 128)
+    results = []
+    for far in (False, True):
+        if far:
+            kp, vp = (torch.empty(shape, dtype=dtype, device=DEV) for _ in range(2))
+            if not by_head:
+                kp, vp = kp.transpose(1, 2), vp.transpose(1, 2)
+            scores = torch.empty(N, 4, 64, device=DEV)
+            kp[N - n:], vp[N - n:], scores[N - n:] = p.kp, p.vp, weights
+            table, pre_table = (torch.where(t >= 0, t + N - n, t) for t in (s.table, s.pre_table))
+        else:
+            kp, vp, scores, table, pre_table = p.kp.clone(), p.vp.clone(), weights.clone(), s.table, s.pre_table
+        out, lse = zb.zc_paged_shared_attention(p.q, kp, vp, pre_table, s.pre, s.groups, table, s.q_start, s.kv)
+        zb.zc_paged_scores(p.q, kp, table, s.q_start, s.kv, lse, scores)
+        new_len, kept, _ = zb.zc_paged_evict(kp, vp, scores, table, s.kv, keep, 333, sinks=2, recent=10)
+        torch.cuda.synchronize()
+        for r, m in enumerate((100, 333, 20)):
+            kept[r, :, m:] = 0
+        results.append([x.clone() for x in (out, lse, new_len, kept, kp[-n:], vp[-n:], scores[-n:])])
+        s.check(out, lse)
+        del kp, vp, scores
+    for a, b in zip(*results):
+        assert torch.equal(a.nan_to_num(-7.0) if a.is_floating_point() else a, b.nan_to_num(-7.0) if b.is_floating_point() else b)

@@ -264,6 +264,33 @@ def test_long_requests_go_first(R, Hq, Hkv, D, dtype):
     run(plain.Shared([0 if i % 11 == 5 else 1 + (i % 13 == 0) for i in range(R)], n, [1, R - 2], [1000], Hq, Hkv, D, dtype))
 
 
+@pytest.mark.parametrize("dtype", [BF, FL])
+@pytest.mark.parametrize("q_len,pre", [([1] * 20, 4000), ([1, 2, 70], 130), ([1], 100)])
+def test_logits_of_minus_infinity(dtype, q_len, pre):
+    """Keys of which no row has any weight, whole tiles of a prefix and of own tokens among them: as keys of very small logits.  All keys: zeros."""
+    R = len(q_len)
+    s = plain.Shared(q_len, [200 + i for i in range(R)], [0, R], [pre], 4, 2, 128, dtype, page=16)
+    p = s.p
+    p.q[:, :, 0] = p.q[:, :, 0].abs() + 0.5
+    pre_page, own_page = s.pre_table[0].long(), s.table[0].long()
+
+    def run_with(x, every=False):
+        kp = p.kp.clone()
+        for pages, n in ((pre_page, pre // 16), (own_page, 8)):
+            some = pages[:n] if every else pages[:min(n, 4)] if n < 8 else torch.cat([pages[:4], pages[5:n:3]])
+            kp[some, :, :, 0] = x
+        if every:
+            kp[:, :, :, 0] = torch.where(kp[:, :, :, 0].isnan(), kp[:, :, :, 0], x)
+        args = list(s.args())
+        args[1] = kp
+        return zb.zc_paged_shared_attention(*args)
+    (out, lse), (want, want_lse) = run_with(-math.inf), run_with(-1e4)
+    T = p.start[R]
+    assert torch.equal(out[:T], want[:T]) and torch.equal(lse[:, :T], want_lse[:, :T]) and bool(out[:T].isfinite().all())
+    out, lse = run_with(-math.inf, every=True)
+    assert bool((out[:T] == 0).all()) and bool((lse[:, :T] == -math.inf).all())
+
+
 def test_many_groups_that_go_together():
     R = 300
     run(plain.Shared([1] * R, [1 + i % 90 for i in range(R)], [0] + list(range(5, 291, 5)), [900 + 7 * g for g in range(58)], 4, 2, 64, BF))
