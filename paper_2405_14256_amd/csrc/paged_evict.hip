@@ -1,7 +1,7 @@
 // zc_paged_evict: of every request the tokens that gathered the most weight, the newest and the first ones stay, and move to the
 // front of the request's pages.
 //
-// Two launches (three where all heads take one choice): who stays, as an ascending list for each request and head, with the
+// Two launches (three where all heads take one choice, one for short lists): who stays, as an ascending list for each request and head, with the
 // lengths and the pages that are left; then the rows, in place.  A token that stays never moves back: the i-th of the list lies at
 // list[i] >= i.  So a workgroup that takes some channels of a (request, head) for itself may go through the list from its start, reading
 // as far ahead as it likes, and needs no copy and no other workgroup: the place i that it fills was read by then, as the
@@ -108,37 +108,37 @@ __device__ void give_back(const EvictArgs& a, int r, int kv, int stay, int (*wav
     if (at + c >= 0 && at + c < a.n_list) a.free_pages[at + c] = a.table[r * a.row + c];
 }
 
-// HELD: chunks of kEach tokens a thread that it holds; scores behind them are read again in every sweep.
-template <int THREADS, int HELD>
-__global__ __launch_bounds__(THREADS) void k_evict_pick(EvictArgs a) {
+template <int THREADS>
+struct PickMemory {
+  int bins[3][kBins];
+  int waves[5][THREADS / 64];
+  int digit[3], above[3], count[3], moved;
+};
+
+// The list of a request and head, in memory and for `also`; the first place of it whose token lies elsewhere, `stay` at most.  HELD: chunks of kEach tokens a thread that it
+// holds; scores behind them are read again in every sweep.  id: the pages of those it holds.
+template <int THREADS, int HELD, typename F>
+__device__ __forceinline__ int pick(const EvictArgs& a, int r, int h, int kv, int stay, const int (&id)[HELD], PickMemory<THREADS>& s, F&& also) {
   constexpr int NW = THREADS / 64, CHUNK = THREADS * kEach, PER = kBins / THREADS;
-  __shared__ __align__(16) int bins[3][kBins];
-  __shared__ int waves[5][NW];
-  __shared__ int s_digit[3], s_above[3], s_count[3], s_moved;
-  const int r = blockIdx.y, h = blockIdx.x, tid = threadIdx.x;
-  int id[HELD];
-#pragma unroll
-  for (int c = 0; c < HELD; ++c) id[c] = page_of(a, r, c * CHUNK + tid * kEach);
-  const int kv = tokens_of(a, r), stay = stay_of(a, r, kv);
-  if (h == a.heads) {                                      // (beside the heads')
-    give_back<THREADS>(a, r, kv, stay, waves);
-    return;
-  }
-  int32_t* list = a.kept + ((int64_t)r * a.heads + h) * a.most;
+  auto& bins = s.bins;
+  auto& waves = s.waves;
+  const int tid = threadIdx.x;
+  int32_t* const kept = a.kept + ((int64_t)r * a.heads + h) * a.most;
+  const auto put = [&](int at, int i) {
+    kept[at] = i;
+    also(at, i);
+  };
   if (stay == kv) {
-    for (int i = tid; i < kv; i += THREADS) list[i] = i;
-    return;
+    for (int i = tid; i < kv; i += THREADS) kept[i] = i;
+    return stay;
   }
   const int recent = min(a.recent, stay), sinks = min(a.sinks, stay - recent);
   const int lo = sinks, hi = kv - recent, need = stay - recent - sinks;     // candidates, and how many of them stay
   const int chunks = (int)(((int64_t)hi + CHUNK - 1) / CHUNK);
-  for (int i = tid; i < sinks; i += THREADS) list[i] = i;
-  for (int i = tid; i < recent; i += THREADS) list[stay - recent + i] = kv - recent + i;
-  if (need == 0) {
-    if (tid == 0) a.moved[r * a.heads + h] = sinks;
-    return;
-  }
-  if (tid == 0) s_moved = stay - recent;
+  for (int i = tid; i < sinks; i += THREADS) put(i, i);
+  for (int i = tid; i < recent; i += THREADS) put(stay - recent + i, kv - recent + i);
+  if (need == 0) return sinks;
+  if (tid == 0) s.moved = stay - recent;
   Images held[HELD];
 #pragma unroll
   for (int c = 0; c < HELD; ++c) held[c] = images(a, r, h, c * CHUNK + tid * kEach, hi, id[c]);
@@ -192,15 +192,15 @@ __global__ __launch_bounds__(THREADS) void k_evict_pick(EvictArgs a) {
       int count = 0;
 #pragma unroll
       for (int v = 0; v < PER; ++v) count = b == v ? n[v] : count;
-      s_digit[pass] = top - b;
-      s_above[pass] = above;
-      s_count[pass] = count;
+      s.digit[pass] = top - b;
+      s.above[pass] = above;
+      s.count[pass] = count;
     }
     __syncthreads();
-    prefix = pass == 0 ? (uint32_t)s_digit[pass] : prefix << bits | (uint32_t)s_digit[pass];
-    ties -= s_above[pass];
+    prefix = pass == 0 ? (uint32_t)s.digit[pass] : prefix << bits | (uint32_t)s.digit[pass];
+    ties -= s.above[pass];
     least = prefix << shift;
-    if (pass < 2 && s_count[pass] == ties && least > 0) {  // (all of them stay)
+    if (pass < 2 && s.count[pass] == ties && least > 0) {  // (all of them stay)
       --least;
       ties = 0;
       break;
@@ -226,7 +226,7 @@ __global__ __launch_bounds__(THREADS) void k_evict_pick(EvictArgs a) {
       left -= tie;
       if (tie || (candidate(i0 + e) && m.x[e] > least)) {
         if (at != i0 + e) first = min(first, at);
-        list[at++] = i0 + e;
+        put(at++, i0 + e);
       }
     }
     equal += all_same;
@@ -234,9 +234,30 @@ __global__ __launch_bounds__(THREADS) void k_evict_pick(EvictArgs a) {
     const uint64_t any = __builtin_amdgcn_ballot_w64(first != INT_MAX);          // (places ascend with the lanes, and with the chunks)
     if (any && moved == INT_MAX) moved = __builtin_amdgcn_readlane(first, __builtin_ctzll(any));
   });
-  if ((tid & 63) == 0 && moved != INT_MAX) atomicMin(&s_moved, moved);
+  if ((tid & 63) == 0 && moved != INT_MAX) atomicMin(&s.moved, moved);
   __syncthreads();
-  if (tid == 0) a.moved[r * a.heads + h] = s_moved;
+  return s.moved;
+}
+
+template <int THREADS, int HELD>
+__device__ inline void first_pages(const EvictArgs& a, int r, int (&id)[HELD]) {
+#pragma unroll
+  for (int c = 0; c < HELD; ++c) id[c] = page_of(a, r, c * THREADS * kEach + threadIdx.x * kEach);
+}
+
+template <int THREADS, int HELD>
+__global__ __launch_bounds__(THREADS) void k_evict_pick(EvictArgs a) {
+  __shared__ __align__(16) PickMemory<THREADS> s;
+  const int r = blockIdx.y, h = blockIdx.x;
+  int id[HELD];
+  first_pages<THREADS>(a, r, id);
+  const int kv = tokens_of(a, r), stay = stay_of(a, r, kv);
+  if (h == a.heads) {                                      // (beside the heads')
+    give_back<THREADS>(a, r, kv, stay, s.waves);
+    return;
+  }
+  const int moved = pick<THREADS, HELD>(a, r, h, kv, stay, id, s, [](int, int) {});
+  if (threadIdx.x == 0) a.moved[r * a.heads + h] = moved;
 }
 
 // ---- the rows -------------------------------------------------------------------------------------
@@ -327,6 +348,59 @@ __global__ __launch_bounds__(THREADS, 4) void k_evict_move(EvictArgs a) {
   }
 }
 
+// ---- short lists: who stays and their rows in one launch ---------------------------------------------
+// A list whose rows a workgroup takes in one step: it moves what it has chosen.  All rows are read before the first is stored.  Bound by latency.  us of two launches and
+// this one: 16 requests of 30 to 250, 64 stay (8 heads of 128 channels, bf16) 15.0 and 12.3, 64 of 100 to 900, 200 stay 30.0 and 23.8, 37 of 20, 10 stay (40 heads) 21.4 and 14.7,
+// 64 of 600 to 3000, 500 stay (64 channels) 48.6 and 37.5.
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void k_evict_short(EvictArgs a) {
+  __shared__ __align__(16) PickMemory<THREADS> s;
+  __shared__ int list[kMove * THREADS / 8];                // (a row has 8 pieces or more)
+  const int r = blockIdx.y, h = blockIdx.x;
+  int id[1];
+  first_pages<THREADS>(a, r, id);
+  const int kv = tokens_of(a, r), stay = stay_of(a, r, kv);
+  if (h == a.heads) {
+    give_back<THREADS>(a, r, kv, stay, s.waves);
+    return;
+  }
+  const int begin = pick<THREADS, 1>(a, r, h, kv, stay, id, s, [&](int at, int i) { list[at] = i; });
+  if (begin >= stay) return;
+  __syncthreads();
+  const int inside = (1 << a.shift) - 1, per = THREADS >> a.lanes, first = threadIdx.x >> a.lanes;
+  const auto row = [&](int what, int slot) {
+    return reinterpret_cast<piece16*>(a.pool[what] + (threadIdx.x & ((1 << a.lanes) - 1)) * 16 + h * a.sH[what] + (slot >> a.shift) * a.sB[what] + (slot & inside) * a.sL[what]);
+  };
+  const auto score = [&](int slot) { return a.scores + (((int64_t)(slot >> a.shift) * a.Hkv + h) << a.shift) + (slot & inside); };
+  const auto find = [&](int i) {
+    Move m = {-1, -1};
+    if (i < stay && list[i] != i) m = {slot_at(a, r, list[i]), slot_at(a, r, i)};
+    return m;
+  };
+  Move m[kMove];
+  piece16 x[2][kMove];
+#pragma unroll
+  for (int u = 0; u < kMove; ++u) m[u] = find(begin + per * u + first);
+  const Move mine = find(begin + threadIdx.x);             // (of the scores, a token a thread)
+#pragma unroll
+  for (int u = 0; u < kMove; ++u)
+#pragma unroll
+    for (int what = 0; what < 2; ++what) {
+      x[what][u] = piece16{0, 0, 0, 0};
+      if (m[u].src >= 0) x[what][u] = *row(what, m[u].src);
+    }
+  const float w = mine.src >= 0 ? *score(mine.src) : 0.f;
+  wait_vmem<0>();
+  __syncthreads();                                         // (everything is read)
+#pragma unroll
+  for (int u = 0; u < kMove; ++u)
+    if (m[u].dst >= 0) {
+      *row(0, m[u].dst) = x[0][u];
+      *row(1, m[u].dst) = x[1][u];
+    }
+  if (mine.dst >= 0) *score(mine.dst) = w;
+}
+
 }  // namespace zc
 
 using namespace zc;
@@ -389,8 +463,18 @@ extern "C" int zc_paged_evict(const zc_tensor4* k_pages, const zc_tensor4* v_pag
     a.sums = sums;
   }
   const dim3 lists((unsigned)a.heads + 1, (unsigned)R);
+  a.rowb = (int)(k_pages->D * eb);
+  // (every head its own list, all of whose rows are one step)
+  a.lanes = __builtin_ctz(a.rowb / 16);
+  const auto is_short = [&](int threads) { return a.heads == H && a.cap <= threads * kEach && (most << a.lanes) <= kMove * threads; };
+  if (is_short(256) || is_short(1024)) {
+    if (is_short(256)) hipLaunchKernelGGL(k_evict_short<256>, lists, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL(k_evict_short<1024>, lists, dim3(1024), 0, st, a);
+    ZC_LAUNCH_CHECK();
+    return ZC_OK;
+  }
   // Threads for four tokens each; short lists in workgroups of 256, of which a CU holds more.  us of 512 and 256 threads (and 1024 and 256 below): 37 requests of 20 tokens, 40 heads
-  // of 128 channels, 39 and 21; 128 of up to 250, 8 heads, 33 and 24; one of up to 900 14.2 and 14.5.
+  // of 128 channels, 39 and 21; 128 of up to 250, 8 heads, 33 and 24; one of up to 900 14.2 and 14.5 (in two launches).
   if (a.cap <= 256 * kEach) hipLaunchKernelGGL((k_evict_pick<256, 1>), lists, dim3(256), 0, st, a);
   else if (a.cap <= 512 * kEach) hipLaunchKernelGGL((k_evict_pick<512, 1>), lists, dim3(512), 0, st, a);
   else if (a.cap <= 1024 * kEach) hipLaunchKernelGGL((k_evict_pick<1024, 1>), lists, dim3(1024), 0, st, a);
@@ -398,7 +482,6 @@ extern "C" int zc_paged_evict(const zc_tensor4* k_pages, const zc_tensor4* v_pag
   else if (a.cap <= 4 * 1024 * kEach) hipLaunchKernelGGL((k_evict_pick<1024, 4>), lists, dim3(1024), 0, st, a);
   else hipLaunchKernelGGL((k_evict_pick<1024, 8>), lists, dim3(1024), 0, st, a);
   ZC_LAUNCH_CHECK();
-  a.rowb = (int)(k_pages->D * eb);
   const int64_t chains = R * H * 2;
   // Rows are cut where that fills the chip and saves steps of the way through the list.  us of whole rows, of 128, 64 and 16 bytes, 8 heads, 256 bytes
   // a row: one request of 4096, 1638 stay 39.0, 26.0, 20.2 and 18.6; of 131072, 32768 stay (64 and 16) 286 and 286; 4 of up to 400, 256 stay 15.7 and 15.7 (20.2 of 32);
