@@ -351,20 +351,20 @@ __global__ __launch_bounds__(THREADS, 4) void k_evict_move(EvictArgs a) {
 // ---- short lists: who stays and their rows in one launch ---------------------------------------------
 // A list whose rows a workgroup takes in one step: it moves what it has chosen.  All rows are read before the first is stored.  Bound by latency.  us of two launches and
 // this one: 16 requests of 30 to 250, 64 stay (8 heads of 128 channels, bf16) 15.0 and 12.3, 64 of 100 to 900, 200 stay 30.0 and 23.8, 37 of 20, 10 stay (40 heads) 21.4 and 14.7,
-// 64 of 600 to 3000, 500 stay (64 channels) 48.6 and 37.5.
-template <int THREADS>
+// 64 of 600 to 3000, 500 stay (64 channels) 48.6 and 37.5, 64 of 3000 to 8192, 128 stay 43.9 and 38.0.
+template <int THREADS, int HELD>
 __global__ __launch_bounds__(THREADS) void k_evict_short(EvictArgs a) {
   __shared__ __align__(16) PickMemory<THREADS> s;
   __shared__ int list[kMove * THREADS / 8];                // (a row has 8 pieces or more)
   const int r = blockIdx.y, h = blockIdx.x;
-  int id[1];
+  int id[HELD];
   first_pages<THREADS>(a, r, id);
   const int kv = tokens_of(a, r), stay = stay_of(a, r, kv);
   if (h == a.heads) {
     give_back<THREADS>(a, r, kv, stay, s.waves);
     return;
   }
-  const int begin = pick<THREADS, 1>(a, r, h, kv, stay, id, s, [&](int at, int i) { list[at] = i; });
+  const int begin = pick<THREADS, HELD>(a, r, h, kv, stay, id, s, [&](int at, int i) { list[at] = i; });
   if (begin >= stay) return;
   __syncthreads();
   const int inside = (1 << a.shift) - 1, per = THREADS >> a.lanes, first = threadIdx.x >> a.lanes;
@@ -466,10 +466,11 @@ extern "C" int zc_paged_evict(const zc_tensor4* k_pages, const zc_tensor4* v_pag
   a.rowb = (int)(k_pages->D * eb);
   // (every head its own list, all of whose rows are one step)
   a.lanes = __builtin_ctz(a.rowb / 16);
-  const auto is_short = [&](int threads) { return a.heads == H && a.cap <= threads * kEach && (most << a.lanes) <= kMove * threads; };
-  if (is_short(256) || is_short(1024)) {
-    if (is_short(256)) hipLaunchKernelGGL(k_evict_short<256>, lists, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(k_evict_short<1024>, lists, dim3(1024), 0, st, a);
+  if (a.heads == H && (most << a.lanes) <= kMove * 1024) {
+    if (a.cap <= 256 * kEach && (most << a.lanes) <= kMove * 256) hipLaunchKernelGGL((k_evict_short<256, 1>), lists, dim3(256), 0, st, a);
+    else if (a.cap <= 1024 * kEach) hipLaunchKernelGGL((k_evict_short<1024, 1>), lists, dim3(1024), 0, st, a);
+    else if (a.cap <= 4 * 1024 * kEach) hipLaunchKernelGGL((k_evict_short<1024, 4>), lists, dim3(1024), 0, st, a);
+    else hipLaunchKernelGGL((k_evict_short<1024, 8>), lists, dim3(1024), 0, st, a);
     ZC_LAUNCH_CHECK();
     return ZC_OK;
   }
