@@ -132,6 +132,11 @@ __device__ inline int2 row_of(const ScoreArgs& a, int j0, int v) {
 // How far from a key a row may stand that sees it, at its position or behind it.
 __device__ inline uint32_t reach_of(const ScoreArgs& a, int key) { return !a.window || key < a.sinks ? 0x80000000u : (uint32_t)a.window; }
 
+__device__ inline int2 row_of_any(const ScoreArgs& a, int v) {
+  const int j = (int)((uint32_t)v / (uint32_t)a.G);
+  return make_int2(j, v - j * a.G);
+}
+
 // A row's normaliser in log2 units; of one that sees nothing (-inf) so that its weights are 0.
 __device__ inline float norm_of(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }
 
@@ -152,7 +157,8 @@ template <int N> __device__ inline float logit(const v16f (&p)[N], int v) {
 // (8 KV heads of 128 channels, bf16, 277 MB): 64 us, 4.4 TB/s.  33 to 64 rows as two sets over one block, against the way of chunks (16 tokens of each of 16 requests over 4096): 49 and
 // 66 us, 9 tokens 43 and 66.
 template <int DT, int D> struct FewMemory { static constexpr int kBlock = 32 * Tile<DT, D>::ROWB, kBytes = 4 * kBlock; };
-template <int DT, int D, int SETS>
+// ANY: any number of rows, 32 at a time, of which every wave has normalisers and positions for itself.
+template <int DT, int D, int SETS, bool ANY>
 __device__ __forceinline__ void score_rows(const ScoreArgs& a, const Span& x, int hk, uint8_t* mem, float* norms, int* where) {
   using T = Tile<DT, D>;
   constexpr int BLK = FewMemory<DT, D>::kBlock, PG = 16 / T::RPI;
@@ -197,20 +203,27 @@ __device__ __forceinline__ void score_rows(const ScoreArgs& a, const Span& x, in
   // the rows, straight into operand registers; their normalisers
   const int rows = x.nq * a.G;
   u32x4 qf[SETS][T::NKC];
-#pragma unroll
-  for (int s = 0; s < SETS; ++s) {
-    const int2 me = row_of(a, 0, min(32 * s + r, rows - 1));       // (places behind the last row: that row once more, of no weight; zeros would make NaN of infinite keys)
+  const auto rows_from = [&](int row0, u32x4 (&to)[T::NKC]) {      // (places behind the last row: that row once more, of no weight; zeros would make NaN of infinite keys)
+    const int2 me = ANY ? row_of_any(a, min(row0 + r, rows - 1)) : row_of(a, 0, min(row0 + r, rows - 1));
     const uint8_t* qr = a.q + (int64_t)(hk * a.G + me.y) * a.q_sH + (int64_t)(x.qs + me.x) * a.q_sT + kh * 16;
 #pragma unroll
-    for (int kc = 0; kc < T::NKC; ++kc) qf[s][kc] = *reinterpret_cast<const u32x4*>(qr + kc * 32);
+    for (int kc = 0; kc < T::NKC; ++kc) to[kc] = *reinterpret_cast<const u32x4*>(qr + kc * 32);
+  };
+  const auto place = [&](int at, int row) {
+    const int2 me = ANY ? row_of_any(a, row) : row_of(a, 0, row);
+    norms[at] = row < rows ? norm_of(a.lse[(int64_t)(hk * a.G + me.y) * a.T + x.qs + me.x]) : INFINITY;
+    where[at] = row < rows ? x.kv - x.nq + me.x : -1;
+  };
+  if constexpr (ANY) {
+    norms += 32 * w;
+    where += 32 * w;
+  } else {
+#pragma unroll
+    for (int s = 0; s < SETS; ++s) rows_from(32 * s, qf[s]);
+    __syncthreads();                             // (the unit before is done with the normalisers)
+    if (tid < 32 * SETS) place(tid, tid);
+    __syncthreads();
   }
-  __syncthreads();                               // (the unit before is done with the normalisers)
-  if (tid < 32 * SETS) {
-    const int2 me = row_of(a, 0, tid);
-    norms[tid] = tid < rows ? norm_of(a.lse[(int64_t)(hk * a.G + me.y) * a.T + x.qs + me.x]) : INFINITY;
-    where[tid] = tid < rows ? x.kv - x.nq + me.x : -1;
-  }
-  __syncthreads();
   typedef __attribute__((address_space(3))) const uint8_t* lds_ptr;
   const uint32_t kaddr = lds + T::slot(r, kh);
   const int p0 = x.kv - x.nq, p1 = x.kv - 1;
@@ -227,20 +240,18 @@ __device__ __forceinline__ void score_rows(const ScoreArgs& a, const Span& x, in
     const float before = old;
     float sum = 0.f;
     v16f acc[SETS][SUMS] = {};
-    if (any) {
+    const auto multiply = [&] {
 #pragma unroll
       for (int kc = 0; kc < T::NKC; ++kc) {
         const u32x4 kf = *(__attribute__((address_space(3))) const u32x4*)(lds_ptr)(uintptr_t)(kaddr ^ (32 * kc));
 #pragma unroll
         for (int s = 0; s < SETS; ++s) mma_chunk<DT>(acc[s][kc % SUMS], qf[s][kc], kf);
       }
-    }
-    dma_reuse_fence();
-    if (b + 4 < blocks) issue(next);
-    if (any) {
+    };
+    const auto weigh = [&](int there) {
 #pragma unroll
       for (int v4 = 0; v4 < 4 * SETS; ++v4) {
-        if (8 * v4 >= rows) break;
+        if (8 * v4 >= there) break;
         const float4 nv = *reinterpret_cast<const float4*>(&norms[8 * v4 + 4 * kh]);
         const int4 pv = *reinterpret_cast<const int4*>(&where[8 * v4 + 4 * kh]);
 #pragma unroll
@@ -249,8 +260,29 @@ __device__ __forceinline__ void score_rows(const ScoreArgs& a, const Span& x, in
           sum += whole || (uint32_t)((&pv.x)[u] - key) < reach ? e : 0.f;
         }
       }
-      sum += __shfl_xor(sum, 32);
+    };
+    if constexpr (ANY) {
+      if (any)
+        for (int row0 = 0; row0 < rows; row0 += 32) {
+          rows_from(row0, qf[0]);
+          if (lane < 32) place(lane, row0 + lane);
+          wait_all_loads();
+          __builtin_amdgcn_wave_barrier();
+          multiply();
+          weigh(rows - row0);
+          __builtin_amdgcn_wave_barrier();
+#pragma unroll
+          for (int i = 0; i < SUMS; ++i) acc[0][i] = v16f{};
+        }
+      dma_reuse_fence();
+      if (b + 4 < blocks) issue(next);
+    } else {
+      if (any) multiply();
+      dma_reuse_fence();
+      if (b + 4 < blocks) issue(next);
+      if (any) weigh(rows);
     }
+    if (any) sum += __shfl_xor(sum, 32);
     if (put) *put = fmaf(before, a.decay, sum);
     key0 = next;
   }
@@ -557,16 +589,31 @@ __global__ __launch_bounds__(256, DT != ZC_F32 ? 2 : D == 64 ? 2 : 1) void k_pag
   Span x;
   for (int u = blockIdx.y; find_span(a, u, x); u += gridDim.y) {
     const int64_t rows = (int64_t)x.nq * a.G;
-    if (rows <= 32) score_rows<DT, D, 1>(a, x, blockIdx.x, mem, norms[0], where[0]);
-    else if (rows <= 64) score_rows<DT, D, 2>(a, x, blockIdx.x, mem, norms[0], where[0]);
+    if (rows <= 32) score_rows<DT, D, 1, false>(a, x, blockIdx.x, mem, norms[0], where[0]);
+    else if (rows <= 64) score_rows<DT, D, 2, false>(a, x, blockIdx.x, mem, norms[0], where[0]);
     else if (x.shift == 7) score_tiles<DT, D, 2>(a, x, blockIdx.x, mem, norms, where, sums);
     else score_tiles<DT, D, 1>(a, x, blockIdx.x, mem, norms, where, sums);
   }
 }
 
+// Steps of single tokens: without the way of chunks there are registers for twice as many workgroups, so twice as many keys on their way.
 template <int DT, int D>
-static int launch_scores(const ScoreArgs& a, int units, hipStream_t st) {
-  hipLaunchKernelGGL((k_paged_scores<DT, D>), dim3((unsigned)a.Hkv, (unsigned)units), dim3(256), 0, st, a);
+__global__ __launch_bounds__(256, DT != ZC_F32 ? 4 : D == 64 ? 3 : 2) void k_token_scores(ScoreArgs a) {
+  __shared__ __align__(1024) uint8_t mem[FewMemory<DT, D>::kBytes];
+  __shared__ __align__(16) float norms[128];
+  __shared__ __align__(16) int where[128];
+  Span x;
+  for (int u = blockIdx.y; find_span(a, u, x); u += gridDim.y) {
+    if ((int64_t)x.nq * a.G <= 32) score_rows<DT, D, 1, false>(a, x, blockIdx.x, mem, norms, where);
+    else score_rows<DT, D, 1, true>(a, x, blockIdx.x, mem, norms, where);
+    __syncthreads();
+  }
+}
+
+template <int DT, int D>
+static int launch_scores(const ScoreArgs& a, int units, bool tokens, hipStream_t st) {
+  if (tokens) hipLaunchKernelGGL((k_token_scores<DT, D>), dim3((unsigned)a.Hkv, (unsigned)units), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((k_paged_scores<DT, D>), dim3((unsigned)a.Hkv, (unsigned)units), dim3(256), 0, st, a);
   ZC_LAUNCH_CHECK();
   return ZC_OK;
 }
@@ -616,8 +663,9 @@ extern "C" int zc_paged_scores(const zc_tensor4* q, const zc_tensor4* k_pages, c
   // (a workgroup takes more units where there are; those that find none cost their places: where a table's room allows few tiles, as many as the chip holds)
   const int64_t all = tiles > 65535 / with ? 65535 : tiles * with, at_once = T * G <= 32 * R && all * Hkv <= 2560 ? ceil_div64(512, Hkv) : target;
   const int64_t units = at_once + with < all ? at_once + with : all;
+  const bool tokens = T * G <= 32 * R;
   hipStream_t st = (hipStream_t)stream;
-#define ZC_PS(DT) (q->D == 128 ? launch_scores<DT, 128>(a, (int)units, st) : launch_scores<DT, 64>(a, (int)units, st))
+#define ZC_PS(DT) (q->D == 128 ? launch_scores<DT, 128>(a, (int)units, tokens, st) : launch_scores<DT, 64>(a, (int)units, tokens, st))
   if (q->dtype == ZC_F32) rc = ZC_PS(ZC_F32);
   else if (q->dtype == ZC_F16) rc = ZC_PS(ZC_F16);
   else rc = ZC_PS(ZC_BF16);

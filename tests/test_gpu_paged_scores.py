@@ -95,6 +95,15 @@ def test_large_and_odd_groups(G, nq):
     Step([nq, 0, nq], [200, 10, 90], 2 * G, 2, 64, HF).run()
 
 
+@pytest.mark.parametrize("dtype,D,G", [(BF, 128, 4), (HF, 64, 3), (FL, 64, 1), (FL, 128, 5), (BF, 64, 33)])
+@pytest.mark.parametrize("window,sinks,decay", [(0, 0, 1.0), (50, 3, 0.5)])
+def test_chunks_among_single_tokens(dtype, D, G, window, sinks, decay):
+    """Steps of few rows a request on average, some of which have many."""
+    q = [1] * 20 + [40, 0, 9, 1, 70, 0, 1, 33] + [0, 1] * 40 + ([0] * 160 if G > 5 else [])
+    kv = [1 + (53 * i) % 400 for i in range(len(q))]
+    Step(q, [max(n, m) if m else n for n, m in zip(kv, q)], 2 * G, 2, D, dtype, pad=3, window=window, sinks=sinks, decay=decay).run()
+
+
 def test_rows_in_front_of_the_first_token_weigh_nothing():
     for nq, kv in ((5, 3), (90, 40), (50, 0)):
         Step([nq, 2], [kv, 30], 4, 2, 64, BF, pad=2).run()
