@@ -596,7 +596,7 @@ __global__ __launch_bounds__(256, DT != ZC_F32 ? 2 : D == 64 ? 2 : 1) void k_pag
   }
 }
 
-// Steps of single tokens, or few rows a request on average: without the way of chunks there are registers for twice as many workgroups, so twice as many keys on their way.  us with both ways in
+// Steps of single tokens: without the way of chunks there are registers for twice as many workgroups, so twice as many keys on their way.  us with both ways in
 // one kernel and so: 64 over 64 to 8192 65.6 and 60.0, 16 over 4096 36.7 and 33.6, 256 over 500 83.9 and 68.9; 8 heads of 64 channels, fp16, 40 over 4795 to 5806 69.8 and 55.2.
 template <int DT, int D>
 __global__ __launch_bounds__(256, DT != ZC_F32 ? 4 : D == 64 ? 3 : 2) void k_token_scores(ScoreArgs a) {
@@ -658,14 +658,16 @@ extern "C" int zc_paged_scores(const zc_tensor4* q, const zc_tensor4* k_pages, c
   a.lse = lse;
   a.scores = scores;
   a.over_G = G == 1 ? 0 : (uint32_t)(((1ull << 32) + G - 1) / G);
-  const bool tokens = T * G <= 32 * R;
+  // One token a request on average, of up to 32 heads each.  (Chunks among more tokens take their own way: us with all steps of up to 32 rows a request on average here, and so: 63 tokens
+  // and a chunk of 200 over 500 to 4000, 32 heads over 8 of 128 channels, bf16, 115 and 77, of 440 129 and 79; 16 requests of 8 tokens over 4096 35.0 and 39.5.)
+  const bool tokens = T <= R && G <= 32;
   // (us of single tokens at 1024 and 2048 units: bf16, 64 over 64 to 8192 60.0 and 59.7, 256 over 500 69 and 73; fp32, 16 over 2000 to 4000, whose products take longer than their keys, 69
   // and 57)
   const int64_t target = ceil_div64(tokens && q->dtype == ZC_F32 ? 2048 : 1024, Hkv), tiles = ceil_div64(room, T * G > 64 * R ? kScoreTile / 2 : kScoreTile), with = R < T ? R : T;
   a.target = (float)target;
   a.near_rows = q->sH >= 0 && q->sL >= 0 && G * a.q_sH + 16 * a.q_sT < 0xffffff00ll;
   // (a workgroup takes more units where there are; those that find none cost their places: where a table's room allows few tiles, as many as the chip holds)
-  const int64_t all = tiles > 65535 / with ? 65535 : tiles * with, at_once = tokens && all * Hkv <= 2560 ? ceil_div64(512, Hkv) : target;
+  const int64_t all = tiles > 65535 / with ? 65535 : tiles * with, at_once = T * G <= 32 * R && all * Hkv <= 2560 ? ceil_div64(512, Hkv) : target;
   const int64_t units = at_once + with < all ? at_once + with : all;
   hipStream_t st = (hipStream_t)stream;
 #define ZC_PS(DT) (q->D == 128 ? launch_scores<DT, 128>(a, (int)units, tokens, st) : launch_scores<DT, 64>(a, (int)units, tokens, st))

@@ -104,6 +104,15 @@ def test_chunks_among_single_tokens(dtype, D, G, window, sinks, decay):
     Step(q, [max(n, m) if m else n for n, m in zip(kv, q)], 2 * G, 2, D, dtype, pad=3, window=window, sinks=sinks, decay=decay).run()
 
 
+@pytest.mark.parametrize("dtype,D,G", [(BF, 128, 4), (HF, 64, 3), (FL, 64, 1), (FL, 128, 5), (BF, 64, 32), (HF, 128, 16)])
+@pytest.mark.parametrize("window,sinks,decay", [(0, 0, 1.0), (50, 3, 0.5)])
+def test_chunks_among_requests_without_tokens(dtype, D, G, window, sinks, decay):
+    """No more tokens than requests, but many of some."""
+    q = [1] * 20 + [40, 0, 9, 1, 70, 0, 1, 33] + [0] * 300
+    kv = [1 + (53 * i) % 400 for i in range(len(q))]
+    Step(q, [max(n, m) if m else n for n, m in zip(kv, q)], 2 * G, 2, D, dtype, pad=3, window=window, sinks=sinks, decay=decay).run()
+
+
 def test_rows_in_front_of_the_first_token_weigh_nothing():
     for nq, kv in ((5, 3), (90, 40), (50, 0)):
         Step([nq, 2], [kv, 30], 4, 2, 64, BF, pad=2).run()
