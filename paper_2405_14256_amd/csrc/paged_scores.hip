@@ -88,7 +88,7 @@ __device__ inline bool find_span(const ScoreArgs& a, int u, Span& x) {
     head = part(lane);
     all *= 2.f;
   }
-  // Work of a unit: as many units as the chip holds twice, where work is little as it holds once.  us at 512, 1024 and 2048 units: 64 tokens over 64 to 8192 (32 heads over 8 of 128
+  // Work of a unit: as many units as the chip holds twice, where work is little as it holds once.  us at 512, 1024 and 2048 units (single tokens in the kernel of chunks): 64 tokens over 64 to 8192 (32 heads over 8 of 128
   // channels, bf16) 74, 65 and 66, 16 over up to 1694 (8 heads of 64) 14.6, 17.2 and 23.3, 3 requests with 6 tokens over up to 3840 (12 of 64) 11.1, 14.7 and 14.7, 2048 tokens over
   // 16384 295, 295 and 298.
   const float share = all / a.target, per = fmaxf(share, fminf(2.f * share, 5.f));
