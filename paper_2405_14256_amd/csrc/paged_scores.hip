@@ -303,10 +303,14 @@ template <typename F> __device__ __forceinline__ void with(bool x, bool y, const
 template <int DT, int D> struct ManyMemory { static constexpr int kRows = DT == ZC_F32 ? 64 : 128, kTileB = kRows * Tile<DT, D>::ROWB, kBytes = 2 * kTileB; };
 constexpr int kMostRows = 128;
 template <int DT, int D, int KEYS>
-__device__ __forceinline__ void score_tiles(const ScoreArgs& a, const Span& x, int hk, uint8_t* mem, float (*norms)[kMostRows], int (*where)[kMostRows], float (*sums)[kScoreTile]) {
+__device__ __forceinline__ void score_tiles(const ScoreArgs& a, const Span& x, int hk, uint8_t* mem, float* norms, int* where, float (*sums)[kScoreTile]) {
   using T = Tile<DT, D>;
   constexpr int QT = ManyMemory<DT, D>::kRows, TILE_B = ManyMemory<DT, D>::kTileB, NI = QT / T::RPI / 4, PG = 16 / T::RPI;
   static_assert(2 * QT >= kScoreTile, "K passes through both row buffers");
+  // Places of a tile's normalisers.  A wave stores those of tile n + 1 in front of the barrier behind which all are done with tile n.  Of 16-bit types only its own are read until
+  // then, of fp32 those of tile n - 1 too (`pending`): with two places one wave could overwrite what another still reads.
+  constexpr int PLACES = 2 * kMostRows / QT;
+  static_assert(PLACES >= (DT == ZC_F32 ? 3 : 2) && (PLACES & (PLACES - 1)) == 0, "nobody reads what is overwritten");
   constexpr int SUMS = DT == ZC_F32 ? 4 : 1, TILE = 64 * KEYS;
   const int tid = (int)opaque(threadIdx.x), lane = tid & 63, r = lane & 31, kh = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6), rw = w >> 1, kw = w & 1;       // rows 32 rw on of 64, keys 32 KEYS kw on of the tile's
@@ -495,14 +499,17 @@ __device__ __forceinline__ void score_tiles(const ScoreArgs& a, const Span& x, i
     };
     __syncthreads();                             // (K is in registers)
     if (i_first < i_end) issue(i_first, j0, g0, 0);
-    int buf = 0;
+    int place = 0;                               // of the tile's normalisers; its rows are in buffer place & 1
     const int mine = 32 * rw + 4 * kh;           // of the tile's rows, the first that this lane's accumulators hold
     bool pending = false;                        // weights of keys 1 of the tile before, which all its rows see
-    for (uint32_t i0 = i_first; i0 < i_end; i0 += QT, buf ^= 1) {
+    for (uint32_t i0 = i_first; i0 < i_end; i0 += QT, place = (place + 1) & (PLACES - 1)) {
       const int2 next = row_of(a, j0, g0 + QT);
+      const int buf = place & 1;
+      float* const norms_of = norms + place * QT;
+      int* const where_of = where + place * QT;
       wait_vmem<0>();
       wait_all_loads();
-      if (tid < QT) { norms[buf][tid] = norm_of(norm); where[buf][tid] = pos; }
+      if (tid < QT) { norms_of[tid] = norm_of(norm); where_of[tid] = pos; }
       __syncthreads();                           // rows and normalisers are there, and nobody still reads the other buffer
       const bool fetch = DT != ZC_F32 && KEYS == 1 && even && i0 + QT < i_end && rows - (i0 + QT) >= QT;      // by the products below
       const uint32_t to_lds = lds + (buf ^ 1) * TILE_B + w * 1024;
@@ -520,12 +527,12 @@ __device__ __forceinline__ void score_tiles(const ScoreArgs& a, const Span& x, i
       const bool whole = key0 + TILE - 1 <= pa && (!a.window || key0 > pb - a.window || key0 + TILE - 1 < a.sinks);
       if constexpr (DT == ZC_F32 && KEYS == 1) {     // (the weights are little beside the products)
         step(std::false_type{}, 0, row, 1, nullptr);
-        if (whole) weigh_only(0, &norms[buf][mine]);
-        else masked(0, &norms[buf][mine], &where[buf][mine]);
+        if (whole) weigh_only(0, norms_of + mine);
+        else masked(0, norms_of + mine, where_of + mine);
       } else if constexpr (DT == ZC_F32) {
-        if (pending) step(std::true_type{}, 0, row, 1, &norms[buf ^ 1][mine]);
+        if (pending) step(std::true_type{}, 0, row, 1, norms + ((place - 1) & (PLACES - 1)) * QT + mine);
         else step(std::false_type{}, 0, row, 1, nullptr);
-        if (whole) step(std::true_type{}, 1, row, 0, &norms[buf][mine]);
+        if (whole) step(std::true_type{}, 1, row, 0, norms_of + mine);
         else step(std::false_type{}, 1, row, 0, nullptr);
       } else {
         const uint32_t first = opaque(row);
@@ -535,22 +542,22 @@ __device__ __forceinline__ void score_tiles(const ScoreArgs& a, const Span& x, i
           constexpr int h = decltype(of)::value;
           using K0 = std::integral_constant<int, 0>;
           using K1 = std::integral_constant<int, 1>;
-          const float* const of_these = &norms[buf][mine + 64 * h];
+          const float* const of_these = norms_of + mine + 64 * h;
           const uint32_t behind = row + 64 * (h + 1) * T::ROWB;
           if constexpr (KEYS == 1) {
             using KH = std::integral_constant<int, h & 1>;
             using MORE = std::bool_constant<h + 1 < QT / 64>;
             with(pending, h == 0 && fetch, [&](auto weigh, auto get) { flow(weigh, get, KH{}, MORE{}, behind, of_these, to_lds, from); });
             pending = whole;
-            if (!whole) masked(h & 1, of_these, &where[buf][mine + 64 * h]);
+            if (!whole) masked(h & 1, of_these, where_of + mine + 64 * h);
             return;
           }
           with(pending, h == 0 && fetch, [&](auto weigh, auto get) { flow(weigh, get, K0{}, std::false_type{}, 0, of_these, to_lds, from); });
           with(whole, false, [&](auto weigh, auto) { flow(weigh, std::false_type{}, K1{}, std::bool_constant<h + 1 < QT / 64>{}, behind, nullptr, 0, nullptr); });
           pending = whole;
           if (!whole) {
-            masked(0, &norms[buf][mine + 64 * h], &where[buf][mine + 64 * h]);
-            masked(1, &norms[buf][mine + 64 * h], &where[buf][mine + 64 * h]);
+            masked(0, norms_of + mine + 64 * h, where_of + mine + 64 * h);
+            masked(1, norms_of + mine + 64 * h, where_of + mine + 64 * h);
           }
         };
         half(std::integral_constant<int, 0>{});
@@ -560,14 +567,14 @@ __device__ __forceinline__ void score_tiles(const ScoreArgs& a, const Span& x, i
       if constexpr (DT == ZC_F32 && KEYS == 2) {
         pending = whole;
         if (!whole) {
-          masked(0, &norms[buf][mine], &where[buf][mine]);
-          masked(1, &norms[buf][mine], &where[buf][mine]);
+          masked(0, norms_of + mine, where_of + mine);
+          masked(1, norms_of + mine, where_of + mine);
         }
       }
       j0 = next.x;
       g0 = next.y;
     }
-    if (pending) weigh_only(1, &norms[buf ^ 1][mine + QT - 64]);
+    if (pending) weigh_only(1, norms + ((place - 1) & (PLACES - 1)) * QT + mine + QT - 64);
 #pragma unroll
     for (int n = 0; n < KEYS; ++n) {
       float all = KEYS == 2 ? sum[n] : sum[0] + sum[1];
@@ -583,14 +590,14 @@ template <int DT, int D>
 __global__ __launch_bounds__(256, DT != ZC_F32 ? 2 : D == 64 ? 2 : 1) void k_paged_scores(ScoreArgs a) {
   constexpr int kFew = FewMemory<DT, D>::kBytes, kMany = ManyMemory<DT, D>::kBytes;
   __shared__ __align__(1024) uint8_t mem[kFew > kMany ? kFew : kMany];
-  __shared__ __align__(16) float norms[2][kMostRows];
-  __shared__ __align__(16) int where[2][kMostRows];
+  __shared__ __align__(16) float norms[2 * kMostRows];
+  __shared__ __align__(16) int where[2 * kMostRows];
   __shared__ float sums[2][kScoreTile];
   Span x;
   for (int u = blockIdx.y; find_span(a, u, x); u += gridDim.y) {
     const int64_t rows = (int64_t)x.nq * a.G;
-    if (rows <= 32) score_rows<DT, D, 1, false>(a, x, blockIdx.x, mem, norms[0], where[0]);
-    else if (rows <= 64) score_rows<DT, D, 2, false>(a, x, blockIdx.x, mem, norms[0], where[0]);
+    if (rows <= 32) score_rows<DT, D, 1, false>(a, x, blockIdx.x, mem, norms, where);
+    else if (rows <= 64) score_rows<DT, D, 2, false>(a, x, blockIdx.x, mem, norms, where);
     else if (x.shift == 7) score_tiles<DT, D, 2>(a, x, blockIdx.x, mem, norms, where, sums);
     else score_tiles<DT, D, 1>(a, x, blockIdx.x, mem, norms, where, sums);
   }
