@@ -28,7 +28,7 @@ struct ScoreArgs {
   float scale_log2, decay;
   const float* lse;                             // [Hq, T]
   float* scores;                                // [page][head][row]
-  int near_rows;                                // 16 rows of whole tokens lie within 4 GB
+  int near_rows;                                // the rows of the four waves' transfers at a time lie within 4 GB
   float target;                                 // units a head's keys are split into, about
   uint32_t over_G;                              // ceil(2^32 / G)
 };
@@ -672,7 +672,8 @@ extern "C" int zc_paged_scores(const zc_tensor4* q, const zc_tensor4* k_pages, c
   // and 57)
   const int64_t target = ceil_div64(tokens && q->dtype == ZC_F32 ? 2048 : 1024, Hkv), tiles = ceil_div64(room, T * G > 64 * R ? kScoreTile / 2 : kScoreTile), with = R < T ? R : T;
   a.target = (float)target;
-  a.near_rows = q->sH >= 0 && q->sL >= 0 && G * a.q_sH + 16 * a.q_sT < 0xffffff00ll;
+  const int64_t hop = 4096 / (q->D * eb);            // rows of the four waves' transfers at a time, of as many tokens at most
+  a.near_rows = q->sH <= 0xffffffff && q->sL <= 0xffffffff && (G - 1) * a.q_sH + hop * a.q_sT < 0xffffff00ll;
   // (a workgroup takes more units where there are; those that find none cost their places: where a table's room allows few tiles, as many as the chip holds)
   const int64_t all = tiles > 65535 / with ? 65535 : tiles * with, at_once = T * G <= 32 * R && all * Hkv <= 2560 ? ceil_div64(512, Hkv) : target;
   const int64_t units = at_once + with < all ? at_once + with : all;
