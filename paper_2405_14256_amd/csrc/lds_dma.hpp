@@ -26,9 +26,10 @@ __device__ inline void gdma16(uint32_t lds_addr, const void* lane_src) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(lds_addr), "v"(lane_src) : "memory");
 }
 // ... with a base that all lanes share and an offset (without sign) of its own per lane.  The base may come from a vector register
-// (one that was spilled does): a memory instruction must not read such a scalar register for five wait states.
+// (one that was spilled does): a memory instruction must not read such a scalar register for five wait states, a scalar one waits by itself.
 __device__ inline void gdma16(uint32_t lds_addr, const void* base, uint32_t lane_off) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(lds_addr), "v"(lane_off), "s"(base) : "memory");
+  uint64_t copy;
+  asm volatile("s_mov_b32 m0, %1\n\ts_mov_b64 %0, %3\n\tglobal_load_lds_dwordx4 %2, %0" : "=&s"(copy) : "s"(lds_addr), "v"(lane_off), "s"(base) : "memory");
 }
 template <int N>
 __device__ inline void wait_vmem() { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory"); }
