@@ -440,9 +440,12 @@ int zc_paged_shared_attention(const zc_tensor4* q, const zc_tensor4* k_pages, co
  * at the token's place in the pages: scores is device float [N, Hkv, page], 16-byte aligned.  A step's new tokens start from 0,
  * whatever their places held, so nothing has to be cleared when a page is taken.  Other places are left as they are, a request's without new tokens too.
  * q, q_start, kv_len, window, sinks, sm_scale and the rows' positions as in zc_paged_attention, lse (device float [Hq, T]) as it returns
- * it, or zc_paged_shared_attention, whose softmax also went over a prefix.  A row of lse = -inf weighs nothing.  decay is 0 (what was there is not read) to 1.
- * fp32 tensors are multiplied on the fp32 matrix pipes; weights and sums are fp32.  Deterministic, and a token's score depends on its own
- * request's rows only.  A request's pages must be its own (not another's, not twice in its row); a token without a page has no score.
+ * it, or zc_paged_shared_attention, whose softmax also went over a prefix (whose own tokens gather nothing here: they are in no row of
+ * block_table).  A row of lse = -inf weighs nothing (if its logits are below infinity).  decay is 0 (what was there is not read) to 1: without one, tokens that more
+ * rows saw have gathered more.  fp32 tensors are multiplied on the fp32 matrix pipes; weights and sums are fp32.  A token's score is
+ * of its own request's rows only.  Deterministic for equal lengths and shapes; its last bits may depend on the step's other requests, R and
+ * T, by which the work is divided, so of nearly equal scores another batch may rank others first.  A request's pages must be
+ * its own (not another's, not twice in its row); a token without a page has no score.
  * T and R may be 0.  Needs no workspace.  R < 2^24, T * Hq < 2^31, Hq / Hkv <= 4096. */
 int zc_paged_scores(const zc_tensor4* q, const zc_tensor4* k_pages, const int32_t* block_table, int64_t row_stride, int64_t max_blocks,
                     const int32_t* q_start, const int32_t* kv_len, int64_t R, int32_t window, int32_t sinks, float sm_scale,
@@ -456,7 +459,7 @@ int zc_paged_scores(const zc_tensor4* q, const zc_tensor4* k_pages, const int32_
  * place in the pages; of NaN any may stay.  With `together` (not 0) all heads keep the same tokens, by the sum of their scores
  * (of 64 bits, rounded once).
  * What stays moves, in its order, to the first places of the request's pages: keys, values and scores; what lies behind it is left as it
- * was.  new_len (device int32 [R], no memory of kv_len or keep) receives the numbers, kept (device int32 [R, Hkv, most], [R, 1, most]
+ * was.  A place is not the token's position any more: windows and sinks of later calls count what is left.  new_len (device int32 [R], no memory of kv_len or keep) receives the numbers, kept (device int32 [R, Hkv, most], [R, 1, most]
  * with `together`) the places that the tokens had, ascending; entries behind them are left as they were.
  * Pages that a request then does not need, entries ceil(new_len / page) to ceil(kv_len / page) - 1 of its row, are written to free_pages
  * (device int32 [n_list]) from *n_free on (device int32), request after request, what passes the list's end left out; *n_freed

@@ -1,11 +1,11 @@
 // zc_paged_evict: of every request the tokens that gathered the most weight, the newest and the first ones stay, and move to the
 // front of the request's pages.
 //
-// Two launches (three where all heads take one choice, one for short lists): who stays, as an ascending list for each request and head, with the
-// lengths and the pages that are left; then the rows, in place.  A token that stays never moves back: the i-th of the list lies at
-// list[i] >= i.  So a workgroup that takes some channels of a (request, head) for itself may go through the list from its start, reading
-// as far ahead as it likes, and needs no copy and no other workgroup: the place i that it fills was read by then, as the
-// token there, if it stays, is the i-th of the list or one before.
+// Two launches (three where all heads take one choice, one for short lists): who stays, as an ascending list for each request
+// and head, with the lengths and the pages that are left; then the rows, in place.  A token that stays never moves back: the
+// i-th of the list lies at list[i] >= i.  So a workgroup that takes some channels of a (request, head) for itself may go
+// through the list from its start, reading as far ahead as it likes, and needs no copy and no other workgroup: the place i
+// that it fills was read by then, as the token there, if it stays, is the i-th of the list or one before.
 #include <limits.h>
 
 #include "lds_dma.hpp"
@@ -115,8 +115,9 @@ struct PickMemory {
   int digit[3], above[3], count[3], moved;
 };
 
-// The list of a request and head, in memory and for `also`; the first place of it whose token lies elsewhere, `stay` at most.  HELD: chunks of kEach tokens a thread that it
-// holds; scores behind them are read again in every sweep.  id: the pages of those it holds.
+// The list of a request and head, in memory and for `also`; the first place of it whose token lies elsewhere, `stay` at most.
+// HELD: chunks of kEach tokens a thread that it holds; scores behind them are read again in every sweep.  id: the pages of
+// those it holds.
 template <int THREADS, int HELD, typename F>
 __device__ __forceinline__ int pick(const EvictArgs& a, int r, int h, int kv, int stay, const int (&id)[HELD], PickMemory<THREADS>& s, F&& also) {
   constexpr int NW = THREADS / 64, CHUNK = THREADS * kEach, PER = kBins / THREADS;
@@ -269,9 +270,11 @@ __device__ inline int slot_at(const EvictArgs& a, int r, int i) {
   return (uint32_t)id < (uint32_t)a.n_pages ? id << a.shift | (i & ((1 << a.shift) - 1)) : -1;
 }
 
-// A workgroup takes `slice` bytes of every row of a (request, head, tensor), a row's by consecutive threads, kMove rows a thread at a time:
-// all of them are read before the first is stored.  Where the next ones lie is looked up meanwhile.  Bound by memory where lists are many (16 requests,
-// 1638 of 4096, 40 heads of 128 channels 131 us, 5.1 TB/s; 32 ragged ones of 8 heads 67 us, 3.8 TB/s), by a step's trips where they are few (one such request of 8 heads 9.2).
+// A workgroup takes `slice` bytes of every row of a (request, head, tensor), a row's by consecutive threads, kMove rows a
+// thread at a time: all of them are read before the first is stored.  Where the next ones lie is looked up meanwhile.  Bound
+// by memory where lists are many (16 requests, 1024 of up to 4096, 40 heads of 128 channels 131 us, 5.1 TB/s; 32 ragged ones
+// of 8 heads, fewer than half as many workgroups, 67 us, 3.8 TB/s: a step waits for its rows and for the stores of the step
+// before, and nothing is on its way meanwhile), by a step's trips where they are few (one such request of 8 heads 9.2).
 constexpr int kMove = 4;
 struct Move { int src, dst; };                           // slots (src < 0: zeros, dst < 0: nothing to do)
 
@@ -349,9 +352,10 @@ __global__ __launch_bounds__(THREADS, 4) void k_evict_move(EvictArgs a) {
 }
 
 // ---- short lists: who stays and their rows in one launch ---------------------------------------------
-// A list whose rows a workgroup takes in one step: it moves what it has chosen.  All rows are read before the first is stored.  Bound by latency.  us of two launches and
-// this one: 16 requests of 30 to 250, 64 stay (8 heads of 128 channels, bf16) 15.0 and 12.3, 64 of 100 to 900, 200 stay 30.0 and 23.8, 37 of 20, 10 stay (40 heads) 21.4 and 14.7,
-// 64 of 600 to 3000, 500 stay (64 channels) 48.6 and 37.5, 64 of 3000 to 8192, 128 stay 43.9 and 38.0.
+// A list whose rows a workgroup takes in one step: it moves what it has chosen.  All rows are read before the first is
+// stored.  Bound by latency.  us of two launches and this one: 16 requests of 30 to 250, 64 stay (8 heads of 128 channels,
+// bf16) 15.0 and 12.3, 64 of 100 to 900, 200 stay 30.0 and 23.8, 37 of 20, 10 stay (40 heads) 21.4 and 14.7, 64 of 600 to
+// 3000, 500 stay (64 channels) 48.6 and 37.5, 64 of 3000 to 8192, 128 stay 43.9 and 38.0.
 template <int THREADS, int HELD>
 __global__ __launch_bounds__(THREADS) void k_evict_short(EvictArgs a) {
   __shared__ __align__(16) PickMemory<THREADS> s;
@@ -474,8 +478,9 @@ extern "C" int zc_paged_evict(const zc_tensor4* k_pages, const zc_tensor4* v_pag
     ZC_LAUNCH_CHECK();
     return ZC_OK;
   }
-  // Threads for four tokens each; short lists in workgroups of 256, of which a CU holds more.  us of 512 and 256 threads (and 1024 and 256 below): 37 requests of 20 tokens, 40 heads
-  // of 128 channels, 39 and 21; 128 of up to 250, 8 heads, 33 and 24; one of up to 900 14.2 and 14.5 (in two launches).
+  // Threads for four tokens each; short lists in workgroups of 256, of which a CU holds more.  us with 512 threads here and
+  // 1024 in the move, and with 256 in both (lists that k_evict_short takes now): 37 requests of 20 tokens, 40 heads of 128
+  // channels, 39 and 21; 128 of up to 250, 8 heads, 33 and 24; one of up to 900 14.2 and 14.5.
   if (a.cap <= 256 * kEach) hipLaunchKernelGGL((k_evict_pick<256, 1>), lists, dim3(256), 0, st, a);
   else if (a.cap <= 512 * kEach) hipLaunchKernelGGL((k_evict_pick<512, 1>), lists, dim3(512), 0, st, a);
   else if (a.cap <= 1024 * kEach) hipLaunchKernelGGL((k_evict_pick<1024, 1>), lists, dim3(1024), 0, st, a);
@@ -484,14 +489,15 @@ extern "C" int zc_paged_evict(const zc_tensor4* k_pages, const zc_tensor4* v_pag
   else hipLaunchKernelGGL((k_evict_pick<1024, 8>), lists, dim3(1024), 0, st, a);
   ZC_LAUNCH_CHECK();
   const int64_t chains = R * H * 2;
-  // Rows are cut where that fills the chip and saves steps of the way through the list.  us of whole rows, of 128, 64 and 16 bytes, 8 heads, 256 bytes
-  // a row: one request of 4096, 1638 stay 39.0, 26.0, 20.2 and 18.6; of 131072, 32768 stay (64 and 16) 286 and 286; 4 of up to 400, 256 stay 15.7 and 15.7 (20.2 of 32);
-  // 15 of up to 8192, 2048 stay 79 whole, 81 of 128.
+  // Rows are cut where that fills the chip and saves steps of the way through the list.  us of whole rows, of 128, 64 and 16
+  // bytes, 8 heads, 256 bytes a row: one request of 4096, 1638 stay 39.0, 26.0, 20.2 and 18.6; of 131072, 32768 stay (64 and
+  // 16) 286 and 286; 4 of up to 400, 256 stay 15.7 and 15.7 (20.2 of 32); 15 of up to 8192, 2048 stay 79 whole, 81 of 128.
   a.slice = a.rowb;
   while (a.slice > 16 && chains * (a.rowb / a.slice) < 256 && most > kMove * 1024 * 16 / a.slice) a.slice /= 2;
   a.lanes = __builtin_ctz(a.slice / 16);
-  // (one step is all that short lists take: a workgroup of a quarter of the threads does.  64 of up to 900 tokens, 64 stay 26.2 and 20.5, 16 of up to 250 15.0 and 15.2)
-  // (parts of a row beside each other in one L2: with the parts of a head as the fastest index the request of 131072 takes 299 us of 32 bytes, 388 of 16)
+  // (one step is all that short lists take: a workgroup of a quarter of the threads does.  64 of up to 900 tokens, 64 stay
+  // 26.2 and 20.5, 16 of up to 250 15.0 and 15.2) (parts of a row beside each other in one L2: with the parts of a head as the
+  // fastest index the request of 131072 takes 299 us of 32 bytes, 388 of 16)
   const dim3 grid((unsigned)(3 * H), (unsigned)(a.rowb / a.slice), (unsigned)R);
   if (most <= kMove * 256 * 16 / a.slice) hipLaunchKernelGGL(k_evict_move<256>, grid, dim3(256), 0, st, a);
   else hipLaunchKernelGGL(k_evict_move<1024>, grid, dim3(1024), 0, st, a);

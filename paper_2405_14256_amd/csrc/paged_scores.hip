@@ -6,8 +6,8 @@
 // puts a key in a lane (column lane & 31) and its rows in the accumulators: the sum over rows is lane-local.  No result is split
 // over workgroups, so there are no partial sums, and the order of every sum is fixed.  Logits, weights and sums are fp32.
 //
-// A unit of work is a range of a request's key tiles.  As for the paged attention the host knows neither lengths nor how rows are spread over
-// requests: every wave finds its unit from the lengths.
+// A unit of work is a range of a request's key tiles.  As for the paged attention the host knows neither lengths nor how rows
+// are spread over requests: every wave finds its unit from the lengths.
 #include <limits.h>
 
 #include <type_traits>
@@ -33,11 +33,13 @@ struct ScoreArgs {
   uint32_t over_G;                              // ceil(2^32 / G)
 };
 
-// A request's keys go in tiles of 128, or 64 where those are few: of up to 64 rows a wave takes every fourth 32 keys, of more the four waves share a tile.
+// A request's keys go in tiles of 128, or 64 where those are few: of up to 64 rows a wave takes every fourth 32 keys, of more
+// the four waves share a tile.
 constexpr int kScoreTile = 128;
-// Tiles of chunks and heads below which they are halved: more workgroups, which all take every row.  us of 128 and 64 keys a tile (32 heads over 8 of 128 channels, bf16): a prompt of
-// 2048 103 and 72, four of 500 42 and 28, 500 tokens over 4096 (256 tiles) 44 and 35, 1000 that see 4096 each (328) 98 and 77, 300 over 6000 (376) 37 and 46, 500 over 8192 (512) 53
-// and 69; fp32, 500 over 4096 (16 heads over 4) 190 and 115.
+// Tiles of chunks and heads below which they are halved: more workgroups, which all take every row.  us of 128 and 64 keys a
+// tile (32 heads over 8 of 128 channels, bf16): a prompt of 2048 103 and 72, four of 500 42 and 28, 500 tokens over 4096 (256
+// tiles) 44 and 35, 1000 that see 4096 each (328) 98 and 77, 300 over 6000 (376) 37 and 46, 500 over 8192 (512) 53 and 69;
+// fp32, 500 over 4096 (16 heads over 4) 190 and 115.
 constexpr float kFewTiles = 340.f;
 
 struct Span {
@@ -88,9 +90,10 @@ __device__ inline bool find_span(const ScoreArgs& a, int u, Span& x) {
     head = part(lane);
     all *= 2.f;
   }
-  // Work of a unit: as many units as the chip holds twice, where work is little as it holds once.  us at 512, 1024 and 2048 units (single tokens in the kernel of chunks): 64 tokens over 64 to 8192 (32 heads over 8 of 128
-  // channels, bf16) 74, 65 and 66, 16 over up to 1694 (8 heads of 64) 14.6, 17.2 and 23.3, 3 requests with 6 tokens over up to 3840 (12 of 64) 11.1, 14.7 and 14.7, 2048 tokens over
-  // 16384 295, 295 and 298.
+  // Work of a unit: as many units as the chip holds twice, where work is little as it holds once.  us at 512, 1024 and 2048
+  // units (single tokens in the kernel of chunks): 64 tokens over 64 to 8192 (32 heads over 8 of 128 channels, bf16) 74, 65
+  // and 66, 16 over up to 1694 (8 heads of 64) 14.6, 17.2 and 23.3, 3 requests with 6 tokens over up to 3840 (12 of 64) 11.1,
+  // 14.7 and 14.7, 2048 tokens over 16384 295, 295 and 298.
   const float share = all / a.target, per = fmaxf(share, fminf(2.f * share, 5.f));
   int units = 0;
   for (int r0 = 0; r0 < a.R; r0 += 64) {
@@ -104,8 +107,9 @@ __device__ inline bool find_span(const ScoreArgs& a, int u, Span& x) {
       const auto of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
       const int n = of(parts), tiles = of(p.tiles), half = (int)(0.25f * a.target);
       int b = u - (units + of(cu) - n);
-      // (a chunk's first keys are seen by most rows: where all units run at once, the second on a CU is one of the last; a window evens that out by itself.  us of units in order and
-      // so, bf16, 32 heads over 8 of 128 channels: a prompt of 4096 161 and 154, 2048 over 32768 that see 4096 each 114 and 139)
+      // (a chunk's first keys are seen by most rows: where all units run at once, the second on a CU is one of the last; a
+      // window evens that out by itself.  us of units in order and so, bf16, 32 heads over 8 of 128 channels: a prompt of 4096
+      // 161 and 154, 2048 over 32768 that see 4096 each 114 and 139)
       if (!a.window && n > half && n <= 2 * half && b >= half) b = n - 1 - (b - half);
       x.r = r0 + l;
       x.qs = of(p.qs); x.nq = of(p.nq); x.kv = of(p.kv);
@@ -146,16 +150,18 @@ __device__ inline float* score_at(const ScoreArgs& a, const Span& x, int hk, int
   return (uint32_t)id < (uint32_t)a.n_pages ? a.scores + (((int64_t)id * a.Hkv + hk) << a.shift) + (key & ((1 << a.shift) - 1)) : nullptr;
 }
 
-// Accumulator v of a 32 x 32 product that was summed in N (of fp32, four: the roundings of one chain of D products are most of a logit's error).
+// Accumulator v of a 32 x 32 product that was summed in N (of fp32, four: the roundings of one chain of D products are most of
+// a logit's error).
 template <int N> __device__ inline float logit(const v16f (&p)[N], int v) {
   if constexpr (N == 4) return (p[0][v] + p[1][v]) + (p[2][v] + p[3][v]);
   else return p[0][v];
 }
 
 // ---- up to 64 rows: single tokens ------------------------------------------------------------------
-// Bound by memory.  A wave has a place for one K block in LDS; the next is requested when it has been multiplied, and the rows' operands stay in registers.  64 tokens over 64 to 8192
-// (8 KV heads of 128 channels, bf16, 274 MB): 57 us, 4.8 TB/s.  33 to 64 rows as two sets over one block, against the way of chunks (16 tokens of each of 16 requests over 4096): 49 and
-// 66 us, 9 tokens 43 and 66.
+// Bound by memory.  A wave has a place for one K block in LDS; the next is requested when it has been multiplied, and the
+// rows' operands stay in registers.  64 tokens over 64 to 8192 (8 KV heads of 128 channels, bf16, 274 MB): 57 us, 4.8 TB/s.
+// 33 to 64 rows as two sets over one block, against the way of chunks (16 tokens of each of 16 requests over 4096): 49 and 66
+// us, 9 tokens 43 and 66.
 template <int DT, int D> struct FewMemory { static constexpr int kBlock = 32 * Tile<DT, D>::ROWB, kBytes = 4 * kBlock; };
 // ANY: any number of rows, 32 at a time, of which every wave has normalisers and positions for itself.
 template <int DT, int D, int SETS, bool ANY>
@@ -301,8 +307,9 @@ template <typename F> __device__ __forceinline__ void with(bool x, bool y, const
 }
 
 // ---- more rows: chunks -----------------------------------------------------------------------------
-// The waves take half of a tile's keys and 32 of every 64 rows each: K operands stay in registers, rows stream through LDS, 128 (fp32 64) at a time, one tile ahead.  Bound by the matrix
-// pipe and the exponentials beside it, which are issued between the products of the next 32 keys (16-bit types) or of the other half: 2048 tokens over 16384 (32 heads over 8 of 128
+// The waves take half of a tile's keys and 32 of every 64 rows each: K operands stay in registers, rows stream through LDS,
+// 128 (fp32 64) at a time, one tile ahead.  Bound by the matrix pipe and the exponentials beside it, which are issued between
+// the products of the next 32 keys (16-bit types) or of the other half: 2048 tokens over 16384 (32 heads over 8 of 128
 // channels, bf16) 294 us, 870 TFLOP/s of logits that are seen.  256 VGPRs allow two workgroups a CU; three spill.
 template <int DT, int D> struct ManyMemory { static constexpr int kRows = DT == ZC_F32 ? 64 : 128, kTileB = kRows * Tile<DT, D>::ROWB, kBytes = 2 * kTileB; };
 constexpr int kMostRows = 128;
@@ -311,8 +318,9 @@ __device__ __forceinline__ void score_tiles(const ScoreArgs& a, const Span& x, i
   using T = Tile<DT, D>;
   constexpr int QT = ManyMemory<DT, D>::kRows, TILE_B = ManyMemory<DT, D>::kTileB, NI = QT / T::RPI / 4, PG = 16 / T::RPI;
   static_assert(2 * QT >= kScoreTile, "K passes through both row buffers");
-  // Places of a tile's normalisers.  A wave stores those of tile n + 1 in front of the barrier behind which all are done with tile n.  Of 16-bit types only its own are read until
-  // then, of fp32 those of tile n - 1 too (`pending`): with two places one wave could overwrite what another still reads.
+  // Places of a tile's normalisers.  A wave stores those of tile n + 1 in front of the barrier behind which all are done with
+  // tile n.  Of 16-bit types only its own are read until then, of fp32 those of tile n - 1 too (`pending`): with two places
+  // one wave could overwrite what another still reads.
   constexpr int PLACES = 2 * kMostRows / QT;
   static_assert(PLACES >= (DT == ZC_F32 ? 3 : 2) && (PLACES & (PLACES - 1)) == 0, "nobody reads what is overwritten");
   constexpr int SUMS = DT == ZC_F32 ? 4 : 1, TILE = 64 * KEYS;
@@ -365,8 +373,8 @@ __device__ __forceinline__ void score_tiles(const ScoreArgs& a, const Span& x, i
     if (a.window && key0 >= a.sinks) j_end = (int)min((int64_t)x.nq, (int64_t)key1 + a.window - past);
     const uint32_t i_first = (uint32_t)j_first * a.G / QT * QT, i_end = (uint32_t)max(j_end, 0) * a.G;
     int j0 = (int)(i_first / (uint32_t)a.G), g0 = (int)(i_first - (uint32_t)j0 * a.G);     // token and head of the tile's first row
-    // Rows to LDS, and this thread's normaliser to a register.  Where 16 rows are whole tokens all tiles but one that is not full lie alike: a
-    // base that advances, and one offset a lane.
+    // Rows to LDS, and this thread's normaliser to a register.  Where 16 rows are whole tokens all tiles but one that is not
+    // full lie alike: a base that advances, and one offset a lane.
     constexpr bool SAME = 4 * T::RPI % 16 == 0;  // (the swizzle repeats from one of a wave's transfers to the next)
     const bool even = SAME && 16 % a.G == 0 && a.near_rows;
     uint32_t off = 0;
@@ -407,9 +415,10 @@ __device__ __forceinline__ void score_tiles(const ScoreArgs& a, const Span& x, i
         pos = there ? past + me.x : -1;
       }
     };
-    // Two products are under way, of both halves of a wave's 64 keys with the same 32 rows or of its 32 keys with one 32 rows after the other.
-    // (sum: of a tile of rows, of 16-bit types of two; total: of those before.  One chain over all rows would round as often as there are rows: constant weights of 7500 to 10000 rows were off by
-    // 120 to 410 steps of 2^-24.  us without and with totals, bf16: 2048 tokens over 16384 272.6 and 274.4, a prompt of 2048 64.4 and 65.7.)
+    // Two products are under way, of both halves of a wave's 64 keys with the same 32 rows or of its 32 keys with one 32 rows
+    // after the other. (sum: of a tile of rows, of 16-bit types of two; total: of those before.  One chain over all rows would
+    // round as often as there are rows: constant weights of 7500 to 10000 rows were off by 120 to 410 steps of 2^-24.  us
+    // without and with totals, bf16: 2048 tokens over 16384 272.6 and 274.4, a prompt of 2048 64.4 and 65.7.)
     float sum[2] = {0.f, 0.f}, total[2] = {0.f, 0.f};
     v16f acc[2][SUMS];
     // Weights of product n's 32 rows and its keys, which not all rows see.
@@ -453,12 +462,13 @@ __device__ __forceinline__ void score_tiles(const ScoreArgs& a, const Span& x, i
         __builtin_amdgcn_sched_barrier(0);
       }
     };
-    // As above of 16-bit types with the rows' operands `q` in registers, and their normalisers `nv` of the weights: what a step has used is replaced by
-    // what the step after the next (q) or the next (nv) needs, so that no step waits for LDS.
+    // As above of 16-bit types with the rows' operands `q` in registers, and their normalisers `nv` of the weights: what a
+    // step has used is replaced by what the step after the next (q) or the next (nv) needs, so that no step waits for LDS.
     u32x4 q[DT == ZC_F32 ? 1 : T::NKC];
     float4 nv[4];
-    // FETCH: the next tile's transfers, one a step: all at once a wave waits until the last has been taken.  That is where one workgroup has a CU for itself (a prompt of 2048 77 -> 71 us;
-    // two hide it from each other, 2048 tokens over 16384 305 and 305).
+    // FETCH: the next tile's transfers, one a step: all at once a wave waits until the last has been taken.  That is where one
+    // workgroup has a CU for itself (a prompt of 2048 77 -> 71 us; two hide it from each other, 2048 tokens over 16384 305 and
+    // 305).
     const auto flow = [&](auto weigh, auto fetch, auto keys, auto refill, uint32_t next_row, const float* next_norm, uint32_t to_lds, const uint8_t* from) {
       constexpr bool WEIGH = decltype(weigh)::value, FETCH = decltype(fetch)::value, REFILL = decltype(refill)::value;
       static_assert(DT == ZC_F32 || NI == T::NKC, "a transfer a step");
@@ -615,8 +625,9 @@ __global__ __launch_bounds__(256, DT != ZC_F32 ? 2 : D == 64 ? 2 : 1) void k_pag
   }
 }
 
-// Steps of single tokens: without the way of chunks there are registers for twice as many workgroups, so twice as many keys on their way.  us with both ways in
-// one kernel and so: 64 over 64 to 8192 65.6 and 60.0, 16 over 4096 36.7 and 33.6, 256 over 500 83.9 and 68.9; 8 heads of 64 channels, fp16, 40 over 4795 to 5806 69.8 and 55.2.
+// Steps of single tokens: without the way of chunks there are registers for twice as many workgroups, so twice as many keys on
+// their way.  us with both ways in one kernel and so: 64 over 64 to 8192 65.6 and 60.0, 16 over 4096 36.7 and 33.6, 256 over
+// 500 83.9 and 68.9; 8 heads of 64 channels, fp16, 40 over 4795 to 5806 69.8 and 55.2.
 template <int DT, int D>
 __global__ __launch_bounds__(256, DT != ZC_F32 ? 4 : D == 64 ? 3 : 2) void k_token_scores(ScoreArgs a) {
   __shared__ __align__(1024) uint8_t mem[FewMemory<DT, D>::kBytes];
@@ -677,16 +688,22 @@ extern "C" int zc_paged_scores(const zc_tensor4* q, const zc_tensor4* k_pages, c
   a.lse = lse;
   a.scores = scores;
   a.over_G = G == 1 ? 0 : (uint32_t)(((1ull << 32) + G - 1) / G);
-  // One token a request on average, of up to 32 heads each.  (Chunks among more tokens take their own way: us with all steps of up to 32 rows a request on average here, and so: 63 tokens
-  // and a chunk of 200 over 500 to 4000, 32 heads over 8 of 128 channels, bf16, 115 and 77, of 440 129 and 79; 16 requests of 8 tokens over 4096 35.0 and 39.5.)
+  // One token a request on average, of up to 32 heads each.  (Chunks among more tokens take their own way: us with all steps
+  // of up to 32 rows a request on average here, and so: 63 tokens and a chunk of 200 over 500 to 4000, 32 heads over 8 of 128
+  // channels, bf16, 115 and 77, of 440 129 and 79; 16 requests of 8 tokens over 4096 35.0 and 39.5.) T and R are all that the
+  // host knows, so the rule is wrong on either side: rows behind the last request's take single tokens to the kernel of chunks
+  // (64 of them 65.6 instead of 60.0, 256 over 500 84 instead of 69), requests without tokens a chunk to this one (us there
+  // and here, as many such requests as just keep it there and 66 more: 440 tokens over 4096 77 and 102, 100 tokens 26 and 31,
+  // 16 tokens 13 and 14, 2000 over themselves 634 and 612; fp32, 440 190 and 208).
   const bool tokens = T <= R && G <= 32;
-  // (us of single tokens at 1024 and 2048 units: bf16, 64 over 64 to 8192 60.0 and 59.7, 256 over 500 69 and 73; fp32, 16 over 2000 to 4000, whose products take longer than their keys, 69
-  // and 57)
+  // (us of single tokens at 1024 and 2048 units: bf16, 64 over 64 to 8192 60.0 and 59.7, 256 over 500 69 and 73; fp32, 16 over
+  // 2000 to 4000, whose products take longer than their keys, 69 and 57)
   const int64_t target = ceil_div64(tokens && q->dtype == ZC_F32 ? 2048 : 1024, Hkv), tiles = ceil_div64(room, T * G > 64 * R ? kScoreTile / 2 : kScoreTile), with = R < T ? R : T;
   a.target = (float)target;
   const int64_t hop = 4096 / (q->D * eb);            // rows of the four waves' transfers at a time, of as many tokens at most
   a.near_rows = q->sH <= 0xffffffff && q->sL <= 0xffffffff && (G - 1) * a.q_sH + hop * a.q_sT < 0xffffff00ll;
-  // (a workgroup takes more units where there are; those that find none cost their places: where a table's room allows few tiles, as many as the chip holds)
+  // (a workgroup takes more units where there are; those that find none cost their places: where a table's room allows few
+  // tiles, as many as the chip holds)
   const int64_t all = tiles > 65535 / with ? 65535 : tiles * with, at_once = T * G <= 32 * R && all * Hkv <= 2560 ? ceil_div64(512, Hkv) : target;
   const int64_t units = at_once + with < all ? at_once + with : all;
   hipStream_t st = (hipStream_t)stream;

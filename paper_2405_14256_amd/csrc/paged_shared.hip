@@ -1,17 +1,18 @@
 // zc_paged_shared_attention: attention of a step's new tokens where groups of requests share a prefix, which lies in pages of its own.
 //
-// Rows (token, query head of the group) of requests that share a prefix see the same keys, so they go through it together, in blocks of 32 or 128
-// rows of many requests, each key read and multiplied once for all of them; every request's own keys follow, and a row's parts are joined
-// in fp32:
+// Rows (token, query head of the group) of requests that share a prefix see the same keys, so they go through it together, in
+// blocks of 32 or 128 rows of many requests, each key read and multiplied once for all of them; every request's own keys
+// follow, and a row's parts are joined in fp32:
 //   m = max(m_p, m_o),  l = l_p e^(m_p - m) + l_o e^(m_o - m),  o = (o_p e^(m_p - m) + o_o e^(m_o - m)) / l
 // A request with more than 64 rows fills blocks of its own: these take the prefix and then its own keys without a join.
 //
-// Lengths and groups are known to the GPU only.  What every unit of work is - a block of rows, a range of tiles of the prefix, one of the
-// request's own - how far long ranges are split, and what is to be joined follows from sums over requests and groups, which every workgroup computes for itself, or where
-// there are many one workgroup in front (k_shared_plan).
+// Lengths and groups are known to the GPU only.  What every unit of work is - a block of rows, a range of tiles of the prefix,
+// one of the request's own - how far long ranges are split, and what is to be joined follows from sums over requests and
+// groups, which every workgroup computes for itself, or where there are many one workgroup in front (k_shared_plan).
 //
-// Bound by memory where rows are few: 64 tokens with 64 to 1024 of their own after 8192 (32 heads over 8 of 128 channels, bf16, 135 MB) 43 us and the join 7 with cold caches, 3.1 TB/s; one
-// after 131072 106 us, 5.1 TB/s; by the matrix cores where they are many: 4 chunks of 512 after 32768 1145 us, 970 TFLOP/s.
+// Bound by memory where rows are few: 64 tokens with 64 to 1024 of their own after 8192 (32 heads over 8 of 128 channels,
+// bf16, 135 MB) 43 us and the join 7 with cold caches, 3.1 TB/s; one after 131072 106 us, 5.1 TB/s; by the matrix cores where
+// they are many: 4 chunks of 512 after 32768 1145 us, 970 TFLOP/s.
 #include "paged_attention_kernel.hpp"
 
 namespace zc {
@@ -38,8 +39,9 @@ struct SharedArgs : PagedArgs {
 // What a unit of the plan is, in words of its entry.
 enum Word { kFew, kGroup, kRequest, kPart, kRow0, kPast, kOwnKeys, kPrefixKeys, kToken, kHead, kRows, kLast, kFrom, kTo, kWords = 16 };
 
-// A unit's keys are one stream of tiles, those of the prefix in front: its keys have negative positions, -kTile * pre_tiles on, so that the last
-// of its tiles, which need not be full, ends in front of the request's own first key.  The places between, from `hole` to -1, are hidden.
+// A unit's keys are one stream of tiles, those of the prefix in front: its keys have negative positions, -kTile * pre_tiles
+// on, so that the last of its tiles, which need not be full, ends in front of the request's own first key.  The places
+// between, from `hole` to -1, are hidden.
 struct SharedUnit {
   static constexpr int kFirst = -1;
   static constexpr int first = 0, sink_tiles = -(1 << 30);     // (tiles follow each other)
@@ -106,8 +108,8 @@ struct PlanMemory {
   int one[kWords], list[kListed];                          // of one unit: its entry, the tokens of its rows
 };
 
-// ALL: units, joins and the list of tokens go to memory.  Otherwise unit `wanted` stays in LDS (false: there is none), with the tokens of its rows, and
-// what it is joined with goes to memory.
+// ALL: units, joins and the list of tokens go to memory.  Otherwise unit `wanted` stays in LDS (false: there is none), with
+// the tokens of its rows, and what it is joined with goes to memory.
 template <int THREADS, bool ALL>
 __device__ bool plan(const SharedArgs& a, int many, int wanted, PlanMemory<THREADS>& s) {
   constexpr int NW = THREADS / 64;
@@ -151,7 +153,8 @@ __device__ bool plan(const SharedArgs& a, int many, int wanted, PlanMemory<THREA
     }
   }
   __syncthreads();
-  // Whether it pays: tiles that need not be read again, of all heads.
+  // Whether it pays: tiles that need not be read again, of all heads, if every request of a group has a few rows (those
+  // without rows, and chunks, are counted too: there may be less to spare).
   float again = 0.f;
   for (int g = tid & 63; g < a.P; g += 64) again += (float)max(s.g_start[g + 1] - s.g_start[g] - 1, 0) * (float)((s.g_kv[g] + kTile - 1) / kTile);
   share = wave_sum(again) * (float)a.Hkv > a.worth;
@@ -192,8 +195,9 @@ __device__ bool plan(const SharedArgs& a, int many, int wanted, PlanMemory<THREA
 #pragma unroll
   for (int w = 0; w < NW; ++w) { work += s.sums[0][w]; n_blocks += s.sums[1][w]; }
   float share_of_work = fmaxf(ceilf(work / (float)a.target), 1.f);               // tiles of a part, at most
-  // Blocks of about one length in a few more parts than the chip has places for: some wait for a whole round of them.  Longer parts that fit, then.  us: 12 chunks of 17 and 31 tokens
-  // after 4096 (32 heads over 8 of 128 channels, bf16; 72 parts a head in 64 places, then 60) 64.7 and 51.8, 74.5 and 61.5.
+  // Blocks of about one length in a few more parts than the chip has places for: some wait for a whole round of them.  Longer
+  // parts that fit, then.  us: 12 chunks of 17 and 31 tokens after 4096 (32 heads over 8 of 128 channels, bf16; 72 parts a
+  // head in 64 places, then 60) 64.7 and 51.8, 74.5 and 61.5.
   const float length = work / fmaxf(n_blocks, 1.f), cuts = ceilf(length / share_of_work);
   if (cuts >= 3.f && cuts * n_blocks > (float)a.places) share_of_work = fmaxf(share_of_work, ceilf(1.04f * length / (cuts - 1.f)));
   const int per = (int)fminf(share_of_work, 1e9f);
@@ -264,8 +268,9 @@ __device__ bool plan(const SharedArgs& a, int many, int wanted, PlanMemory<THREA
     int all[5];                                            // units, joins, partial results, tokens that go together, units of long requests
     if (ALL || r0) __syncthreads();                        // (the entries before are done with)
     const int t = x.together ? x.nq : 0, mine = x.blocks * n;
-    // Units that do not run all at once: requests longer than the mean of the blocks first (of those in hand), or one of them begins last.  us in order and so (32 heads over 8 of 128
-    // channels, bf16): 100 tokens of 64 to 1000 after 4096 65.1 and 58.2, 64 after 8192 56.7 and 53.6; 40 of 500 to 1500 after 8192 (16 heads of 64, fp16) 52.6 and 54.9.  Where they do, it
+    // Units that do not run all at once: requests longer than the mean of the blocks first (of those in hand), or one of them
+    // begins last.  us in order and so (32 heads over 8 of 128 channels, bf16): 100 tokens of 64 to 1000 after 4096 65.1 and
+    // 58.2, 64 after 8192 56.7 and 53.6; 40 of 500 to 1500 after 8192 (16 heads of 64, fp16) 52.6 and 54.9.  Where they do, it
     // costs: 32 of up to 2000 after 4096 39.0 and 40.9.
     const bool late = !ALL && (float)x.tiles <= length;
     int upto[5] = {mine, apart ? x.blocks : 0, apart ? mine : 0, t, late ? 0 : mine};
@@ -466,15 +471,17 @@ static Most most_of(int64_t P, int64_t R, int64_t T, int64_t G, int64_t Hkv, boo
   Most m;
   const int64_t with = R < T ? R : T, rows = T * G, many = fp32 ? 32 : 128, groups = P < with ? P : with;
   m.slot = fp32 || rows <= 32 ? 32 : 128;
-  // What the chip holds at a time: more parts cost more on their way through memory than they even out.  us at 256, 384, 512, 768 and 1024 units: bf16, 32 heads over 8 of 128
-  // channels, 64 tokens after 8192 56.8, 56.7, 56.7, 63.5 and 68.4; fp16, 16 over 4 of 64, 20 tokens and 7 chunks after up to 4000 35.8, 32.7, 36.7, 41.0 and 42.9; 24 over 8 of 64, 90
-  // tokens of up to 3843 after up to 2314 115, 115, 110 and 105; fp32, 16 heads of 128, 74 tokens after up to 593 91.7, 97.2, 101 and 106.
+  // What the chip holds at a time: more parts cost more on their way through memory than they even out.  us at 256, 384, 512,
+  // 768 and 1024 units: bf16, 32 heads over 8 of 128 channels, 64 tokens after 8192 56.8, 56.7, 56.7, 63.5 and 68.4; fp16, 16
+  // over 4 of 64, 20 tokens and 7 chunks after up to 4000 35.8, 32.7, 36.7, 41.0 and 42.9; 24 over 8 of 64, 90 tokens of up to
+  // 3843 after up to 2314 115, 115, 110 and 105; fp32, 16 heads of 128, 74 tokens after up to 593 91.7, 97.2, 101 and 106.
   m.target = ceil_div64(fp32 && D == 128 ? 256 : 512, Hkv);
   // (a request has one block that is not full; where blocks of 128 rows are the rule, one of 33 to 64 rows is two of 32)
   const int64_t two = rows / 33 < with ? rows / 33 : with, blocks = rows / many + with + two;
   const int64_t few = rows / 32 + with < 2 * with ? rows / 32 + with : 2 * with;
   const int64_t together = rows < kFewRows * with ? rows : kFewRows * with, pre = together / many + 2 * groups;
-  // a block is cut into at most tiles / (all work / target) + 1 parts; one of many rows leaves none if it is not cut (2: sums of work are rounded)
+  // a block is cut into at most tiles / (all work / target) + 1 parts; one of many rows leaves none if it is not cut (2: sums
+  // of work are rounded)
   m.units = m.target + blocks + pre + 2;
   m.parts = 2 * m.target + few + pre + 2;
   m.joins = blocks;
@@ -484,9 +491,10 @@ static Most most_of(int64_t P, int64_t R, int64_t T, int64_t G, int64_t Hkv, boo
 
 template <int DT, int D>
 static int launch_shared(SharedArgs& a, hipStream_t st) {
-  // A workgroup finds its unit in about 2 us, a plan takes a launch of 5 to 8.  us found and planned: bf16, 32 heads over 8 of 128 channels, 8 tokens after 1000 19.3 and 24.9 (one
-  // round of workgroups), 64 after 8192 56.2 and 58.8 (two); fp16, 40 heads, 42 tokens 47.0 and 39.3 (eight), 12 chunks after 4096 307 and 312 (five); fp32, 16 heads of
-  // 128, 21 requests 32.8 and 29.9 (five), 74 104.8 and 88.4 (ten); 16 over 4 of 64, 22 chunks 85.7 and 73.6 (five).
+  // A workgroup finds its unit in about 2 us, a plan takes a launch of 5 to 8.  us found and planned: bf16, 32 heads over 8 of
+  // 128 channels, 8 tokens after 1000 19.3 and 24.9 (one round of workgroups), 64 after 8192 56.2 and 58.8 (two); fp16, 40
+  // heads, 42 tokens 47.0 and 39.3 (eight), 12 chunks after 4096 307 and 312 (five); fp32, 16 heads of 128, 21 requests 32.8
+  // and 29.9 (five), 74 104.8 and 88.4 (ten); 16 over 4 of 64, 22 chunks 85.7 and 73.6 (five).
   const int64_t places = DT == ZC_F32 && D == 128 ? 256 : DT != ZC_F32 && D == 64 ? 768 : 512;
   a.places = (int)(places / a.Hkv);
   const bool planned = a.most_units * a.Hkv > 4 * places;
@@ -577,12 +585,16 @@ extern "C" int zc_paged_shared_attention(const zc_tensor4* q, const zc_tensor4* 
   a.pre_table = prefix_table; a.pre_len = prefix_len; a.group_start = group_start; a.pre_row = prefix_row_stride;
   a.pre_cols = (int)prefix_max_blocks; a.pre_cap = (int)room(prefix_max_blocks); a.P = (int)P;
   a.least = q->D == 64 ? 4 : 2;
-  // Rows that go through their prefix together have parts to be joined, so as much has to be spared.  us together and each request by itself: 8 tokens after 1000
-  // (32 heads over 8 of 128 channels; 29 MB spared) 19.5 and 20.3, 22 after up to 1412 (8 heads of 64; 48 MB) 18.2 and 21.8, 16 chunks of up to 17 after 355 (8 of 64; 12 MB) 18.9 and
-  // 15.9, 64 after 8192 (2.1 GB) 55.6 and 189.
+  // Rows that go through their prefix together have parts to be joined, so as much has to be spared (of a group's requests but
+  // one, with or without tokens in this step: counting those with a few rows would be a sweep more.  8 tokens after 1000 19.5
+  // us, with 56 requests without tokens beside them 19.7; one after 4096, which then has a join for nothing, 21.0 and 22.8).
+  // us together and each request by itself: 8 tokens after 1000 (32 heads over 8 of 128 channels; 29 MB spared) 19.5 and 20.3,
+  // 22 after up to 1412 (8 heads of 64; 48 MB) 18.2 and 21.8, 16 chunks of up to 17 after 355 (8 of 64; 12 MB) 18.9 and 15.9,
+  // 64 after 8192 (2.1 GB) 55.6 and 189.
   a.worth = 28e6f / (float)(2 * kTile * q->D * eb);
-  // Two blocks of 32 rows read a prefix twice, the second time from the caches as long as these hold it (256 MB); one of 128 is half empty.  us of two and of one, 16 tokens (32 heads
-  // over 8 of 128 channels, bf16) after 1000 26 and 38, 16384 (67 MB) 36 and 40, 131072 (537 MB) 166 and 120.
+  // Two blocks of 32 rows read a prefix twice, the second time from the caches as long as these hold it (256 MB); one of 128
+  // is half empty.  us of two and of one, 16 tokens (32 heads over 8 of 128 channels, bf16) after 1000 26 and 38, 16384 (67
+  // MB) 36 and 40, 131072 (537 MB) 166 and 120.
   a.far = (int)(128e6f / (float)(2 * kTile * q->D * eb * Hkv));
   a.most_units = (int)m.units; a.most_joins = (int)m.joins;
   uint8_t* at = (uint8_t*)ws;
